@@ -75,6 +75,7 @@ extern "C" {
 #define GOOSE_ST_TIMEOUT      4   /* a device-side wait ran out of polls */
 #define GOOSE_ST_BAD_ROWS     8   /* row_off[] / ctx_len[] put a sequence's rows outside [0, kv_rows): nothing moved */
 #define GOOSE_ST_BAD_NODES   16   /* n_nodes[s] outside [0, B]: the sequence is treated as having left the batch */
+#define GOOSE_ST_BAD_POS     32   /* a token's position is outside the table of rotations */
 
 /* attention kernel selection (goose_set_attn_impl) */
 #define GOOSE_ATTN_AUTO  0
@@ -244,6 +245,60 @@ int goose_verify_step_harvest(goose_ctx* ctx, const void* q, void* k_cache, void
                               void* out, float* lse, int32_t* argmax, int32_t* topk_ids, float* topk_vals,
                               int32_t* path, int32_t* accept_len, int32_t* bonus, int32_t* new_ctx_len,
                               float* row_lse, int table_rows, int32_t* adj_ids, float* adj_scores, void* stream);
+
+/* New tokens into the cache: norm of every query and key head, rotation by position, K and V rows where
+ * goose_tree_attn expects the tree nodes' rows, in one pass.  For each token i < n_nodes[s] of sequence s:
+ *   y = x * rsqrt(mean(x^2) + eps) * w         for every head of q (w = q_weight) and k (w = k_weight); a NULL weight: y = x
+ *   (a, b) -> (a cos t - b sin t, b cos t + a sin t)   for the pairs of the first rope_dim elements of y: elements (j, j + rope_dim/2),
+ *            or (2j, 2j+1) with interleaved != 0; cos t = rope[pos][j], sin t = rope[pos][rope_dim/2 + j]
+ *   q_out[s][i] = q's result; row row_off[s] + ctx_len[s] + i of the caches = k's result, and v as it is
+ * in fp32, rounded once to bf16.  pos = pos_off[s] + ctx_len[s] + depth of node i in the tree parent[s], or + i with parent == NULL:
+ * a run of tokens (a prompt), which may be longer than GOOSE_MAX_B.  pos_off counts what stands in front of the sequence elsewhere,
+ * such as the rows of a shared prefix (goose_tree_attn_shared).
+ *   q, k, v  bf16, a token's heads dense [heads][D], ldq / ldk / ldv elements from token to token (multiples of 8, so that the three
+ *            may be parts of one projection's output), token (s, i) at s * B + i; 16-byte aligned
+ *   q_weight, k_weight  bf16 [D] or NULL, 16-byte aligned; eps >= 0
+ *   rope  fp32 [rope_rows][rope_dim], 16-byte aligned; rope_dim a multiple of 16, at most D, 0 = no rotation (rope may be NULL)
+ *   row_off int64 [S], ctx_len int32 [S], pos_off int32 [S] or NULL (0), parent int32 [S][B] or NULL, n_nodes int32 [S] or NULL
+ *   q_out bf16 [S][B][H][D], may be q itself (ldq == H * D); k_cache, v_cache bf16 [kv_rows][Hkv][D]; none of them may overlap an
+ *            input otherwise
+ * H and Hkv <= max_H, S <= max_S; B <= max_B with parent, S * B < 2^31 without.  A sequence whose parent[] is no tree or whose rows leave the
+ * cache, and a token whose position is outside the table (GOOSE_ST_BAD_POS): zeros in q_out, no cache row written.             */
+int goose_append_kv(goose_ctx* ctx, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv,
+                    const void* q_weight, const void* k_weight, float eps, const float* rope, int rope_rows, int rope_dim,
+                    int interleaved, const int64_t* row_off, const int32_t* ctx_len, const int32_t* pos_off,
+                    const int32_t* parent, const int32_t* n_nodes, int S, int B, int H, int Hkv, int D,
+                    void* q_out, void* k_cache, void* v_cache, int64_t kv_rows, void* stream);
+
+/* Logits of a tree's nodes ahead of goose_node_topk: penalties for tokens that occurred, bias, grammar mask.  A sequence's
+ * tokens are hist[s][0 .. hist_len[s]-1], of which the first n_prompt[s] are its prompt; node i's row has behind them the draft tokens on
+ * the path from the root to node i, both included (the row predicts the token after node i).  For every row of a node that exists and v < V:
+ *   n = occurrences of v in hist behind the prompt and on the path
+ *   x = logits[row][v];  if v occurs in hist or on the path:  x = x > 0 ? x / repetition[s] : x * repetition[s]
+ *   x = x - frequency[s] * n - presence[s] * (n > 0) + bias[v];   bit v & 31 of mask[row][v >> 5] is 0:  x = -inf
+ * in fp32, rounded once to bf16 (a result beyond the largest bf16 becomes an infinity).  Masked places may hold anything, NaN included; a row
+ * whose mask leaves nothing is -inf throughout, and goose_node_topk gives it the lowest tokens.  Tokens outside [0, V) count nowhere.
+ *   logits, out  bf16 [S*B][ldl], [S*B][ldo], 16-byte aligned, ldl and ldo multiples of 8 and >= V; out may be logits itself
+ *            (ldo == ldl); elements from V on are not written
+ *   hist int32 [S][ldh] or NULL (hist_len, n_prompt are ignored then), hist_len int32 [S], n_prompt int32 [S] or NULL (0)
+ *   draft_tok int32 [S][B] or NULL (no token on any path), parent int32 [S][B], n_nodes int32 [S] or NULL
+ *   repetition, frequency, presence  fp32 [S] or NULL (1, 0, 0)
+ *   bias  fp32, row s at s * bias_stride (0: one row for all), or NULL;   mask uint32 [S*B][ldm], ldm * 32 >= V, or NULL
+ * hist_len[s] outside [0, ldh]: GOOSE_ST_BAD_ROWS, the sequence counts as one without history; parent[] no tree: zeros.       */
+int goose_adjust_logits(goose_ctx* ctx, const void* logits, int64_t ldl, int S, int B, int V, const int32_t* hist, int64_t ldh,
+                        const int32_t* hist_len, const int32_t* n_prompt, const int32_t* draft_tok, const int32_t* parent,
+                        const int32_t* n_nodes, const float* repetition, const float* frequency, const float* presence,
+                        const float* bias, int64_t bias_stride, const uint32_t* mask, int64_t ldm, void* out, int64_t ldo,
+                        void* stream);
+
+/* The accepted path's tokens behind each sequence's history (the hist of the next goose_adjust_logits):
+ *   hist[s][hist_len[s] + j] = draft_tok[s][path[s][j]], j = 0 .. accept_len[s];   new_len[s] = hist_len[s] + 1 + accept_len[s]
+ * path, accept_len as goose_accept produces them; n_nodes[s] = 0: nothing is appended, new_len[s] = hist_len[s].  An invalid path
+ * (GOOSE_ST_BAD_PATH) or a row without room, hist_len[s] + 1 + accept_len[s] > ldh (GOOSE_ST_BAD_ROWS): likewise.
+ * new_len must not overlap hist_len (GOOSE_EINVAL), as in goose_kv_compact.                                              */
+int goose_append_tokens(goose_ctx* ctx, const int32_t* draft_tok, const int32_t* path, const int32_t* accept_len,
+                        const int32_t* n_nodes, int S, int B, int32_t* hist, int64_t ldh, const int32_t* hist_len,
+                        int32_t* new_len, void* stream);
 
 /* Host-buffer variant of the whole step (the end-to-end call).  The prefix KV cache stays on the
  * device (k_cache / v_cache are device pointers, state carried from step to step); everything a

@@ -22,11 +22,11 @@ EXPORTS = [
     "goose_verify_step_host", "goose_last_status", "goose_launch_count", "goose_node_topk_static", "goose_harvest",
     "goose_build_spine_tree", "goose_pad_tree", "goose_context_match", "goose_spine_ratio_tier", "goose_spine_ema",
     "goose_selftest_bounded_wait", "goose_tree_attn_gqa", "goose_verify_step_gqa", "goose_verify_step_host_gqa",
-    "goose_verify_step_harvest",
+    "goose_verify_step_harvest", "goose_append_kv", "goose_adjust_logits", "goose_append_tokens",
 ]
 
 ATTN_AUTO, ATTN_MMA, ATTN_UMMA = 0, 1, 2
-ST_BAD_PARENT, ST_BAD_PATH, ST_TIMEOUT, ST_BAD_ROWS, ST_BAD_NODES = 1, 2, 4, 8, 16
+ST_BAD_PARENT, ST_BAD_PATH, ST_TIMEOUT, ST_BAD_ROWS, ST_BAD_NODES, ST_BAD_POS = 1, 2, 4, 8, 16, 32
 
 _lib: Optional[ctypes.CDLL] = None
 _native = None
@@ -115,6 +115,27 @@ def _nn(n_nodes: Optional[torch.Tensor], S: int) -> Optional[torch.Tensor]:
     if n_nodes.numel() != S:
         raise GooseError("n_nodes must have one entry per sequence")
     return n_nodes
+
+
+def _opt(t: Optional[torch.Tensor], kind: str, name: str, *shape) -> Optional[torch.Tensor]:
+    """An optional argument: None, or a contiguous CUDA tensor of the kind and shape."""
+    if t is not None:
+        _all_dev(kind, name, t)
+        if tuple(t.shape) != shape:
+            raise GooseError("%s must have the shape %s" % (name, list(shape)))
+    return t
+
+
+def _token_stride(t: torch.Tensor, S: int, B: int, D: int, name: str) -> int:
+    """Elements from token to token of a bf16 CUDA tensor [S][B][heads][D], or of such a part of a wider one."""
+    st = t.stride()
+    if not t.is_cuda or t.dtype != torch.bfloat16 or t.dim() != 4 or t.shape[0] != S or t.shape[1] != B or t.shape[3] != D:
+        raise GooseError("%s must be a bf16 CUDA tensor [S][B][heads][D]" % name)
+    heads = t.shape[2]
+    ld = st[1] if B > 1 else st[0] if S > 1 else heads * D
+    if (D > 1 and st[3] != 1) or (heads > 1 and st[2] != D) or (S > 1 and st[0] != B * ld):
+        raise GooseError("%s must have a token's heads next to one another and all tokens at one distance" % name)
+    return ld
 
 
 def _host_nn(h_n_nodes: Optional[torch.Tensor], S: int) -> Optional[torch.Tensor]:
@@ -266,6 +287,86 @@ class Goose:
         _check(self.call.kv_compact(self._h, k_cache, v_cache, rows, row_off, ctx_len, path, accept_len, _nn(n_nodes, S), S, B,
                                     H, D, new_ctx), "goose_kv_compact")
         return new_ctx
+
+    # ------------------------------------------------------------------ around the step
+    def append_kv(self, q, k, v, k_cache, v_cache, row_off, ctx_len, rope: Optional[torch.Tensor] = None,
+                  parent: Optional[torch.Tensor] = None, n_nodes: Optional[torch.Tensor] = None,
+                  pos_off: Optional[torch.Tensor] = None, q_weight: Optional[torch.Tensor] = None,
+                  k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6, interleaved: bool = False,
+                  out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Norm and rotation of new tokens' queries and keys, K and V rows into the caches behind ``ctx_len``.  q [S][B][H][D], k and v
+        [S][B][Hkv][D] may be parts of one tensor [S][B][H + 2 Hkv][D].  ``rope`` fp32 [positions][rope_dim]: cosines, then
+        sines.  Without ``parent`` the B tokens are a run (a prompt).  Returns the queries (``out``; q itself is allowed)."""
+        _all_dev("bbli", "k_cache v_cache row_off ctx_len", k_cache, v_cache, row_off, ctx_len)
+        S, B, H, D = q.shape
+        Hkv = _kv_heads(k_cache, v_cache)
+        ldq, ldk, ldv = (_token_stride(t, S, B, D, n) for t, n in ((q, "q"), (k, "k"), (v, "v")))
+        if k.shape[2] != Hkv or v.shape[2] != Hkv or k_cache.shape[2] != D:
+            raise GooseError("append_kv: k and v must have the caches' heads")
+        if row_off.numel() != S or ctx_len.numel() != S:
+            raise GooseError("row_off and ctx_len must have one entry per sequence")
+        if rope is not None:
+            _all_dev("f", "rope", rope)
+            if rope.dim() != 2:
+                raise GooseError("rope must be [positions][rope_dim]")
+        if out is None:
+            out = torch.empty((S, B, H, D), dtype=torch.bfloat16, device=q.device)
+        _opt(out, "b", "out", S, B, H, D)
+        _check(self.call.append_kv(self._h, q, ldq, k, ldk, v, ldv, _opt(q_weight, "b", "q_weight", D), _opt(k_weight, "b", "k_weight", D),
+                                   eps, rope, 0 if rope is None else rope.shape[0], 0 if rope is None else rope.shape[1], interleaved,
+                                   row_off, ctx_len, _opt(pos_off, "i", "pos_off", S), _opt(parent, "i", "parent", S, B),
+                                   _nn(n_nodes, S), S, B, H, Hkv, D, out, k_cache, v_cache, k_cache.shape[0]), "goose_append_kv")
+        return out
+
+    def adjust_logits(self, logits, hist, hist_len, draft_tok, parent, V: Optional[int] = None,
+                      n_nodes: Optional[torch.Tensor] = None, n_prompt: Optional[torch.Tensor] = None,
+                      repetition: Optional[torch.Tensor] = None, frequency: Optional[torch.Tensor] = None,
+                      presence: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
+                      mask: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Penalties over hist [S][room] (hist_len [S] of it) and every node's path, bias fp32 [V] or [S][V], grammar mask int32
+        [S*B][words] (bit 1: allowed).  ``out`` may be ``logits`` itself.  hist, hist_len and draft_tok may be None."""
+        _all_dev("bi", "logits parent", logits, parent)
+        S, B = parent.shape
+        rows, ldl = logits.shape
+        V = ldl if V is None else V
+        if rows != S * B:
+            raise GooseError("logits must have a row per node")
+        if hist is not None:
+            _all_dev("ii", "hist hist_len", hist, hist_len)
+            if hist.dim() != 2 or hist.shape[0] != S or hist_len.numel() != S:
+                raise GooseError("hist must be [S][room], hist_len [S]")
+        if bias is not None:
+            _opt(bias, "f", "bias", *((V,) if bias.dim() == 1 else (S, V)))
+        if mask is not None:
+            _all_dev("i", "mask", mask)
+            if mask.dim() != 2 or mask.shape[0] != rows or 32 * mask.shape[1] < V:
+                raise GooseError("mask must have a row per node and a bit per token")
+        if out is None:
+            out = torch.empty_like(logits)
+        _all_dev("b", "out", out)
+        if out.dim() != 2 or out.shape[0] != rows:
+            raise GooseError("out must have a row per node")
+        _check(self.call.adjust_logits(self._h, logits, ldl, S, B, V, hist, 0 if hist is None else hist.shape[1], hist_len,
+                                       _opt(n_prompt, "i", "n_prompt", S), _opt(draft_tok, "i", "draft_tok", S, B), parent,
+                                       _nn(n_nodes, S), _opt(repetition, "f", "repetition", S), _opt(frequency, "f", "frequency", S),
+                                       _opt(presence, "f", "presence", S), bias, V if bias is not None and bias.dim() == 2 else 0, mask,
+                                       0 if mask is None else mask.shape[1], out, out.shape[1]), "goose_adjust_logits")
+        return out
+
+    def append_tokens(self, draft_tok, path, accept_len, hist, hist_len, n_nodes: Optional[torch.Tensor] = None,
+                      new_len: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """The accepted path's tokens behind each sequence's history (``hist`` [S][room], updated in place); returns the new
+        lengths (``new_len``, which must not be ``hist_len`` itself)."""
+        _all_dev("iiiii", "draft_tok path accept_len hist hist_len", draft_tok, path, accept_len, hist, hist_len)
+        S, B = path.shape
+        if tuple(draft_tok.shape) != (S, B) or hist.dim() != 2 or hist.shape[0] != S or accept_len.numel() != S or hist_len.numel() != S:
+            raise GooseError("append_tokens: draft_tok and path are [S][B], hist [S][room], accept_len and hist_len [S]")
+        if new_len is None:
+            new_len = torch.empty_like(hist_len)
+        _opt(new_len, "i", "new_len", S)
+        _check(self.call.append_tokens(self._h, draft_tok, path, accept_len, _nn(n_nodes, S), S, B, hist, hist.shape[1], hist_len,
+                                       new_len), "goose_append_tokens")
+        return new_len
 
     # ------------------------------------------------------------------ whole step
     def alloc_step_outputs(self, S: int, B: int, H: int, D: int, k: int, device=None) -> dict:

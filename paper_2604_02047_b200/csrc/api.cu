@@ -312,6 +312,69 @@ int goose_kv_compact(goose_ctx* c, void* k_cache, void* v_cache, int64_t kv_rows
     return GOOSE_OK;
 }
 
+int goose_append_kv(goose_ctx* c, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv,
+                    const void* q_weight, const void* k_weight, float eps, const float* rope, int rope_rows, int rope_dim,
+                    int interleaved, const int64_t* row_off, const int32_t* ctx_len, const int32_t* pos_off,
+                    const int32_t* parent, const int32_t* n_nodes, int S, int B, int H, int Hkv, int D,
+                    void* q_out, void* k_cache, void* v_cache, int64_t kv_rows, void* stream) {
+    // (a run of tokens has no tree: its length is not that of one)
+    int rc = check_shape(c, S, parent ? B : 1, H, D);
+    if (rc) return rc;
+    if (B < 1 || (int64_t)S * B > 0x7FFFFFFFLL || Hkv < 1 || Hkv > c->max_H) return GOOSE_EINVAL;
+    if (!q || !k || !v || !row_off || !ctx_len || !q_out || !k_cache || !v_cache) return GOOSE_EINVAL;
+    for (const void* p : {q, k, v, q_weight, k_weight, (const void*)rope, (const void*)q_out, (const void*)k_cache, (const void*)v_cache})
+        if (!aligned16(p)) return GOOSE_EINVAL;
+    if (ldq < (int64_t)H * D || ldk < (int64_t)Hkv * D || ldv < (int64_t)Hkv * D || ((ldq | ldk | ldv) & 7)) return GOOSE_EINVAL;
+    if (rope_dim < 0 || rope_dim > D || rope_dim % 16 || (rope_dim && (!rope || rope_rows < 1))) return GOOSE_EINVAL;
+    if (!(eps >= 0.f) || kv_rows < 1 || kv_rows > 0x7FFFFFFFLL) return GOOSE_EINVAL;
+    if (q == q_out && ldq != (int64_t)H * D) return GOOSE_EINVAL;
+    goose::AppendKv a{};
+    a.q = (const __nv_bfloat16*)q; a.k = (const __nv_bfloat16*)k; a.v = (const __nv_bfloat16*)v;
+    a.ldq = ldq; a.ldk = ldk; a.ldv = ldv;
+    a.q_weight = (const __nv_bfloat16*)q_weight; a.k_weight = (const __nv_bfloat16*)k_weight; a.eps = eps;
+    a.rope = rope; a.rope_rows = rope_rows; a.rope_dim = rope_dim; a.interleaved = interleaved;
+    a.row_off = row_off; a.ctx_len = ctx_len; a.pos_off = pos_off; a.parent = parent; a.n_nodes = n_nodes;
+    a.B = B; a.H = H; a.Hkv = Hkv;
+    a.q_out = (__nv_bfloat16*)q_out; a.k_cache = (__nv_bfloat16*)k_cache; a.v_cache = (__nv_bfloat16*)v_cache; a.kv_rows = kv_rows;
+    cudaError_t e = goose::launch_append_kv(c, a, S, static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) return cuda_fail(e);
+    return GOOSE_OK;
+}
+
+int goose_adjust_logits(goose_ctx* c, const void* logits, int64_t ldl, int S, int B, int V, const int32_t* hist, int64_t ldh,
+                        const int32_t* hist_len, const int32_t* n_prompt, const int32_t* draft_tok, const int32_t* parent,
+                        const int32_t* n_nodes, const float* repetition, const float* frequency, const float* presence,
+                        const float* bias, int64_t bias_stride, const uint32_t* mask, int64_t ldm, void* out, int64_t ldo,
+                        void* stream) {
+    if (!c || !on_ctx_device(c) || !logits || !parent || !out) return GOOSE_EINVAL;
+    if (S < 0 || S > c->max_S || B < 1 || B > c->max_B) return GOOSE_EINVAL;
+    if (V < 1 || V > GOOSE_MAX_V || ldl < V || ldo < V || ((ldl | ldo) & 7) || !aligned16(logits) || !aligned16(out)) return GOOSE_EINVAL;
+    if (hist && (!hist_len || ldh < 0 || ldh > 0x7FFFFFFFLL)) return GOOSE_EINVAL;
+    if (bias && bias_stride != 0 && bias_stride < V) return GOOSE_EINVAL;
+    if (mask && (ldm < 1 || ldm * 32 < V)) return GOOSE_EINVAL;
+    if (logits == out && ldl != ldo) return GOOSE_EINVAL;
+    goose::AdjustLogits a{};
+    a.logits = (const __nv_bfloat16*)logits; a.ldl = ldl; a.V = V; a.B = B;
+    a.hist = hist; a.ldh = ldh; a.hist_len = hist_len; a.n_prompt = n_prompt; a.draft_tok = draft_tok; a.parent = parent; a.n_nodes = n_nodes;
+    a.repetition = repetition; a.frequency = frequency; a.presence = presence; a.bias = bias; a.bias_stride = bias_stride;
+    a.mask = mask; a.ldm = ldm; a.out = (__nv_bfloat16*)out; a.ldo = ldo;
+    cudaError_t e = goose::launch_adjust_logits(c, a, S, static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) return cuda_fail(e);
+    return GOOSE_OK;
+}
+
+int goose_append_tokens(goose_ctx* c, const int32_t* draft_tok, const int32_t* path, const int32_t* accept_len,
+                        const int32_t* n_nodes, int S, int B, int32_t* hist, int64_t ldh, const int32_t* hist_len,
+                        int32_t* new_len, void* stream) {
+    if (!c || !on_ctx_device(c) || !draft_tok || !path || !accept_len || !hist || !hist_len || !new_len) return GOOSE_EINVAL;
+    if (S < 0 || S > c->max_S || B < 1 || B > c->max_B || ldh < 0) return GOOSE_EINVAL;
+    if (ctx_arrays_overlap(hist_len, new_len, S)) return GOOSE_EINVAL;
+    cudaError_t e = goose::launch_append_tokens(c, draft_tok, path, accept_len, n_nodes, S, B, hist, ldh, hist_len, new_len,
+                                                static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) return cuda_fail(e);
+    return GOOSE_OK;
+}
+
 int goose_verify_step(goose_ctx* c, const void* q, void* k_cache, void* v_cache, int64_t kv_rows,
                       const int64_t* row_off, const int32_t* ctx_len, const int32_t* parent,
                       const int32_t* n_nodes, const int32_t* draft_tok, const void* logits, int64_t ldl,

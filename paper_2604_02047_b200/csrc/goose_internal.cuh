@@ -214,6 +214,42 @@ int attn_cluster(const goose_ctx* c, int S, int B, int H, int Hkv, int64_t kv_ro
 struct StepSplit { int cluster, topk_ctas; };
 StepSplit step_split(const goose_ctx* c, int S, int B, int H, int Hkv, int64_t kv_rows, int V, int k, bool harvest, bool counts);
 
+// arguments of goose_append_kv and goose_adjust_logits as the kernels take them (status: the launcher's)
+struct AppendKv {
+    const __nv_bfloat16 *q, *k, *v;
+    int64_t ldq, ldk, ldv;                                 // elements from token to token
+    const __nv_bfloat16 *q_weight, *k_weight;
+    float eps;
+    const float* rope;
+    int rope_rows, rope_dim, interleaved;
+    const int64_t* row_off;
+    const int32_t *ctx_len, *pos_off, *parent, *n_nodes;
+    int B, H, Hkv;
+    __nv_bfloat16 *q_out, *k_cache, *v_cache;
+    int64_t kv_rows;
+    int32_t* status;
+};
+cudaError_t launch_append_kv(goose_ctx* c, AppendKv a, int S, cudaStream_t st);
+cudaError_t launch_append_tokens(goose_ctx* c, const int32_t* draft_tok, const int32_t* path, const int32_t* accept_len,
+                                 const int32_t* n_nodes, int S, int B, int32_t* hist, int64_t ldh, const int32_t* hist_len,
+                                 int32_t* new_len, cudaStream_t st);
+struct AdjustLogits {
+    const __nv_bfloat16* logits;
+    int64_t ldl;
+    int V, B;
+    const int32_t* hist;
+    int64_t ldh;
+    const int32_t *hist_len, *n_prompt, *draft_tok, *parent, *n_nodes;
+    const float *repetition, *frequency, *presence, *bias;
+    int64_t bias_stride;
+    const uint32_t* mask;
+    int64_t ldm;
+    __nv_bfloat16* out;
+    int64_t ldo;
+    int32_t* status;
+};
+cudaError_t launch_adjust_logits(goose_ctx* c, AdjustLogits a, int S, cudaStream_t st);
+
 cudaError_t launch_bounded_wait_selftest(goose_ctx* c, long long limit_cycles, int32_t* result, cudaStream_t st);
 
 // split count of the mma kernel's fixed grid: ctx_len lives on the device, so it depends only on S, H and the SM count
@@ -236,9 +272,12 @@ cudaError_t init_topk_kernel();
 cudaError_t init_table_kernel();
 cudaError_t init_compact_kernel();
 cudaError_t init_accept_kernel();
+cudaError_t init_append_kernels();
+cudaError_t init_adjust_kernel();
 inline cudaError_t init_kernels(goose_ctx* c) {
     cudaError_t e = init_umma_kernel(c);
-    for (cudaError_t (*init)() : {init_topk_kernel, init_compact_kernel, init_merge_kernel, init_accept_kernel, init_table_kernel, init_mma_kernel})
+    for (cudaError_t (*init)() : {init_topk_kernel, init_compact_kernel, init_merge_kernel, init_accept_kernel, init_table_kernel, init_mma_kernel,
+                                  init_append_kernels, init_adjust_kernel})
         if (e == cudaSuccess) e = init();
     return e;
 }

@@ -112,6 +112,9 @@ PyMethodDef methods[] = {
     entry<&goose_verify_step>("verify_step"),
     entry<&goose_verify_step_gqa>("verify_step_gqa"),
     entry<&goose_verify_step_harvest>("verify_step_harvest"),
+    entry<&goose_append_kv>("append_kv"),
+    entry<&goose_adjust_logits>("adjust_logits"),
+    entry<&goose_append_tokens>("append_tokens"),
     {"check", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&check)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 
