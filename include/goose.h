@@ -129,6 +129,22 @@ int goose_tree_attn_gqa(goose_ctx* ctx, const void* q, const void* k_cache, cons
                         const int64_t* row_off, const int32_t* ctx_len, const int32_t* parent, const int32_t* n_nodes,
                         int S, int B, int H, int Hkv, int D, float scale, void* out, float* lse, void* stream);
 
+/* Tree attention of a batch whose sequences share a long prefix (a system prompt, a document), which the cache holds once: as
+ * goose_tree_attn_gqa, with the visible keys of every node extended by the rows shared_row .. shared_row + shared_len - 1, in
+ * front of the sequence's own prefix row_off[s] .. row_off[s] + ctx_len[s] - 1 and its tree rows behind that.
+ * The shared rows are read once for 256 query rows of all sequences, not once per sequence.
+ *   shared_row, shared_len  host numbers: rows inside the cache; shared_len 0: no shared rows.  A different prefix per part of a batch is a
+ *            call per part.  The positions of a sequence's own rows start at shared_len (pos_off of goose_append_kv).
+ *   out bf16 [S][B][H][D], may be q itself; lse as in goose_tree_attn, of all keys
+ * What a sequence's own rows hold never reaches another sequence's output.  The call's workspace (33 KB for 128 query rows of a
+ * head, about three times) is allocated by the context's first call, and again by one that needs more: such a call waits for the
+ * device, and cannot be captured into a graph (make one of that size before).  Other arguments, limits and errors as goose_tree_attn_gqa;
+ * the kernel needs tensor maps (GOOSE_ECUDA where the driver cannot make them).                                          */
+int goose_tree_attn_shared(goose_ctx* ctx, const void* q, const void* k_cache, const void* v_cache, int64_t kv_rows,
+                           int64_t shared_row, int32_t shared_len, const int64_t* row_off, const int32_t* ctx_len,
+                           const int32_t* parent, const int32_t* n_nodes, int S, int B, int H, int Hkv, int D, float scale,
+                           void* out, float* lse, void* stream);
+
 /* Per-node argmax and top-k (Algorithm 3 step 2; App. C.1 "aggressive logit harvesting": every
  * row of the forward's logits is harvested, rejected branches included).
  * For each of `rows` rows: the ids of the k largest of the first V values, ordered by

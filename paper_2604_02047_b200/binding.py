@@ -22,7 +22,7 @@ EXPORTS = [
     "goose_verify_step_host", "goose_last_status", "goose_launch_count", "goose_node_topk_static", "goose_harvest",
     "goose_build_spine_tree", "goose_pad_tree", "goose_context_match", "goose_spine_ratio_tier", "goose_spine_ema",
     "goose_selftest_bounded_wait", "goose_tree_attn_gqa", "goose_verify_step_gqa", "goose_verify_step_host_gqa",
-    "goose_verify_step_harvest", "goose_append_kv", "goose_adjust_logits", "goose_append_tokens",
+    "goose_verify_step_harvest", "goose_tree_attn_shared", "goose_append_kv", "goose_adjust_logits", "goose_append_tokens",
 ]
 
 ATTN_AUTO, ATTN_MMA, ATTN_UMMA = 0, 1, 2
@@ -317,6 +317,25 @@ class Goose:
                                    row_off, ctx_len, _opt(pos_off, "i", "pos_off", S), _opt(parent, "i", "parent", S, B),
                                    _nn(n_nodes, S), S, B, H, Hkv, D, out, k_cache, v_cache, k_cache.shape[0]), "goose_append_kv")
         return out
+
+    def tree_attn_shared(self, q, k_cache, v_cache, shared_row: int, shared_len: int, row_off, ctx_len, parent, scale: float,
+                         out: Optional[torch.Tensor] = None, want_lse: bool = False,
+                         lse: Optional[torch.Tensor] = None, n_nodes: Optional[torch.Tensor] = None):
+        """Tree attention, multi-head or grouped-query, of a batch whose sequences all see the cache rows ``shared_row`` ..
+        ``shared_row + shared_len - 1`` in front of their own.  Returns out, or (out, lse) with ``want_lse`` or ``lse``."""
+        _all_dev("bbblii", "q k_cache v_cache row_off ctx_len parent", q, k_cache, v_cache, row_off, ctx_len, parent)
+        S, B, H, D = q.shape
+        Hkv = _kv_heads(k_cache, v_cache)
+        if tuple(parent.shape) != (S, B) or row_off.numel() != S or ctx_len.numel() != S or k_cache.shape[2] != D:
+            raise GooseError("tree_attn_shared: q is [S][B][H][D], parent [S][B], row_off and ctx_len [S]")
+        if out is None:
+            out = torch.empty_like(q)
+        if want_lse and lse is None:
+            lse = torch.empty((S, B, H), dtype=torch.float32, device=q.device)
+        _check(self.call.tree_attn_shared(self._h, q, k_cache, v_cache, k_cache.shape[0], shared_row, shared_len, row_off, ctx_len, parent,
+                                          _nn(n_nodes, S), S, B, H, Hkv, D, scale, _opt(out, "b", "out", S, B, H, D),
+                                          _opt(lse, "f", "lse", S, B, H)), "goose_tree_attn_shared")
+        return out if lse is None else (out, lse)
 
     def adjust_logits(self, logits, hist, hist_len, draft_tok, parent, V: Optional[int] = None,
                       n_nodes: Optional[torch.Tensor] = None, n_prompt: Optional[torch.Tensor] = None,

@@ -201,6 +201,7 @@ int goose_destroy(goose_ctx* c) {
     cudaSetDevice(c->device);
     cudaFree(c->partials); cudaFree(c->head_counters); cudaFree(c->topk_cand);
     cudaFree(c->row_counters); cudaFree(c->topk_lse_ws); cudaFree(c->status); cudaFree(c->selftest_word); cudaFree(c->stage);
+    cudaFree(c->shared_parts);
     if (c->pin) cudaFreeHost(c->pin);
     if (c->side) cudaStreamDestroy(c->side);
     if (c->ev_fork) cudaEventDestroy(c->ev_fork);
@@ -250,6 +251,26 @@ int goose_tree_attn_gqa(goose_ctx* c, const void* q, const void* k_cache, const 
         e = goose::launch_tree_attn_mma(c, (const __nv_bfloat16*)q, (const __nv_bfloat16*)k_cache,
                                         (const __nv_bfloat16*)v_cache, kv_rows, row_off, ctx_len, parent, n_nodes, S, B, H,
                                         Hkv, scale, (__nv_bfloat16*)out, lse, st);
+    if (e != cudaSuccess) return cuda_fail(e);
+    return GOOSE_OK;
+}
+
+int goose_tree_attn_shared(goose_ctx* c, const void* q, const void* k_cache, const void* v_cache, int64_t kv_rows,
+                           int64_t shared_row, int32_t shared_len, const int64_t* row_off, const int32_t* ctx_len,
+                           const int32_t* parent, const int32_t* n_nodes, int S, int B, int H, int Hkv, int D, float scale,
+                           void* out, float* lse, void* stream) {
+    int rc = check_shape(c, S, B, H, D);
+    if (rc) return rc;
+    if (Hkv < 1 || H % Hkv != 0 || H / Hkv > GOOSE_MAX_GROUP) return GOOSE_EINVAL;
+    if (!q || !k_cache || !v_cache || !row_off || !ctx_len || !parent || !out) return GOOSE_EINVAL;
+    if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(out)) return GOOSE_EINVAL;
+    if (kv_rows < 1 || kv_rows > 0x7FFFFFFFLL) return GOOSE_EINVAL;
+    if (shared_len < 0 || shared_row < 0 || shared_row > kv_rows - shared_len) return GOOSE_EINVAL;
+    if (!(scale > 0.f) || !(scale < 1e30f)) return GOOSE_EINVAL;
+    cudaError_t e = goose::launch_tree_attn_shared(c, (const __nv_bfloat16*)q, (const __nv_bfloat16*)k_cache, (const __nv_bfloat16*)v_cache,
+                                                   kv_rows, shared_row, shared_len, row_off, ctx_len, parent, n_nodes, S, B, H, Hkv,
+                                                   scale, (__nv_bfloat16*)out, lse, static_cast<cudaStream_t>(stream));
+    if (e == cudaErrorMemoryAllocation) return GOOSE_ENOMEM;
     if (e != cudaSuccess) return cuda_fail(e);
     return GOOSE_OK;
 }

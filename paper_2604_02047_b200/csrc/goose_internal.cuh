@@ -35,6 +35,9 @@ struct goose_ctx {
     float* topk_lse_ws;       // [topk_rows_cap][chunks][2]: per-chunk (max, sum) of the log-sum-exp
     int64_t topk_cand_cap;    // elements
     int topk_rows_cap;
+    // partial results of the shared-prefix attention: made by the first call that needs them, and again by one that needs more
+    float* shared_parts;
+    size_t shared_bytes;
     // per-sequence status words
     int32_t* status;          // [max_S]
     int32_t* selftest_word;   // result word of goose_selftest_bounded_wait
@@ -250,6 +253,11 @@ struct AdjustLogits {
 };
 cudaError_t launch_adjust_logits(goose_ctx* c, AdjustLogits a, int S, cudaStream_t st);
 
+cudaError_t launch_tree_attn_shared(goose_ctx* c, const __nv_bfloat16* q, const __nv_bfloat16* kc, const __nv_bfloat16* vc,
+                                    int64_t kv_rows, int64_t shared_row, int shared_len, const int64_t* row_off,
+                                    const int32_t* ctx_len, const int32_t* parent, const int32_t* n_nodes, int S, int B, int H,
+                                    int Hkv, float scale, __nv_bfloat16* out, float* lse, cudaStream_t st);
+
 cudaError_t launch_bounded_wait_selftest(goose_ctx* c, long long limit_cycles, int32_t* result, cudaStream_t st);
 
 // split count of the mma kernel's fixed grid: ctx_len lives on the device, so it depends only on S, H and the SM count
@@ -274,10 +282,11 @@ cudaError_t init_compact_kernel();
 cudaError_t init_accept_kernel();
 cudaError_t init_append_kernels();
 cudaError_t init_adjust_kernel();
+cudaError_t init_shared_kernel();
 inline cudaError_t init_kernels(goose_ctx* c) {
     cudaError_t e = init_umma_kernel(c);
     for (cudaError_t (*init)() : {init_topk_kernel, init_compact_kernel, init_merge_kernel, init_accept_kernel, init_table_kernel, init_mma_kernel,
-                                  init_append_kernels, init_adjust_kernel})
+                                  init_append_kernels, init_adjust_kernel, init_shared_kernel})
         if (e == cudaSuccess) e = init();
     return e;
 }

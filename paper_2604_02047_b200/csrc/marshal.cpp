@@ -112,6 +112,7 @@ PyMethodDef methods[] = {
     entry<&goose_verify_step>("verify_step"),
     entry<&goose_verify_step_gqa>("verify_step_gqa"),
     entry<&goose_verify_step_harvest>("verify_step_harvest"),
+    entry<&goose_tree_attn_shared>("tree_attn_shared"),
     entry<&goose_append_kv>("append_kv"),
     entry<&goose_adjust_logits>("adjust_logits"),
     entry<&goose_append_tokens>("append_tokens"),

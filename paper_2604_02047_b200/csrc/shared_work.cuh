@@ -1,0 +1,129 @@
+// Work partition of the shared-prefix attention: the same arithmetic for its main kernel and for the merge behind it.  It compiles for
+// the host too, where a test walks it.
+//
+// The work list is a row of items, each a run of 128-key tiles: first, head by head, the pairs of M tiles of the whole batch over the shared
+// rows, then, sequence by sequence and head by head, the pairs of M tiles of one sequence over its own rows.  It is dealt to the CTAs in
+// ranges of equal length.  What a CTA does of one item is a segment.  A segment has two lanes, each with a softmax warpgroup and
+// accumulators of its own: the two M tiles of the pair, which share the key tiles, or, where an item is a single M tile, even and odd
+// key tiles of it.  Every lane of a segment leaves a partial result.
+#pragma once
+
+#include "goose_internal.cuh"
+
+namespace goose {
+
+constexpr int kSharedTile = 128;                 // keys of a tile, rows of an M tile
+
+struct SharedWork {
+    const int32_t* ctx_len;
+    const int32_t* n_nodes;   // or NULL
+    int S, B, Hkv, kv_rows;
+    int shared_tiles;         // tiles of the shared rows
+    int shared_m, own_m;      // M tiles a key/value head: of the whole batch; of one sequence
+    int G;                    // CTAs
+    // worked out
+    int pad;                  // idle places in front of every item, the price of a segment
+    long long shared_total, total, quantum;
+
+    __host__ __device__ __forceinline__ int shared_pairs() const { return (shared_m + 1) >> 1; }
+    __host__ __device__ __forceinline__ int own_pairs() const { return (own_m + 1) >> 1; }
+    // a negative length counts as 0, one beyond the cache as the whole cache: such a sequence is flagged, and the list stays one that every
+    // division below is right for
+    __host__ __device__ __forceinline__ int prefix(int ctx) const {
+        const int c = ctx < 0 ? 0 : ctx;
+        return c < kv_rows ? c : kv_rows;
+    }
+    __host__ __device__ __forceinline__ int tiles(int s) const {
+        const int nn = nodes_of(n_nodes, s, B);
+        return nn == 0 ? 0 : (int)(((uint32_t)prefix(ctx_len[s]) + (uint32_t)nn + kSharedTile - 1) / kSharedTile);
+    }
+    __host__ __device__ __forceinline__ int width(int T) const { return T > 0 ? T + pad : 0; }
+    // sum: tiles of a head of all sequences;  live: sequences that have any
+    __host__ __device__ __forceinline__ void set(long long sum, int live) {
+        const long long all = (long long)Hkv * shared_pairs() * shared_tiles + (long long)Hkv * own_pairs() * sum;
+        pad = all >= 2ll * G ? 2 : 0;
+        shared_total = (long long)Hkv * shared_pairs() * width(shared_tiles);
+        total = shared_total + (long long)Hkv * own_pairs() * (sum + (long long)pad * live);
+        quantum = total > 0 ? divide(total + G - 1, G) : 1;
+    }
+    __host__ __device__ __forceinline__ void init() {
+        long long sum = 0;
+        int live = 0;
+        for (int s = 0; s < S; ++s) {
+            const int T = tiles(s);
+            sum += T;
+            live += T > 0;
+        }
+        set(sum, live);
+    }
+    static __host__ __device__ __forceinline__ long long divide(long long a, long long b) {   // 64-bit division is slow on the GPU
+        return (a | b) >> 32 ? a / b : (long long)((uint32_t)a / (uint32_t)b);
+    }
+    __host__ __device__ __forceinline__ long long start(int c) const { return min(c * quantum, total); }
+    __host__ __device__ __forceinline__ int cta_of(long long w) const { return (int)divide(w, quantum); }
+    __host__ __device__ __forceinline__ int items() const { return Hkv * (shared_tiles > 0 ? shared_pairs() : 0) + S * Hkv * own_pairs(); }
+    __host__ __device__ __forceinline__ int item(int s, int i) const {    // s < 0: the shared rows;  i = head * pairs + pair
+        return s < 0 ? i : Hkv * (shared_tiles > 0 ? shared_pairs() : 0) + s * Hkv * own_pairs() + i;
+    }
+    // Where the partial result of a lane lies.  A segment that is a whole item has the item's place; of any other a CTA has at most one
+    // that does not start its item (its first) and one that does (its last).
+    __host__ __device__ __forceinline__ int slot(int item, int cta, bool from_start, bool to_end, int lane) const {
+        return from_start && to_end ? 2 * item + lane : 2 * items() + 4 * cta + (from_start ? 2 : 0) + lane;
+    }
+    __host__ __device__ __forceinline__ int slots() const { return 2 * items() + 4 * G; }
+};
+
+struct SharedCursor {         // walks the list
+    long long w;              // place in it
+    int s, i, t, T;           // sequence or -1, item of it (head * pairs + pair), tile, tiles
+    // at place `rem` of the items of width wd that begin here
+    __host__ __device__ __forceinline__ void enter(const SharedWork& wk, long long rem) {
+        const int wd = wk.width(T);
+        i = (int)SharedWork::divide(rem, wd);
+        t = (int)(rem - (long long)i * wd) - wk.pad;
+        if (t < 0) { w -= t; t = 0; }
+    }
+    __host__ __device__ __forceinline__ void seek(const SharedWork& wk, long long w0) {
+        w = w0; s = -1; T = wk.shared_tiles;
+        if (w0 < wk.shared_total) { enter(wk, w0); return; }
+        long long rem = w0 - wk.shared_total;
+        for (s = 0; s < wk.S; ++s) {
+            T = wk.tiles(s);
+            const long long mine = (long long)wk.Hkv * wk.own_pairs() * wk.width(T);
+            if (rem < mine) break;
+            rem -= mine;
+        }
+        if (s < wk.S) enter(wk, rem);
+    }
+    __host__ __device__ __forceinline__ int run(long long w_end) const { return (int)min((long long)(T - t), w_end - w); }
+    __host__ __device__ __forceinline__ void skip(const SharedWork& wk, int n) {
+        w += n; t += n;
+        if (t < T) return;
+        t = 0; ++i; w += wk.pad;
+        if (i < wk.Hkv * (s < 0 ? wk.shared_pairs() : wk.own_pairs())) return;
+        i = 0;
+        do { ++s; } while (s < wk.S && (T = wk.tiles(s)) == 0);
+    }
+};
+
+// the partial results of one M tile of an item, in the order of the keys
+struct SharedParts {
+    long long w0;             // place of the item's first tile
+    int T, item, c0, n, lanes, lane;
+    // single: the item is one M tile (two lanes of key tiles); else `m` says which of the two
+    __host__ __device__ __forceinline__ void set(const SharedWork& wk, int s, int i, long long first, int tiles, bool single, int m) {
+        w0 = first + wk.pad; T = tiles; item = wk.item(s, i);
+        lanes = single ? 2 : 1; lane = single ? 0 : m;
+        if (T > 0) { c0 = wk.cta_of(w0); n = (wk.cta_of(w0 + T - 1) - c0 + 1) * lanes; }
+        else { c0 = 0; n = 0; }
+    }
+    // slot of part k, or -1: that CTA has nothing of the item for the lane
+    __host__ __device__ __forceinline__ int slot(const SharedWork& wk, int k) const {
+        const int c = c0 + (lanes == 2 ? k >> 1 : k), l = lanes == 2 ? k & 1 : lane;
+        const long long a = c * wk.quantum - w0, b = a + wk.quantum;
+        const int ta = (int)max(a, 0ll), tb = (int)min(b, (long long)T);
+        return tb - ta > (lanes == 2 ? l : 0) ? wk.slot(item, c, ta == 0, tb == T, l) : -1;
+    }
+};
+
+}  // namespace goose
