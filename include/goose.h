@@ -300,7 +300,8 @@ int goose_append_kv(goose_ctx* ctx, const void* q, int64_t ldq, const void* k, i
  *   draft_tok int32 [S][B] or NULL (no token on any path), parent int32 [S][B], n_nodes int32 [S] or NULL
  *   repetition, frequency, presence  fp32 [S] or NULL (1, 0, 0)
  *   bias  fp32, row s at s * bias_stride (0: one row for all), or NULL;   mask uint32 [S*B][ldm], ldm * 32 >= V, or NULL
- * hist_len[s] outside [0, ldh]: GOOSE_ST_BAD_ROWS, the sequence counts as one without history; parent[] no tree: zeros.       */
+ * The call's workspace (4 bytes for every token of every sequence's vocabulary, where there is a history) is allocated as in
+ * goose_tree_attn_shared.  hist_len[s] outside [0, ldh]: GOOSE_ST_BAD_ROWS, the sequence counts as one without history; parent[] no tree: zeros.       */
 int goose_adjust_logits(goose_ctx* ctx, const void* logits, int64_t ldl, int S, int B, int V, const int32_t* hist, int64_t ldh,
                         const int32_t* hist_len, const int32_t* n_prompt, const int32_t* draft_tok, const int32_t* parent,
                         const int32_t* n_nodes, const float* repetition, const float* frequency, const float* presence,

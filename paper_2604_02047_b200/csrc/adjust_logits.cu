@@ -7,64 +7,103 @@
 // in fp32, rounded once.  What a tree makes different is the path: every row of logits has counts of its own, which differ from its
 // sequence's in the few tokens of its ancestors.
 //
-// What bounds it: 2 bytes in and 2 out for every logit, and an eighth for its mask: HBM.  A block has kVocab tokens of one sequence and
-// a share of its nodes.  It counts the history into shared memory (every block reads the whole history, from L2; tokens outside its
-// piece of the vocabulary fall through) and keeps what that makes of 8 tokens in a thread's registers for all of its rows, which then stream
-// past.  Tokens of the path are put right behind the stream, a thread a (row, node of the path) pair: where the tokens are those of text,
-// most of a tree's lie in the first few of the vocabulary, and whatever thread has those in the stream would do the others' work.
+// What bounds it: 2 bytes in and 2 out for every logit, and an eighth for its mask: HBM.  Two kernels.  The first makes of each
+// sequence's history a word per token of the vocabulary, of its tree the nodes' paths and which nodes have the same token.  In the second
+// a block has kVocab tokens and a few rows: a thread reads the words of its 8 tokens once and the rows stream past.  The blocks are many and
+// short, since trees differ in size and sequences leave; the first rows are on their way before the first kernel has ended.  Tokens of the
+// path are put right behind the stream, a thread a (row, node of the path) pair: where the tokens are those of text, most of a tree's
+// lie in the first few of the vocabulary, and whatever thread has those in the stream would do the others' work.
 #include "goose_internal.cuh"
 
 namespace goose {
 
-constexpr int kAdjustColumns = 256;                  // threads beside one another, 8 tokens each
-constexpr int kAdjustThreads = 2 * kAdjustColumns;   // two rows at a time
-constexpr int kVocab = 8 * kAdjustColumns;           // tokens of a block
+constexpr int kAdjustThreads = 256;
+constexpr int kVocab = 8 * kAdjustThreads;           // tokens of a block
 constexpr int kAdjustRows = 4;                       // rows of a thread in flight
-constexpr int kPathTasks = 2;                        // (row, node) pairs of a thread in a batch of rows
+constexpr int kBlockRows = 8;                        // rows of a block, at most
+constexpr int kCountThreads = 512;
 constexpr uint32_t kInPrompt = 0x80000000u;          // of a token's word: it occurs in the prompt; below: its count behind it
 
-__device__ __forceinline__ uint32_t common(const uint4& a, const uint4& b, int w) {
-    return w == 0 ? a.x & b.x : w == 1 ? a.y & b.y : w == 2 ? a.z & b.z : a.w & b.w;
+// what the first kernel leaves of a sequence
+struct AdjustTree {
+    uint4 path[kMaxB];                               // a node's path, as a set of nodes
+    uint4 same[kMaxB];                               // the nodes that have its token
+    int bad;                                         // parent[] is no tree
+    int pad[3];
+};
+
+// Of a path's nodes that have the token of node j (same): is j the first?  n: how many there are.
+__device__ __forceinline__ bool first_of_path(const uint4& path, const uint4& same, int j, uint32_t& n) {
+    const uint32_t both[4] = {path.x & same.x, path.y & same.y, path.z & same.z, path.w & same.w};
+    int first = kMaxB;
+    n = 0;
+#pragma unroll
+    for (int w = 3; w >= 0; --w) {
+        n += __popc(both[w]);
+        if (both[w]) first = 32 * w + __ffs(both[w]) - 1;
+    }
+    return first == j;
 }
 
-__global__ void __launch_bounds__(kAdjustThreads, 2)
-adjust_logits_kernel(const AdjustLogits a, int rows_per_block) {
+// the words of kVocab tokens (blocks 0 .. pieces - 1), the tree (the last block) of a sequence
+__global__ void __launch_bounds__(kCountThreads)
+adjust_tables_kernel(const AdjustLogits a, int pieces, int64_t ldw, uint32_t* __restrict__ words, AdjustTree* __restrict__ trees) {
     __shared__ uint32_t s_count[kVocab];
-    __shared__ uint4 s_path[kMaxB];                  // a node's path, as a set of nodes
-    __shared__ uint4 s_same[kMaxB];                  // of the list below: the nodes that have the same token
-    __shared__ int s_up[kMaxB], s_tok[kMaxB];        // s_tok: relative to this piece of the vocabulary
-    __shared__ unsigned char s_list[kMaxB];          // nodes whose token lies in it
-    __shared__ int s_listed;
-    const int s = blockIdx.z, tid = threadIdx.x, base = blockIdx.x * kVocab;
+    __shared__ uint4 s_path[kMaxB];
+    __shared__ int s_up[kMaxB], s_tok[kMaxB];
+    const int s = blockIdx.y, tid = threadIdx.x;
     pdl_wait();
     pdl_trigger();
     const int nn = nodes_of(a.n_nodes, s, a.B);
-    if (blockIdx.x == 0 && blockIdx.y == 0 && tid == 0 && nodes_bad(a.n_nodes, s, a.B)) atomicOr(&a.status[s], GOOSE_ST_BAD_NODES);
-    const int i0 = blockIdx.y * rows_per_block, i1 = min(i0 + rows_per_block, nn);
-    if (i0 >= nn) return;
-
-    // ---- the sequence's tokens
-    static_assert(kVocab == 4 * kAdjustThreads, "one store a thread");
-    reinterpret_cast<uint4*>(s_count)[tid] = make_uint4(0, 0, 0, 0);
-    if (tid == 0) s_listed = 0;
-    int len = a.hist ? a.hist_len[s] : 0;
-    const int prompt = a.n_prompt ? a.n_prompt[s] : 0;
-    const bool bad_len = len < 0 || len > a.ldh;
-    if (bad_len) len = 0;
-    const bool node = tid < nn;
-    int up = node ? a.parent[(size_t)s * a.B + tid] : 0;
-    const int tok = node && a.draft_tok ? a.draft_tok[(size_t)s * a.B + tid] - base : -1;
-    const bool no_tree = node && (tid == 0 ? up != -1 : (up < 0 || up >= tid));
-    if (tid == 0) up = 0;
-    uint4 path = make_uint4(0, 0, 0, 0);
-    if (node) {
-        const uint32_t bit = 1u << (tid & 31);
-        (tid < 32 ? path.x : tid < 64 ? path.y : tid < 96 ? path.z : path.w) = bit;
-        s_tok[tid] = tok;
+    if ((int)blockIdx.x == pieces) {
+        const bool node = tid < nn;
+        int up = node ? a.parent[(size_t)s * a.B + tid] : 0;
+        const int tok = node && a.draft_tok ? a.draft_tok[(size_t)s * a.B + tid] : -1;
+        const bool no_tree = node && (tid == 0 ? up != -1 : (up < 0 || up >= tid));
+        const bool bad_len = a.hist && nn > 0 && (a.hist_len[s] < 0 || a.hist_len[s] > a.ldh);
+        if (tid == 0) up = 0;
+        uint4 path = make_uint4(0, 0, 0, 0), same = path;
+        if (node) {
+            const uint32_t bit = 1u << (tid & 31);
+            (tid < 32 ? path.x : tid < 64 ? path.y : tid < 96 ? path.z : path.w) = bit;
+            s_tok[tid] = tok;
+        }
+        const bool bad = __syncthreads_or(no_tree);
+        if (tid == 0) {
+            trees[s].bad = bad;
+            const int flaws = (bad ? GOOSE_ST_BAD_PARENT : 0) | (bad_len ? GOOSE_ST_BAD_ROWS : 0) | (nodes_bad(a.n_nodes, s, a.B) ? GOOSE_ST_BAD_NODES : 0);
+            if (flaws) atomicOr(&a.status[s], flaws);
+        }
+        if (bad) return;
+        // in steps up the tree that double
+        for (int reach = 1; reach < kMaxB; reach *= 2) {
+            if (node) { s_path[tid] = path; s_up[tid] = up; }
+            if (!__syncthreads_or(node && up != 0)) break;
+            if (node) {
+                const uint4 more = s_path[up];
+                path.x |= more.x; path.y |= more.y; path.z |= more.z; path.w |= more.w;
+                up = s_up[up];
+            }
+            __syncthreads();
+        }
+        if (!node) return;
+        path.x |= 1u;                                          // (the root is on every path)
+        for (int j = 0; j < nn; ++j) {
+            const uint32_t bit = s_tok[j] == tok ? 1u << (j & 31) : 0;
+            (j < 32 ? same.x : j < 64 ? same.y : j < 96 ? same.z : same.w) |= bit;
+        }
+        trees[s].path[tid] = path;
+        trees[s].same[tid] = same;
+        return;
     }
-    const bool bad = __syncthreads_or(no_tree);
-    if (tid == 0 && blockIdx.x == 0 && blockIdx.y == 0 && (bad || bad_len))
-        atomicOr(&a.status[s], (bad ? GOOSE_ST_BAD_PARENT : 0) | (bad_len ? GOOSE_ST_BAD_ROWS : 0));
+    if (nn == 0) return;
+    const int base = blockIdx.x * kVocab;
+    static_assert(kVocab == 4 * kCountThreads, "a store a thread");
+    reinterpret_cast<uint4*>(s_count)[tid] = make_uint4(0, 0, 0, 0);
+    int len = a.hist_len[s];
+    const int prompt = a.n_prompt ? a.n_prompt[s] : 0;
+    if (len < 0 || len > a.ldh) len = 0;
+    __syncthreads();
     auto count = [&](int t, int j) {
         const uint32_t u = (uint32_t)(t - base);
         if (u < (uint32_t)kVocab) {
@@ -79,7 +118,7 @@ adjust_logits_kernel(const AdjustLogits a, int rows_per_block) {
         const int4* h4 = reinterpret_cast<const int4*>(hist + head);
         const int quads = (len - head) >> 2;
 #pragma unroll 4
-        for (int j = tid; j < quads; j += kAdjustThreads) {
+        for (int j = tid; j < quads; j += kCountThreads) {
             const int4 t = h4[j];
             const int at = head + 4 * j;
             count(t.x, at); count(t.y, at + 1); count(t.z, at + 2); count(t.w, at + 3);
@@ -87,124 +126,121 @@ adjust_logits_kernel(const AdjustLogits a, int rows_per_block) {
         const int tail = head + 4 * quads;
         if (tid < len - tail) count(hist[tail + tid], tail + tid);
     }
-    if (!bad) {
-        if (node && (uint32_t)tok < (uint32_t)kVocab) {
-            uint4 same = make_uint4(0, 0, 0, 0);
-            for (int j = 0; j < nn; ++j) {
-                const uint32_t bit = s_tok[j] == tok ? 1u << (j & 31) : 0;
-                (j < 32 ? same.x : j < 64 ? same.y : j < 96 ? same.z : same.w) |= bit;
-            }
-            s_same[tid] = same;
-            s_list[atomicAdd(&s_listed, 1)] = (unsigned char)tid;   // (in any order: each pair writes an element of its own)
-        }
-        // paths, in steps up the tree that double
-        for (int reach = 1; reach < kMaxB; reach *= 2) {
-            if (node) { s_path[tid] = path; s_up[tid] = up; }
-            if (!__syncthreads_or(node && up != 0)) break;
-            if (node) {
-                const uint4 more = s_path[up];
-                path.x |= more.x; path.y |= more.y; path.z |= more.z; path.w |= more.w;
-                up = s_up[up];
-            }
-            __syncthreads();
-        }
-        if (node) { path.x |= 1u; s_path[tid] = path; }    // (the root is on every path)
-    }
     __syncthreads();
+    reinterpret_cast<uint4*>(words + (size_t)s * ldw + base)[tid] = reinterpret_cast<const uint4*>(s_count)[tid];
+}
 
-    // ---- this thread's tokens
-    const int column = tid & (kAdjustColumns - 1), v0 = base + 8 * column, n_v = min(8, a.V - v0);
+__global__ void __launch_bounds__(kAdjustThreads, 4)
+adjust_logits_kernel(const AdjustLogits a, int rows_per_block, int64_t ldw, const uint32_t* __restrict__ words,
+                     const AdjustTree* __restrict__ trees) {
+    __shared__ __nv_bfloat16 s_logit[kBlockRows * kMaxB];      // the pairs' logits: the stream may write over them
+    __shared__ unsigned char s_list[kMaxB];                    // nodes whose token lies in this piece of the vocabulary
+    __shared__ short s_tok[kMaxB];                             // and where
+    __shared__ int s_listed;
+    const int s = blockIdx.z, tid = threadIdx.x, base = blockIdx.x * kVocab;
+    const int v0 = base + 8 * tid, n_v = min(8, a.V - v0);
+    // The first kernel has waited for all that is in front of it and writes none of the inputs: they are read ahead of the wait.
+    const int nn = nodes_of(a.n_nodes, s, a.B);
+    const int i0 = blockIdx.y * rows_per_block, i1 = min(i0 + rows_per_block, nn);
+    const size_t row0 = (size_t)s * a.B + i0;
+    const int rows = i1 - i0;
+    const __nv_bfloat16* from = a.logits + row0 * a.ldl + v0;
+    const unsigned char* open_at = reinterpret_cast<const unsigned char*>(a.mask + row0 * a.ldm) + (v0 >> 3);
+    uint4 x[kAdjustRows];
+    uint32_t open[kAdjustRows];
+    auto load = [&](int left) {
+#pragma unroll
+        for (int u = 0; u < kAdjustRows; ++u) {
+            open[u] = 0xFFu;
+            if (u < left && n_v > 0) {
+                x[u] = *reinterpret_cast<const uint4*>(from);
+                if (a.mask) open[u] = *open_at;
+                from += a.ldl;
+                open_at += 4 * a.ldm;
+            }
+        }
+    };
+    load(rows);
+    if (tid == 0) s_listed = 0;
+    const int tok = tid < nn && a.draft_tok ? a.draft_tok[(size_t)s * a.B + tid] - base : -1;
     const float rep = a.repetition ? a.repetition[s] : 1.f, freq = a.frequency ? a.frequency[s] : 0.f, pres = a.presence ? a.presence[s] : 0.f;
     const float inv_rep = 1.f / rep;
     const float* bias = a.bias ? a.bias + (size_t)s * a.bias_stride : nullptr;
-    float add[8];
-    uint32_t seen = 0;
+    // x' = x * (x > 0 ? up : down) + add
+    float add[8], m_up[8], m_down[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const uint32_t word = s_count[8 * column + e], n = word & ~kInPrompt;
-        if (word) seen |= 1u << e;
-        add[e] = bias && e < n_v ? bias[v0 + e] : 0.f;
-        if (n) add[e] += -freq * (float)n - pres;
+    for (int e = 0; e < 8; ++e) add[e] = bias && e < n_v ? bias[v0 + e] : 0.f;
+    __syncthreads();
+    if ((uint32_t)tok < (uint32_t)kVocab) {
+        const int k = atomicAdd(&s_listed, 1);                 // (in any order: each pair writes an element of its own)
+        s_list[k] = (unsigned char)tid;
+        s_tok[k] = (short)tok;
     }
-
-    // ---- rows, in batches of as many as a batch's pairs allow
-    const int listed = s_listed, batch = listed ? max(1, kPathTasks * kAdjustThreads / listed) : i1 - i0;
-    const size_t row0 = (size_t)s * a.B;
-    for (int b0 = i0; b0 < i1; b0 += batch) {
-        const int b1 = min(b0 + batch, i1);
-        // what the pairs make of their logits, read ahead of the stream, which may write them in place
-        float fixed[kPathTasks];
-        int fixed_row[kPathTasks], fixed_tok[kPathTasks];
+    __syncthreads();
+    pdl_wait();
+    pdl_trigger();
+    if (rows <= 0) return;
+    const AdjustTree& tree = trees[s];
+    const bool bad = tree.bad != 0;
+    const uint32_t* w = words ? words + (size_t)s * ldw + base : nullptr;
 #pragma unroll
-        for (int u = 0; u < kPathTasks; ++u) {
-            const int task = tid + u * kAdjustThreads, of_row = listed ? task / listed : 0, i = b0 + of_row;
-            fixed_row[u] = -1;
-            if (listed && i < b1) {
-                const int j = s_list[task - of_row * listed], t = s_tok[j], v = base + t;
-                const uint4 anc = s_path[i], same = s_same[j];
-                uint32_t n = 0;
-                int first = kMaxB;
+    for (int e = 0; e < 8; e += 4) {
+        const uint4 w4 = w ? *reinterpret_cast<const uint4*>(w + 8 * tid + e) : make_uint4(0, 0, 0, 0);
+        const uint32_t word[4] = {w4.x, w4.y, w4.z, w4.w};
 #pragma unroll
-                for (int w = 3; w >= 0; --w) {
-                    const uint32_t here = common(anc, same, w);
-                    n += __popc(here);
-                    if (here) first = 32 * w + __ffs(here) - 1;
+        for (int f = 0; f < 4; ++f) {
+            const uint32_t n = word[f] & ~kInPrompt;
+            m_up[e + f] = word[f] ? inv_rep : 1.f;
+            m_down[e + f] = word[f] ? rep : 1.f;
+            if (n) add[e + f] += -freq * (float)n - pres;
+        }
+    }
+    const int listed = bad ? 0 : s_listed, pairs = rows * listed;
+    for (int k = tid; k < pairs; k += kAdjustThreads) {
+        const int of_row = k / listed, l = k - of_row * listed, j = s_list[l], v = base + s_tok[l];
+        uint32_t n;
+        if (v < a.V && first_of_path(tree.path[i0 + of_row], tree.same[j], j, n)) s_logit[k] = a.logits[(row0 + of_row) * a.ldl + v];
+    }
+    if (listed) __syncthreads();
+    if (n_v > 0) {
+        __nv_bfloat16* to = a.out + row0 * a.ldo + v0;
+        for (int left = rows; left > 0; left -= kAdjustRows) {
+            if (left != rows) load(left);
+#pragma unroll
+            for (int u = 0; u < kAdjustRows; ++u) {
+                if (u >= left) break;
+                const uint32_t in[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
+                uint32_t out[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float y0 = __uint_as_float(in[e] << 16), y1 = __uint_as_float(in[e] & 0xFFFF0000u);
+                    y0 = fmaf(y0, y0 > 0.f ? m_up[2 * e] : m_down[2 * e], add[2 * e]);
+                    y1 = fmaf(y1, y1 > 0.f ? m_up[2 * e + 1] : m_down[2 * e + 1], add[2 * e + 1]);
+                    if (!(open[u] & (1u << (2 * e)))) y0 = -INFINITY;
+                    if (!(open[u] & (2u << (2 * e)))) y1 = -INFINITY;
+                    const __nv_bfloat162 b2 = __floats2bfloat162_rn(y0, y1);
+                    out[e] = bad ? 0u : *reinterpret_cast<const uint32_t*>(&b2);
                 }
-                // of a path's nodes with one token the first has the pair
-                if (first == j && v < a.V && !(a.mask && !((a.mask[(row0 + i) * a.ldm + (v >> 5)] >> (v & 31)) & 1u))) {
-                    const float l = __bfloat162float(a.logits[(row0 + i) * a.ldl + v]);
-                    n += s_count[t] & ~kInPrompt;
-                    fixed[u] = (l > 0.f ? l * inv_rep : l * rep) + ((bias ? bias[v] : 0.f) + (-freq * (float)n - pres));
-                    fixed_row[u] = i;
-                    fixed_tok[u] = v;
-                }
+                if (n_v == 8) *reinterpret_cast<uint4*>(to) = make_uint4(out[0], out[1], out[2], out[3]);
+                else
+#pragma unroll
+                    for (int e = 0; e < 7; ++e)
+                        if (e < n_v) reinterpret_cast<uint16_t*>(to)[e] = (uint16_t)(out[e >> 1] >> (16 * (e & 1)));
+                to += a.ldo;
             }
         }
-        if (listed) __syncthreads();
-        if (n_v > 0) {
-            for (int i = b0 + (tid >= kAdjustColumns); i < b1; i += 2 * kAdjustRows) {
-                uint4 x[kAdjustRows];
-                uint32_t open[kAdjustRows];
-#pragma unroll
-                for (int u = 0; u < kAdjustRows; ++u) {
-                    if (i + 2 * u < b1) {
-                        const size_t r = row0 + i + 2 * u;
-                        x[u] = *reinterpret_cast<const uint4*>(a.logits + r * a.ldl + v0);
-                        open[u] = a.mask ? reinterpret_cast<const unsigned char*>(a.mask + r * a.ldm)[v0 >> 3] : 0xFFu;
-                    }
-                }
-#pragma unroll
-                for (int u = 0; u < kAdjustRows; ++u) {
-                    if (i + 2 * u >= b1) break;
-                    const uint32_t in[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
-                    uint32_t out[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        float y[2] = {__uint_as_float(in[e] << 16), __uint_as_float(in[e] & 0xFFFF0000u)};
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            if ((seen >> (2 * e + h)) & 1u) y[h] = y[h] > 0.f ? y[h] * inv_rep : y[h] * rep;
-                            y[h] += add[2 * e + h];
-                            if (!((open[u] >> (2 * e + h)) & 1u)) y[h] = -INFINITY;
-                        }
-                        const __nv_bfloat162 b2 = __floats2bfloat162_rn(y[0], y[1]);
-                        out[e] = bad ? 0u : *reinterpret_cast<const uint32_t*>(&b2);
-                    }
-                    __nv_bfloat16* to = a.out + (row0 + i + 2 * u) * a.ldo + v0;
-                    if (n_v == 8) *reinterpret_cast<uint4*>(to) = make_uint4(out[0], out[1], out[2], out[3]);
-                    else
-#pragma unroll
-                        for (int e = 0; e < 7; ++e)
-                            if (e < n_v) reinterpret_cast<uint16_t*>(to)[e] = (uint16_t)(out[e >> 1] >> (16 * (e & 1)));
-                }
-            }
-        }
-        if (listed) {
-            __syncthreads();                           // the stream's stores are in front of these
-#pragma unroll
-            for (int u = 0; u < kPathTasks; ++u)
-                if (fixed_row[u] >= 0) a.out[(row0 + fixed_row[u]) * a.ldo + fixed_tok[u]] = __float2bfloat16_rn(fixed[u]);
-        }
+    }
+    if (!listed) return;
+    __syncthreads();                                           // the stream's stores are in front of these
+    for (int k = tid; k < pairs; k += kAdjustThreads) {
+        const int of_row = k / listed, l = k - of_row * listed, j = s_list[l], t = s_tok[l], v = base + t;
+        const size_t r = row0 + of_row;
+        uint32_t n;
+        if (v >= a.V || !first_of_path(tree.path[i0 + of_row], tree.same[j], j, n)) continue;
+        if (a.mask && !((a.mask[r * a.ldm + (v >> 5)] >> (v & 31)) & 1u)) continue;
+        if (w) n += w[t] & ~kInPrompt;
+        const float x1 = __bfloat162float(s_logit[k]);
+        a.out[r * a.ldo + v] = __float2bfloat16_rn((x1 > 0.f ? x1 * inv_rep : x1 * rep) + ((bias ? bias[v] : 0.f) + (-freq * (float)n - pres)));
     }
 }
 
@@ -212,21 +248,23 @@ cudaError_t launch_adjust_logits(goose_ctx* c, AdjustLogits a, int S, cudaStream
     if (S == 0) return cudaSuccess;
     a.status = c->status;
     const int pieces = (a.V + kVocab - 1) / kVocab;
-    // Blocks share a sequence's rows as ends earliest by this count: waves of two blocks an SM, each as long as its rows and what stands in
-    // front of them, worth about seven rows.
-    long long best = 0;
-    int groups = 1;
-    for (int n = 1; n <= a.B; ++n) {
-        const long long waves = ((long long)S * pieces * n + 2 * c->num_sms - 1) / (2 * c->num_sms), cost = waves * ((a.B + n - 1) / n + 7);
-        if (n == 1 || cost < best) { best = cost; groups = n; }
-    }
-    const int rows = (a.B + groups - 1) / groups;
-    const dim3 grid(pieces, (a.B + rows - 1) / rows, S);
-    cudaError_t e = launch_pdl(adjust_logits_kernel, grid, dim3(kAdjustThreads), 0, st, a, rows);
+    const bool counts = a.hist && (a.repetition || a.frequency || a.presence);
+    const int64_t ldw = counts ? (int64_t)pieces * kVocab : 0;
+    const size_t tree_bytes = sizeof(AdjustTree) * (size_t)S, need = tree_bytes + sizeof(uint32_t) * (size_t)ldw * S;
+    if (cudaError_t e = grow(&c->adjust_tables, &c->adjust_bytes, need)) return e;
+    AdjustTree* trees = static_cast<AdjustTree*>(c->adjust_tables);
+    uint32_t* words = counts ? reinterpret_cast<uint32_t*>(static_cast<char*>(c->adjust_tables) + tree_bytes) : nullptr;
+    cudaError_t e = launch_pdl(adjust_tables_kernel, dim3((counts ? pieces : 0) + 1, S), dim3(kCountThreads), 0, st, a, counts ? pieces : 0, ldw, words, trees);
+    c->launches++;
+    if (e != cudaSuccess) return e;
+    // rows of a block: kBlockRows, fewer where there would not be two blocks an SM
+    const long long all = (long long)S * pieces * a.B / (2LL * c->num_sms);
+    const int rows = all >= kBlockRows ? kBlockRows : all < 1 ? 1 : (int)all;
+    e = launch_pdl(adjust_logits_kernel, dim3(pieces, (a.B + rows - 1) / rows, S), dim3(kAdjustThreads), 0, st, a, rows, ldw, words, trees);
     c->launches++;
     return e;
 }
 
-cudaError_t init_adjust_kernel() { return load_kernels({(const void*)adjust_logits_kernel}); }
+cudaError_t init_adjust_kernel() { return load_kernels({(const void*)adjust_tables_kernel, (const void*)adjust_logits_kernel}); }
 
 }  // namespace goose

@@ -201,7 +201,7 @@ int goose_destroy(goose_ctx* c) {
     cudaSetDevice(c->device);
     cudaFree(c->partials); cudaFree(c->head_counters); cudaFree(c->topk_cand);
     cudaFree(c->row_counters); cudaFree(c->topk_lse_ws); cudaFree(c->status); cudaFree(c->selftest_word); cudaFree(c->stage);
-    cudaFree(c->shared_parts);
+    cudaFree(c->shared_parts); cudaFree(c->adjust_tables);
     if (c->pin) cudaFreeHost(c->pin);
     if (c->side) cudaStreamDestroy(c->side);
     if (c->ev_fork) cudaEventDestroy(c->ev_fork);
@@ -380,6 +380,7 @@ int goose_adjust_logits(goose_ctx* c, const void* logits, int64_t ldl, int S, in
     a.repetition = repetition; a.frequency = frequency; a.presence = presence; a.bias = bias; a.bias_stride = bias_stride;
     a.mask = mask; a.ldm = ldm; a.out = (__nv_bfloat16*)out; a.ldo = ldo;
     cudaError_t e = goose::launch_adjust_logits(c, a, S, static_cast<cudaStream_t>(stream));
+    if (e == cudaErrorMemoryAllocation) return GOOSE_ENOMEM;
     if (e != cudaSuccess) return cuda_fail(e);
     return GOOSE_OK;
 }

@@ -9,7 +9,7 @@
 //
 // What bounds it: a row of 256 bytes in, one out, and some 60 instructions for 16 bytes: HBM in long calls, the chain
 // ctx_len -> table row -> store in short ones.  16 lanes have a row (8 elements, one 16-byte load a lane), so that the norm is four
-// shuffles and the partner of a half-split pair another lane's element of the same place; a group of 16 lanes takes up to
+// shuffles and the partner of a half-split pair another lane's element of the same place; a group of 16 lanes takes
 // kRows rows of one token at a time, whose loads are all in flight together, and keeps the token's cosines and sines in registers.
 #include "goose_internal.cuh"
 
@@ -59,15 +59,33 @@ __device__ __forceinline__ bool tree_depths(const int32_t* __restrict__ parent, 
 
 // kTree: positions by the depth in a tree, else by the place in a run of tokens
 template <bool kTree>
-__global__ void __launch_bounds__(kAppendThreads)
+__global__ void __launch_bounds__(kAppendThreads, kTree ? 3 : 4)
 append_kv_kernel(const AppendKv a, int groups_log2 /* groups of 16 lanes a token */) {
     __shared__ int s_up[kMaxB], s_depth[kMaxB];
     const int s = blockIdx.y, lane = threadIdx.x & 15, group = threadIdx.x >> 4;
     const int per_token = 1 << groups_log2;
     const int first = blockIdx.x * (kAppendGroups >> groups_log2);
     const int i = first + (group >> groups_log2);              // token of this group
+    const int H = a.H, Hkv = a.Hkv, rows = H + 2 * Hkv;
+    const size_t tok = (size_t)s * a.B + i;
     pdl_wait();
     pdl_trigger();
+    // rows r, r + per_token, ... of the token; they depend on no length, so the first leave ahead of everything
+    auto load = [&](int r0, uint4 (&x)[kRows]) {
+#pragma unroll
+        for (int u = 0; u < kRows; ++u) {
+            const int r = r0 + u * per_token;
+            if (r < rows) {
+                const __nv_bfloat16* from = r < H ? a.q + tok * a.ldq + r * kHeadDim
+                                          : r < H + Hkv ? a.k + tok * a.ldk + (r - H) * kHeadDim
+                                                        : a.v + tok * a.ldv + (r - H - Hkv) * kHeadDim;
+                x[u] = reinterpret_cast<const uint4*>(from)[lane];
+            }
+        }
+    };
+    uint4 x[kRows];
+    const int r_first = group & (per_token - 1);
+    if (i < a.B) load(r_first, x);
     const int nn = nodes_of(a.n_nodes, s, a.B);
     if (blockIdx.x == 0 && threadIdx.x == 0 && nodes_bad(a.n_nodes, s, a.B)) atomicOr(&a.status[s], GOOSE_ST_BAD_NODES);
     if (first >= nn) return;
@@ -83,7 +101,7 @@ append_kv_kernel(const AppendKv a, int groups_log2 /* groups of 16 lanes a token
     if (i >= nn) return;                                       // (whole groups: the shuffles below name their 16 lanes)
     const int64_t pos = pos0 + depth;
     if (a.rope_dim && (pos < 0 || pos >= a.rope_rows)) flaw |= GOOSE_ST_BAD_POS;
-    if (flaw && lane == 0 && (group & (per_token - 1)) == 0) atomicOr(&a.status[s], flaw);
+    if (flaw && lane == 0 && r_first == 0) atomicOr(&a.status[s], flaw);
 
     const int half = a.rope_dim >> 1;
     // cosines and sines of this lane's elements, and the lane that has their partners (half-split pairs)
@@ -109,25 +127,10 @@ append_kv_kernel(const AppendKv a, int groups_log2 /* groups of 16 lanes a token
             }
         }
     }
-    const uint4 zero = make_uint4(0, 0, 0, 0);
-    const uint4 wq = a.q_weight ? reinterpret_cast<const uint4*>(a.q_weight)[lane] : zero;
-    const uint4 wk = a.k_weight ? reinterpret_cast<const uint4*>(a.k_weight)[lane] : zero;
     const uint32_t mask = 0xFFFFu << (threadIdx.x & 16);
-    const size_t tok = (size_t)s * a.B + i;
-    const int H = a.H, Hkv = a.Hkv, rows = H + 2 * Hkv;
     const size_t cache_row = ((size_t)row0 + ctx + i) * Hkv;
-    for (int r0 = group & (per_token - 1); r0 < rows; r0 += kRows * per_token) {
-        uint4 x[kRows];
-#pragma unroll
-        for (int u = 0; u < kRows; ++u) {
-            const int r = r0 + u * per_token;
-            if (r < rows) {
-                const __nv_bfloat16* from = r < H ? a.q + tok * a.ldq + (size_t)r * kHeadDim
-                                          : r < H + Hkv ? a.k + tok * a.ldk + (size_t)(r - H) * kHeadDim
-                                                        : a.v + tok * a.ldv + (size_t)(r - H - Hkv) * kHeadDim;
-                x[u] = reinterpret_cast<const uint4*>(from)[lane];
-            }
-        }
+    for (int r0 = r_first; r0 < rows; r0 += kRows * per_token) {
+        if (r0 != r_first) load(r0, x);
 #pragma unroll
         for (int u = 0; u < kRows; ++u) {
             const int r = r0 + u * per_token;
@@ -135,22 +138,23 @@ append_kv_kernel(const AppendKv a, int groups_log2 /* groups of 16 lanes a token
             uint4* to = r < H ? reinterpret_cast<uint4*>(a.q_out + (tok * H + r) * kHeadDim)
                       : r < H + Hkv ? reinterpret_cast<uint4*>(a.k_cache + (cache_row + r - H) * kHeadDim)
                                     : reinterpret_cast<uint4*>(a.v_cache + (cache_row + r - H - Hkv) * kHeadDim);
+            const bool is_q = r < H;
             if (flaw) {                                        // queries of zeros, no row of the cache touched
-                if (r < H) to[lane] = zero;
+                if (is_q) to[lane] = make_uint4(0, 0, 0, 0);
                 continue;
             }
-            const bool is_q = r < H;
             if (r < H + Hkv) {
                 float y[8];
                 unpack8(x[u], y);
-                if (is_q ? a.q_weight != nullptr : a.k_weight != nullptr) {
+                const __nv_bfloat16* weight = is_q ? a.q_weight : a.k_weight;
+                if (weight) {
                     float ss = 0.f, w[8];
 #pragma unroll
                     for (int e = 0; e < 8; ++e) ss = fmaf(y[e], y[e], ss);
 #pragma unroll
                     for (int o = 8; o > 0; o >>= 1) ss += __shfl_xor_sync(mask, ss, o, 16);
                     const float inv = rsqrtf(ss * (1.f / kHeadDim) + a.eps);
-                    unpack8(is_q ? wq : wk, w);
+                    unpack8(reinterpret_cast<const uint4*>(weight)[lane], w);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) y[e] = y[e] * inv * w[e];
                 }
@@ -178,10 +182,11 @@ append_kv_kernel(const AppendKv a, int groups_log2 /* groups of 16 lanes a token
 cudaError_t launch_append_kv(goose_ctx* c, AppendKv a, int S, cudaStream_t st) {
     if (S == 0) return cudaSuccess;
     a.status = c->status;
-    // groups a token: as many as leave each kRows rows, a block of one token at most
+    // groups a token: as few as give every SM three blocks (a token's lengths, tree and table row are then looked up for more rows),
+    // at most as many as leave each kRows rows, and a block of one token
     const int rows = a.H + 2 * a.Hkv;
     int lg = 0;
-    while ((1 << lg) < kAppendGroups && (kRows << lg) < rows) ++lg;
+    while ((1 << lg) < kAppendGroups && (kRows << lg) < rows && (((long long)S * a.B) << lg) < 3LL * kAppendGroups * c->num_sms) ++lg;
     const int per_block = kAppendGroups >> lg;
     const dim3 grid((a.B + per_block - 1) / per_block, S);
     cudaError_t e = launch_pdl(a.parent ? append_kv_kernel<true> : append_kv_kernel<false>, grid, dim3(kAppendThreads), 0, st, a, lg);

@@ -36,8 +36,11 @@ struct goose_ctx {
     int64_t topk_cand_cap;    // elements
     int topk_rows_cap;
     // partial results of the shared-prefix attention: made by the first call that needs them, and again by one that needs more
-    float* shared_parts;
+    void* shared_parts;
     size_t shared_bytes;
+    // words and trees of goose_adjust_logits: likewise
+    void* adjust_tables;
+    size_t adjust_bytes;
     // per-sequence status words
     int32_t* status;          // [max_S]
     int32_t* selftest_word;   // result word of goose_selftest_bounded_wait
@@ -262,6 +265,17 @@ cudaError_t launch_bounded_wait_selftest(goose_ctx* c, long long limit_cycles, i
 
 // split count of the mma kernel's fixed grid: ctx_len lives on the device, so it depends only on S, H and the SM count
 int mma_splits(const goose_ctx* c, int S, int H);
+
+// a workspace that a call needs `need` bytes of (the old one is freed, which waits for whatever uses it)
+inline cudaError_t grow(void** p, size_t* bytes, size_t need) {
+    if (need <= *bytes) return cudaSuccess;
+    cudaFree(*p);
+    *p = nullptr; *bytes = 0;
+    cudaError_t e = cudaMalloc(p, need);
+    if (e != cudaSuccess) { cudaGetLastError(); return e; }
+    *bytes = need;
+    return cudaSuccess;
+}
 
 // Called once from goose_create: the kernels are loaded, with their attributes (dynamic shared memory limits), those of a step next to one
 // another and the two that no step runs behind them.  Where a kernel's code lies is decided by the order of loading, and three short kernels
