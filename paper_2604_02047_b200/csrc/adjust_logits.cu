@@ -19,7 +19,6 @@ namespace goose {
 
 constexpr int kAdjustThreads = 256;
 constexpr int kVocab = 8 * kAdjustThreads;           // tokens of a block
-constexpr int kAdjustRows = 4;                       // rows of a thread in flight
 constexpr int kBlockRows = 8;                        // rows of a block, at most
 constexpr int kCountThreads = 512;
 constexpr uint32_t kInPrompt = 0x80000000u;          // of a token's word: it occurs in the prompt; below: its count behind it
@@ -130,53 +129,66 @@ adjust_tables_kernel(const AdjustLogits a, int pieces, int64_t ldw, uint32_t* __
     reinterpret_cast<uint4*>(words + (size_t)s * ldw + base)[tid] = reinterpret_cast<const uint4*>(s_count)[tid];
 }
 
+// bulk copy into shared memory: size a multiple of 16, both addresses too
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, unsigned long long* bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src), "r"(bytes), "r"((uint32_t)__cvta_generic_to_shared(bar)) : "memory");
+}
+
+// kMask: a mask is given
+template <bool kMask>
 __global__ void __launch_bounds__(kAdjustThreads, 4)
 adjust_logits_kernel(const AdjustLogits a, int rows_per_block, int64_t ldw, const uint32_t* __restrict__ words,
                      const AdjustTree* __restrict__ trees) {
-    __shared__ __nv_bfloat16 s_logit[kBlockRows * kMaxB];      // the pairs' logits: the stream may write over them
-    __shared__ unsigned char s_list[kMaxB];                    // nodes whose token lies in this piece of the vocabulary
-    __shared__ short s_tok[kMaxB];                             // and where
+    __shared__ __align__(128) uint4 s_row[kBlockRows][kAdjustThreads];   // the block's logits as they were
+    __shared__ unsigned long long s_full;
+    __shared__ volatile int s_abort;
     __shared__ int s_listed;
+    __shared__ short s_tok[kMaxB];                             // nodes whose token lies in this piece of the vocabulary: where
+    __shared__ unsigned char s_list[kMaxB];                    // and which
     const int s = blockIdx.z, tid = threadIdx.x, base = blockIdx.x * kVocab;
     const int v0 = base + 8 * tid, n_v = min(8, a.V - v0);
     // The first kernel has waited for all that is in front of it and writes none of the inputs: they are read ahead of the wait.
     const int nn = nodes_of(a.n_nodes, s, a.B);
-    const int i0 = blockIdx.y * rows_per_block, i1 = min(i0 + rows_per_block, nn);
+    const int i0 = blockIdx.y * rows_per_block, rows = min(rows_per_block, nn - i0);
     const size_t row0 = (size_t)s * a.B + i0;
-    const int rows = i1 - i0;
-    const __nv_bfloat16* from = a.logits + row0 * a.ldl + v0;
-    const unsigned char* open_at = reinterpret_cast<const unsigned char*>(a.mask + row0 * a.ldm) + (v0 >> 3);
-    uint4 x[kAdjustRows];
-    uint32_t open[kAdjustRows];
-    auto load = [&](int left) {
-#pragma unroll
-        for (int u = 0; u < kAdjustRows; ++u) {
-            open[u] = 0xFFu;
-            if (u < left && n_v > 0) {
-                x[u] = *reinterpret_cast<const uint4*>(from);
-                if (a.mask) open[u] = *open_at;
-                from += a.ldl;
-                open_at += 4 * a.ldm;
-            }
+    if (tid == 0) {
+        s_listed = 0;
+        s_abort = 0;
+        if (rows > 0) {
+            const uint32_t bar = (uint32_t)__cvta_generic_to_shared(&s_full), bytes = 16u * ((min(kVocab, a.V - base) + 7) / 8);
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar));
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+            asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes * rows) : "memory");
+            for (int u = 0; u < rows; ++u) bulk_load(s_row[u], a.logits + (row0 + u) * a.ldl + base, bytes, &s_full);
         }
-    };
-    load(rows);
-    if (tid == 0) s_listed = 0;
-    const int tok = tid < nn && a.draft_tok ? a.draft_tok[(size_t)s * a.B + tid] - base : -1;
+    }
+    uint32_t open[2] = {0, 0};                                 // a byte a row
+    if (kMask && n_v > 0) {
+        const unsigned char* at = reinterpret_cast<const unsigned char*>(a.mask + row0 * a.ldm) + (v0 >> 3);
+#pragma unroll
+        for (int u = 0; u < kBlockRows; ++u)
+            if (u < rows) open[u >> 2] |= (uint32_t)at[(size_t)u * 4 * a.ldm] << (8 * (u & 3));
+    }
+    const int tok = tid < nn && rows > 0 && a.draft_tok ? a.draft_tok[(size_t)s * a.B + tid] - base : -1;
     const float rep = a.repetition ? a.repetition[s] : 1.f, freq = a.frequency ? a.frequency[s] : 0.f, pres = a.presence ? a.presence[s] : 0.f;
     const float inv_rep = 1.f / rep;
-    const float* bias = a.bias ? a.bias + (size_t)s * a.bias_stride : nullptr;
+    const float* bias = a.bias ? a.bias + (size_t)s * a.bias_stride + base : nullptr;
     // x' = x * (x > 0 ? up : down) + add
     float add[8], m_up[8], m_down[8];
+    if (bias && n_v == 8 && (reinterpret_cast<uintptr_t>(bias) & 15) == 0) {
+        *reinterpret_cast<float4*>(add) = reinterpret_cast<const float4*>(bias)[2 * tid];
+        *reinterpret_cast<float4*>(add + 4) = reinterpret_cast<const float4*>(bias)[2 * tid + 1];
+    } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) add[e] = bias && e < n_v ? bias[v0 + e] : 0.f;
+        for (int e = 0; e < 8; ++e) add[e] = bias && e < n_v ? bias[8 * tid + e] : 0.f;
+    }
     __syncthreads();
     if ((uint32_t)tok < (uint32_t)kVocab) {
         const int k = atomicAdd(&s_listed, 1);                 // (in any order: each pair writes an element of its own)
         s_list[k] = (unsigned char)tid;
         s_tok[k] = (short)tok;
     }
-    __syncthreads();
     pdl_wait();
     pdl_trigger();
     if (rows <= 0) return;
@@ -195,52 +207,50 @@ adjust_logits_kernel(const AdjustLogits a, int rows_per_block, int64_t ldw, cons
             if (n) add[e + f] += -freq * (float)n - pres;
         }
     }
-    const int listed = bad ? 0 : s_listed, pairs = rows * listed;
-    for (int k = tid; k < pairs; k += kAdjustThreads) {
-        const int of_row = k / listed, l = k - of_row * listed, j = s_list[l], v = base + s_tok[l];
-        uint32_t n;
-        if (v < a.V && first_of_path(tree.path[i0 + of_row], tree.same[j], j, n)) s_logit[k] = a.logits[(row0 + of_row) * a.ldl + v];
+    const int arrived = mbar_wait_bounded(&s_full, 0, 2000000000ll, &s_abort);
+    if (arrived == 2) {                                        // (nothing raises the flag: every thread finds out for itself)
+        atomicOr(&a.status[s], GOOSE_ST_TIMEOUT);
+        return;
     }
-    if (listed) __syncthreads();
     if (n_v > 0) {
         __nv_bfloat16* to = a.out + row0 * a.ldo + v0;
-        for (int left = rows; left > 0; left -= kAdjustRows) {
-            if (left != rows) load(left);
+#pragma unroll 2
+        for (int u = 0; u < rows; ++u, to += a.ldo) {
+            const uint4 x = s_row[u][tid];
+            const uint32_t in[4] = {x.x, x.y, x.z, x.w};
+            const uint32_t m = kMask ? (u < 4 ? open[0] : open[1]) >> (8 * (u & 3)) : 0;
+            uint32_t out[4];
 #pragma unroll
-            for (int u = 0; u < kAdjustRows; ++u) {
-                if (u >= left) break;
-                const uint32_t in[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
-                uint32_t out[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float y0 = __uint_as_float(in[e] << 16), y1 = __uint_as_float(in[e] & 0xFFFF0000u);
-                    y0 = fmaf(y0, y0 > 0.f ? m_up[2 * e] : m_down[2 * e], add[2 * e]);
-                    y1 = fmaf(y1, y1 > 0.f ? m_up[2 * e + 1] : m_down[2 * e + 1], add[2 * e + 1]);
-                    if (!(open[u] & (1u << (2 * e)))) y0 = -INFINITY;
-                    if (!(open[u] & (2u << (2 * e)))) y1 = -INFINITY;
-                    const __nv_bfloat162 b2 = __floats2bfloat162_rn(y0, y1);
-                    out[e] = bad ? 0u : *reinterpret_cast<const uint32_t*>(&b2);
+            for (int e = 0; e < 4; ++e) {
+                float y0 = __uint_as_float(in[e] << 16), y1 = __uint_as_float(in[e] & 0xFFFF0000u);
+                y0 = fmaf(y0, y0 > 0.f ? m_up[2 * e] : m_down[2 * e], add[2 * e]);
+                y1 = fmaf(y1, y1 > 0.f ? m_up[2 * e + 1] : m_down[2 * e + 1], add[2 * e + 1]);
+                if (kMask) {
+                    if (!(m & (1u << (2 * e)))) y0 = -INFINITY;
+                    if (!(m & (2u << (2 * e)))) y1 = -INFINITY;
                 }
-                if (n_v == 8) *reinterpret_cast<uint4*>(to) = make_uint4(out[0], out[1], out[2], out[3]);
-                else
-#pragma unroll
-                    for (int e = 0; e < 7; ++e)
-                        if (e < n_v) reinterpret_cast<uint16_t*>(to)[e] = (uint16_t)(out[e >> 1] >> (16 * (e & 1)));
-                to += a.ldo;
+                const __nv_bfloat162 b2 = __floats2bfloat162_rn(y0, y1);
+                out[e] = *reinterpret_cast<const uint32_t*>(&b2);
             }
+            if (bad) out[0] = out[1] = out[2] = out[3] = 0;
+            if (n_v == 8) *reinterpret_cast<uint4*>(to) = make_uint4(out[0], out[1], out[2], out[3]);
+            else
+#pragma unroll
+                for (int e = 0; e < 7; ++e)
+                    if (e < n_v) reinterpret_cast<uint16_t*>(to)[e] = (uint16_t)(out[e >> 1] >> (16 * (e & 1)));
         }
     }
-    if (!listed) return;
-    __syncthreads();                                           // the stream's stores are in front of these
+    __syncthreads();                                           // the list is complete, the stream's stores are in front of these
+    const int listed = bad ? 0 : s_listed, pairs = rows * listed;
     for (int k = tid; k < pairs; k += kAdjustThreads) {
         const int of_row = k / listed, l = k - of_row * listed, j = s_list[l], t = s_tok[l], v = base + t;
         const size_t r = row0 + of_row;
         uint32_t n;
         if (v >= a.V || !first_of_path(tree.path[i0 + of_row], tree.same[j], j, n)) continue;
-        if (a.mask && !((a.mask[r * a.ldm + (v >> 5)] >> (v & 31)) & 1u)) continue;
+        if (kMask && !((a.mask[r * a.ldm + (v >> 5)] >> (v & 31)) & 1u)) continue;
         if (w) n += w[t] & ~kInPrompt;
-        const float x1 = __bfloat162float(s_logit[k]);
-        a.out[r * a.ldo + v] = __float2bfloat16_rn((x1 > 0.f ? x1 * inv_rep : x1 * rep) + ((bias ? bias[v] : 0.f) + (-freq * (float)n - pres)));
+        const float x1 = __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(s_row[of_row])[t]);
+        a.out[r * a.ldo + v] = __float2bfloat16_rn((x1 > 0.f ? x1 * inv_rep : x1 * rep) + ((bias ? bias[t] : 0.f) + (-freq * (float)n - pres)));
     }
 }
 
@@ -260,11 +270,11 @@ cudaError_t launch_adjust_logits(goose_ctx* c, AdjustLogits a, int S, cudaStream
     // rows of a block: kBlockRows, fewer where there would not be two blocks an SM
     const long long all = (long long)S * pieces * a.B / (2LL * c->num_sms);
     const int rows = all >= kBlockRows ? kBlockRows : all < 1 ? 1 : (int)all;
-    e = launch_pdl(adjust_logits_kernel, dim3(pieces, (a.B + rows - 1) / rows, S), dim3(kAdjustThreads), 0, st, a, rows, ldw, words, trees);
+    e = launch_pdl(a.mask ? adjust_logits_kernel<true> : adjust_logits_kernel<false>, dim3(pieces, (a.B + rows - 1) / rows, S), dim3(kAdjustThreads), 0, st, a, rows, ldw, words, trees);
     c->launches++;
     return e;
 }
 
-cudaError_t init_adjust_kernel() { return load_kernels({(const void*)adjust_tables_kernel, (const void*)adjust_logits_kernel}); }
+cudaError_t init_adjust_kernel() { return load_kernels({(const void*)adjust_tables_kernel, (const void*)adjust_logits_kernel<false>, (const void*)adjust_logits_kernel<true>}); }
 
 }  // namespace goose
