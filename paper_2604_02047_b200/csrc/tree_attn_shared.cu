@@ -1,19 +1,21 @@
 // Tree attention of a batch whose sequences share a long prefix: the shared rows are streamed once for 256 query rows of all
 // sequences, every sequence's own rows (its prefix and its tree) once for its own queries, and the two are merged by their
-// log-sum-exp:  out = sum_p 2^(e_p - M) x_p / sum_p 2^(e_p - M),  x_p the normalised result over the keys of part p, e_p the logarithm
-// (base 2) of its sum of exponentials, M the largest e_p.
+// maxima and sums:  out = sum_p 2^(m_p - M) O_p / sum_p 2^(m_p - M) l_p,  where O_p = sum_j 2^(x_j - m_p) v_j and l_p = sum_j 2^(x_j - m_p) over
+// the keys of part p, x_j the scaled scores (base 2), M the largest m_p.
 //
 // Main kernel: persistent, one CTA an SM, tcgen05 with TMEM accumulators, TMA loads, mbarrier pipeline; work list and lanes:
 // shared_work.cuh.  A sequence's own rows are never met by another sequence's queries, not even masked: what they hold (infinities, NaN)
 // stays in that sequence.  Roles (384 threads):
 //   warp 0, lane 0    TMA producer: the queries of a segment, then K and V tiles into a ring of 32 KB stages
-//   warp 1, lane 0    MMA issuer: S = Q K^T, O += P V, the two lanes in turn: while one lane's softmax runs, the tensor cores have the other's
-//                     products
+//   warps 1, 3        MMA issuers of lane 0 and of lane 1: S = Q K^T, O += P V; while one lane's softmax runs, the tensor cores have the
+//                     other's products
+//   warp 2            planner: walks the work list ahead of the others and puts the segments' descriptions into a ring, parents included
 //   warps 4..7, 8..11 softmax of lane 0 and of lane 1: one query row a thread: maximum, exponentials, P (bf16) over S in tensor
 //                     memory, lazy rescaling of O, at the segment's end the partial result into the workspace.
 // Tensor memory: S of both lanes in columns 0..255, O of both in 256..511.
 // Every wait is bounded: one that runs out raises the CTA's abort flag and GOOSE_ST_TIMEOUT, and every role unwinds.
 #include <cuda_fp16.h>
+#include <stddef.h>
 
 #include "goose_internal.cuh"
 #include "shared_work.cuh"
@@ -29,33 +31,53 @@ constexpr int kStageBytes = kSharedTile * kHeadDim * 2;      // 32 KB: one K or 
 constexpr int kHalfBytes = kSharedTile * 128;                // 16 KB: 128 rows x 64 bf16 (one swizzle-atom column)
 constexpr int kQBytes = 2 * kHalfBytes;
 constexpr int kHeaderBytes = 1024;
-constexpr int kSharedSmem = kHeaderBytes + 1024 /*alignment slack*/ + 2 * kQBytes + kStages * kStageBytes;
+constexpr int kSharedSmem = 1008 /*alignment slack*/ + 2 * kQBytes + kStages * kStageBytes + kHeaderBytes;
 constexpr int kSharedThreads = 384;
 // registers: 168 a thread at launch; the warps of the loads and products give 112 each to the others (56 + 2 x 224 = 3 x 168)
 constexpr int kRegsFew = 56, kRegsMany = 224;
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kColS = 0, kColO = 256;
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kByPolynomial = 2;                             // pairs of exponentials in eight
 constexpr float kRescaleThreshold = 8.0f;                    // rescale O only when the running max grew by > 2^8
 constexpr long long kWaitCycles = 2000000000ll;              // bound of every wait: about one second of SM clock
 
-// Partial result: x / scale as fp16, uint4 [16 groups of 8 columns][128 rows], then (e, scale) fp32 [128].  scale is the power of two of
-// the row's largest element, so that a row of any size has 11 bits of its largest elements (the output has 8);  0: a sequence that
-// cannot be computed (no tree, rows outside the cache).
+// Partial result of an M tile: O / scale as fp16, uint4 [16 groups of 8 columns][128 rows];  m fp32 [128], the maximum that the
+// exponentials are relative to (base 2);  (l, scale) fp32 [128], the exponentials' sum and the power of two of the row's largest element, so
+// that a row of any size has 11 bits of its largest elements (the output has 8).  l < 0: a sequence that cannot be computed (no
+// tree, rows outside the cache).
 constexpr int kPartWords = 16 * 128 * 4;
-constexpr int kPartFloats = kPartWords + 2 * 128;
+constexpr int kPartFloats = kPartWords + 3 * 128;
+
+// a segment, as the planner describes it
+struct Segment {
+    int n;                                                   // key tiles; 0: the end
+    int t_first;
+    int ctx, n_keys;                                         // keys in front of the tree, and all
+    int single, own;                                         // one M tile; a sequence's own rows
+    int hk, token;                                           // key/value head, first token of the first M tile
+    int row;                                                 // cache row of the first key tile
+    int slot;                                                // of lane 0's partial result
+    int rows[2];                                             // query rows of the M tiles
+    int node;                                                // tree node of the first M tile's first row
+    int bad;
+    int pad[2];
+};
+constexpr int kSegments = 3;
 
 struct Header {
+    Segment seg[kSegments];
+    signed char par[kSegments][kMaxB];                       // parent[] of the segment's sequence
     unsigned long long kv_full[kStages];
     unsigned long long kv_empty[kStages];
+    unsigned long long seg_full[kSegments], seg_empty[kSegments];
     unsigned long long q_full, q_empty;
-    unsigned long long s_full[2], p_ready[2], pv_done[2], o_free[2], group_bar[2];
+    unsigned long long s_full[2], p_ready[2], o_full[2], o_free[2];
     uint32_t tmem_base;
     volatile int abort_flag;
-    int bad[2];
-    signed char par[2][kMaxB];                               // parent[] of the current sequence, a copy a lane
 };
 static_assert(sizeof(Header) <= kHeaderBytes, "header");
+static_assert(kSharedSmem <= 232448, "shared memory of a block");
 
 struct SharedArgs {
     const int64_t* row_off;
@@ -81,6 +103,14 @@ __device__ __forceinline__ void drain(unsigned long long* bar, uint32_t parity) 
     const long long t0 = clock64();
     while (!mbar_try_wait(bar, parity) && clock64() - t0 < kWaitCycles) {}
 }
+
+// a place in a ring of n and its phase
+struct Ring {
+    uint32_t at, phase;
+    __device__ __forceinline__ void next(uint32_t n) {
+        if (++at == n) { at = 0; phase ^= 1; }
+    }
+};
 
 // the list's length and a place in it, by a whole warp (lane = sequence)
 __device__ __forceinline__ void locate(SharedWork& wk, SharedCursor& cu, long long& w_end, int cta, int lane) {
@@ -121,38 +151,63 @@ __device__ __forceinline__ void locate(SharedWork& wk, SharedCursor& cu, long lo
     }
 }
 
-// the item at the cursor: its key/value head, its M tiles and their first tokens
-struct Item {
-    int hk, m, tokens[2];
-    bool single;
-    __device__ __forceinline__ Item(const SharedArgs& a, const SharedCursor& cu) {
-        const bool shared = cu.s < 0;
-        const int pairs = shared ? a.wk.shared_pairs() : a.wk.own_pairs(), n_m = shared ? a.wk.shared_m : a.wk.own_m;
-        const int nb = shared ? a.shared_nb : a.own_nb;
-        hk = cu.i / pairs;
-        m = 2 * (cu.i - hk * pairs);
-        single = m + 1 >= n_m;
-        tokens[0] = (shared ? 0 : cu.s * a.wk.B) + m * nb;
-        tokens[1] = tokens[0] + nb;
+// 2^x of two numbers without the special function unit, which at 16 results a cycle and SM would take as long for a tile as the tensor
+// cores: x = n + f with n the nearest integer, 2^f on [-1/2, 1/2] by the cubic of least relative error (7.5e-5, from a Remez
+// exchange; P is rounded to 2^-9), n into the exponent.  Below 2^-126: 2^-126.
+__device__ __forceinline__ float2 ex2_by_polynomial(float2 x) {
+    constexpr float kMagic = 12582912.f;                     // 1.5 * 2^23: a sum with it has the nearest integer in its lowest bits
+    const unsigned long long xx = pack_f32x2(fmaxf(x.x, -126.f), fmaxf(x.y, -126.f));
+    const unsigned long long r = add_f32x2(xx, pack_f32x2(kMagic, kMagic)), n = add_f32x2(r, pack_f32x2(-kMagic, -kMagic));
+    const unsigned long long f = fma_f32x2(n, pack_f32x2(-1.f, -1.f), xx);
+    unsigned long long p = fma_f32x2(f, pack_f32x2(0.05517166852951f, 0.05517166852951f), pack_f32x2(0.24261112511158f, 0.24261112511158f));
+    p = fma_f32x2(p, f, pack_f32x2(0.69326096773148f, 0.69326096773148f));
+    p = fma_f32x2(p, f, pack_f32x2(0.99992805719376f, 0.99992805719376f));
+    const float2 pp = unpack_f32x2(p), rr = unpack_f32x2(r);
+    return make_float2(__uint_as_float(__float_as_uint(pp.x) + (__float_as_uint(rr.x) << 23)),
+                       __uint_as_float(__float_as_uint(pp.y) + (__float_as_uint(rr.y) << 23)));
+}
+
+// The same wait for the softmax warps, which have few registers to spare: 32-bit addresses and clock.
+__device__ __forceinline__ bool wait_at(uint32_t bar, uint32_t parity, uint32_t abort_flag, int32_t* status) {
+    auto done = [&]() {
+        uint32_t ok;
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                     : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+        return ok != 0;
+    };
+    if (done()) return true;
+    const uint32_t t0 = (uint32_t)clock();
+    for (;;) {
+        if (done()) return true;
+        uint32_t raised;
+        asm volatile("ld.volatile.shared.u32 %0, [%1];" : "=r"(raised) : "r"(abort_flag) : "memory");
+        if (raised) return false;
+        if ((uint32_t)clock() - t0 > (uint32_t)kWaitCycles) break;
     }
-};
+    asm volatile("st.volatile.shared.u32 [%0], %1;" ::"r"(abort_flag), "r"(1) : "memory");
+    atomicOr(status, GOOSE_ST_TIMEOUT);
+    return false;
+}
+__device__ __forceinline__ void arrive_at(uint32_t bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
 
 __global__ void __launch_bounds__(kSharedThreads, 1)
 tree_attn_shared_kernel(const __grid_constant__ CUtensorMap tmap_q_shared, const __grid_constant__ CUtensorMap tmap_q_own,
-                        const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const SharedArgs a) {
+                        const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
+                        const __grid_constant__ SharedArgs a) {
     extern __shared__ unsigned char smem_raw[];
-    Header* hd = reinterpret_cast<Header*>(smem_raw);
-    unsigned char* q_smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + kHeaderBytes + 1023) & ~(uintptr_t)1023);
+    unsigned char* q_smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     unsigned char* kv_smem = q_smem + 2 * kQBytes;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    Header* hd = reinterpret_cast<Header*>(kv_smem + kStages * kStageBytes);
+    const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
 
     if (threadIdx.x == 0) {
-        for (int i = 0; i < kStages; ++i) { mbar_init(&hd->kv_full[i], 1); mbar_init(&hd->kv_empty[i], 1); }
-        mbar_init(&hd->q_full, 1); mbar_init(&hd->q_empty, 1);
+        for (int i = 0; i < kStages; ++i) { mbar_init(&hd->kv_full[i], 1); mbar_init(&hd->kv_empty[i], 2); }
+        for (int i = 0; i < kSegments; ++i) { mbar_init(&hd->seg_full[i], 1); mbar_init(&hd->seg_empty[i], 3 + 8); }
+        mbar_init(&hd->q_full, 1); mbar_init(&hd->q_empty, 2);
         for (int l = 0; l < 2; ++l) {
-            mbar_init(&hd->s_full[l], 1); mbar_init(&hd->p_ready[l], 128); mbar_init(&hd->pv_done[l], 1);
-            mbar_init(&hd->o_free[l], 128); mbar_init(&hd->group_bar[l], 128);
-            hd->bad[l] = 0;
+            mbar_init(&hd->s_full[l], 1); mbar_init(&hd->p_ready[l], 4); mbar_init(&hd->o_full[l], 1); mbar_init(&hd->o_free[l], 4);
         }
         hd->abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -165,306 +220,343 @@ tree_attn_shared_kernel(const __grid_constant__ CUtensorMap tmap_q_shared, const
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = hd->tmem_base;
+    const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, hd->tmem_base, 0);
     pdl_wait();
     pdl_trigger();
 
-    SharedWork wk = a.wk;
-    if (wk.n_nodes && blockIdx.x == 0 && threadIdx.x == 33)
-        for (int s = 0; s < wk.S; ++s)
-            if (nodes_bad(wk.n_nodes, s, wk.B)) atomicOr(&a.status[s], GOOSE_ST_BAD_NODES);
-    SharedCursor cu;
-    long long w_end;
-    locate(wk, cu, w_end, blockIdx.x, lane);
-
-    if (cu.w < w_end) {
-      if (warp < 4) {
+    if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsFew));
-        if (warp == 0) {
+        if (warp == 2) {
+            // =========================================================== planner
+            SharedWork wk = a.wk;
+            if (wk.n_nodes && blockIdx.x == 0)
+                for (int s = lane; s < wk.S; s += 32)
+                    if (nodes_bad(wk.n_nodes, s, wk.B)) atomicOr(&a.status[s], GOOSE_ST_BAD_NODES);
+            SharedCursor cu;
+            long long w_end;
+            locate(wk, cu, w_end, blockIdx.x, lane);
+            Ring ring{0, 0};
+            for (;;) {
+                if (!wait_for(hd, &hd->seg_empty[ring.at], ring.phase ^ 1, a.status)) break;
+                const bool any = cu.w < w_end, shared = cu.s < 0;
+                Segment* sg = &hd->seg[ring.at];
+                if (any) {
+                    const int s = cu.s, n = cu.run(w_end);
+                    const int pairs = shared ? wk.shared_pairs() : wk.own_pairs(), n_m = shared ? wk.shared_m : wk.own_m;
+                    const int nb = shared ? a.shared_nb : a.own_nb;
+                    const int hk = cu.i / pairs, m = 2 * (cu.i - hk * pairs);
+                    const int nn = shared ? 0 : nodes_of(wk.n_nodes, s, wk.B), ctx = shared ? a.shared_len : wk.prefix(wk.ctx_len[s]);
+                    const int64_t row0 = shared ? a.shared_row : a.row_off[s];
+                    bool bad = false;
+                    if (!shared) {
+                        // a sequence of a parent[] that is no tree, or whose rows leave the cache: every part of it says so
+                        bool no_tree = false;
+                        for (int i = lane; i < nn; i += 32) {
+                            const int p = a.parent[(size_t)s * wk.B + i];
+                            hd->par[ring.at][i] = (signed char)p;
+                            no_tree |= i == 0 ? p != -1 : (p < 0 || p >= i);
+                        }
+                        no_tree = __any_sync(0xFFFFFFFFu, no_tree);
+                        const bool bad_rows = rows_outside(row0, wk.ctx_len[s], nn, wk.kv_rows);
+                        bad = no_tree || bad_rows;
+                        if (bad && lane == 0) atomicOr(&a.status[s], (no_tree ? GOOSE_ST_BAD_PARENT : 0) | (bad_rows ? GOOSE_ST_BAD_ROWS : 0));
+                    }
+                    if (lane == 0) {
+                        sg->n = n; sg->t_first = cu.t; sg->ctx = ctx; sg->n_keys = ctx + nn;
+                        sg->single = m + 1 >= n_m; sg->own = !shared; sg->hk = hk;
+                        sg->token = (shared ? 0 : s * wk.B) + m * nb;
+                        sg->row = (int)((uint64_t)row0 + (uint64_t)cu.t * kSharedTile);
+                        sg->slot = wk.slot(wk.item(s, cu.i), blockIdx.x, cu.t == 0, cu.t + n == cu.T, 0);
+                        const int left = shared ? wk.S * wk.B : nn;
+                        sg->rows[0] = max(min(nb, left - m * nb), 0) * a.g;
+                        sg->rows[1] = max(min(nb, left - (m + 1) * nb), 0) * a.g;
+                        sg->node = m * nb; sg->bad = bad;
+                    }
+                    cu.skip(wk, n);
+                } else if (lane == 0) {
+                    sg->n = 0;
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&hd->seg_full[ring.at]);
+                if (!any) break;
+                ring.next(kSegments);
+            }
+        } else if (warp == 0) {
             // =========================================================== TMA producer
             if (lane == 0) {
-                // the shared rows are read by many CTAs, a sequence's own by one or two
+                // a sequence's own rows are read by one or two CTAs, the shared ones by many
                 const unsigned long long pol_own = l2_policy_evict_first(), pol_shared = l2_policy_evict_last();
-                uint32_t ring = 0, st = 0, phase = 0, seg = 0;
+                uint32_t loads = 0, segs = 0;
+                Ring st{0, 0}, ring{0, 0};
                 bool ok = true;
-                while (ok && cu.w < w_end) {
-                    const Item it(a, cu);
-                    const bool shared = cu.s < 0;
-                    ok = wait_for(hd, &hd->q_empty, (seg & 1) ^ 1, a.status);
+                while (ok) {
+                    ok = wait_for(hd, &hd->seg_full[ring.at], ring.phase, a.status);
                     if (!ok) break;
-                    const int tiles_q = it.single ? 1 : 2;
-                    mbar_expect_tx(&hd->q_full, (uint32_t)(tiles_q * (shared ? a.shared_nb : a.own_nb) * a.g) * 256u);
-                    const CUtensorMap* mq = shared ? &tmap_q_shared : &tmap_q_own;
+                    const Segment sg = hd->seg[ring.at];
+                    mbar_arrive(&hd->seg_empty[ring.at]);
+                    ring.next(kSegments);
+                    if (sg.n == 0) break;
+                    ok = wait_for(hd, &hd->q_empty, (segs & 1) ^ 1, a.status);
+                    if (!ok) break;
+                    const int nb = sg.own ? a.own_nb : a.shared_nb, tiles_q = sg.single ? 1 : 2;
+                    mbar_expect_tx(&hd->q_full, (uint32_t)(tiles_q * nb * a.g) * 256u);
+                    const CUtensorMap* mq = sg.own ? &tmap_q_own : &tmap_q_shared;
                     for (int m = 0; m < tiles_q; ++m) {
-                        tma_load_4d(q_smem + m * kQBytes, mq, &hd->q_full, 0, 0, it.hk, it.tokens[m]);
-                        tma_load_4d(q_smem + m * kQBytes + kHalfBytes, mq, &hd->q_full, 64, 0, it.hk, it.tokens[m]);
+                        tma_load_4d(q_smem + m * kQBytes, mq, &hd->q_full, 0, 0, sg.hk, sg.token + m * nb);
+                        tma_load_4d(q_smem + m * kQBytes + kHalfBytes, mq, &hd->q_full, 64, 0, sg.hk, sg.token + m * nb);
                     }
-                    ++seg;
-                    const int n = cu.run(w_end);
-                    int krow = (int)((shared ? a.shared_row : a.row_off[cu.s]) + (int64_t)cu.t * kSharedTile);
-                    const unsigned long long pol = shared ? pol_shared : pol_own;
-                    for (int i = 0; i < n && ok; ++i, krow += kSharedTile) {
+                    ++segs;
+                    uint32_t krow = (uint32_t)sg.row;
+                    const unsigned long long pol = sg.own ? pol_own : pol_shared;
+                    for (int i = 0; i < sg.n && ok; ++i, krow += kSharedTile) {
                         for (int kv = 0; kv < 2 && ok; ++kv) {
-                            ok = wait_for(hd, &hd->kv_empty[st], phase ^ 1, a.status);
+                            ok = wait_for(hd, &hd->kv_empty[st.at], st.phase ^ 1, a.status);
                             if (!ok) break;
-                            unsigned char* dst = kv_smem + st * kStageBytes;
-                            mbar_expect_tx(&hd->kv_full[st], kStageBytes);
+                            unsigned char* dst = kv_smem + st.at * kStageBytes;
+                            mbar_expect_tx(&hd->kv_full[st.at], kStageBytes);
                             const CUtensorMap* mp = kv ? &tmap_v : &tmap_k;
-                            tma_load_3d_hint(dst, mp, &hd->kv_full[st], 0, it.hk, krow, pol);
-                            tma_load_3d_hint(dst + kHalfBytes, mp, &hd->kv_full[st], 64, it.hk, krow, pol);
-                            ++ring;
-                            if (++st == kStages) { st = 0; phase ^= 1; }
+                            tma_load_3d_hint(dst, mp, &hd->kv_full[st.at], 0, sg.hk, (int)krow, pol);
+                            tma_load_3d_hint(dst + kHalfBytes, mp, &hd->kv_full[st.at], 64, sg.hk, (int)krow, pol);
+                            ++loads;
+                            st.next(kStages);
                         }
                     }
-                    cu.skip(wk, n);
                 }
                 if (!ok) {                                   // copies still in flight land before the CTA ends
-                    for (uint32_t r = ring > kStages ? ring - kStages : 0; r < ring; ++r) drain(&hd->kv_full[r % kStages], (r / kStages) & 1);
-                    if (seg > 0) drain(&hd->q_full, (seg - 1) & 1);
+                    for (uint32_t r = loads > kStages ? loads - kStages : 0; r < loads; ++r) drain(&hd->kv_full[r % kStages], (r / kStages) & 1);
+                    if (segs > 0) drain(&hd->q_full, (segs - 1) & 1);
                 }
             }
-        } else if (warp == 1) {
-            // =========================================================== MMA issuer
-            if (lane == 0) {
+        } else {
+            // =========================================================== MMA issuers: warp 1 for lane 0, warp 3 for lane 1
+            {
+                const bool leader = elect_leader();          // the warp runs converged, this lane acts
+                const uint32_t l = warp >> 1;
                 const uint32_t q_addr = smem_u32(q_smem), kv_addr = smem_u32(kv_smem);
+                const uint32_t s_tmem = tmem + kColS + l * 128, o_tmem = tmem + kColO + l * 128;
                 constexpr uint32_t idesc_qk = instr_desc(false), idesc_pv = instr_desc(true);
-                uint32_t k_st = 0, k_phase = 0, v_st = 1, v_phase = 0;   // every second stage of the ring
-                auto next_stage = [](uint32_t& st, uint32_t& phase) {
-                    st += 2;
-                    if (st >= kStages) { st -= kStages; phase ^= 1; }
-                };
-                uint32_t ops[2] = {0, 0}, segs[2] = {0, 0}, seg = 0;     // products and segments of a lane; segments
+                uint32_t ops = 0, segs = 0, seg = 0, tile0 = 0;   // products, segments of this lane; segments, tiles of the CTA
+                Ring ring{0, 0};
                 bool ok = true;
-                while (ok && cu.w < w_end) {
-                    const Item it(a, cu);
+                // K of tile i of the CTA is load 2 i, V load 2 i + 1
+                auto stage_full = [&](uint32_t load) { return wait_for(hd, &hd->kv_full[load % kStages], (load / kStages) & 1, a.status); };
+                while (ok) {
+                    ok = wait_for(hd, &hd->seg_full[ring.at], ring.phase, a.status);
+                    if (!ok) break;
+                    const int n = __shfl_sync(0xFFFFFFFFu, hd->seg[ring.at].n, 0);   // (uniform registers)
+                    const bool single = __shfl_sync(0xFFFFFFFFu, hd->seg[ring.at].single, 0) != 0;
+                    __syncwarp();
+                    if (leader) mbar_arrive(&hd->seg_empty[ring.at]);
+                    ring.next(kSegments);
+                    if (n == 0) break;
                     ok = wait_for(hd, &hd->q_full, seg & 1, a.status);
                     if (!ok) break;
-                    const int n = cu.run(w_end), n_ops = it.single ? n : 2 * n;
-                    // step o: P V of step o - 2 (the same lane), then Q K^T of step o over what that P was
-                    for (int o = 0; o < n_ops + 2 && ok; ++o) {
-                        const int l = o & 1;
-                        if (o >= 2) {
-                            if (!(ok = wait_for(hd, &hd->p_ready[l], ops[l] & 1, a.status))) break;
-                            if (!(ok = wait_for(hd, &hd->kv_full[v_st], v_phase, a.status))) break;
-                            if (o < 4 && segs[l] > 0 && !(ok = wait_for(hd, &hd->o_free[l], (segs[l] - 1) & 1, a.status))) break;
-                            tc_fence_after();
-                            const uint32_t v_lo = smem_desc_lo(kv_addr + v_st * kStageBytes, kHalfBytes);   // MN-major: LBO = next 64 d
+                    const uint32_t q_lo = smem_desc_lo(q_addr + (single ? 0 : l) * kQBytes, 16);
+                    const uint32_t step = single ? 2 : 1, end = tile0 + n;
+                    auto release = [&](uint32_t load) {      // every stage has two arrivals
+                        umma_commit_by(leader, &hd->kv_empty[load % kStages]);
+                        if (single && leader) mbar_arrive(&hd->kv_empty[load % kStages]);
+                    };
+                    auto scores = [&](uint32_t t) {
+                        tc_fence_after();
+                        const uint32_t k_lo = smem_desc_lo(kv_addr + (2 * t % kStages) * kStageBytes, 16);
 #pragma unroll
-                            for (int kk = 0; kk < 8; ++kk)   // 16 keys per instruction
-                                umma_f16_ts(tmem + kColO + l * 128, tmem + kColS + l * 128 + kk * 8, smem_desc(v_lo + kk * (2048 >> 4)), idesc_pv,
-                                            (o >= 4 || kk > 0) ? 1u : 0u);
-                            const bool last_use = it.single || l == 1;
-                            if (last_use) umma_commit(&hd->kv_empty[v_st]);
-                            umma_commit(&hd->pv_done[l]);
-                            if (last_use) next_stage(v_st, v_phase);
-                            ++ops[l];
+                        for (int kk = 0; kk < 8; ++kk) {     // 16 of the 128 head dims per instruction
+                            const uint32_t off = ((kk >> 2) * kHalfBytes + (kk & 3) * 32) >> 4;
+                            umma_f16_by(leader, s_tmem, smem_desc(q_lo + off), smem_desc(k_lo + off), idesc_qk, kk > 0 ? 1u : 0u);
                         }
-                        if (o < n_ops) {
-                            if (!(ok = wait_for(hd, &hd->kv_full[k_st], k_phase, a.status))) break;
-                            tc_fence_after();
-                            const uint32_t q_lo = smem_desc_lo(q_addr + (it.single ? 0 : l) * kQBytes, 16);
-                            const uint32_t k_lo = smem_desc_lo(kv_addr + k_st * kStageBytes, 16);
+                        umma_commit_by(leader, &hd->s_full[l]);         // (and with it the product in front of it)
+                    };
+                    uint32_t t = tile0 + (single ? l : 0);
+                    const bool any = t < end;
+                    if (any) {
+                        ok = stage_full(2 * t);
+                        if (!ok) break;
+                        scores(t);
+                        release(2 * t);
+                    }
+                    if (t + step >= end) {                   // the lane's last Q K^T of the segment
+                        if (any) umma_commit_by(leader, &hd->q_empty);
+                        else if (leader) mbar_arrive(&hd->q_empty);
+                    }
+                    if (any && segs > 0) ok = wait_for(hd, &hd->o_free[l], (segs - 1) & 1, a.status);
+                    for (bool first = true; t < end && ok; t += step, first = false) {
+                        const bool more = t + step < end;
+                        // A look at a barrier takes some 150 cycles beside the tensor cores' reads of shared memory: those at the tiles come
+                        // first, while P is still being made.  (The next K of a single M tile may only be on its way behind the other
+                        // lane's product.)
+                        if (!(ok = stage_full(2 * t + 1))) break;
+                        if (more && !single && !(ok = stage_full(2 * (t + step)))) break;
+                        if (!(ok = wait_for(hd, &hd->p_ready[l], ops & 1, a.status))) break;
+                        ++ops;
+                        tc_fence_after();
+                        const uint32_t v_lo = smem_desc_lo(kv_addr + ((2 * t + 1) % kStages) * kStageBytes, kHalfBytes);   // MN-major: LBO = next 64 d
 #pragma unroll
-                            for (int kk = 0; kk < 8; ++kk) { // 16 of the 128 head dims per instruction
-                                const uint32_t off = ((kk >> 2) * kHalfBytes + (kk & 3) * 32) >> 4;
-                                umma_f16(tmem + kColS + l * 128, smem_desc(q_lo + off), smem_desc(k_lo + off), idesc_qk, kk > 0 ? 1u : 0u);
-                            }
-                            umma_commit(&hd->s_full[l]);
-                            if (it.single || l == 1) {
-                                umma_commit(&hd->kv_empty[k_st]);
-                                next_stage(k_st, k_phase);
-                            }
-                            if (o == n_ops - 1) umma_commit(&hd->q_empty);
+                        for (int kk = 0; kk < 8; ++kk)       // 16 keys per instruction
+                            umma_f16_ts_by(leader, o_tmem, s_tmem + kk * 8, smem_desc(v_lo + kk * (2048 >> 4)), idesc_pv, !first || kk > 0 ? 1u : 0u);
+                        if (more) {
+                            if (single && !(ok = stage_full(2 * (t + step)))) break;
+                            scores(t + step);
+                        } else {
+                            umma_commit_by(leader, &hd->o_full[l]);
+                        }
+                        release(2 * t + 1);
+                        if (more) {
+                            release(2 * (t + step));
+                            if (t + 2 * step >= end) umma_commit_by(leader, &hd->q_empty);
                         }
                     }
                     if (!ok) break;
-                    ++segs[0];
-                    if (n_ops > 1) ++segs[1];
+                    segs += any;
                     ++seg;
-                    cu.skip(wk, n);
+                    tile0 = end;
                 }
             }
         }
-      } else {
-            asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsMany));
-            // =========================================================== softmax and partial results (two groups of 128 threads)
-            const int l = warp >= 8;                         // lane of the segment
-            const int row = 32 * (warp & 3) + lane;          // TMEM lane == query row
-            const uint32_t lane_sel = (uint32_t)(32 * (warp & 3)) << 16;
-            const uint32_t s_addr = tmem + kColS + l * 128 + lane_sel, o_addr = tmem + kColO + l * 128 + lane_sel;
-            const int tid = threadIdx.x - 128 - 128 * l;
-            const int g = a.g, i_local = row / g;
-            uint32_t ops = 0, tile0 = 0, syncs = 0;          // products of this lane; tiles of the CTA in front of this segment
-            bool ok = true;
-            uint32_t v[128];
-            int cur_s = -1;
-            bool bad = false;
-            auto group_sync = [&]() {
-                mbar_arrive(&hd->group_bar[l]);
-                const bool done = wait_for(hd, &hd->group_bar[l], syncs & 1, a.status);
-                ++syncs;
-                return done;
-            };
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsMany));
+        // =============================================================== softmax and partial results
+        const int l = (warp - 4) >> 2;                       // lane of the segments
+        const int row = 32 * (warp & 3) + lane;              // TMEM lane == query row
+        const uint32_t s_addr = tmem + kColS + l * 128 + ((uint32_t)(32 * (warp & 3)) << 16);   // O: kColO - kColS further
+        const uint32_t base = smem_u32(hd), my_bars = base + 8 * l, abort_at = base + (uint32_t)offsetof(Header, abort_flag);
+        constexpr uint32_t kAtFull = offsetof(Header, s_full), kAtReady = offsetof(Header, p_ready), kAtDone = offsetof(Header, o_full);
+        constexpr uint32_t kAtFree = offsetof(Header, o_free);
+        uint32_t ops = 0, segs = 0, tile0 = 0;               // products and segments of this lane; tiles of the CTA in front of this segment
+        Ring ring{0, 0};
+        bool ok = true;
+        uint32_t v[128];
 
-            while (ok && cu.w < w_end) {
-                const Item it(a, cu);
-                const bool shared = cu.s < 0;
-                const int s = cu.s, n = cu.run(w_end), t_first = cu.t, t_end = t_first + n;
-                const int step = it.single ? 2 : 1;
-                const int t_mine = it.single ? t_first + l : t_first;        // this lane's first tile
-                if (t_mine >= t_end) {                       // one key tile: lane 0 has it
-                    tile0 += n;
-                    cu.skip(wk, n);
-                    continue;
+        for (;;) {
+            ok = wait_for(hd, &hd->seg_full[ring.at], ring.phase, a.status);
+            if (!ok) break;
+            const Segment& sg = hd->seg[ring.at];
+            if (sg.n == 0) break;
+            const int step = sg.single ? 2 : 1, t_end = sg.t_first + sg.n;
+            const int rows = sg.rows[sg.single ? 0 : l];
+            const bool row_valid = row < rows, warp_has_rows = (row & ~31) < rows;
+            const int t_masked = sg.ctx / kSharedTile;       // from here on a tile reaches the tree rows, or the ragged end
+            // the row's ancestors, where the segment reaches the tree (while its first scores are on their way)
+            uint32_t anc[4] = {0, 0, 0, 0};
+            if (sg.own && t_end > t_masked && row_valid && !sg.bad) {
+                int vtx = sg.node + (sg.single ? 0 : l) * a.own_nb + row / a.g;
+                for (int up = 0; up < kMaxB && vtx >= 0; ++up) {
+                    const uint32_t bit = 1u << (vtx & 31);
+                    const int wsel = vtx >> 5;
+                    anc[0] |= (wsel == 0) ? bit : 0; anc[1] |= (wsel == 1) ? bit : 0;
+                    anc[2] |= (wsel == 2) ? bit : 0; anc[3] |= (wsel == 3) ? bit : 0;
+                    vtx = hd->par[ring.at][vtx];
                 }
-                const int m = it.m + (it.single ? 0 : l);
-                const int nn = shared ? 0 : nodes_of(wk.n_nodes, s, wk.B);
-                const int ctx = shared ? a.shared_len : wk.prefix(wk.ctx_len[s]);
-                const int n_keys = ctx + nn;
-                const int rows = shared ? min(a.shared_nb, wk.S * wk.B - m * a.shared_nb) * g : min(a.own_nb, nn - m * a.own_nb) * g;
-                const bool row_valid = row < rows, warp_has_rows = 32 * (warp & 3) < rows;
-                const int node = m * a.own_nb + i_local;     // (of a sequence's own rows)
-                if (!shared && s != cur_s) {
-                    // parent[] and rows of the sequence: both groups come to the same verdict
-                    cur_s = s;
-                    if (tid < nn) {
-                        const int p = a.parent[(size_t)s * wk.B + tid];
-                        hd->par[l][tid] = (signed char)p;
-                        if (tid == 0 ? p != -1 : (p < 0 || p >= tid)) hd->bad[l] = 1;
-                    }
-                    const bool bad_rows = rows_outside(a.row_off[s], wk.ctx_len[s], nn, wk.kv_rows);
-                    if (bad_rows && tid == 0) { hd->bad[l] = 1; atomicOr(&a.status[s], GOOSE_ST_BAD_ROWS); }
-                    ok = group_sync();
-                    bad = hd->bad[l] != 0;
-                    ok = ok && group_sync();
-                    if (!ok) break;
-                    if (tid == 0 && bad) { hd->bad[l] = 0; if (!bad_rows) atomicOr(&a.status[s], GOOSE_ST_BAD_PARENT); }
-                }
-                uint32_t anc[4] = {0, 0, 0, 0};
-                if (!shared && t_end * kSharedTile > ctx && row_valid && !bad) {
-                    int vtx = node;
-                    for (int up = 0; up < kMaxB && vtx >= 0; ++up) {
-                        const uint32_t bit = 1u << (vtx & 31);
-                        const int wsel = vtx >> 5;
-                        anc[0] |= (wsel == 0) ? bit : 0; anc[1] |= (wsel == 1) ? bit : 0;
-                        anc[2] |= (wsel == 2) ? bit : 0; anc[3] |= (wsel == 3) ? bit : 0;
-                        vtx = hd->par[l][vtx];
-                    }
-                }
-                float m_run = -INFINITY, l_run = 0.f;
-                for (int t = t_mine; t < t_end; t += step) {
-                    const bool first = t == t_mine;
-                    ok = wait_for(hd, &hd->s_full[l], ops & 1, a.status);
-                    if (!ok) break;
-                    tc_fence_after();
-                    if (warp_has_rows) {
-                        TMEM_LD32(s_addr, v, 0); TMEM_LD32(s_addr + 32, v, 32);
-                        TMEM_LD32(s_addr + 64, v, 64); TMEM_LD32(s_addr + 96, v, 96);
-                        tmem_wait_ld();
-                        const int key0 = t * kSharedTile;
-                        if (key0 + kSharedTile > ctx) {      // the tree rows, or the ragged end
-                            // visibility of the tile's 128 keys as one mask: the prefix keys, and the ancestors shifted to where
-                            // the tree rows start
-                            const int pc = ctx - key0;       // tile column of tree node 0 (may be < 0 or >= 128)
-                            const unsigned __int128 a128 =
-                                ((unsigned __int128)(((unsigned long long)anc[3] << 32) | anc[2]) << 64) |
-                                (unsigned __int128)(((unsigned long long)anc[1] << 32) | anc[0]);
-                            unsigned __int128 vm;
-                            if (pc >= 128) vm = ~(unsigned __int128)0;
-                            else if (pc > 0) vm = (((unsigned __int128)1 << pc) - 1) | (a128 << pc);
-                            else if (pc > -128) vm = a128 >> (-pc);
-                            else vm = 0;
-                            const uint32_t vw[4] = {(uint32_t)vm, (uint32_t)(vm >> 32), (uint32_t)(vm >> 64), (uint32_t)(vm >> 96)};
-#pragma unroll
-                            for (int c = 0; c < 128; ++c) v[c] = ((vw[c >> 5] >> (c & 31)) & 1u) ? v[c] : 0xFF800000u;   // -inf
-                        }
-                        float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-                        for (int c = 0; c < 128; c += 8)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) mx4[e] = max3(mx4[e], __uint_as_float(v[c + 2 * e]), __uint_as_float(v[c + 2 * e + 1]));
-                        const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * a.scale_log2;   // scale > 0
-                        const float m_new = fmaxf(m_run, mx);
-                        if (__any_sync(0xFFFFFFFFu, first || (row_valid && m_new > m_run + kRescaleThreshold))) {
-                            const float alpha = (m_run == -INFINITY) ? 0.f : ex2(m_run - m_new);
-                            if (!first) {
-                                ok = wait_for(hd, &hd->pv_done[l], (ops - 1) & 1, a.status);
-                                if (ok) {
-                                    tc_fence_after();
-                                    uint32_t o[16];
-#pragma unroll
-                                    for (int cc = 0; cc < 8; ++cc) {
-                                        TMEM_LD16(o_addr + cc * 16, o, 0);
-                                        tmem_wait_ld();
-#pragma unroll
-                                        for (int c = 0; c < 16; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * alpha);
-                                        TMEM_ST16(o_addr + cc * 16, o, 0);
-                                    }
-                                    tmem_wait_st();
-                                }
-                            }
-                            l_run *= alpha;
-                            m_run = m_new;
-                        }
-                        const float neg_m = (m_run == -INFINITY) ? 0.f : -m_run;
-                        const unsigned long long scale2 = pack_f32x2(a.scale_log2, a.scale_log2), neg2 = pack_f32x2(neg_m, neg_m);
-                        unsigned long long ls2[2] = {0, 0};
-#pragma unroll
-                        for (int e = 0; e < 64; ++e) {
-                            const float2 x2 = unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1])), scale2, neg2));
-                            const float p0 = ex2(x2.x), p1 = ex2(x2.y);
-                            ls2[e & 1] = add_f32x2(ls2[e & 1], pack_f32x2(p0, p1));
-                            v[e] = pack_bf16x2(p0, p1);
-                        }
-                        const float2 l2 = unpack_f32x2(add_f32x2(ls2[0], ls2[1]));
-                        l_run += l2.x + l2.y;
-                        TMEM_ST32(s_addr, v, 0);
-                        TMEM_ST32(s_addr + 32, v, 32);
-                        tmem_wait_st();
-                    }
-                    // observe every phase of pv_done in order
-                    if (ok && ops > 0) ok = wait_for(hd, &hd->pv_done[l], (ops - 1) & 1, a.status);
-                    if (!ok) break;
-                    // ragged end: V rows past the last key may hold anything -> zeros, in a tile that both lanes use by lane 0, whose
-                    // product comes first
-                    if ((t + 1) * kSharedTile > n_keys && (it.single || l == 0)) {
-                        const uint32_t ring = 2 * (tile0 + (t - t_first)) + 1, st = ring % kStages;
-                        ok = wait_for(hd, &hd->kv_full[st], (ring / kStages) & 1, a.status);
-                        if (!ok) break;
-                        const int first_off = max(n_keys - t * kSharedTile, 0) * 128;
-                        for (int off = first_off + tid * 16; off < kHalfBytes; off += 128 * 16) {
-                            *reinterpret_cast<uint4*>(kv_smem + st * kStageBytes + off) = make_uint4(0, 0, 0, 0);
-                            *reinterpret_cast<uint4*>(kv_smem + st * kStageBytes + kHalfBytes + off) = make_uint4(0, 0, 0, 0);
-                        }
-                        fence_proxy_async();
-                    }
-                    tc_fence_before();
-                    mbar_arrive(&hd->p_ready[l]);
-                    ++ops;
-                }
-                if (!ok) break;
-                // ---------------- partial result of this lane
-                ok = wait_for(hd, &hd->pv_done[l], (ops - 1) & 1, a.status);
+            }
+            float m_run = -INFINITY, l_run = 0.f;
+            bool first = true;
+            for (int t = sg.t_first + (sg.single ? l : 0); t < t_end; t += step) {
+                ok = wait_at(my_bars + kAtFull, ops & 1, abort_at, a.status);
                 if (!ok) break;
                 tc_fence_after();
                 if (warp_has_rows) {
+                    TMEM_LD32(s_addr, v, 0); TMEM_LD32(s_addr + 32, v, 32);
+                    TMEM_LD32(s_addr + 64, v, 64); TMEM_LD32(s_addr + 96, v, 96);
+                    tmem_wait_ld();
+                    if (t >= t_masked) {
+                        const int pc = sg.ctx - t * kSharedTile;   // tile column of the first key behind the prefix
+                        // visibility of the tile's 128 keys as one mask: the prefix keys, and the row's ancestors from where the tree rows start
+                        const unsigned __int128 a128 =
+                            ((unsigned __int128)(((unsigned long long)anc[3] << 32) | anc[2]) << 64) |
+                            (unsigned __int128)(((unsigned long long)anc[1] << 32) | anc[0]);
+                        unsigned __int128 vm;
+                        if (pc > 0) vm = (((unsigned __int128)1 << pc) - 1) | (a128 << pc);
+                        else if (pc > -128) vm = a128 >> (-pc);
+                        else vm = 0;
+                        const uint32_t vw[4] = {(uint32_t)vm, (uint32_t)(vm >> 32), (uint32_t)(vm >> 64), (uint32_t)(vm >> 96)};
+#pragma unroll
+                        for (int c = 0; c < 128; ++c) v[c] = ((vw[c >> 5] >> (c & 31)) & 1u) ? v[c] : 0xFF800000u;   // -inf
+                    }
+                    float mx[8] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                    for (int c = 0; c < 128; c += 16)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) mx[e] = max3(mx[e], __uint_as_float(v[c + 2 * e]), __uint_as_float(v[c + 2 * e + 1]));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) mx[e] = fmaxf(mx[e], mx[e + 4]);
+                    const float m_new = fmaxf(m_run, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale_log2);   // scale > 0
+                    if (__any_sync(0xFFFFFFFFu, first || (row_valid && m_new > m_run + kRescaleThreshold))) {
+                        const float alpha = (m_run == -INFINITY) ? 0.f : ex2(m_run - m_new);
+                        if (!first) {                        // (these scores are there: so is the product in front of them)
+                            uint32_t o[16];
+#pragma unroll
+                            for (int cc = 0; cc < 8; ++cc) {
+                                TMEM_LD16(s_addr + (kColO - kColS) + cc * 16, o, 0);
+                                tmem_wait_ld();
+#pragma unroll
+                                for (int c = 0; c < 16; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * alpha);
+                                TMEM_ST16(s_addr + (kColO - kColS) + cc * 16, o, 0);
+                            }
+                            tmem_wait_st();
+                        }
+                        l_run *= alpha;
+                        m_run = m_new;
+                    }
+                    const float neg_m = (m_run == -INFINITY) ? 0.f : -m_run;
+                    const unsigned long long scale2 = pack_f32x2(a.scale_log2, a.scale_log2), neg2 = pack_f32x2(neg_m, neg_m);
+                    unsigned long long ls2[2] = {0, 0};
+#pragma unroll
+                    for (int e = 0; e < 64; ++e) {
+                        const unsigned long long x = fma_f32x2(pack_f32x2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1])), scale2, neg2);
+                        float2 p = unpack_f32x2(x);
+                        if (e % 8 < kByPolynomial) p = ex2_by_polynomial(p);
+                        else p = make_float2(ex2(p.x), ex2(p.y));
+                        ls2[e & 1] = add_f32x2(ls2[e & 1], pack_f32x2(p.x, p.y));
+                        v[e] = pack_bf16x2(p.x, p.y);
+                    }
+                    const float2 l2 = unpack_f32x2(add_f32x2(ls2[0], ls2[1]));
+                    l_run += l2.x + l2.y;
+                    TMEM_ST32(s_addr, v, 0);
+                    TMEM_ST32(s_addr + 32, v, 32);
+                    tmem_wait_st();
+                }
+                first = false;
+                // ragged end: V rows past the last key may hold anything -> zeros (by either lane of a tile that both use)
+                if (t >= t_masked && (t + 1) * kSharedTile > sg.n_keys) {
+                    const uint32_t load = 2 * (tile0 + (t - sg.t_first)) + 1, st = load % kStages;
+                    ok = wait_for(hd, &hd->kv_full[st], (load / kStages) & 1, a.status);
+                    if (!ok) break;
+                    const int first_off = max(sg.n_keys - t * kSharedTile, 0) * 128;
+                    for (int off = first_off + row * 16; off < kHalfBytes; off += 128 * 16) {
+                        *reinterpret_cast<uint4*>(kv_smem + st * kStageBytes + off) = make_uint4(0, 0, 0, 0);
+                        *reinterpret_cast<uint4*>(kv_smem + st * kStageBytes + kHalfBytes + off) = make_uint4(0, 0, 0, 0);
+                    }
+                    fence_proxy_async();
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) arrive_at(my_bars + kAtReady);
+                ++ops;
+            }
+            if (!ok) break;
+            if (!first) {
+                // ---------------- partial result of this lane
+                ok = wait_at(my_bars + kAtDone, segs & 1, abort_at, a.status);
+                if (!ok) break;
+                ++segs;
+                tc_fence_after();
+                if (warp_has_rows) {
+                    const uint32_t o_addr = s_addr + (kColO - kColS);
                     TMEM_LD32(o_addr, v, 0); TMEM_LD32(o_addr + 32, v, 32);
                     TMEM_LD32(o_addr + 64, v, 64); TMEM_LD32(o_addr + 96, v, 96);
                     tmem_wait_ld();
                 }
                 tc_fence_before();
-                mbar_arrive(&hd->o_free[l]);
+                __syncwarp();
+                if (lane == 0) arrive_at(my_bars + kAtFree);
                 if (row_valid) {
-                    float* part = a.parts + (size_t)wk.slot(wk.item(s, cu.i), blockIdx.x, t_first == 0, t_end == cu.T, l) * kPartFloats;
-                    float top = 0.f;
+                    float* part = a.parts + (size_t)(sg.slot + l) * kPartFloats;
+                    float top4[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int c = 0; c < 128; ++c) top = fmaxf(top, fabsf(__uint_as_float(v[c])));
-                    float inv = l_run == 0.f ? 0.f : 1.f / l_run;
-                    top *= inv;
+                    for (int c = 0; c < 128; ++c) top4[c & 3] = fmaxf(top4[c & 3], fabsf(__uint_as_float(v[c])));
                     // power of two of the largest element; 1 where there is none (zeros, infinities)
-                    const uint32_t ex = __float_as_uint(top) & 0x7F800000u;
-                    const float scale = ex == 0 || ex >= 0x7F000000u ? 1.f : __uint_as_float(ex);
-                    inv *= 1.f / scale;
+                    const uint32_t ex = __float_as_uint(fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3]))) & 0x7F800000u;
+                    const float scale = ex == 0 || ex >= 0x7F000000u ? 1.f : __uint_as_float(ex), inv = 1.f / scale;
                     uint4* dst = reinterpret_cast<uint4*>(part) + row;
 #pragma unroll
                     for (int c = 0; c < 16; ++c) {
@@ -476,13 +568,15 @@ tree_attn_shared_kernel(const __grid_constant__ CUtensorMap tmap_q_shared, const
                         }
                         dst[c * 128] = make_uint4(hw[0], hw[1], hw[2], hw[3]);
                     }
-                    reinterpret_cast<float2*>(part + kPartWords)[row] =
-                        make_float2(l_run == 0.f ? -INFINITY : m_run + log2f(l_run), !shared && bad ? 0.f : scale);
+                    part[kPartWords + row] = m_run;
+                    reinterpret_cast<float2*>(part + kPartWords + 128)[row] = make_float2(sg.bad ? -1.f : l_run, scale);
                 }
-                tile0 += n;
-                cu.skip(wk, n);
             }
-      }
+            tile0 += sg.n;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&hd->seg_empty[ring.at]);
+            ring.next(kSegments);
+        }
     }
 
     __syncwarp();
@@ -494,79 +588,94 @@ tree_attn_shared_kernel(const __grid_constant__ CUtensorMap tmap_q_shared, const
     }
 }
 
-// Merge: 32 rows of one key/value head of one sequence (lane <-> row, warp <-> 16 columns), parts in rounds of kCombineRound.
+// Merge: 32 rows of one key/value head of one sequence (lane <-> row, warp <-> 16 columns), parts in rounds of kCombineRound.  The rows
+// lie in two M tiles at most of the shared rows' work, and in two of the sequence's own; a warp makes the list of each tile's parts.
+constexpr int kMaxParts = 2 * 256;                           // lanes x CTAs that an item may lie in
+
 __global__ void __launch_bounds__(kCombineThreads)
-tree_attn_shared_merge_kernel(const SharedArgs a, int H, __nv_bfloat16* __restrict__ out, float* __restrict__ lse) {
+tree_attn_shared_merge_kernel(const __grid_constant__ SharedArgs a, int H, __nv_bfloat16* __restrict__ out, float* __restrict__ lse) {
+    __shared__ int s_slot[4][kMaxParts];
+    __shared__ int s_parts[4];
     const int s = blockIdx.z, hk = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    SharedWork wk = a.wk;
-    // (the lengths are final: the main kernel has let this one in behind its own wait)
-    long long sum = 0, before = 0;                           // tiles of all sequences, of those in front of this one
-    int live_all = 0, live = 0;                              // and how many have any
-    for (int s0 = 0; s0 < wk.S; s0 += 32) {
-        const int T = s0 + lane < wk.S ? wk.tiles(s0 + lane) : 0;
-        sum += __reduce_add_sync(0xFFFFFFFFu, (uint32_t)T);
-        live_all += __popc(__ballot_sync(0xFFFFFFFFu, T > 0));
-        const bool ahead = s0 + lane < s;
-        before += __reduce_add_sync(0xFFFFFFFFu, (uint32_t)(ahead ? T : 0));
-        live += __popc(__ballot_sync(0xFFFFFFFFu, ahead && T > 0));
+    const int nn = nodes_of(a.wk.n_nodes, s, a.wk.B), g = a.g;
+    const int r0 = blockIdx.x * 32, r = r0 + lane, node = r / g, member = r - node * g;
+    const int shared_first = (s * a.wk.B + r0 / g) / a.shared_nb, own_first = r0 / g / a.own_nb;   // M tiles of the block's first row
+    if (warp < 4) {
+        // (the lengths are final: the main kernel has let this one in behind its own wait)
+        SharedWork wk = a.wk;
+        long long sum = 0, before = 0;                       // tiles of all sequences, of those in front of this one
+        int live_all = 0, live = 0;                          // and how many have any
+        for (int s0 = 0; s0 < wk.S; s0 += 32) {
+            const int T = s0 + lane < wk.S ? wk.tiles(s0 + lane) : 0;
+            sum += __reduce_add_sync(0xFFFFFFFFu, (uint32_t)T);
+            live_all += __popc(__ballot_sync(0xFFFFFFFFu, T > 0));
+            const bool ahead = s0 + lane < s;
+            before += __reduce_add_sync(0xFFFFFFFFu, (uint32_t)(ahead ? T : 0));
+            live += __popc(__ballot_sync(0xFFFFFFFFu, ahead && T > 0));
+        }
+        wk.set(sum, live_all);
+        const bool own = warp >= 2;
+        const int m = (own ? own_first : shared_first) + (warp & 1), n_m = own ? wk.own_m : wk.shared_m;
+        int n = 0;
+        if (m < n_m) {
+            const int T = own ? wk.tiles(s) : wk.shared_tiles, i = hk * (own ? wk.own_pairs() : wk.shared_pairs()) + (m >> 1);
+            const long long first = own ? wk.shared_total + (long long)wk.Hkv * wk.own_pairs() * (before + wk.pad * live) : 0;
+            SharedParts ps;
+            ps.set(wk, own ? s : -1, i, first + (long long)i * wk.width(T), T, (m | 1) >= n_m, m & 1);
+            for (int k0 = 0; k0 < ps.n; k0 += 32) {
+                const int slot = k0 + lane < ps.n ? ps.slot(wk, k0 + lane) : -1;
+                const uint32_t there = __ballot_sync(0xFFFFFFFFu, slot >= 0);
+                if (slot >= 0) s_slot[warp][n + __popc(there & ((1u << lane) - 1))] = slot;
+                n += __popc(there);
+            }
+        }
+        if (lane == 0) s_parts[warp] = n;
     }
-    wk.set(sum, live_all);
-    const int T = wk.tiles(s), nn = nodes_of(wk.n_nodes, s, wk.B);
-    const int g = a.g, r = blockIdx.x * 32 + lane, node = r / g, member = r - node * g;
-    SharedParts ps[2];
-    int at_row[2];
-    {
-        const int tok = s * wk.B + node, m = tok / a.shared_nb, pair = m >> 1;
-        const int i = hk * wk.shared_pairs() + pair;
-        ps[0].set(wk, -1, i, (long long)i * wk.width(wk.shared_tiles), wk.shared_tiles, (m | 1) >= wk.shared_m, m & 1);
-        at_row[0] = (tok - m * a.shared_nb) * g + member;
-    }
-    {
-        const int m = node / a.own_nb, pair = m >> 1;
-        const int i = hk * wk.own_pairs() + pair;
-        const long long per = (long long)wk.Hkv * wk.own_pairs();
-        ps[1].set(wk, s, i, wk.shared_total + per * (before + wk.pad * live) + (long long)i * wk.width(T), T, (m | 1) >= wk.own_m, m & 1);
-        at_row[1] = (node - m * a.own_nb) * g + member;
-    }
+    __syncthreads();
     pdl_wait();
     pdl_trigger();
     if (node >= nn) return;
 
+    // this row's lists and its rows in the M tiles
+    const int tok = s * a.wk.B + node, m_shared = tok / a.shared_nb, m_own = node / a.own_nb;
+    const int list0 = m_shared - shared_first, list1 = 2 + m_own - own_first;
+    const int row0 = (tok - m_shared * a.shared_nb) * g + member, row1 = (node - m_own * a.own_nb) * g + member;
+    const int n0 = s_parts[list0], n = n0 + s_parts[list1];
     float M = -INFINITY, L = 0.f, acc[16];
     bool bad = false;
 #pragma unroll
     for (int c = 0; c < 16; ++c) acc[c] = 0.f;
-    const int n = ps[0].n + ps[1].n;
     for (int k0 = 0; k0 < n; k0 += kCombineRound) {
-        float2 meta[kCombineRound];
+        float m[kCombineRound];
+        float2 ls[kCombineRound];
         uint4 x[kCombineRound][2];
 #pragma unroll
         for (int q = 0; q < kCombineRound; ++q) {
             const int k = k0 + q;
-            const bool own = k >= ps[0].n;
-            const int slot = k < n ? (own ? ps[1].slot(wk, k - ps[0].n) : ps[0].slot(wk, k)) : -1;
-            meta[q] = make_float2(-INFINITY, 1.f);
+            m[q] = -INFINITY;
+            ls[q] = make_float2(0.f, 1.f);
             x[q][0] = x[q][1] = make_uint4(0, 0, 0, 0);
-            if (slot >= 0) {
-                const float* part = a.parts + (size_t)slot * kPartFloats;
-                const int rr = own ? at_row[1] : at_row[0];
-                meta[q] = __ldcg(reinterpret_cast<const float2*>(part + kPartWords) + rr);
+            if (k < n) {
+                const float* part = a.parts + (size_t)(k < n0 ? s_slot[list0][k] : s_slot[list1][k - n0]) * kPartFloats;
+                const int rr = k < n0 ? row0 : row1;
+                m[q] = __ldcg(part + kPartWords + rr);
+                ls[q] = __ldcg(reinterpret_cast<const float2*>(part + kPartWords + 128) + rr);
                 x[q][0] = __ldcg(reinterpret_cast<const uint4*>(part) + (2 * warp) * 128 + rr);
                 x[q][1] = __ldcg(reinterpret_cast<const uint4*>(part) + (2 * warp + 1) * 128 + rr);
             }
         }
         float M_new = M;
 #pragma unroll
-        for (int q = 0; q < kCombineRound; ++q) { M_new = fmaxf(M_new, meta[q].x); bad |= meta[q].y == 0.f; }
+        for (int q = 0; q < kCombineRound; ++q) { M_new = fmaxf(M_new, m[q]); bad |= ls[q].x < 0.f; }
         const float old = M == -INFINITY ? 0.f : ex2(M - M_new);
         L *= old;
 #pragma unroll
         for (int c = 0; c < 16; ++c) acc[c] *= old;
 #pragma unroll
         for (int q = 0; q < kCombineRound; ++q) {
-            if (meta[q].x == -INFINITY) continue;
-            const float w = ex2(meta[q].x - M_new), wx = w * meta[q].y;
-            L += w;
+            if (m[q] == -INFINITY && ls[q].x == 0.f) continue; // no key of the part is visible to the row
+            const float w = ex2(m[q] - M_new), wx = w * ls[q].y;
+            L += w * ls[q].x;
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 const uint32_t hw[4] = {x[q][u].x, x[q][u].y, x[q][u].z, x[q][u].w};
@@ -580,7 +689,7 @@ tree_attn_shared_merge_kernel(const SharedArgs a, int H, __nv_bfloat16* __restri
         }
         M = M_new;
     }
-    const size_t at = ((size_t)s * wk.B + node) * H + hk * g + member;
+    const size_t at = ((size_t)s * a.wk.B + node) * H + hk * g + member;
     if (bad) {
         uint4* dst = reinterpret_cast<uint4*>(out + at * kHeadDim + 16 * warp);
         dst[0] = dst[1] = make_uint4(0, 0, 0, 0);
@@ -607,7 +716,7 @@ static SharedArgs shared_args(const goose_ctx* c, int64_t kv_rows, int64_t share
     a.wk.shared_tiles = (int)(((int64_t)shared_len + kSharedTile - 1) / kSharedTile);
     a.wk.shared_m = (S * B + a.shared_nb - 1) / a.shared_nb;
     a.wk.own_m = (B + a.own_nb - 1) / a.own_nb;
-    a.wk.G = c->num_sms;
+    a.wk.G = c->num_sms < kMaxParts / 2 ? c->num_sms : kMaxParts / 2;
     a.status = c->status;
     return a;
 }
