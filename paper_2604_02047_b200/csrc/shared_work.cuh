@@ -2,8 +2,9 @@
 // the host too, where a test walks it.
 //
 // The work list is a row of items, each a run of 128-key tiles: first, head by head, the pairs of M tiles of the whole batch over the shared
-// rows, then, sequence by sequence and head by head, the pairs of M tiles of one sequence over its own rows.  It is dealt to the CTAs in
-// ranges of equal length.  What a CTA does of one item is a segment.  A segment has two lanes, each with a softmax warpgroup and
+// rows, then, sequence by sequence and head by head, the pairs of M tiles of one sequence over its own rows.  A tile takes as many places as
+// it costs, and the list is dealt to the CTAs in ranges of equal length: a tile is of the range that its first place is in.  What a CTA does of
+// one item is a segment.  A segment has two lanes, each with a softmax warpgroup and
 // accumulators of its own: the two M tiles of the pair, which share the key tiles, or, where an item is a single M tile, even and odd
 // key tiles of it.  Every lane of a segment leaves a partial result.
 #pragma once
@@ -13,6 +14,8 @@
 namespace goose {
 
 constexpr int kSharedTile = 128;                 // keys of a tile, rows of an M tile
+// places of a key tile, and of the change to another item, for a pair of M tiles and for a single one
+constexpr int kPairPlaces = 5, kSinglePlaces = 4, kPairChange = 16, kSingleChange = 4;
 
 struct SharedWork {
     const int32_t* ctx_len;
@@ -22,7 +25,7 @@ struct SharedWork {
     int shared_m, own_m;      // M tiles a key/value head: of the whole batch; of one sequence
     int G;                    // CTAs
     // worked out
-    int pad;                  // idle places in front of every item, the price of a segment
+    bool changes;             // do changes count?  (not in lists of a tile or two a CTA)
     long long shared_total, total, quantum;
 
     __host__ __device__ __forceinline__ int shared_pairs() const { return (shared_m + 1) >> 1; }
@@ -37,13 +40,16 @@ struct SharedWork {
         const int nn = nodes_of(n_nodes, s, B);
         return nn == 0 ? 0 : (int)(((uint32_t)prefix(ctx_len[s]) + (uint32_t)nn + kSharedTile - 1) / kSharedTile);
     }
-    __host__ __device__ __forceinline__ int width(int T) const { return T > 0 ? T + pad : 0; }
+    // places of a tile of the shared rows (s < 0), of a sequence's own; of an item of T tiles (its region's items count alike)
+    __host__ __device__ __forceinline__ int places(int s) const { return (s < 0 ? shared_m : own_m) > 1 ? kPairPlaces : kSinglePlaces; }
+    __host__ __device__ __forceinline__ int change(int s) const { return !changes ? 0 : (s < 0 ? shared_m : own_m) > 1 ? kPairChange : kSingleChange; }
+    __host__ __device__ __forceinline__ int width(int s, int T) const { return T > 0 ? T * places(s) + change(s) : 0; }
     // sum: tiles of a head of all sequences;  live: sequences that have any
     __host__ __device__ __forceinline__ void set(long long sum, int live) {
         const long long all = (long long)Hkv * shared_pairs() * shared_tiles + (long long)Hkv * own_pairs() * sum;
-        pad = all >= 2ll * G ? 2 : 0;
-        shared_total = (long long)Hkv * shared_pairs() * width(shared_tiles);
-        total = shared_total + (long long)Hkv * own_pairs() * (sum + (long long)pad * live);
+        changes = all >= 2ll * G;
+        shared_total = (long long)Hkv * shared_pairs() * width(-1, shared_tiles);
+        total = shared_total + (long long)Hkv * own_pairs() * (sum * places(0) + (long long)change(0) * live);
         quantum = total > 0 ? divide(total + G - 1, G) : 1;
     }
     __host__ __device__ __forceinline__ void init() {
@@ -76,12 +82,14 @@ struct SharedWork {
 struct SharedCursor {         // walks the list
     long long w;              // place in it
     int s, i, t, T;           // sequence or -1, item of it (head * pairs + pair), tile, tiles
-    // at place `rem` of the items of width wd that begin here
+    // at place `rem` of the items that begin here, or at the next tile behind it
     __host__ __device__ __forceinline__ void enter(const SharedWork& wk, long long rem) {
-        const int wd = wk.width(T);
+        const int wd = wk.width(s, T), u = wk.places(s);
         i = (int)SharedWork::divide(rem, wd);
-        t = (int)(rem - (long long)i * wd) - wk.pad;
-        if (t < 0) { w -= t; t = 0; }
+        const int at = (int)(rem - (long long)i * wd) - wk.change(s);
+        t = at > 0 ? (at + u - 1) / u : 0;
+        w += t * u - at;
+        if (t == T) next(wk);
     }
     __host__ __device__ __forceinline__ void seek(const SharedWork& wk, long long w0) {
         w = w0; s = -1; T = wk.shared_tiles;
@@ -89,39 +97,49 @@ struct SharedCursor {         // walks the list
         long long rem = w0 - wk.shared_total;
         for (s = 0; s < wk.S; ++s) {
             T = wk.tiles(s);
-            const long long mine = (long long)wk.Hkv * wk.own_pairs() * wk.width(T);
+            const long long mine = (long long)wk.Hkv * wk.own_pairs() * wk.width(s, T);
             if (rem < mine) break;
             rem -= mine;
         }
         if (s < wk.S) enter(wk, rem);
     }
-    __host__ __device__ __forceinline__ int run(long long w_end) const { return (int)min((long long)(T - t), w_end - w); }
+    // tiles from here on that are of a range which ends at w_end
+    __host__ __device__ __forceinline__ int run(const SharedWork& wk, long long w_end) const {
+        const int u = wk.places(s);
+        const long long n = SharedWork::divide(w_end - w + u - 1, u);
+        return n < T - t ? (int)n : T - t;
+    }
+    // the next item's first tile
+    __host__ __device__ __forceinline__ void next(const SharedWork& wk) {
+        t = 0; ++i;
+        if (i == wk.Hkv * (s < 0 ? wk.shared_pairs() : wk.own_pairs())) {
+            i = 0;
+            do { ++s; } while (s < wk.S && (T = wk.tiles(s)) == 0);
+        }
+        w += wk.change(s);
+    }
     __host__ __device__ __forceinline__ void skip(const SharedWork& wk, int n) {
-        w += n; t += n;
-        if (t < T) return;
-        t = 0; ++i; w += wk.pad;
-        if (i < wk.Hkv * (s < 0 ? wk.shared_pairs() : wk.own_pairs())) return;
-        i = 0;
-        do { ++s; } while (s < wk.S && (T = wk.tiles(s)) == 0);
+        w += n * wk.places(s); t += n;
+        if (t == T) next(wk);
     }
 };
 
 // the partial results of one M tile of an item, in the order of the keys
 struct SharedParts {
     long long w0;             // place of the item's first tile
-    int T, item, c0, n, lanes, lane;
-    // single: the item is one M tile (two lanes of key tiles); else `m` says which of the two
+    int T, u, item, c0, n, lanes, lane;
+    // first: the item's first place.  single: the item is one M tile (two lanes of key tiles); else `m` says which of the two
     __host__ __device__ __forceinline__ void set(const SharedWork& wk, int s, int i, long long first, int tiles, bool single, int m) {
-        w0 = first + wk.pad; T = tiles; item = wk.item(s, i);
+        w0 = first + wk.change(s); T = tiles; u = wk.places(s); item = wk.item(s, i);
         lanes = single ? 2 : 1; lane = single ? 0 : m;
-        if (T > 0) { c0 = wk.cta_of(w0); n = (wk.cta_of(w0 + T - 1) - c0 + 1) * lanes; }
+        if (T > 0) { c0 = wk.cta_of(w0); n = (wk.cta_of(w0 + (long long)(T - 1) * u) - c0 + 1) * lanes; }
         else { c0 = 0; n = 0; }
     }
     // slot of part k, or -1: that CTA has nothing of the item for the lane
     __host__ __device__ __forceinline__ int slot(const SharedWork& wk, int k) const {
         const int c = c0 + (lanes == 2 ? k >> 1 : k), l = lanes == 2 ? k & 1 : lane;
-        const long long a = c * wk.quantum - w0, b = a + wk.quantum;
-        const int ta = (int)max(a, 0ll), tb = (int)min(b, (long long)T);
+        const long long a = c * wk.quantum - w0, b = a + wk.quantum, all = (long long)T * u;
+        const int ta = a > 0 ? (int)SharedWork::divide(a + u - 1, u) : 0, tb = (int)SharedWork::divide((b < all ? b : all) + u - 1, u);
         return tb - ta > (lanes == 2 ? l : 0) ? wk.slot(item, c, ta == 0, tb == T, l) : -1;
     }
 };

@@ -38,7 +38,6 @@ constexpr int kRegsFew = 56, kRegsMany = 224;
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kColS = 0, kColO = 256;
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kByPolynomial = 2;                             // pairs of exponentials in eight
 constexpr float kRescaleThreshold = 8.0f;                    // rescale O only when the running max grew by > 2^8
 constexpr long long kWaitCycles = 2000000000ll;              // bound of every wait: about one second of SM clock
 
@@ -132,8 +131,8 @@ __device__ __forceinline__ void locate(SharedWork& wk, SharedCursor& cu, long lo
     const long long per = (long long)wk.Hkv * wk.own_pairs();
     for (int s0 = 0; s0 < wk.S; s0 += 32) {
         const int T = s0 == 0 ? mine : s0 + lane < wk.S ? wk.tiles(s0 + lane) : 0;
-        const uint32_t own = (uint32_t)wk.width(T);
-        uint32_t upto = own;                                 // (32 widths of 2^24 + 2 at most)
+        const uint32_t own = (uint32_t)wk.width(s0, T);
+        uint32_t upto = own;                                 // (32 widths of 5 * 2^24 + 16 at most: below 2^32)
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const uint32_t u = __shfl_up_sync(0xFFFFFFFFu, upto, o);
@@ -149,22 +148,6 @@ __device__ __forceinline__ void locate(SharedWork& wk, SharedCursor& cu, long lo
         }
         rem -= per * __shfl_sync(0xFFFFFFFFu, upto, 31);
     }
-}
-
-// 2^x of two numbers without the special function unit, which at 16 results a cycle and SM would take as long for a tile as the tensor
-// cores: x = n + f with n the nearest integer, 2^f on [-1/2, 1/2] by the cubic of least relative error (7.5e-5, from a Remez
-// exchange; P is rounded to 2^-9), n into the exponent.  Below 2^-126: 2^-126.
-__device__ __forceinline__ float2 ex2_by_polynomial(float2 x) {
-    constexpr float kMagic = 12582912.f;                     // 1.5 * 2^23: a sum with it has the nearest integer in its lowest bits
-    const unsigned long long xx = pack_f32x2(fmaxf(x.x, -126.f), fmaxf(x.y, -126.f));
-    const unsigned long long r = add_f32x2(xx, pack_f32x2(kMagic, kMagic)), n = add_f32x2(r, pack_f32x2(-kMagic, -kMagic));
-    const unsigned long long f = fma_f32x2(n, pack_f32x2(-1.f, -1.f), xx);
-    unsigned long long p = fma_f32x2(f, pack_f32x2(0.05517166852951f, 0.05517166852951f), pack_f32x2(0.24261112511158f, 0.24261112511158f));
-    p = fma_f32x2(p, f, pack_f32x2(0.69326096773148f, 0.69326096773148f));
-    p = fma_f32x2(p, f, pack_f32x2(0.99992805719376f, 0.99992805719376f));
-    const float2 pp = unpack_f32x2(p), rr = unpack_f32x2(r);
-    return make_float2(__uint_as_float(__float_as_uint(pp.x) + (__float_as_uint(rr.x) << 23)),
-                       __uint_as_float(__float_as_uint(pp.y) + (__float_as_uint(rr.y) << 23)));
 }
 
 // The same wait for the softmax warps, which have few registers to spare: 32-bit addresses and clock.
@@ -241,7 +224,7 @@ tree_attn_shared_kernel(const __grid_constant__ CUtensorMap tmap_q_shared, const
                 const bool any = cu.w < w_end, shared = cu.s < 0;
                 Segment* sg = &hd->seg[ring.at];
                 if (any) {
-                    const int s = cu.s, n = cu.run(w_end);
+                    const int s = cu.s, n = cu.run(wk, w_end);
                     const int pairs = shared ? wk.shared_pairs() : wk.own_pairs(), n_m = shared ? wk.shared_m : wk.own_m;
                     const int nb = shared ? a.shared_nb : a.own_nb;
                     const int hk = cu.i / pairs, m = 2 * (cu.i - hk * pairs);
@@ -502,12 +485,10 @@ tree_attn_shared_kernel(const __grid_constant__ CUtensorMap tmap_q_shared, const
                     unsigned long long ls2[2] = {0, 0};
 #pragma unroll
                     for (int e = 0; e < 64; ++e) {
-                        const unsigned long long x = fma_f32x2(pack_f32x2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1])), scale2, neg2);
-                        float2 p = unpack_f32x2(x);
-                        if (e % 8 < kByPolynomial) p = ex2_by_polynomial(p);
-                        else p = make_float2(ex2(p.x), ex2(p.y));
-                        ls2[e & 1] = add_f32x2(ls2[e & 1], pack_f32x2(p.x, p.y));
-                        v[e] = pack_bf16x2(p.x, p.y);
+                        const float2 x2 = unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1])), scale2, neg2));
+                        const float p0 = ex2(x2.x), p1 = ex2(x2.y);
+                        ls2[e & 1] = add_f32x2(ls2[e & 1], pack_f32x2(p0, p1));
+                        v[e] = pack_bf16x2(p0, p1);
                     }
                     const float2 l2 = unpack_f32x2(add_f32x2(ls2[0], ls2[1]));
                     l_run += l2.x + l2.y;
@@ -619,9 +600,9 @@ tree_attn_shared_merge_kernel(const __grid_constant__ SharedArgs a, int H, __nv_
         int n = 0;
         if (m < n_m) {
             const int T = own ? wk.tiles(s) : wk.shared_tiles, i = hk * (own ? wk.own_pairs() : wk.shared_pairs()) + (m >> 1);
-            const long long first = own ? wk.shared_total + (long long)wk.Hkv * wk.own_pairs() * (before + wk.pad * live) : 0;
+            const long long first = own ? wk.shared_total + (long long)wk.Hkv * wk.own_pairs() * (before * wk.places(0) + (long long)wk.change(0) * live) : 0;
             SharedParts ps;
-            ps.set(wk, own ? s : -1, i, first + (long long)i * wk.width(T), T, (m | 1) >= n_m, m & 1);
+            ps.set(wk, own ? s : -1, i, first + (long long)i * wk.width(own ? s : -1, T), T, (m | 1) >= n_m, m & 1);
             for (int k0 = 0; k0 < ps.n; k0 += 32) {
                 const int slot = k0 + lane < ps.n ? ps.slot(wk, k0 + lane) : -1;
                 const uint32_t there = __ballot_sync(0xFFFFFFFFu, slot >= 0);

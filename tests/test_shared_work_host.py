@@ -37,7 +37,7 @@ extern "C" int walk(int S, int B, int Hkv, int shared_tiles, int shared_m, int o
             if (cu.s >= S || cu.s < -1 || cu.i < 0) return 2;
             const int pairs = cu.s < 0 ? wk.shared_pairs() : wk.own_pairs(), n_m = cu.s < 0 ? shared_m : own_m;
             if (cu.i >= Hkv * pairs || cu.T != (cu.s < 0 ? shared_tiles : wk.tiles(cu.s))) return 3;
-            const int item = wk.item(cu.s, cu.i), n = cu.run(w_end);
+            const int item = wk.item(cu.s, cu.i), n = cu.run(wk, w_end);
             const bool single = 2 * (cu.i % pairs) + 1 >= n_m;
             if (item < 0 || item >= wk.items() || n < 1 || cu.t != dealt[item] || cu.t + n > cu.T) return 4;
             for (int l = 0; l < 2; ++l) {
@@ -47,7 +47,7 @@ extern "C" int walk(int S, int B, int Hkv, int shared_tiles, int shared_m, int o
                 if (slot < 0 || slot >= wk.slots() || written.count(slot)) return 5;
                 written[slot] = {item, tiles};
             }
-            dealt[item] += n; mine += n;
+            dealt[item] += n; mine += n * wk.places(cu.s);
             cu.skip(wk, n);
         }
         *longest = max(*longest, mine);
@@ -62,7 +62,7 @@ extern "C" int walk(int S, int B, int Hkv, int shared_tiles, int shared_m, int o
             if (dealt[wk.item(s, i)] != T) return 6;
             for (int m = 2 * (i % pairs); m < min(n_m, 2 * (i % pairs) + 2); ++m) {
                 SharedParts ps;
-                ps.set(wk, s, i, first + (long long)i * wk.width(T), T, (m | 1) >= n_m, m & 1);
+                ps.set(wk, s, i, first + (long long)i * wk.width(s, T), T, (m | 1) >= n_m, m & 1);
                 int tiles = 0;
                 for (int k = 0; k < ps.n; ++k) {
                     const int slot = ps.slot(wk, k);
@@ -73,7 +73,7 @@ extern "C" int walk(int S, int B, int Hkv, int shared_tiles, int shared_m, int o
                 if (tiles != T) return 8;
             }
         }
-        first += (long long)Hkv * pairs * wk.width(T);
+        first += (long long)Hkv * pairs * wk.width(s, T);
     }
     if (first != wk.total) return 9;
     return read == written.size() ? 0 : 10;
@@ -114,9 +114,9 @@ def test_random_lists(lib):
 
 
 def test_shares_are_even(lib):
-    """No CTA has more than an equal share, rounded up."""
+    """No CTA has more than an equal share of the places, up to one tile."""
     tiles = 8 * 16 * 64 + 16 * 8 * 17                       # 16 pairs a head over 8192 rows; 16 sequences of 2048 + 64 rows, a pair a head
-    assert _walk(lib, 16, 64, 8, 8192, 32, 2, 148, [2048] * 16) <= (tiles + 2 * (8 * 16 + 16 * 8)) // 148 + 1
+    assert _walk(lib, 16, 64, 8, 8192, 32, 2, 148, [2048] * 16) <= (5 * tiles + 16 * (8 * 16 + 16 * 8)) // 148 + 5
 
 
 def test_lengths_that_no_kernel_should_meet(lib):
