@@ -71,7 +71,8 @@ struct Header {
     unsigned long long kv_empty[kStages];
     unsigned long long seg_full[kSegments], seg_empty[kSegments];
     unsigned long long q_full, q_empty;
-    unsigned long long s_full[2], p_ready[2], o_full[2], o_free[2];
+    unsigned long long s_full[2], o_full[2], o_free[2];
+    unsigned long long p_ready[2][2];                        // of a lane, P of either half of a tile's keys
     uint32_t tmem_base;
     volatile int abort_flag;
 };
@@ -190,7 +191,7 @@ tree_attn_shared_kernel(const __grid_constant__ CUtensorMap tmap_q_shared, const
         for (int i = 0; i < kSegments; ++i) { mbar_init(&hd->seg_full[i], 1); mbar_init(&hd->seg_empty[i], 3 + 8); }
         mbar_init(&hd->q_full, 1); mbar_init(&hd->q_empty, 2);
         for (int l = 0; l < 2; ++l) {
-            mbar_init(&hd->s_full[l], 1); mbar_init(&hd->p_ready[l], 4); mbar_init(&hd->o_full[l], 1); mbar_init(&hd->o_free[l], 4);
+            mbar_init(&hd->s_full[l], 1); mbar_init(&hd->p_ready[l][0], 4); mbar_init(&hd->p_ready[l][1], 4); mbar_init(&hd->o_full[l], 1); mbar_init(&hd->o_free[l], 4);
         }
         hd->abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -370,13 +371,18 @@ tree_attn_shared_kernel(const __grid_constant__ CUtensorMap tmap_q_shared, const
                         // lane's product.)
                         if (!(ok = stage_full(2 * t + 1))) break;
                         if (more && !single && !(ok = stage_full(2 * (t + step)))) break;
-                        if (!(ok = wait_for(hd, &hd->p_ready[l], ops & 1, a.status))) break;
-                        ++ops;
-                        tc_fence_after();
                         const uint32_t v_lo = smem_desc_lo(kv_addr + ((2 * t + 1) % kStages) * kStageBytes, kHalfBytes);   // MN-major: LBO = next 64 d
+                        // the product with the first half's P runs beside the exponentials of the second
 #pragma unroll
-                        for (int kk = 0; kk < 8; ++kk)       // 16 keys per instruction
-                            umma_f16_ts_by(leader, o_tmem, s_tmem + kk * 8, smem_desc(v_lo + kk * (2048 >> 4)), idesc_pv, !first || kk > 0 ? 1u : 0u);
+                        for (int h = 0; h < 2; ++h) {
+                            if (!(ok = wait_for(hd, &hd->p_ready[l][h], ops & 1, a.status))) break;
+                            tc_fence_after();
+#pragma unroll
+                            for (int kk = 4 * h; kk < 4 * h + 4; ++kk)   // 16 keys per instruction
+                                umma_f16_ts_by(leader, o_tmem, s_tmem + kk * 8, smem_desc(v_lo + kk * (2048 >> 4)), idesc_pv, !first || kk > 0 ? 1u : 0u);
+                        }
+                        if (!ok) break;
+                        ++ops;
                         if (more) {
                             if (single && !(ok = stage_full(2 * (t + step)))) break;
                             scores(t + step);
@@ -403,8 +409,9 @@ tree_attn_shared_kernel(const __grid_constant__ CUtensorMap tmap_q_shared, const
         const int row = 32 * (warp & 3) + lane;              // TMEM lane == query row
         const uint32_t s_addr = tmem + kColS + l * 128 + ((uint32_t)(32 * (warp & 3)) << 16);   // O: kColO - kColS further
         const uint32_t base = smem_u32(hd), my_bars = base + 8 * l, abort_at = base + (uint32_t)offsetof(Header, abort_flag);
-        constexpr uint32_t kAtFull = offsetof(Header, s_full), kAtReady = offsetof(Header, p_ready), kAtDone = offsetof(Header, o_full);
+        constexpr uint32_t kAtFull = offsetof(Header, s_full), kAtDone = offsetof(Header, o_full);
         constexpr uint32_t kAtFree = offsetof(Header, o_free);
+        const uint32_t at_ready = base + (uint32_t)offsetof(Header, p_ready) + 16 * l;
         uint32_t ops = 0, segs = 0, tile0 = 0;               // products and segments of this lane; tiles of the CTA in front of this segment
         Ring ring{0, 0};
         bool ok = true;
@@ -437,6 +444,18 @@ tree_attn_shared_kernel(const __grid_constant__ CUtensorMap tmap_q_shared, const
                 ok = wait_at(my_bars + kAtFull, ops & 1, abort_at, a.status);
                 if (!ok) break;
                 tc_fence_after();
+                // ragged end: V rows past the last key may hold anything -> zeros (by either lane of a tile that both use)
+                if (t >= t_masked && (t + 1) * kSharedTile > sg.n_keys) {
+                    const uint32_t load = 2 * (tile0 + (t - sg.t_first)) + 1, st = load % kStages;
+                    ok = wait_for(hd, &hd->kv_full[st], (load / kStages) & 1, a.status);
+                    if (!ok) break;
+                    const int first_off = max(sg.n_keys - t * kSharedTile, 0) * 128;
+                    for (int off = first_off + row * 16; off < kHalfBytes; off += 128 * 16) {
+                        *reinterpret_cast<uint4*>(kv_smem + st * kStageBytes + off) = make_uint4(0, 0, 0, 0);
+                        *reinterpret_cast<uint4*>(kv_smem + st * kStageBytes + kHalfBytes + off) = make_uint4(0, 0, 0, 0);
+                    }
+                    fence_proxy_async();
+                }
                 if (warp_has_rows) {
                     TMEM_LD32(s_addr, v, 0); TMEM_LD32(s_addr + 32, v, 32);
                     TMEM_LD32(s_addr + 64, v, 64); TMEM_LD32(s_addr + 96, v, 96);
@@ -484,34 +503,27 @@ tree_attn_shared_kernel(const __grid_constant__ CUtensorMap tmap_q_shared, const
                     const unsigned long long scale2 = pack_f32x2(a.scale_log2, a.scale_log2), neg2 = pack_f32x2(neg_m, neg_m);
                     unsigned long long ls2[2] = {0, 0};
 #pragma unroll
-                    for (int e = 0; e < 64; ++e) {
-                        const float2 x2 = unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1])), scale2, neg2));
-                        const float p0 = ex2(x2.x), p1 = ex2(x2.y);
-                        ls2[e & 1] = add_f32x2(ls2[e & 1], pack_f32x2(p0, p1));
-                        v[e] = pack_bf16x2(p0, p1);
+                    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                        for (int e = 32 * h; e < 32 * h + 32; ++e) {
+                            const float2 x2 = unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1])), scale2, neg2));
+                            const float p0 = ex2(x2.x), p1 = ex2(x2.y);
+                            ls2[e & 1] = add_f32x2(ls2[e & 1], pack_f32x2(p0, p1));
+                            v[e] = pack_bf16x2(p0, p1);
+                        }
+                        TMEM_ST32(s_addr + 32 * h, v, 32 * h);
+                        tmem_wait_st();
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) arrive_at(at_ready + 8 * h);
                     }
                     const float2 l2 = unpack_f32x2(add_f32x2(ls2[0], ls2[1]));
                     l_run += l2.x + l2.y;
-                    TMEM_ST32(s_addr, v, 0);
-                    TMEM_ST32(s_addr + 32, v, 32);
-                    tmem_wait_st();
+                } else {
+                    tc_fence_before();
+                    if (lane == 0) { arrive_at(at_ready); arrive_at(at_ready + 8); }
                 }
                 first = false;
-                // ragged end: V rows past the last key may hold anything -> zeros (by either lane of a tile that both use)
-                if (t >= t_masked && (t + 1) * kSharedTile > sg.n_keys) {
-                    const uint32_t load = 2 * (tile0 + (t - sg.t_first)) + 1, st = load % kStages;
-                    ok = wait_for(hd, &hd->kv_full[st], (load / kStages) & 1, a.status);
-                    if (!ok) break;
-                    const int first_off = max(sg.n_keys - t * kSharedTile, 0) * 128;
-                    for (int off = first_off + row * 16; off < kHalfBytes; off += 128 * 16) {
-                        *reinterpret_cast<uint4*>(kv_smem + st * kStageBytes + off) = make_uint4(0, 0, 0, 0);
-                        *reinterpret_cast<uint4*>(kv_smem + st * kStageBytes + kHalfBytes + off) = make_uint4(0, 0, 0, 0);
-                    }
-                    fence_proxy_async();
-                }
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) arrive_at(my_bars + kAtReady);
                 ++ops;
             }
             if (!ok) break;
