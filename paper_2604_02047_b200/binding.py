@@ -117,24 +117,22 @@ def _nn(n_nodes: Optional[torch.Tensor], S: int) -> Optional[torch.Tensor]:
     return n_nodes
 
 
-def _opt(t: Optional[torch.Tensor], kind: str, name: str, *shape) -> Optional[torch.Tensor]:
-    """An optional argument: None, or a contiguous CUDA tensor of the kind and shape."""
-    if t is not None:
-        _all_dev(kind, name, t)
-        if tuple(t.shape) != shape:
-            raise GooseError("%s must have the shape %s" % (name, list(shape)))
-    return t
+def _shapes(names: str, what: str, letters: str, *args) -> None:
+    """``_native.shapes``: contiguous CUDA tensors of a kind and a shape each, with their names for the message."""
+    bad = _native.shapes(what, letters, *args)
+    if bad >= 0:
+        word = what.split()[bad]
+        size = dict(zip(letters, args))
+        raise GooseError("%s must be a contiguous CUDA tensor of dtype %s and shape %s" %
+                         (names.split()[bad], _KINDS[word[0]], [size[c] for c in word[1:].rstrip("?")]))
 
 
-def _token_stride(t: torch.Tensor, S: int, B: int, D: int, name: str) -> int:
+def _token_stride(t: torch.Tensor, S: int, B: int, heads: int, D: int, name: str) -> int:
     """Elements from token to token of a bf16 CUDA tensor [S][B][heads][D], or of such a part of a wider one."""
-    st = t.stride()
-    if not t.is_cuda or t.dtype != torch.bfloat16 or t.dim() != 4 or t.shape[0] != S or t.shape[1] != B or t.shape[3] != D:
-        raise GooseError("%s must be a bf16 CUDA tensor [S][B][heads][D]" % name)
-    heads = t.shape[2]
-    ld = st[1] if B > 1 else st[0] if S > 1 else heads * D
-    if (D > 1 and st[3] != 1) or (heads > 1 and st[2] != D) or (S > 1 and st[0] != B * ld):
-        raise GooseError("%s must have a token's heads next to one another and all tokens at one distance" % name)
+    ld = _native.token_stride(t, S, B, heads, D)
+    if ld < 0:
+        raise GooseError("%s must be a bf16 CUDA tensor [S][B][heads][D] = %s with a token's heads next to one another and all "
+                         "tokens at one distance" % (name, [S, B, heads, D]))
     return ld
 
 
@@ -297,25 +295,20 @@ class Goose:
         """Norm and rotation of new tokens' queries and keys, K and V rows into the caches behind ``ctx_len``.  q [S][B][H][D], k and v
         [S][B][Hkv][D] may be parts of one tensor [S][B][H + 2 Hkv][D].  ``rope`` fp32 [positions][rope_dim]: cosines, then
         sines.  Without ``parent`` the B tokens are a run (a prompt).  Returns the queries (``out``; q itself is allowed)."""
-        _all_dev("bbli", "k_cache v_cache row_off ctx_len", k_cache, v_cache, row_off, ctx_len)
         S, B, H, D = q.shape
-        Hkv = _kv_heads(k_cache, v_cache)
-        ldq, ldk, ldv = (_token_stride(t, S, B, D, n) for t, n in ((q, "q"), (k, "k"), (v, "v")))
-        if k.shape[2] != Hkv or v.shape[2] != Hkv or k_cache.shape[2] != D:
-            raise GooseError("append_kv: k and v must have the caches' heads")
-        if row_off.numel() != S or ctx_len.numel() != S:
-            raise GooseError("row_off and ctx_len must have one entry per sequence")
-        if rope is not None:
-            _all_dev("f", "rope", rope)
-            if rope.dim() != 2:
-                raise GooseError("rope must be [positions][rope_dim]")
+        rows, Hkv = k_cache.shape[:2]
+        positions, rope_dim = (0, 0) if rope is None else rope.shape
+        ldq = _token_stride(q, S, B, H, D, "q")
+        ldk = _token_stride(k, S, B, Hkv, D, "k")
+        ldv = _token_stride(v, S, B, Hkv, D, "v")
         if out is None:
             out = torch.empty((S, B, H, D), dtype=torch.bfloat16, device=q.device)
-        _opt(out, "b", "out", S, B, H, D)
-        _check(self.call.append_kv(self._h, q, ldq, k, ldk, v, ldv, _opt(q_weight, "b", "q_weight", D), _opt(k_weight, "b", "k_weight", D),
-                                   eps, rope, 0 if rope is None else rope.shape[0], 0 if rope is None else rope.shape[1], interleaved,
-                                   row_off, ctx_len, _opt(pos_off, "i", "pos_off", S), _opt(parent, "i", "parent", S, B),
-                                   _nn(n_nodes, S), S, B, H, Hkv, D, out, k_cache, v_cache, k_cache.shape[0]), "goose_append_kv")
+        _shapes("k_cache v_cache row_off ctx_len out rope parent n_nodes pos_off q_weight k_weight",
+                "bRKD bRKD lS iS bSBHD fPr? iSB? iS? iS? bD? bD?", "SBHDRKPr", S, B, H, D, rows, Hkv, positions, rope_dim,
+                k_cache, v_cache, row_off, ctx_len, out, rope, parent, n_nodes, pos_off, q_weight, k_weight)
+        _check(self.call.append_kv(self._h, q, ldq, k, ldk, v, ldv, q_weight, k_weight, eps, rope, positions, rope_dim, interleaved,
+                                   row_off, ctx_len, pos_off, parent, n_nodes, S, B, H, Hkv, D, out, k_cache, v_cache, rows),
+               "goose_append_kv")
         return out
 
     def tree_attn_shared(self, q, k_cache, v_cache, shared_row: int, shared_len: int, row_off, ctx_len, parent, scale: float,
@@ -323,18 +316,16 @@ class Goose:
                          lse: Optional[torch.Tensor] = None, n_nodes: Optional[torch.Tensor] = None):
         """Tree attention, multi-head or grouped-query, of a batch whose sequences all see the cache rows ``shared_row`` ..
         ``shared_row + shared_len - 1`` in front of their own.  Returns out, or (out, lse) with ``want_lse`` or ``lse``."""
-        _all_dev("bbblii", "q k_cache v_cache row_off ctx_len parent", q, k_cache, v_cache, row_off, ctx_len, parent)
         S, B, H, D = q.shape
-        Hkv = _kv_heads(k_cache, v_cache)
-        if tuple(parent.shape) != (S, B) or row_off.numel() != S or ctx_len.numel() != S or k_cache.shape[2] != D:
-            raise GooseError("tree_attn_shared: q is [S][B][H][D], parent [S][B], row_off and ctx_len [S]")
+        rows, Hkv = k_cache.shape[:2]
         if out is None:
             out = torch.empty_like(q)
         if want_lse and lse is None:
             lse = torch.empty((S, B, H), dtype=torch.float32, device=q.device)
-        _check(self.call.tree_attn_shared(self._h, q, k_cache, v_cache, k_cache.shape[0], shared_row, shared_len, row_off, ctx_len, parent,
-                                          _nn(n_nodes, S), S, B, H, Hkv, D, scale, _opt(out, "b", "out", S, B, H, D),
-                                          _opt(lse, "f", "lse", S, B, H)), "goose_tree_attn_shared")
+        _shapes("q k_cache v_cache row_off ctx_len parent out lse n_nodes", "bSBHD bRKD bRKD lS iS iSB bSBHD fSBH? iS?", "SBHDRK",
+                S, B, H, D, rows, Hkv, q, k_cache, v_cache, row_off, ctx_len, parent, out, lse, n_nodes)
+        _check(self.call.tree_attn_shared(self._h, q, k_cache, v_cache, rows, shared_row, shared_len, row_off, ctx_len, parent, n_nodes,
+                                          S, B, H, Hkv, D, scale, out, lse), "goose_tree_attn_shared")
         return out if lse is None else (out, lse)
 
     def adjust_logits(self, logits, hist, hist_len, draft_tok, parent, V: Optional[int] = None,
@@ -344,47 +335,39 @@ class Goose:
                       mask: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Penalties over hist [S][room] (hist_len [S] of it) and every node's path, bias fp32 [V] or [S][V], grammar mask int32
         [S*B][words] (bit 1: allowed).  ``out`` may be ``logits`` itself.  hist, hist_len and draft_tok may be None."""
-        _all_dev("bi", "logits parent", logits, parent)
         S, B = parent.shape
         rows, ldl = logits.shape
         V = ldl if V is None else V
-        if rows != S * B:
-            raise GooseError("logits must have a row per node")
-        if hist is not None:
-            _all_dev("ii", "hist hist_len", hist, hist_len)
-            if hist.dim() != 2 or hist.shape[0] != S or hist_len.numel() != S:
-                raise GooseError("hist must be [S][room], hist_len [S]")
-        if bias is not None:
-            _opt(bias, "f", "bias", *((V,) if bias.dim() == 1 else (S, V)))
-        if mask is not None:
-            _all_dev("i", "mask", mask)
-            if mask.dim() != 2 or mask.shape[0] != rows or 32 * mask.shape[1] < V:
-                raise GooseError("mask must have a row per node and a bit per token")
         if out is None:
             out = torch.empty_like(logits)
-        _all_dev("b", "out", out)
-        if out.dim() != 2 or out.shape[0] != rows:
-            raise GooseError("out must have a row per node")
-        _check(self.call.adjust_logits(self._h, logits, ldl, S, B, V, hist, 0 if hist is None else hist.shape[1], hist_len,
-                                       _opt(n_prompt, "i", "n_prompt", S), _opt(draft_tok, "i", "draft_tok", S, B), parent,
-                                       _nn(n_nodes, S), _opt(repetition, "f", "repetition", S), _opt(frequency, "f", "frequency", S),
-                                       _opt(presence, "f", "presence", S), bias, V if bias is not None and bias.dim() == 2 else 0, mask,
-                                       0 if mask is None else mask.shape[1], out, out.shape[1]), "goose_adjust_logits")
+        room = 0 if hist is None else hist.shape[-1]
+        words = 0 if mask is None else mask.shape[-1]
+        own_bias = bias is not None and bias.dim() == 2
+        _shapes("logits parent out hist draft_tok n_nodes n_prompt repetition frequency presence bias mask",
+                "bRl iSB bRo iSh? iSB? iS? iS? fS? fS? fS? %s? iRw?" % ("fSV" if own_bias else "fV"), "SBRVlohw", S, B, S * B, V, ldl,
+                out.shape[-1], room, words, logits, parent, out, hist, draft_tok, n_nodes, n_prompt, repetition, frequency, presence,
+                bias, mask)
+        if hist is not None:
+            _shapes("hist_len", "iS", "S", S, hist_len)
+        if mask is not None and 32 * words < V:
+            raise GooseError("mask must have a bit per token")
+        _check(self.call.adjust_logits(self._h, logits, ldl, S, B, V, hist, room, hist_len, n_prompt, draft_tok, parent, n_nodes, repetition,
+                                       frequency, presence, bias, V if own_bias else 0, mask, words, out, out.shape[-1]),
+               "goose_adjust_logits")
         return out
 
     def append_tokens(self, draft_tok, path, accept_len, hist, hist_len, n_nodes: Optional[torch.Tensor] = None,
                       new_len: Optional[torch.Tensor] = None) -> torch.Tensor:
         """The accepted path's tokens behind each sequence's history (``hist`` [S][room], updated in place); returns the new
         lengths (``new_len``, which must not be ``hist_len`` itself)."""
-        _all_dev("iiiii", "draft_tok path accept_len hist hist_len", draft_tok, path, accept_len, hist, hist_len)
         S, B = path.shape
-        if tuple(draft_tok.shape) != (S, B) or hist.dim() != 2 or hist.shape[0] != S or accept_len.numel() != S or hist_len.numel() != S:
-            raise GooseError("append_tokens: draft_tok and path are [S][B], hist [S][room], accept_len and hist_len [S]")
+        room = hist.shape[-1]
         if new_len is None:
             new_len = torch.empty_like(hist_len)
-        _opt(new_len, "i", "new_len", S)
-        _check(self.call.append_tokens(self._h, draft_tok, path, accept_len, _nn(n_nodes, S), S, B, hist, hist.shape[1], hist_len,
-                                       new_len), "goose_append_tokens")
+        _shapes("draft_tok path accept_len hist hist_len new_len n_nodes", "iSB iSB iS iSh iS iS iS?", "SBh", S, B, room, draft_tok, path,
+                accept_len, hist, hist_len, new_len, n_nodes)
+        _check(self.call.append_tokens(self._h, draft_tok, path, accept_len, n_nodes, S, B, hist, room, hist_len, new_len),
+               "goose_append_tokens")
         return new_len
 
     # ------------------------------------------------------------------ whole step

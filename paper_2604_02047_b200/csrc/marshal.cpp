@@ -80,6 +80,8 @@ struct Entry<F> {
     }
 };
 
+at::ScalarType kind_of(char k) { return k == 'b' ? at::kBFloat16 : k == 'l' ? at::kLong : k == 'i' ? at::kInt : at::kFloat; }
+
 // check(kinds, tensors...): the index of the first one that is not a contiguous CUDA tensor of its kind, -1 if there is none
 PyObject* check(PyObject*, PyObject* const* args, Py_ssize_t n) {
     Py_ssize_t len = 0;
@@ -90,10 +92,70 @@ PyObject* check(PyObject*, PyObject* const* args, Py_ssize_t n) {
         for (Py_ssize_t i = 0; i < len; ++i) {
             if (!THPVariable_Check(args[i + 1])) return PyLong_FromSsize_t(i);
             const at::Tensor& t = THPVariable_Unpack(args[i + 1]);
-            const at::ScalarType want = kinds[i] == 'b' ? at::kBFloat16 : kinds[i] == 'l' ? at::kLong : kinds[i] == 'i' ? at::kInt : at::kFloat;
-            if (!t.is_cuda() || t.scalar_type() != want || !t.is_contiguous()) return PyLong_FromSsize_t(i);
+            if (!t.is_cuda() || t.scalar_type() != kind_of(kinds[i]) || !t.is_contiguous()) return PyLong_FromSsize_t(i);
         }
         return PyLong_FromLong(-1);
+    });
+}
+
+// shapes(what, letters, sizes..., tensors...): the index of the first tensor that is not what `what` says, -1 if there is none.  A word a tensor: its
+// kind as in check(), a letter a dimension, `?` where it may be None: shapes("iSB iS?", "SB", 2, 60, parent, n_nodes)
+PyObject* shapes(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    Py_ssize_t n_letters = 0;
+    const char* what = n > 1 ? PyUnicode_AsUTF8(args[0]) : nullptr;
+    const char* letters = what ? PyUnicode_AsUTF8AndSize(args[1], &n_letters) : nullptr;
+    if (!letters) return PyErr_Occurred() ? nullptr : PyErr_Format(PyExc_TypeError, "words, letters, sizes and tensors expected");
+    if (n < 2 + n_letters) return PyErr_Format(PyExc_TypeError, "%zd letters, fewer sizes", n_letters);
+    return guarded([&]() -> PyObject* {
+        long long size[256] = {};
+        for (Py_ssize_t i = 0; i < n_letters; ++i) {
+            const long long v = PyLong_AsLongLong(args[2 + i]);
+            if (v == -1 && PyErr_Occurred()) return nullptr;
+            size[(unsigned char)letters[i]] = v;
+        }
+        Py_ssize_t at = 2 + n_letters;
+        for (const char* w = what; *w; ++at) {
+            while (*w == ' ') ++w;
+            if (!*w) break;
+            if (at >= n) return PyErr_Format(PyExc_TypeError, "fewer tensors than words");
+            const char kind = *w++;
+            const char* dims = w;
+            while (*w && *w != ' ' && *w != '?') ++w;
+            const Py_ssize_t n_dims = w - dims;
+            const bool optional = *w == '?';
+            if (optional) ++w;
+            if (args[at] == Py_None && optional) continue;
+            bool ok = THPVariable_Check(args[at]);
+            if (ok) {
+                const at::Tensor& t = THPVariable_Unpack(args[at]);
+                ok = t.is_cuda() && t.scalar_type() == kind_of(kind) && t.is_contiguous() && t.dim() == n_dims;
+                for (Py_ssize_t i = 0; ok && i < n_dims; ++i) ok = t.size(i) == size[(unsigned char)dims[i]];
+            }
+            if (!ok) return PyLong_FromSsize_t(at - 2 - n_letters);
+        }
+        return PyLong_FromLong(-1);
+    });
+}
+
+// token_stride(tensor, S, B, heads, D): elements from token to token of a bf16 CUDA tensor [S][B][heads][D], or of such a part of a wider
+// one; -1: it is none, or its tokens are not at one distance with their heads next to one another
+PyObject* token_stride(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    if (n != 5) return PyErr_Format(PyExc_TypeError, "a tensor and four sizes expected");
+    return guarded([&]() -> PyObject* {
+        long long size[4];
+        for (int i = 0; i < 4; ++i) {
+            size[i] = PyLong_AsLongLong(args[i + 1]);
+            if (size[i] == -1 && PyErr_Occurred()) return nullptr;
+        }
+        if (!THPVariable_Check(args[0])) return PyLong_FromLong(-1);
+        const at::Tensor& t = THPVariable_Unpack(args[0]);
+        if (!t.is_cuda() || t.scalar_type() != at::kBFloat16 || t.dim() != 4) return PyLong_FromLong(-1);
+        for (int i = 0; i < 4; ++i)
+            if (t.size(i) != size[i]) return PyLong_FromLong(-1);
+        const long long S = size[0], B = size[1], heads = size[2], D = size[3];
+        const long long ld = B > 1 ? t.stride(1) : S > 1 ? t.stride(0) : heads * D;
+        if ((D > 1 && t.stride(3) != 1) || (heads > 1 && t.stride(2) != D) || (S > 1 && t.stride(0) != B * ld)) return PyLong_FromLong(-1);
+        return PyLong_FromLongLong(ld);
     });
 }
 
@@ -117,6 +179,8 @@ PyMethodDef methods[] = {
     entry<&goose_adjust_logits>("adjust_logits"),
     entry<&goose_append_tokens>("append_tokens"),
     {"check", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&check)), METH_FASTCALL, nullptr},
+    {"shapes", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&shapes)), METH_FASTCALL, nullptr},
+    {"token_stride", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&token_stride)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
