@@ -20,7 +20,9 @@ namespace goose {
 constexpr int kAdjustThreads = 256;
 constexpr int kVocab = 8 * kAdjustThreads;           // tokens of a block
 constexpr int kBlockRows = 8;                        // rows of a block, at most
-constexpr int kCountThreads = 512;
+constexpr int kCountThreads = 1024;
+constexpr int kCountVocab = 4 * kCountThreads;       // tokens of a block of the first kernel
+static_assert(kCountVocab % kVocab == 0, "the second kernel's pieces lie in the first's");
 constexpr uint32_t kInPrompt = 0x80000000u;          // of a token's word: it occurs in the prompt; below: its count behind it
 
 // what the first kernel leaves of a sequence
@@ -44,10 +46,10 @@ __device__ __forceinline__ bool first_of_path(const uint4& path, const uint4& sa
     return first == j;
 }
 
-// the words of kVocab tokens (blocks 0 .. pieces - 1), the tree (the last block) of a sequence
+// the words of kCountVocab tokens (blocks 0 .. pieces - 1), the tree (the last block) of a sequence
 __global__ void __launch_bounds__(kCountThreads)
 adjust_tables_kernel(const AdjustLogits a, int pieces, int64_t ldw, uint32_t* __restrict__ words, AdjustTree* __restrict__ trees) {
-    __shared__ uint32_t s_count[kVocab];
+    __shared__ uint32_t s_count[kCountVocab];
     __shared__ uint4 s_path[kMaxB];
     __shared__ int s_up[kMaxB], s_tok[kMaxB];
     const int s = blockIdx.y, tid = threadIdx.x;
@@ -96,8 +98,7 @@ adjust_tables_kernel(const AdjustLogits a, int pieces, int64_t ldw, uint32_t* __
         return;
     }
     if (nn == 0) return;
-    const int base = blockIdx.x * kVocab;
-    static_assert(kVocab == 4 * kCountThreads, "a store a thread");
+    const int base = blockIdx.x * kCountVocab;
     reinterpret_cast<uint4*>(s_count)[tid] = make_uint4(0, 0, 0, 0);
     int len = a.hist_len[s];
     const int prompt = a.n_prompt ? a.n_prompt[s] : 0;
@@ -105,7 +106,7 @@ adjust_tables_kernel(const AdjustLogits a, int pieces, int64_t ldw, uint32_t* __
     __syncthreads();
     auto count = [&](int t, int j) {
         const uint32_t u = (uint32_t)(t - base);
-        if (u < (uint32_t)kVocab) {
+        if (u < (uint32_t)kCountVocab) {
             if (j < prompt) atomicOr(&s_count[u], kInPrompt);
             else atomicAdd(&s_count[u], 1u);
         }
@@ -135,12 +136,14 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
                  ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src), "r"(bytes), "r"((uint32_t)__cvta_generic_to_shared(bar)) : "memory");
 }
 
-// kMask: a mask is given
-template <bool kMask>
+// kMask: 0 none, 1 its bytes loaded by the threads, 2 its rows lie on 16 bytes and come with the logits
+template <int kMask>
 __global__ void __launch_bounds__(kAdjustThreads, 4)
 adjust_logits_kernel(const AdjustLogits a, int rows_per_block, int64_t ldw, const uint32_t* __restrict__ words,
                      const AdjustTree* __restrict__ trees) {
     __shared__ __align__(128) uint4 s_row[kBlockRows][kAdjustThreads];   // the block's logits as they were
+    __shared__ __align__(16) unsigned char s_mask[kMask == 2 ? kBlockRows : 1][kMask == 2 ? kAdjustThreads : 1];
+    __shared__ uint4 s_keep[kMask ? kAdjustThreads : 1];      // a mask byte as 16 bits a token: eight selects less a row
     __shared__ unsigned long long s_full;
     __shared__ volatile int s_abort;
     __shared__ int s_listed;
@@ -157,14 +160,25 @@ adjust_logits_kernel(const AdjustLogits a, int rows_per_block, int64_t ldw, cons
         s_abort = 0;
         if (rows > 0) {
             const uint32_t bar = (uint32_t)__cvta_generic_to_shared(&s_full), bytes = 16u * ((min(kVocab, a.V - base) + 7) / 8);
+            const uint32_t mask_bytes = kMask == 2 ? (uint32_t)min((int64_t)kAdjustThreads, 4 * a.ldm - base / 8) : 0;   // (ldm * 4 is a multiple of 16)
             asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar));
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-            asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes * rows) : "memory");
-            for (int u = 0; u < rows; ++u) bulk_load(s_row[u], a.logits + (row0 + u) * a.ldl + base, bytes, &s_full);
+            asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"((bytes + mask_bytes) * rows) : "memory");
+            for (int u = 0; u < rows; ++u) {
+                bulk_load(s_row[u], a.logits + (row0 + u) * a.ldl + base, bytes, &s_full);
+                if (kMask == 2) bulk_load(s_mask[u], reinterpret_cast<const unsigned char*>(a.mask + (row0 + u) * a.ldm) + base / 8, mask_bytes, &s_full);
+            }
         }
     }
+    if (kMask) {
+        static_assert(kAdjustThreads == 256, "an entry a thread");
+        uint32_t keep[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) keep[e] = ((tid >> (2 * e)) & 1 ? 0xFFFFu : 0u) | ((tid >> (2 * e + 1)) & 1 ? 0xFFFF0000u : 0u);
+        s_keep[tid] = make_uint4(keep[0], keep[1], keep[2], keep[3]);
+    }
     uint32_t open[2] = {0, 0};                                 // a byte a row
-    if (kMask && n_v > 0) {
+    if (kMask == 1 && n_v > 0) {
         const unsigned char* at = reinterpret_cast<const unsigned char*>(a.mask + row0 * a.ldm) + (v0 >> 3);
 #pragma unroll
         for (int u = 0; u < kBlockRows; ++u)
@@ -218,19 +232,17 @@ adjust_logits_kernel(const AdjustLogits a, int rows_per_block, int64_t ldw, cons
         for (int u = 0; u < rows; ++u, to += a.ldo) {
             const uint4 x = s_row[u][tid];
             const uint32_t in[4] = {x.x, x.y, x.z, x.w};
-            const uint32_t m = kMask ? (u < 4 ? open[0] : open[1]) >> (8 * (u & 3)) : 0;
+            const uint4 keep4 = kMask ? s_keep[kMask == 2 ? s_mask[u][tid] : ((u < 4 ? open[0] : open[1]) >> (8 * (u & 3))) & 0xFF] : make_uint4(0, 0, 0, 0);
+            const uint32_t keep[4] = {keep4.x, keep4.y, keep4.z, keep4.w};
             uint32_t out[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 float y0 = __uint_as_float(in[e] << 16), y1 = __uint_as_float(in[e] & 0xFFFF0000u);
                 y0 = fmaf(y0, y0 > 0.f ? m_up[2 * e] : m_down[2 * e], add[2 * e]);
                 y1 = fmaf(y1, y1 > 0.f ? m_up[2 * e + 1] : m_down[2 * e + 1], add[2 * e + 1]);
-                if (kMask) {
-                    if (!(m & (1u << (2 * e)))) y0 = -INFINITY;
-                    if (!(m & (2u << (2 * e)))) y1 = -INFINITY;
-                }
                 const __nv_bfloat162 b2 = __floats2bfloat162_rn(y0, y1);
                 out[e] = *reinterpret_cast<const uint32_t*>(&b2);
+                if (kMask) out[e] = (out[e] & keep[e]) | (0xFF80FF80u & ~keep[e]);   // -inf
             }
             if (bad) out[0] = out[1] = out[2] = out[3] = 0;
             if (n_v == 8) *reinterpret_cast<uint4*>(to) = make_uint4(out[0], out[1], out[2], out[3]);
@@ -257,24 +269,27 @@ adjust_logits_kernel(const AdjustLogits a, int rows_per_block, int64_t ldw, cons
 cudaError_t launch_adjust_logits(goose_ctx* c, AdjustLogits a, int S, cudaStream_t st) {
     if (S == 0) return cudaSuccess;
     a.status = c->status;
-    const int pieces = (a.V + kVocab - 1) / kVocab;
+    const int pieces = (a.V + kVocab - 1) / kVocab, count_pieces = (a.V + kCountVocab - 1) / kCountVocab;
     const bool counts = a.hist && (a.repetition || a.frequency || a.presence);
-    const int64_t ldw = counts ? (int64_t)pieces * kVocab : 0;
+    const int64_t ldw = counts ? (int64_t)count_pieces * kCountVocab : 0;
     const size_t tree_bytes = sizeof(AdjustTree) * (size_t)S, need = tree_bytes + sizeof(uint32_t) * (size_t)ldw * S;
     if (cudaError_t e = grow(&c->adjust_tables, &c->adjust_bytes, need)) return e;
     AdjustTree* trees = static_cast<AdjustTree*>(c->adjust_tables);
     uint32_t* words = counts ? reinterpret_cast<uint32_t*>(static_cast<char*>(c->adjust_tables) + tree_bytes) : nullptr;
-    cudaError_t e = launch_pdl(adjust_tables_kernel, dim3((counts ? pieces : 0) + 1, S), dim3(kCountThreads), 0, st, a, counts ? pieces : 0, ldw, words, trees);
+    cudaError_t e = launch_pdl(adjust_tables_kernel, dim3((counts ? count_pieces : 0) + 1, S), dim3(kCountThreads), 0, st, a, counts ? count_pieces : 0, ldw, words, trees);
     c->launches++;
     if (e != cudaSuccess) return e;
     // rows of a block: kBlockRows, fewer where there would not be two blocks an SM
     const long long all = (long long)S * pieces * a.B / (2LL * c->num_sms);
     const int rows = all >= kBlockRows ? kBlockRows : all < 1 ? 1 : (int)all;
-    e = launch_pdl(a.mask ? adjust_logits_kernel<true> : adjust_logits_kernel<false>, dim3(pieces, (a.B + rows - 1) / rows, S), dim3(kAdjustThreads), 0, st, a, rows, ldw, words, trees);
+    const bool on_16 = ((reinterpret_cast<uintptr_t>(a.mask) | (uintptr_t)(4 * a.ldm)) & 15) == 0;
+    auto kernel = !a.mask ? adjust_logits_kernel<0> : on_16 ? adjust_logits_kernel<2> : adjust_logits_kernel<1>;
+    e = launch_pdl(kernel, dim3(pieces, (a.B + rows - 1) / rows, S), dim3(kAdjustThreads), 0, st, a, rows, ldw, words, trees);
     c->launches++;
     return e;
 }
 
-cudaError_t init_adjust_kernel() { return load_kernels({(const void*)adjust_tables_kernel, (const void*)adjust_logits_kernel<false>, (const void*)adjust_logits_kernel<true>}); }
+cudaError_t init_adjust_kernel() { return load_kernels({(const void*)adjust_tables_kernel, (const void*)adjust_logits_kernel<0>, (const void*)adjust_logits_kernel<1>,
+                         (const void*)adjust_logits_kernel<2>}); }
 
 }  // namespace goose
