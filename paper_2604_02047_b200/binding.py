@@ -28,6 +28,8 @@ EXPORTS = [
 ATTN_AUTO, ATTN_MMA, ATTN_UMMA = 0, 1, 2
 ST_BAD_PARENT, ST_BAD_PATH, ST_TIMEOUT, ST_BAD_ROWS, ST_BAD_NODES, ST_BAD_POS = 1, 2, 4, 8, 16, 32
 
+HEAD_DIM = 128                   # GOOSE_HEAD_DIM
+
 _lib: Optional[ctypes.CDLL] = None
 _native = None
 
