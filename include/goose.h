@@ -137,9 +137,10 @@ int goose_tree_attn_gqa(goose_ctx* ctx, const void* q, const void* k_cache, cons
  *            call per part.  The positions of a sequence's own rows start at shared_len (pos_off of goose_append_kv).
  *   out bf16 [S][B][H][D], may be q itself; lse as in goose_tree_attn, of all keys
  * What a sequence's own rows hold never reaches another sequence's output.  The call's workspace (33 KB for 128 query rows of a
- * head, about three times) is allocated by the context's first call, and again by one that needs more: such a call waits for the
- * device, and cannot be captured into a graph (make one of that size before).  Other arguments, limits and errors as goose_tree_attn_gqa;
- * the kernel needs tensor maps (GOOSE_ECUDA where the driver cannot make them).                                          */
+ * head, about three times) is allocated by the context's first call, and again by one that needs more: such a call cannot be
+ * captured into a graph (make one of that size before); graphs captured before it stay valid, and the memory of both is the context's
+ * until it is destroyed.  Other arguments, limits and errors as goose_tree_attn_gqa; the kernel needs tensor maps (GOOSE_ECUDA where the
+ * driver cannot make them).                                                                                     */
 int goose_tree_attn_shared(goose_ctx* ctx, const void* q, const void* k_cache, const void* v_cache, int64_t kv_rows,
                            int64_t shared_row, int32_t shared_len, const int64_t* row_off, const int32_t* ctx_len,
                            const int32_t* parent, const int32_t* n_nodes, int S, int B, int H, int Hkv, int D, float scale,

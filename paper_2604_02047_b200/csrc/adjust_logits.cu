@@ -105,7 +105,7 @@ adjust_tables_kernel(const AdjustLogits a, int pieces, int64_t ldw, uint32_t* __
     if (len < 0 || len > a.ldh) len = 0;
     __syncthreads();
     auto count = [&](int t, int j) {
-        const uint32_t u = (uint32_t)(t - base);
+        const uint32_t u = (uint32_t)t - (uint32_t)base;
         if (u < (uint32_t)kCountVocab) {
             if (j < prompt) atomicOr(&s_count[u], kInPrompt);
             else atomicAdd(&s_count[u], 1u);
@@ -184,7 +184,7 @@ adjust_logits_kernel(const AdjustLogits a, int rows_per_block, int64_t ldw, cons
         for (int u = 0; u < kBlockRows; ++u)
             if (u < rows) open[u >> 2] |= (uint32_t)at[(size_t)u * 4 * a.ldm] << (8 * (u & 3));
     }
-    const int tok = tid < nn && rows > 0 && a.draft_tok ? a.draft_tok[(size_t)s * a.B + tid] - base : -1;
+    const uint32_t tok = tid < nn && rows > 0 && a.draft_tok ? (uint32_t)a.draft_tok[(size_t)s * a.B + tid] - (uint32_t)base : ~0u;
     const float rep = a.repetition ? a.repetition[s] : 1.f, freq = a.frequency ? a.frequency[s] : 0.f, pres = a.presence ? a.presence[s] : 0.f;
     const float inv_rep = 1.f / rep;
     const float* bias = a.bias ? a.bias + (size_t)s * a.bias_stride + base : nullptr;
@@ -198,7 +198,7 @@ adjust_logits_kernel(const AdjustLogits a, int rows_per_block, int64_t ldw, cons
         for (int e = 0; e < 8; ++e) add[e] = bias && e < n_v ? bias[8 * tid + e] : 0.f;
     }
     __syncthreads();
-    if ((uint32_t)tok < (uint32_t)kVocab) {
+    if (tok < (uint32_t)kVocab) {
         const int k = atomicAdd(&s_listed, 1);                 // (in any order: each pair writes an element of its own)
         s_list[k] = (unsigned char)tid;
         s_tok[k] = (short)tok;
@@ -273,7 +273,7 @@ cudaError_t launch_adjust_logits(goose_ctx* c, AdjustLogits a, int S, cudaStream
     const bool counts = a.hist && (a.repetition || a.frequency || a.presence);
     const int64_t ldw = counts ? (int64_t)count_pieces * kCountVocab : 0;
     const size_t tree_bytes = sizeof(AdjustTree) * (size_t)S, need = tree_bytes + sizeof(uint32_t) * (size_t)ldw * S;
-    if (cudaError_t e = grow(&c->adjust_tables, &c->adjust_bytes, need)) return e;
+    if (cudaError_t e = grow(c, &c->adjust_tables, &c->adjust_bytes, need)) return e;
     AdjustTree* trees = static_cast<AdjustTree*>(c->adjust_tables);
     uint32_t* words = counts ? reinterpret_cast<uint32_t*>(static_cast<char*>(c->adjust_tables) + tree_bytes) : nullptr;
     cudaError_t e = launch_pdl(adjust_tables_kernel, dim3((counts ? count_pieces : 0) + 1, S), dim3(kCountThreads), 0, st, a, counts ? count_pieces : 0, ldw, words, trees);

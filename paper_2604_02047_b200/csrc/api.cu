@@ -202,6 +202,7 @@ int goose_destroy(goose_ctx* c) {
     cudaFree(c->partials); cudaFree(c->head_counters); cudaFree(c->topk_cand);
     cudaFree(c->row_counters); cudaFree(c->topk_lse_ws); cudaFree(c->status); cudaFree(c->selftest_word); cudaFree(c->stage);
     cudaFree(c->shared_parts); cudaFree(c->adjust_tables);
+    for (int i = 0; i < c->n_outgrown; ++i) cudaFree(c->outgrown[i]);
     if (c->pin) cudaFreeHost(c->pin);
     if (c->side) cudaStreamDestroy(c->side);
     if (c->ev_fork) cudaEventDestroy(c->ev_fork);

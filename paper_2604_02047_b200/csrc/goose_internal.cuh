@@ -35,12 +35,14 @@ struct goose_ctx {
     float* topk_lse_ws;       // [topk_rows_cap][chunks][2]: per-chunk (max, sum) of the log-sum-exp
     int64_t topk_cand_cap;    // elements
     int topk_rows_cap;
-    // partial results of the shared-prefix attention: made by the first call that needs them, and again by one that needs more
+    // workspaces that the first call which needs them makes, and one that needs more makes again (see grow()): partial results of the
+    // shared-prefix attention, words and trees of goose_adjust_logits
     void* shared_parts;
     size_t shared_bytes;
-    // words and trees of goose_adjust_logits: likewise
     void* adjust_tables;
     size_t adjust_bytes;
+    void* outgrown[128];      // they live as long as the context: a captured graph may still name them
+    int n_outgrown;
     // per-sequence status words
     int32_t* status;          // [max_S]
     int32_t* selftest_word;   // result word of goose_selftest_bounded_wait
@@ -266,14 +268,17 @@ cudaError_t launch_bounded_wait_selftest(goose_ctx* c, long long limit_cycles, i
 // split count of the mma kernel's fixed grid: ctx_len lives on the device, so it depends only on S, H and the SM count
 int mma_splits(const goose_ctx* c, int S, int H);
 
-// a workspace that a call needs `need` bytes of (the old one is freed, which waits for whatever uses it)
-inline cudaError_t grow(void** p, size_t* bytes, size_t need) {
+// A workspace that a call needs `need` bytes of.  A new one has at least twice the old one's size, so that all of them together have less than
+// twice the last one's; the old one is kept, since a graph that was captured with it may be replayed as long as the context lives.
+inline cudaError_t grow(goose_ctx* c, void** p, size_t* bytes, size_t need) {
     if (need <= *bytes) return cudaSuccess;
-    cudaFree(*p);
-    *p = nullptr; *bytes = 0;
-    cudaError_t e = cudaMalloc(p, need);
+    if (*p && c->n_outgrown == (int)(sizeof c->outgrown / sizeof c->outgrown[0])) return cudaErrorMemoryAllocation;
+    const size_t size = need > 2 * *bytes ? need : 2 * *bytes;
+    void* fresh = nullptr;
+    cudaError_t e = cudaMalloc(&fresh, size);
     if (e != cudaSuccess) { cudaGetLastError(); return e; }
-    *bytes = need;
+    if (*p) c->outgrown[c->n_outgrown++] = *p;
+    *p = fresh; *bytes = size;
     return cudaSuccess;
 }
 

@@ -722,7 +722,7 @@ cudaError_t launch_tree_attn_shared(goose_ctx* c, const __nv_bfloat16* q, const 
     if (S == 0) return cudaSuccess;
     SharedArgs a = shared_args(c, kv_rows, shared_row, shared_len, row_off, ctx_len, parent, n_nodes, S, B, H, Hkv, scale);
     const size_t need = sizeof(float) * (size_t)a.wk.slots() * kPartFloats;
-    if (cudaError_t e = grow(&c->shared_parts, &c->shared_bytes, need)) return e;
+    if (cudaError_t e = grow(c, &c->shared_parts, &c->shared_bytes, need)) return e;
     a.parts = static_cast<float*>(c->shared_parts);
     CUtensorMap mqs, mqo, mk, mv;
     if (!make_q_map(c->encode_tiled, &mqs, q, (int64_t)S * B, Hkv, a.g, a.shared_nb) ||

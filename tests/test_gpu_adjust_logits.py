@@ -62,8 +62,10 @@ def _case(goose, S, B, V, lens, *, seed=0, parents=None, nodes=None, prompts=Non
     hist = rng.integers(0, top, (S, room))
     hist[:, ::7] = V + 5                                       # tokens of no row of the table count nowhere
     hist[:, ::11] = -1
+    hist[:, ::13] = -2 ** 31
     tok = rng.integers(0, top, (S, B))
     tok[:, ::5] = -3
+    tok[:, 3::17] = -2 ** 31
     parents = [synth.random_tree(rng, B) for _ in range(S)] if parents is None else parents
     rep, freq, pres = rng.uniform(1, 2, S), rng.uniform(-.5, 1, S), rng.uniform(-.5, 1, S)
     b = {"none": None, "one": rng.standard_normal(V), "own": rng.standard_normal((S, V))}[bias]

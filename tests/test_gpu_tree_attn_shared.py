@@ -227,6 +227,27 @@ def test_other_stream_in_place_and_graph(goose):
     assert torch.equal(out, want)
 
 
+def test_a_graph_outlives_its_workspace():
+    """A graph captured with a small workspace is replayed behind calls that needed a larger one."""
+    from paper_2604_02047_b200 import binding
+    g = binding.Goose(max_S=16, max_B=128, max_H=32)
+    small, large = Case(2, 8, 2, 5, 600, [100, 30]), Case(16, 32, 8, 64, 700, [40] * 16)
+    want = small.run(g)[0].clone()
+    args = (small.k, small.v, small.shared_row, small.shared, torch.tensor(small.off, device="cuda"), _i32(small.ctxs), _i32(small.parents),
+            small.scale)
+    out, graph = torch.zeros_like(want), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        g.tree_attn_shared(small.q, *args, out=out)
+    for _ in range(2):
+        large.check(g)
+        other = torch.full((large.S * 64 * 1024,), float("nan"), device="cuda")      # whatever was freed is somebody else's now
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.isnan(other).all()
+    g.close()
+
+
 def test_offsets_beyond_32_bits(goose):
     """Rows whose byte offset passes 2^32 (and whose element offset passes 2^31)."""
     rows = 2_200_000
