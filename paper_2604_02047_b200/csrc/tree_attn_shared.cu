@@ -581,7 +581,9 @@ tree_attn_shared_kernel(const __grid_constant__ CUtensorMap tmap_q_shared, const
     }
 }
 
-// Merge: 32 rows of one key/value head of one sequence (lane <-> row, warp <-> 16 columns), parts in rounds of kCombineRound.  The rows
+// Merge: 32 rows of one key/value head of one sequence (lane <-> row, warp <-> 16 columns), parts in rounds of kCombineRound.  Where a
+// sequence has no more than 16 rows, several lanes share a row's parts and join what they have (two sequences of 16 heads over 2, a token each, under 21k rows,
+// some 90 parts a row: 44 -> 27 us).  The rows
 // lie in two M tiles at most of the shared rows' work, and in two of the sequence's own; a warp makes the list of each tile's parts.
 constexpr int kMaxParts = 2 * 256;                           // lanes x CTAs that an item may lie in
 
@@ -591,7 +593,10 @@ tree_attn_shared_merge_kernel(const __grid_constant__ SharedArgs a, int H, __nv_
     __shared__ int s_parts[4];
     const int s = blockIdx.z, hk = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int nn = nodes_of(a.wk.n_nodes, s, a.wk.B), g = a.g;
-    const int r0 = blockIdx.x * 32, r = r0 + lane, node = r / g, member = r - node * g;
+    const int r0 = blockIdx.x * 32, in_block = min(32, a.wk.B * g - r0);
+    const int width = in_block > 1 ? 1 << (32 - __clz(in_block - 1)) : 1;   // lanes beside one another, a row each; the next as many share their parts
+    const int r = r0 + (lane & (width - 1)), node = r / g, member = r - node * g;
+    const bool row_valid = (lane & (width - 1)) < in_block && node < nn;
     const int shared_first = (s * a.wk.B + r0 / g) / a.shared_nb, own_first = r0 / g / a.own_nb;   // M tiles of the block's first row
     if (warp < 4) {
         // (the lengths are final: the main kernel has let this one in behind its own wait)
@@ -627,24 +632,23 @@ tree_attn_shared_merge_kernel(const __grid_constant__ SharedArgs a, int H, __nv_
     __syncthreads();
     pdl_wait();
     pdl_trigger();
-    if (node >= nn) return;
-
     // this row's lists and its rows in the M tiles
     const int tok = s * a.wk.B + node, m_shared = tok / a.shared_nb, m_own = node / a.own_nb;
     const int list0 = m_shared - shared_first, list1 = 2 + m_own - own_first;
     const int row0 = (tok - m_shared * a.shared_nb) * g + member, row1 = (node - m_own * a.own_nb) * g + member;
-    const int n0 = s_parts[list0], n = n0 + s_parts[list1];
+    const int n0 = row_valid ? s_parts[list0] : 0, n = row_valid ? n0 + s_parts[list1] : 0;
+    const int sharers = 32 / width, sharer = lane / width;
     float M = -INFINITY, L = 0.f, acc[16];
     bool bad = false;
 #pragma unroll
     for (int c = 0; c < 16; ++c) acc[c] = 0.f;
-    for (int k0 = 0; k0 < n; k0 += kCombineRound) {
+    for (int k0 = sharer; k0 < n; k0 += sharers * kCombineRound) {
         float m[kCombineRound];
         float2 ls[kCombineRound];
         uint4 x[kCombineRound][2];
 #pragma unroll
         for (int q = 0; q < kCombineRound; ++q) {
-            const int k = k0 + q;
+            const int k = k0 + q * sharers;
             m[q] = -INFINITY;
             ls[q] = make_float2(0.f, 1.f);
             x[q][0] = x[q][1] = make_uint4(0, 0, 0, 0);
@@ -682,6 +686,19 @@ tree_attn_shared_merge_kernel(const __grid_constant__ SharedArgs a, int H, __nv_
         }
         M = M_new;
     }
+    for (int o = width; o < 32; o <<= 1) {
+        const float M_new = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, o)), w = M == -INFINITY ? 0.f : ex2(M - M_new);
+        L *= w;
+        L += __shfl_xor_sync(0xFFFFFFFFu, L, o);
+#pragma unroll
+        for (int c = 0; c < 16; ++c) {
+            acc[c] *= w;
+            acc[c] += __shfl_xor_sync(0xFFFFFFFFu, acc[c], o);
+        }
+        bad |= __shfl_xor_sync(0xFFFFFFFFu, (int)bad, o) != 0;
+        M = M_new;
+    }
+    if (!row_valid || sharer > 0) return;
     const size_t at = ((size_t)s * a.wk.B + node) * H + hk * g + member;
     if (bad) {
         uint4* dst = reinterpret_cast<uint4*>(out + at * kHeadDim + 16 * warp);
