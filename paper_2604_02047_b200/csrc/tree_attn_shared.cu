@@ -581,17 +581,22 @@ tree_attn_shared_kernel(const __grid_constant__ CUtensorMap tmap_q_shared, const
     }
 }
 
-// Merge: 32 rows of one key/value head of one sequence (lane <-> row, warp <-> 16 columns), parts in rounds of kCombineRound.  Where a
-// sequence has no more than 16 rows, several lanes share a row's parts and join what they have (two sequences of 16 heads over 2, a token each, under 21k rows,
-// some 90 parts a row: 44 -> 27 us).  The rows
-// lie in two M tiles at most of the shared rows' work, and in two of the sequence's own; a warp makes the list of each tile's parts.
+// Merge: 32 rows of one key/value head of one sequence (lane <-> row, warp & 7 <-> 16 columns), parts in rounds of kCombineRound.  Where a
+// sequence has no more than 16 rows, several lanes share a row's parts and join what they have, and where the blocks are fewer than the
+// SMs and parts may be many, so do three times eight warps: with few heads a row has a hundred parts and more.  (16 heads over 2: two sequences, a token each, under
+// 21k rows 44 -> 23 us; one sequence, 4 nodes, under 30k 51 -> 33; joined without need, 4 x 32 over 8, a token each, under 512 11.5 -> 12.2.)  The rows lie in two M tiles at most of the shared rows' work, and
+// in two of the sequence's own; a warp makes the list of each tile's parts.
 constexpr int kMaxParts = 2 * 256;                           // lanes x CTAs that an item may lie in
 
-__global__ void __launch_bounds__(kCombineThreads)
+constexpr int kJoiners = 3;                                  // warps that share the parts of 16 columns, at most
+
+__global__ void __launch_bounds__(kJoiners * kCombineThreads)
 tree_attn_shared_merge_kernel(const __grid_constant__ SharedArgs a, int H, __nv_bfloat16* __restrict__ out, float* __restrict__ lse) {
     __shared__ int s_slot[4][kMaxParts];
     __shared__ int s_parts[4];
-    const int s = blockIdx.z, hk = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    __shared__ float s_join[18][8][32];
+    const int s = blockIdx.z, hk = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, columns = warp & 7, joiner = warp >> 3;
+    const int joiners = blockDim.x / kCombineThreads;
     const int nn = nodes_of(a.wk.n_nodes, s, a.wk.B), g = a.g;
     const int r0 = blockIdx.x * 32, in_block = min(32, a.wk.B * g - r0);
     const int width = in_block > 1 ? 1 << (32 - __clz(in_block - 1)) : 1;   // lanes beside one another, a row each; the next as many share their parts
@@ -637,7 +642,7 @@ tree_attn_shared_merge_kernel(const __grid_constant__ SharedArgs a, int H, __nv_
     const int list0 = m_shared - shared_first, list1 = 2 + m_own - own_first;
     const int row0 = (tok - m_shared * a.shared_nb) * g + member, row1 = (node - m_own * a.own_nb) * g + member;
     const int n0 = row_valid ? s_parts[list0] : 0, n = row_valid ? n0 + s_parts[list1] : 0;
-    const int sharers = 32 / width, sharer = lane / width;
+    const int sharers = 32 / width * joiners, sharer = lane / width + 32 / width * joiner;
     float M = -INFINITY, L = 0.f, acc[16];
     bool bad = false;
 #pragma unroll
@@ -657,8 +662,8 @@ tree_attn_shared_merge_kernel(const __grid_constant__ SharedArgs a, int H, __nv_
                 const int rr = k < n0 ? row0 : row1;
                 m[q] = __ldcg(part + kPartWords + rr);
                 ls[q] = __ldcg(reinterpret_cast<const float2*>(part + kPartWords + 128) + rr);
-                x[q][0] = __ldcg(reinterpret_cast<const uint4*>(part) + (2 * warp) * 128 + rr);
-                x[q][1] = __ldcg(reinterpret_cast<const uint4*>(part) + (2 * warp + 1) * 128 + rr);
+                x[q][0] = __ldcg(reinterpret_cast<const uint4*>(part) + (2 * columns) * 128 + rr);
+                x[q][1] = __ldcg(reinterpret_cast<const uint4*>(part) + (2 * columns + 1) * 128 + rr);
             }
         }
         float M_new = M;
@@ -686,25 +691,40 @@ tree_attn_shared_merge_kernel(const __grid_constant__ SharedArgs a, int H, __nv_
         }
         M = M_new;
     }
-    for (int o = width; o < 32; o <<= 1) {
-        const float M_new = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, o)), w = M == -INFINITY ? 0.f : ex2(M - M_new);
-        L *= w;
-        L += __shfl_xor_sync(0xFFFFFFFFu, L, o);
+    auto join = [&](float m, float l, auto part) {           // another's share
+        const float M_new = fmaxf(M, m), mine = M == -INFINITY ? 0.f : ex2(M - M_new), theirs = m == -INFINITY ? 0.f : ex2(m - M_new);
+        L = L * mine + l * theirs;
 #pragma unroll
-        for (int c = 0; c < 16; ++c) {
-            acc[c] *= w;
-            acc[c] += __shfl_xor_sync(0xFFFFFFFFu, acc[c], o);
-        }
-        bad |= __shfl_xor_sync(0xFFFFFFFFu, (int)bad, o) != 0;
+        for (int c = 0; c < 16; ++c) acc[c] = acc[c] * mine + part(c) * theirs;
         M = M_new;
+    };
+    for (int o = width; o < 32; o <<= 1) {
+        const float m = __shfl_xor_sync(0xFFFFFFFFu, M, o), l = __shfl_xor_sync(0xFFFFFFFFu, L, o);
+        bad |= __shfl_xor_sync(0xFFFFFFFFu, (int)bad, o) != 0;
+        join(m, l, [&](int c) { return __shfl_xor_sync(0xFFFFFFFFu, acc[c], o); });
+    }
+    for (int j = joiners - 1; j > 0; --j) {
+        if (joiner == j) {
+            s_join[16][columns][lane] = M;
+            s_join[17][columns][lane] = bad ? -1.f : L;
+#pragma unroll
+            for (int c = 0; c < 16; ++c) s_join[c][columns][lane] = acc[c];
+        }
+        __syncthreads();
+        if (joiner == 0) {
+            const float l = s_join[17][columns][lane];
+            bad |= l < 0.f;
+            join(s_join[16][columns][lane], l, [&](int c) { return s_join[c][columns][lane]; });
+        }
+        __syncthreads();
     }
     if (!row_valid || sharer > 0) return;
     const size_t at = ((size_t)s * a.wk.B + node) * H + hk * g + member;
     if (bad) {
-        uint4* dst = reinterpret_cast<uint4*>(out + at * kHeadDim + 16 * warp);
+        uint4* dst = reinterpret_cast<uint4*>(out + at * kHeadDim + 16 * columns);
         dst[0] = dst[1] = make_uint4(0, 0, 0, 0);
     } else {
-        store_merged(out + at * kHeadDim + 16 * warp, acc, L);
+        store_merged(out + at * kHeadDim + 16 * columns, acc, L);
     }
     if (lse && warp == 0) lse[at] = bad ? 0.f : (M + log2f(L)) * kLn2;
 }
@@ -749,7 +769,12 @@ cudaError_t launch_tree_attn_shared(goose_ctx* c, const __nv_bfloat16* q, const 
     cudaError_t e = launch_pdl(tree_attn_shared_kernel, dim3(a.wk.G), dim3(kSharedThreads), kSharedSmem, st, mqs, mqo, mk, mv, a);
     c->launches++;
     if (e != cudaSuccess) return e;
-    e = launch_pdl(tree_attn_shared_merge_kernel, dim3((B * a.g + 31) / 32, Hkv, S), dim3(kCombineThreads), 0, st, a, H, out, lse);
+    const dim3 blocks((B * a.g + 31) / 32, Hkv, S);
+    // CTAs that an item may lie in, as far as the host knows: more warps a row where that makes many parts
+    auto ctas = [&](long long tiles, long long items) { return tiles < a.wk.G / items ? tiles : a.wk.G / items; };
+    const long long most = ctas(a.wk.shared_tiles, Hkv * a.wk.shared_pairs()) + ctas((kv_rows + kSharedTile - 1) / kSharedTile, (long long)S * Hkv * a.wk.own_pairs());
+    const int joiners = (long long)blocks.x * Hkv * S < c->num_sms && most >= 12 ? kJoiners : 1;
+    e = launch_pdl(tree_attn_shared_merge_kernel, blocks, dim3(joiners * kCombineThreads), 0, st, a, H, out, lse);
     c->launches++;
     return e;
 }
