@@ -583,20 +583,22 @@ tree_attn_shared_kernel(const __grid_constant__ CUtensorMap tmap_q_shared, const
 
 // Merge: 32 rows of one key/value head of one sequence (lane <-> row, warp & 7 <-> 16 columns), parts in rounds of kCombineRound.  Where a
 // sequence has no more than 16 rows, several lanes share a row's parts and join what they have, and where the blocks are fewer than the
-// SMs and parts may be many, so do three times eight warps: with few heads a row has a hundred parts and more.  (16 heads over 2: two sequences, a token each, under
-// 21k rows 44 -> 23 us; one sequence, 4 nodes, under 30k 51 -> 33; joined without need, 4 x 32 over 8, a token each, under 512 11.5 -> 12.2.)  The rows lie in two M tiles at most of the shared rows' work, and
-// in two of the sequence's own; a warp makes the list of each tile's parts.
+// SMs and parts may be many, so do three times eight warps (kJoin): with few heads a row has a hundred parts and more.  (16 heads over 2: two
+// sequences, a token each, under 21k rows 44 -> 23 us; one sequence, 4 nodes, under 30k 51 -> 33; joined without need, 4 sequences of 32
+// heads over 8, a token each, under 512 rows 11.4 -> 12.2.)  The rows lie in two M tiles at most of the shared rows' work, and in two of the
+// sequence's own; a warp makes the list of each tile's parts.
 constexpr int kMaxParts = 2 * 256;                           // lanes x CTAs that an item may lie in
 
-constexpr int kJoiners = 3;                                  // warps that share the parts of 16 columns, at most
+constexpr int kJoiners = 3;                                  // warps that share the parts of 16 columns
 
-__global__ void __launch_bounds__(kJoiners * kCombineThreads)
+template <bool kJoin>
+__global__ void __launch_bounds__(kJoin ? kJoiners * kCombineThreads : kCombineThreads)
 tree_attn_shared_merge_kernel(const __grid_constant__ SharedArgs a, int H, __nv_bfloat16* __restrict__ out, float* __restrict__ lse) {
     __shared__ int s_slot[4][kMaxParts];
     __shared__ int s_parts[4];
-    __shared__ float s_join[18][8][32];
-    const int s = blockIdx.z, hk = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, columns = warp & 7, joiner = warp >> 3;
-    const int joiners = blockDim.x / kCombineThreads;
+    __shared__ float s_join[kJoin ? 18 : 1][8][32];
+    const int s = blockIdx.z, hk = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, columns = kJoin ? warp & 7 : warp;
+    const int joiner = kJoin ? warp >> 3 : 0, joiners = kJoin ? kJoiners : 1;
     const int nn = nodes_of(a.wk.n_nodes, s, a.wk.B), g = a.g;
     const int r0 = blockIdx.x * 32, in_block = min(32, a.wk.B * g - r0);
     const int width = in_block > 1 ? 1 << (32 - __clz(in_block - 1)) : 1;   // lanes beside one another, a row each; the next as many share their parts
@@ -773,15 +775,16 @@ cudaError_t launch_tree_attn_shared(goose_ctx* c, const __nv_bfloat16* q, const 
     // CTAs that an item may lie in, as far as the host knows: more warps a row where that makes many parts
     auto ctas = [&](long long tiles, long long items) { return tiles < a.wk.G / items ? tiles : a.wk.G / items; };
     const long long most = ctas(a.wk.shared_tiles, Hkv * a.wk.shared_pairs()) + ctas((kv_rows + kSharedTile - 1) / kSharedTile, (long long)S * Hkv * a.wk.own_pairs());
-    const int joiners = (long long)blocks.x * Hkv * S < c->num_sms && most >= 12 ? kJoiners : 1;
-    e = launch_pdl(tree_attn_shared_merge_kernel, blocks, dim3(joiners * kCombineThreads), 0, st, a, H, out, lse);
+    const bool join = (long long)blocks.x * Hkv * S < c->num_sms && most >= 12;
+    e = launch_pdl(join ? tree_attn_shared_merge_kernel<true> : tree_attn_shared_merge_kernel<false>, blocks,
+                   dim3(join ? kJoiners * kCombineThreads : kCombineThreads), 0, st, a, H, out, lse);
     c->launches++;
     return e;
 }
 
 cudaError_t init_shared_kernel() {
     cudaError_t e = cudaFuncSetAttribute(tree_attn_shared_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedSmem);
-    return e == cudaSuccess ? load_kernels({(const void*)tree_attn_shared_merge_kernel}) : e;
+    return e == cudaSuccess ? load_kernels({(const void*)tree_attn_shared_merge_kernel<false>, (const void*)tree_attn_shared_merge_kernel<true>}) : e;
 }
 
 }  // namespace goose
