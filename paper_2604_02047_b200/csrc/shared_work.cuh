@@ -37,8 +37,8 @@ struct SharedWork {
         return c < kv_rows ? c : kv_rows;
     }
     __host__ __device__ __forceinline__ int tiles(int s) const {
-        const int nn = nodes_of(n_nodes, s, B);
-        return nn == 0 ? 0 : (int)(((uint32_t)prefix(ctx_len[s]) + (uint32_t)nn + kSharedTile - 1) / kSharedTile);
+        const int ctx = prefix(ctx_len[s]), nn = nodes_of(n_nodes, s, B);
+        return nn == 0 ? 0 : (int)(((uint32_t)ctx + (uint32_t)nn + kSharedTile - 1) / kSharedTile);
     }
     // places of a tile of the shared rows (s < 0), of a sequence's own; of an item of T tiles (its region's items count alike)
     __host__ __device__ __forceinline__ int places(int s) const { return (s < 0 ? shared_m : own_m) > 1 ? kPairPlaces : kSinglePlaces; }

@@ -30,7 +30,7 @@ constexpr int kStages = 5;
 constexpr int kStageBytes = kSharedTile * kHeadDim * 2;      // 32 KB: one K or one V tile
 constexpr int kHalfBytes = kSharedTile * 128;                // 16 KB: 128 rows x 64 bf16 (one swizzle-atom column)
 constexpr int kQBytes = 2 * kHalfBytes;
-constexpr int kHeaderBytes = 1024;
+constexpr int kHeaderBytes = 2048;
 constexpr int kSharedSmem = 1008 /*alignment slack*/ + 2 * kQBytes + kStages * kStageBytes + kHeaderBytes;
 constexpr int kSharedThreads = 384;
 // registers: 168 a thread at launch; the warps of the loads and products give 112 each to the others (56 + 2 x 224 = 3 x 168)
@@ -56,22 +56,26 @@ struct Segment {
     int single, own;                                         // one M tile; a sequence's own rows
     int hk, token;                                           // key/value head, first token of the first M tile
     int row;                                                 // cache row of the first key tile
-    int slot;                                                // of lane 0's partial result
+    int slot;                                                // of the pair's first M tile; of a single one's first key tile
     int rows[2];                                             // query rows of the M tiles
     int node;                                                // tree node of the first M tile's first row
     int bad;
     int pad[2];
 };
-constexpr int kSegments = 3;
+constexpr int kSegments = 6;
 
 struct Header {
     Segment seg[kSegments];
     signed char par[kSegments][kMaxB];                       // parent[] of the segment's sequence
-    unsigned long long kv_full[kStages];
+    // Full: of the key tiles of single M tiles lane by lane (0, 1), of pairs (2).  A parity tells two phases apart, not three: nobody may wait
+    // for a phase of a barrier whose phases it has not all followed, and a lane does not follow the tiles of the other one.
+    unsigned long long kv_full[3][kStages];
     unsigned long long kv_empty[kStages];
     unsigned long long seg_full[kSegments], seg_empty[kSegments];
-    unsigned long long q_full, q_empty;
-    unsigned long long s_full[2], o_full[2], o_free[2];
+    // The two places of query tiles.  A pair has both, each lane its own; single M tiles have them in turn, so that the next one's queries come
+    // while the segment in front still uses the other.  With barriers of their own nobody waits on a phase that it has not followed.
+    unsigned long long pair_full[2], pair_empty[2], single_full[2], single_empty[2];
+    unsigned long long s_full[2], v_there[2], o_full[2], o_free[2];
     unsigned long long p_ready[2][2];                        // of a lane, P of either half of a tile's keys
     uint32_t tmem_base;
     volatile int abort_flag;
@@ -98,6 +102,12 @@ __device__ __forceinline__ bool wait_for(Header* hd, unsigned long long* bar, ui
         atomicOr(status, GOOSE_ST_TIMEOUT);
     }
     return r == 0;
+}
+__device__ __forceinline__ bool mbar_done(unsigned long long* bar, uint32_t parity) {   // a look, no wait
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity) : "memory");
+    return ok != 0;
 }
 __device__ __forceinline__ void drain(unsigned long long* bar, uint32_t parity) {   // after an abort
     const long long t0 = clock64();
@@ -187,11 +197,11 @@ tree_attn_shared_kernel(const __grid_constant__ CUtensorMap tmap_q_shared, const
     const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
 
     if (threadIdx.x == 0) {
-        for (int i = 0; i < kStages; ++i) { mbar_init(&hd->kv_full[i], 1); mbar_init(&hd->kv_empty[i], 2); }
+        for (int i = 0; i < kStages; ++i) { for (int u = 0; u < 3; ++u) mbar_init(&hd->kv_full[u][i], 1); mbar_init(&hd->kv_empty[i], 2); }
         for (int i = 0; i < kSegments; ++i) { mbar_init(&hd->seg_full[i], 1); mbar_init(&hd->seg_empty[i], 3 + 8); }
-        mbar_init(&hd->q_full, 1); mbar_init(&hd->q_empty, 2);
         for (int l = 0; l < 2; ++l) {
-            mbar_init(&hd->s_full[l], 1); mbar_init(&hd->p_ready[l][0], 4); mbar_init(&hd->p_ready[l][1], 4); mbar_init(&hd->o_full[l], 1); mbar_init(&hd->o_free[l], 4);
+            mbar_init(&hd->pair_full[l], 1); mbar_init(&hd->pair_empty[l], 1); mbar_init(&hd->single_full[l], 1); mbar_init(&hd->single_empty[l], 2);
+            mbar_init(&hd->s_full[l], 1); mbar_init(&hd->v_there[l], 1); mbar_init(&hd->p_ready[l][0], 4); mbar_init(&hd->p_ready[l][1], 4); mbar_init(&hd->o_full[l], 1); mbar_init(&hd->o_free[l], 4);
         }
         hd->abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -219,6 +229,10 @@ tree_attn_shared_kernel(const __grid_constant__ CUtensorMap tmap_q_shared, const
             SharedCursor cu;
             long long w_end;
             locate(wk, cu, w_end, blockIdx.x, lane);
+            // of the sequence that the items are of (a head after the other): asked for together, kept until the next one's
+            int of = -1, nn = 0, ctx = 0, par[kMaxB / 32];
+            int64_t row0 = 0;
+            bool bad = false;
             Ring ring{0, 0};
             for (;;) {
                 if (!wait_for(hd, &hd->seg_empty[ring.at], ring.phase ^ 1, a.status)) break;
@@ -229,21 +243,32 @@ tree_attn_shared_kernel(const __grid_constant__ CUtensorMap tmap_q_shared, const
                     const int pairs = shared ? wk.shared_pairs() : wk.own_pairs(), n_m = shared ? wk.shared_m : wk.own_m;
                     const int nb = shared ? a.shared_nb : a.own_nb;
                     const int hk = cu.i / pairs, m = 2 * (cu.i - hk * pairs);
-                    const int nn = shared ? 0 : nodes_of(wk.n_nodes, s, wk.B), ctx = shared ? a.shared_len : wk.prefix(wk.ctx_len[s]);
-                    const int64_t row0 = shared ? a.shared_row : a.row_off[s];
-                    bool bad = false;
-                    if (!shared) {
-                        // a sequence of a parent[] that is no tree, or whose rows leave the cache: every part of it says so
-                        bool no_tree = false;
-                        for (int i = lane; i < nn; i += 32) {
-                            const int p = a.parent[(size_t)s * wk.B + i];
-                            hd->par[ring.at][i] = (signed char)p;
-                            no_tree |= i == 0 ? p != -1 : (p < 0 || p >= i);
+                    if (shared) {
+                        ctx = a.shared_len; row0 = a.shared_row;
+                    } else {
+                        if (s != of) {
+#pragma unroll
+                            for (int j = 0; j < kMaxB / 32; ++j) par[j] = lane + 32 * j < wk.B ? a.parent[(size_t)s * wk.B + lane + 32 * j] : 0;
+                            row0 = a.row_off[s];
+                            const int given = wk.ctx_len[s];
+                            nn = nodes_of(wk.n_nodes, s, wk.B);
+                            ctx = wk.prefix(given);
+                            of = s;
+                            // a sequence of a parent[] that is no tree, or whose rows leave the cache: every part of it says so
+                            bool no_tree = false;
+#pragma unroll
+                            for (int j = 0; j < kMaxB / 32; ++j) {
+                                const int i = lane + 32 * j;
+                                no_tree |= i < nn && (i == 0 ? par[j] != -1 : (par[j] < 0 || par[j] >= i));
+                            }
+                            no_tree = __any_sync(0xFFFFFFFFu, no_tree);
+                            const bool bad_rows = rows_outside(row0, given, nn, wk.kv_rows);
+                            bad = no_tree || bad_rows;
+                            if (bad && lane == 0) atomicOr(&a.status[s], (no_tree ? GOOSE_ST_BAD_PARENT : 0) | (bad_rows ? GOOSE_ST_BAD_ROWS : 0));
                         }
-                        no_tree = __any_sync(0xFFFFFFFFu, no_tree);
-                        const bool bad_rows = rows_outside(row0, wk.ctx_len[s], nn, wk.kv_rows);
-                        bad = no_tree || bad_rows;
-                        if (bad && lane == 0) atomicOr(&a.status[s], (no_tree ? GOOSE_ST_BAD_PARENT : 0) | (bad_rows ? GOOSE_ST_BAD_ROWS : 0));
+#pragma unroll
+                        for (int j = 0; j < kMaxB / 32; ++j)
+                            if (lane + 32 * j < nn) hd->par[ring.at][lane + 32 * j] = (signed char)par[j];
                     }
                     if (lane == 0) {
                         sg->n = n; sg->t_first = cu.t; sg->ctx = ctx; sg->n_keys = ctx + nn;
@@ -270,45 +295,86 @@ tree_attn_shared_kernel(const __grid_constant__ CUtensorMap tmap_q_shared, const
             if (lane == 0) {
                 // a sequence's own rows are read by one or two CTAs, the shared ones by many
                 const unsigned long long pol_own = l2_policy_evict_first(), pol_shared = l2_policy_evict_last();
-                uint32_t loads = 0, segs = 0;
+                uint32_t pairs = 0, singles = 0, tile0 = 0;  // segments of either kind, tiles in front of this segment
+                uint32_t phases = 0, users = 0;              // a bit a kv_full barrier; two bits a stage: who has it, 3: nobody yet
+                for (int i = 0; i < kStages; ++i) users |= 3u << 2 * i;
                 Ring st{0, 0}, ring{0, 0};
                 bool ok = true;
+                Segment sg{};
+                uint32_t asked = 0;                          // query tiles of the segment that still wait for their place
+                auto load_q = [&](int b) {
+                    const int nb = sg.own ? a.own_nb : a.shared_nb, m = sg.single ? 0 : b;
+                    const CUtensorMap* mq = sg.own ? &tmap_q_own : &tmap_q_shared;
+                    unsigned long long* full = sg.single ? &hd->single_full[b] : &hd->pair_full[b];
+                    mbar_expect_tx(full, (uint32_t)(nb * a.g) * 256u);
+                    tma_load_4d(q_smem + b * kQBytes, mq, full, 0, 0, sg.hk, sg.token + m * nb);
+                    tma_load_4d(q_smem + b * kQBytes + kHalfBytes, mq, full, 64, 0, sg.hk, sg.token + m * nb);
+                    asked &= ~(1u << b);
+                };
+                // place b is free when the last pair and the last single M tile that had it are done
+                auto pair_parity = [&]() { return (pairs & 1) ^ 1; };
+                auto single_parity = [&](int b) { return ((singles + 1 - b) >> 1 & 1) ^ 1; };
+                auto load_free_q = [&]() {
+                    for (int b = 0; b < 2; ++b)
+                        if ((asked >> b & 1) && mbar_done(&hd->pair_empty[b], pair_parity()) && mbar_done(&hd->single_empty[b], single_parity(b)))
+                            load_q(b);
+                };
+                // The key tiles do not wait for the queries' place: a pair's is free only when the products of the segment in front
+                // are done, and the ring would run dry meanwhile.
+                auto stage_free = [&]() {
+                    const long long t0 = clock64();
+                    while (asked) {
+                        load_free_q();
+                        if (mbar_done(&hd->kv_empty[st.at], st.phase ^ 1)) return true;
+                        if (hd->abort_flag || clock64() - t0 > kWaitCycles) break;   // (the wait below says so)
+                    }
+                    return wait_for(hd, &hd->kv_empty[st.at], st.phase ^ 1, a.status);
+                };
                 while (ok) {
-                    ok = wait_for(hd, &hd->seg_full[ring.at], ring.phase, a.status);
+                    for (int b = 0; b < 2 && ok; ++b)        // of the segment in front
+                        if (asked >> b & 1) {
+                            ok = wait_for(hd, &hd->pair_empty[b], pair_parity(), a.status) && wait_for(hd, &hd->single_empty[b], single_parity(b), a.status);
+                            if (ok) load_q(b);
+                        }
+                    if (ok && sg.n > 0) { if (sg.single) ++singles; else ++pairs; sg.n = 0; }
+                    ok = ok && wait_for(hd, &hd->seg_full[ring.at], ring.phase, a.status);
                     if (!ok) break;
-                    const Segment sg = hd->seg[ring.at];
+                    sg = hd->seg[ring.at];
                     mbar_arrive(&hd->seg_empty[ring.at]);
                     ring.next(kSegments);
                     if (sg.n == 0) break;
-                    ok = wait_for(hd, &hd->q_empty, (segs & 1) ^ 1, a.status);
-                    if (!ok) break;
-                    const int nb = sg.own ? a.own_nb : a.shared_nb, tiles_q = sg.single ? 1 : 2;
-                    mbar_expect_tx(&hd->q_full, (uint32_t)(tiles_q * nb * a.g) * 256u);
-                    const CUtensorMap* mq = sg.own ? &tmap_q_own : &tmap_q_shared;
-                    for (int m = 0; m < tiles_q; ++m) {
-                        tma_load_4d(q_smem + m * kQBytes, mq, &hd->q_full, 0, 0, sg.hk, sg.token + m * nb);
-                        tma_load_4d(q_smem + m * kQBytes + kHalfBytes, mq, &hd->q_full, 64, 0, sg.hk, sg.token + m * nb);
-                    }
-                    ++segs;
+                    asked = sg.single ? 1u << (singles & 1) : 3u;
                     uint32_t krow = (uint32_t)sg.row;
                     const unsigned long long pol = sg.own ? pol_own : pol_shared;
                     for (int i = 0; i < sg.n && ok; ++i, krow += kSharedTile) {
+                        const uint32_t user = sg.single ? (tile0 + i) & 1 : 2;
                         for (int kv = 0; kv < 2 && ok; ++kv) {
-                            ok = wait_for(hd, &hd->kv_empty[st.at], st.phase ^ 1, a.status);
+                            ok = stage_free();
                             if (!ok) break;
                             unsigned char* dst = kv_smem + st.at * kStageBytes;
-                            mbar_expect_tx(&hd->kv_full[st.at], kStageBytes);
+                            unsigned long long* full = &hd->kv_full[user][st.at];
+                            mbar_expect_tx(full, kStageBytes);
                             const CUtensorMap* mp = kv ? &tmap_v : &tmap_k;
-                            tma_load_3d_hint(dst, mp, &hd->kv_full[st.at], 0, sg.hk, (int)krow, pol);
-                            tma_load_3d_hint(dst + kHalfBytes, mp, &hd->kv_full[st.at], 64, sg.hk, (int)krow, pol);
-                            ++loads;
+                            tma_load_3d_hint(dst, mp, full, 0, sg.hk, (int)krow, pol);
+                            tma_load_3d_hint(dst + kHalfBytes, mp, full, 64, sg.hk, (int)krow, pol);
+                            phases ^= 1u << (user * kStages + st.at);
+                            users = (users & ~(3u << 2 * st.at)) | user << 2 * st.at;
                             st.next(kStages);
                         }
                     }
+                    tile0 += sg.n;
                 }
                 if (!ok) {                                   // copies still in flight land before the CTA ends
-                    for (uint32_t r = loads > kStages ? loads - kStages : 0; r < loads; ++r) drain(&hd->kv_full[r % kStages], (r / kStages) & 1);
-                    if (segs > 0) drain(&hd->q_full, (segs - 1) & 1);
+                    for (int i = 0; i < kStages; ++i) {
+                        const uint32_t user = users >> 2 * i & 3;
+                        if (user < 3) drain(&hd->kv_full[user][i], (phases >> (user * kStages + i) & 1) ^ 1);
+                    }
+                    if (sg.n > 0 && sg.single && !asked) ++singles;   // (only copies that began)
+                    for (int b = 0; b < 2; ++b) {
+                        const uint32_t of_pairs = pairs + (sg.n > 0 && !sg.single && !(asked >> b & 1)), of_singles = (singles + 1 - b) >> 1;
+                        if (of_pairs > 0) drain(&hd->pair_full[b], (of_pairs - 1) & 1);
+                        if (of_singles > 0) drain(&hd->single_full[b], (of_singles - 1) & 1);
+                    }
                 }
             }
         } else {
@@ -319,23 +385,34 @@ tree_attn_shared_kernel(const __grid_constant__ CUtensorMap tmap_q_shared, const
                 const uint32_t q_addr = smem_u32(q_smem), kv_addr = smem_u32(kv_smem);
                 const uint32_t s_tmem = tmem + kColS + l * 128, o_tmem = tmem + kColO + l * 128;
                 constexpr uint32_t idesc_qk = instr_desc(false), idesc_pv = instr_desc(true);
-                uint32_t ops = 0, segs = 0, seg = 0, tile0 = 0;   // products, segments of this lane; segments, tiles of the CTA
+                uint32_t ops = 0, segs = 0, tile0 = 0;       // products, segments of this lane; tiles of the CTA
+                uint32_t pairs = 0, singles = 0;             // segments of the CTA
                 Ring ring{0, 0};
                 bool ok = true;
-                // K of tile i of the CTA is load 2 i, V load 2 i + 1
-                auto stage_full = [&](uint32_t load) { return wait_for(hd, &hd->kv_full[load % kStages], (load / kStages) & 1, a.status); };
+                uint32_t phases = 0;                         // a bit a kv_full barrier of this lane and, kStages further, of pairs
+                bool single = false;
+                // K of tile i of the CTA is load 2 i, V load 2 i + 1; once a load
+                auto stage_full = [&](uint32_t load) {
+                    const uint32_t at = load % kStages, bit = single ? at : kStages + at;
+                    const uint32_t parity = phases >> bit & 1;
+                    phases ^= 1u << bit;
+                    return wait_for(hd, &hd->kv_full[single ? l : 2][at], parity, a.status);
+                };
                 while (ok) {
                     ok = wait_for(hd, &hd->seg_full[ring.at], ring.phase, a.status);
                     if (!ok) break;
                     const int n = __shfl_sync(0xFFFFFFFFu, hd->seg[ring.at].n, 0);   // (uniform registers)
-                    const bool single = __shfl_sync(0xFFFFFFFFu, hd->seg[ring.at].single, 0) != 0;
+                    single = __shfl_sync(0xFFFFFFFFu, hd->seg[ring.at].single, 0) != 0;
                     __syncwarp();
                     if (leader) mbar_arrive(&hd->seg_empty[ring.at]);
                     ring.next(kSegments);
                     if (n == 0) break;
-                    ok = wait_for(hd, &hd->q_full, seg & 1, a.status);
+                    const uint32_t place = single ? singles & 1 : l;
+                    unsigned long long* const q_full = single ? &hd->single_full[place] : &hd->pair_full[l];
+                    unsigned long long* const q_empty = single ? &hd->single_empty[place] : &hd->pair_empty[l];
+                    ok = wait_for(hd, q_full, (single ? singles >> 1 : pairs) & 1, a.status);
                     if (!ok) break;
-                    const uint32_t q_lo = smem_desc_lo(q_addr + (single ? 0 : l) * kQBytes, 16);
+                    const uint32_t q_lo = smem_desc_lo(q_addr + place * kQBytes, 16);
                     const uint32_t step = single ? 2 : 1, end = tile0 + n;
                     auto release = [&](uint32_t load) {      // every stage has two arrivals
                         umma_commit_by(leader, &hd->kv_empty[load % kStages]);
@@ -351,7 +428,7 @@ tree_attn_shared_kernel(const __grid_constant__ CUtensorMap tmap_q_shared, const
                         }
                         umma_commit_by(leader, &hd->s_full[l]);         // (and with it the product in front of it)
                     };
-                    uint32_t t = tile0 + (single ? l : 0);
+                    uint32_t t = tile0 + (single ? (tile0 ^ l) & 1 : 0);
                     const bool any = t < end;
                     if (any) {
                         ok = stage_full(2 * t);
@@ -360,8 +437,8 @@ tree_attn_shared_kernel(const __grid_constant__ CUtensorMap tmap_q_shared, const
                         release(2 * t);
                     }
                     if (t + step >= end) {                   // the lane's last Q K^T of the segment
-                        if (any) umma_commit_by(leader, &hd->q_empty);
-                        else if (leader) mbar_arrive(&hd->q_empty);
+                        if (any) umma_commit_by(leader, q_empty);
+                        else if (leader) mbar_arrive(q_empty);
                     }
                     if (any && segs > 0) ok = wait_for(hd, &hd->o_free[l], (segs - 1) & 1, a.status);
                     for (bool first = true; t < end && ok; t += step, first = false) {
@@ -370,6 +447,7 @@ tree_attn_shared_kernel(const __grid_constant__ CUtensorMap tmap_q_shared, const
                         // first, while P is still being made.  (The next K of a single M tile may only be on its way behind the other
                         // lane's product.)
                         if (!(ok = stage_full(2 * t + 1))) break;
+                        if (leader) mbar_arrive(&hd->v_there[l]);
                         if (more && !single && !(ok = stage_full(2 * (t + step)))) break;
                         const uint32_t v_lo = smem_desc_lo(kv_addr + ((2 * t + 1) % kStages) * kStageBytes, kHalfBytes);   // MN-major: LBO = next 64 d
                         // the product with the first half's P runs beside the exponentials of the second
@@ -392,12 +470,12 @@ tree_attn_shared_kernel(const __grid_constant__ CUtensorMap tmap_q_shared, const
                         release(2 * t + 1);
                         if (more) {
                             release(2 * (t + step));
-                            if (t + 2 * step >= end) umma_commit_by(leader, &hd->q_empty);
+                            if (t + 2 * step >= end) umma_commit_by(leader, q_empty);
                         }
                     }
                     if (!ok) break;
                     segs += any;
-                    ++seg;
+                    if (single) ++singles; else ++pairs;
                     tile0 = end;
                 }
             }
@@ -415,7 +493,8 @@ tree_attn_shared_kernel(const __grid_constant__ CUtensorMap tmap_q_shared, const
         uint32_t ops = 0, segs = 0, tile0 = 0;               // products and segments of this lane; tiles of the CTA in front of this segment
         Ring ring{0, 0};
         bool ok = true;
-        uint32_t v[128];
+        uint32_t v[128], anc[4] = {0, 0, 0, 0};
+        int anc_of = -1;                                     // first token of the M tile that anc[] is of
 
         for (;;) {
             ok = wait_for(hd, &hd->seg_full[ring.at], ring.phase, a.status);
@@ -423,14 +502,17 @@ tree_attn_shared_kernel(const __grid_constant__ CUtensorMap tmap_q_shared, const
             const Segment& sg = hd->seg[ring.at];
             if (sg.n == 0) break;
             const int step = sg.single ? 2 : 1, t_end = sg.t_first + sg.n;
+            const int turn = sg.single ? (tile0 ^ l) & 1 : l;   // a single M tile's key tiles are dealt on where the segment in front ended
             const int rows = sg.rows[sg.single ? 0 : l];
             const bool row_valid = row < rows, warp_has_rows = (row & ~31) < rows;
             const int t_masked = sg.ctx / kSharedTile;       // from here on a tile reaches the tree rows, or the ragged end
-            // the row's ancestors, where the segment reaches the tree (while its first scores are on their way)
-            uint32_t anc[4] = {0, 0, 0, 0};
-            if (sg.own && t_end > t_masked && row_valid && !sg.bad) {
+            // the row's ancestors, where the segment reaches the tree (while its first scores are on their way); the heads of a sequence have
+            // the same
+            if (sg.own && t_end > t_masked && anc_of != sg.token + (sg.single ? 0 : l) * a.own_nb) {
+                anc_of = sg.token + (sg.single ? 0 : l) * a.own_nb;
+                anc[0] = anc[1] = anc[2] = anc[3] = 0;
                 int vtx = sg.node + (sg.single ? 0 : l) * a.own_nb + row / a.g;
-                for (int up = 0; up < kMaxB && vtx >= 0; ++up) {
+                for (int up = row_valid && !sg.bad ? 0 : kMaxB; up < kMaxB && vtx >= 0; ++up) {
                     const uint32_t bit = 1u << (vtx & 31);
                     const int wsel = vtx >> 5;
                     anc[0] |= (wsel == 0) ? bit : 0; anc[1] |= (wsel == 1) ? bit : 0;
@@ -440,14 +522,14 @@ tree_attn_shared_kernel(const __grid_constant__ CUtensorMap tmap_q_shared, const
             }
             float m_run = -INFINITY, l_run = 0.f;
             bool first = true;
-            for (int t = sg.t_first + (sg.single ? l : 0); t < t_end; t += step) {
+            for (int t = sg.t_first + (sg.single ? turn : 0); t < t_end; t += step) {
                 ok = wait_at(my_bars + kAtFull, ops & 1, abort_at, a.status);
                 if (!ok) break;
                 tc_fence_after();
                 // ragged end: V rows past the last key may hold anything -> zeros (by either lane of a tile that both use)
                 if (t >= t_masked && (t + 1) * kSharedTile > sg.n_keys) {
                     const uint32_t load = 2 * (tile0 + (t - sg.t_first)) + 1, st = load % kStages;
-                    ok = wait_for(hd, &hd->kv_full[st], (load / kStages) & 1, a.status);
+                    ok = wait_for(hd, &hd->v_there[l], ops & 1, a.status);
                     if (!ok) break;
                     const int first_off = max(sg.n_keys - t * kSharedTile, 0) * 128;
                     for (int off = first_off + row * 16; off < kHalfBytes; off += 128 * 16) {
@@ -543,7 +625,7 @@ tree_attn_shared_kernel(const __grid_constant__ CUtensorMap tmap_q_shared, const
                 __syncwarp();
                 if (lane == 0) arrive_at(my_bars + kAtFree);
                 if (row_valid) {
-                    float* part = a.parts + (size_t)(sg.slot + l) * kPartFloats;
+                    float* part = a.parts + (size_t)(sg.slot + turn) * kPartFloats;
                     float top4[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                     for (int c = 0; c < 128; ++c) top4[c & 3] = fmaxf(top4[c & 3], fabsf(__uint_as_float(v[c])));
