@@ -58,7 +58,7 @@ __device__ __forceinline__ bool tree_depths(const int32_t* __restrict__ parent, 
 }
 
 // kTree: positions by the depth in a tree, else by the place in a run of tokens.  kStream: the next rows are on their way while a group's
-// rows are worked on (two prompts of 6001 tokens, 40 heads: 137 -> 132 us; 16 trees of 64 nodes, two rounds a group: 8.0 -> 8.8)
+// rows are worked on (two prompts of 6001 tokens, 40 heads, in blocks of 16 tokens: 137 -> 132 us; 16 trees of 64 nodes, two rounds a group: 8.0 -> 8.8)
 template <bool kTree, bool kStream>
 __global__ void __launch_bounds__(kAppendThreads, 3)
 append_kv_kernel(const AppendKv a, int groups_log2 /* groups of 16 lanes a token */) {
@@ -189,10 +189,12 @@ cudaError_t launch_append_kv(goose_ctx* c, AppendKv a, int S, cudaStream_t st) {
     if (S == 0) return cudaSuccess;
     a.status = c->status;
     // groups a token: as few as give every SM three blocks (a token's lengths, tree and table row are then looked up for more rows),
-    // at most as many as leave each kRows rows, and a block of one token
+    // at most as many as leave each kRows rows, and a block of one token; more, up to sixteen blocks an SM, where each keeps four rounds of rows:
+    // the last blocks then end together (64 trees of 128 nodes, 40 heads: 153 -> 118 us; with two rounds left to each, 157)
     const int rows = a.H + 2 * a.Hkv;
     int lg = 0;
     while ((1 << lg) < kAppendGroups && (kRows << lg) < rows && (((long long)S * a.B) << lg) < 3LL * kAppendGroups * c->num_sms) ++lg;
+    while ((1 << lg) < kAppendGroups && (8 * kRows << lg) <= rows && (((long long)S * a.B) << lg) < 16LL * kAppendGroups * c->num_sms) ++lg;
     const int per_block = kAppendGroups >> lg;
     const dim3 grid((a.B + per_block - 1) / per_block, S);
     const bool stream = rows >= (4 * kRows << lg);            // four rounds a group and more
