@@ -13,6 +13,8 @@
 // short, since trees differ in size and sequences leave; the first rows are on their way before the first kernel has ended.  Tokens of the
 // path are put right behind the stream, a thread a (row, node of the path) pair: where the tokens are those of text, most of a tree's
 // lie in the first few of the vocabulary, and whatever thread has those in the stream would do the others' work.
+// Measured: 16 trees of 64 nodes, 32000 tokens, everything on 22.7 us (82 MB, 3.6 TB/s; an elementwise addition of as many bytes 14.2); 4 trees of
+// 32 nodes, 128256 tokens 18.1 us; 16 nodes, 32000 tokens, penalties alone 4.9 us: two launches and the history's latency.
 #include "goose_internal.cuh"
 
 namespace goose {

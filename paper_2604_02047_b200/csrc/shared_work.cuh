@@ -5,8 +5,8 @@
 // rows, then, sequence by sequence and head by head, the pairs of M tiles of one sequence over its own rows.  A tile takes as many places as
 // it costs, and the list is dealt to the CTAs in ranges of equal length: a tile is of the range that its first place is in.  What a CTA does of
 // one item is a segment.  A segment has two lanes, each with a softmax warpgroup and
-// accumulators of its own: the two M tiles of the pair, which share the key tiles, or, where an item is a single M tile, even and odd
-// key tiles of it.  Every lane of a segment leaves a partial result.
+// accumulators of its own: the two M tiles of the pair, which share the key tiles, or, where an item is a single M tile, every other
+// key tile of it.  Every lane of a segment leaves a partial result.
 #pragma once
 
 #include "goose_internal.cuh"
@@ -14,7 +14,9 @@
 namespace goose {
 
 constexpr int kSharedTile = 128;                 // keys of a tile, rows of an M tile
-// places of a key tile, and of the change to another item, for a pair of M tiles and for a single one
+// places of a key tile, and of the change to another item, for a pair of M tiles and for a single one.  (Changes of 10 and 4, 16 and 2 or 16
+// and 3 instead: 26 x 52 heads, 32 nodes, 128 shared rows 59.7 -> 59.1, 63.5, 62.9 us; 16 x 32 heads, 16 nodes, 1500 shared rows 61.3 -> 63.7, 59.4, 60.7;
+// 8 x 52 heads, 128 nodes, 5423 shared rows 183 -> 185, 192, 189.)
 constexpr int kPairPlaces = 5, kSinglePlaces = 4, kPairChange = 16, kSingleChange = 4;
 
 struct SharedWork {
