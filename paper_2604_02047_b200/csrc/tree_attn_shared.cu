@@ -670,19 +670,25 @@ tree_attn_shared_kernel(const __grid_constant__ CUtensorMap tmap_q_shared, const
     }
 }
 
-// Merge: 32 rows of one key/value head of one sequence (lane <-> row, warp & 7 <-> 16 columns), parts in rounds of kCombineRound.  Where a
-// sequence has no more than 16 rows, several lanes share a row's parts and join what they have, and where the blocks are fewer than the
-// SMs and parts may be many, so do three times eight warps (kJoin): with few heads a row has a hundred parts and more.  (16 heads over 2: two
-// sequences, a token each, under 21k rows 44 -> 23 us; one sequence, 4 nodes, under 30k 51 -> 33; joined without need, 4 sequences of 32
-// heads over 8, a token each, under 512 rows 11.4 -> 12.2.)  The rows lie in two M tiles at most of the shared rows' work, and in two of the
-// sequence's own; a warp makes the list of each tile's parts.
+// Merge: 32 rows of one key/value head of one sequence (lane <-> row, warp & 7 <-> 16 columns).  The rows lie in two M tiles at most of the shared
+// rows' work, and in two of the sequence's own; a warp makes the list of each tile's parts.  Where a sequence has no more than 16 rows, several
+// lanes share a row's parts and join what they have.  What bounds it is latency: lists, a barrier, a round of loads or two.  Three forms:
+//   few blocks     four parts a round in flight
+//   many           (more than two an SM) two parts a round in 64 registers, four blocks an SM.  16 x 64 nodes, 32 heads over 8: 151.4 -> 147.8 us
+//                  with the main kernel; 42 sequences, 52 heads, a token each, under 203 rows 180 -> 170; 256 blocks 46.1 -> 46.5, 32 blocks 11.9 -> 12.8
+//   long lists     (blocks fewer than the SMs, parts may be many) three times eight warps, which share the parts too: with few heads a row
+//                  has a hundred and more.  16 heads over 2: two sequences, a token each, under 21k rows 44 -> 23 us; one sequence, 4 nodes, under
+//                  30k 51 -> 33; joined without need, 4 sequences of 32 heads over 8, a token each, under 512 rows 11.4 -> 12.2
+enum MergeForm { kFewBlocks, kManyBlocks, kLongLists };
 constexpr int kMaxParts = 2 * 256;                           // lanes x CTAs that an item may lie in
 
 constexpr int kJoiners = 3;                                  // warps that share the parts of 16 columns
 
-template <bool kJoin>
-__global__ void __launch_bounds__(kJoin ? kJoiners * kCombineThreads : kCombineThreads)
+template <MergeForm kForm>
+__global__ void __launch_bounds__(kForm == kLongLists ? kJoiners * kCombineThreads : kCombineThreads, kForm == kManyBlocks ? 4 : 1)
 tree_attn_shared_merge_kernel(const __grid_constant__ SharedArgs a, int H, __nv_bfloat16* __restrict__ out, float* __restrict__ lse) {
+    constexpr bool kJoin = kForm == kLongLists;
+    constexpr int kRound = kForm == kManyBlocks ? 2 : 4;     // parts whose loads are in flight together
     __shared__ int s_slot[4][kMaxParts];
     __shared__ int s_parts[4];
     __shared__ float s_join[kJoin ? 18 : 1][8][32];
@@ -738,12 +744,12 @@ tree_attn_shared_merge_kernel(const __grid_constant__ SharedArgs a, int H, __nv_
     bool bad = false;
 #pragma unroll
     for (int c = 0; c < 16; ++c) acc[c] = 0.f;
-    for (int k0 = sharer; k0 < n; k0 += sharers * kCombineRound) {
-        float m[kCombineRound];
-        float2 ls[kCombineRound];
-        uint4 x[kCombineRound][2];
+    for (int k0 = sharer; k0 < n; k0 += sharers * kRound) {
+        float m[kRound];
+        float2 ls[kRound];
+        uint4 x[kRound][2];
 #pragma unroll
-        for (int q = 0; q < kCombineRound; ++q) {
+        for (int q = 0; q < kRound; ++q) {
             const int k = k0 + q * sharers;
             m[q] = -INFINITY;
             ls[q] = make_float2(0.f, 1.f);
@@ -759,13 +765,13 @@ tree_attn_shared_merge_kernel(const __grid_constant__ SharedArgs a, int H, __nv_
         }
         float M_new = M;
 #pragma unroll
-        for (int q = 0; q < kCombineRound; ++q) { M_new = fmaxf(M_new, m[q]); bad |= ls[q].x < 0.f; }
+        for (int q = 0; q < kRound; ++q) { M_new = fmaxf(M_new, m[q]); bad |= ls[q].x < 0.f; }
         const float old = M == -INFINITY ? 0.f : ex2(M - M_new);
         L *= old;
 #pragma unroll
         for (int c = 0; c < 16; ++c) acc[c] *= old;
 #pragma unroll
-        for (int q = 0; q < kCombineRound; ++q) {
+        for (int q = 0; q < kRound; ++q) {
             if (m[q] == -INFINITY && ls[q].x == 0.f) continue; // no key of the part is visible to the row
             const float w = ex2(m[q] - M_new), wx = w * ls[q].y;
             L += w * ls[q].x;
@@ -864,16 +870,19 @@ cudaError_t launch_tree_attn_shared(goose_ctx* c, const __nv_bfloat16* q, const 
     // CTAs that an item may lie in, as far as the host knows: more warps a row where that makes many parts
     auto ctas = [&](long long tiles, long long items) { return tiles < a.wk.G / items ? tiles : a.wk.G / items; };
     const long long most = ctas(a.wk.shared_tiles, Hkv * a.wk.shared_pairs()) + ctas((kv_rows + kSharedTile - 1) / kSharedTile, (long long)S * Hkv * a.wk.own_pairs());
-    const bool join = (long long)blocks.x * Hkv * S < c->num_sms && most >= 12;
-    e = launch_pdl(join ? tree_attn_shared_merge_kernel<true> : tree_attn_shared_merge_kernel<false>, blocks,
-                   dim3(join ? kJoiners * kCombineThreads : kCombineThreads), 0, st, a, H, out, lse);
+    const long long n_blocks = (long long)blocks.x * Hkv * S;
+    const bool join = n_blocks < c->num_sms && most >= 12;
+    auto merge = join ? tree_attn_shared_merge_kernel<kLongLists> : n_blocks > 2 * c->num_sms ? tree_attn_shared_merge_kernel<kManyBlocks>
+                                                                                               : tree_attn_shared_merge_kernel<kFewBlocks>;
+    e = launch_pdl(merge, blocks, dim3(join ? kJoiners * kCombineThreads : kCombineThreads), 0, st, a, H, out, lse);
     c->launches++;
     return e;
 }
 
 cudaError_t init_shared_kernel() {
     cudaError_t e = cudaFuncSetAttribute(tree_attn_shared_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedSmem);
-    return e == cudaSuccess ? load_kernels({(const void*)tree_attn_shared_merge_kernel<false>, (const void*)tree_attn_shared_merge_kernel<true>}) : e;
+    return e == cudaSuccess ? load_kernels({(const void*)tree_attn_shared_merge_kernel<kFewBlocks>, (const void*)tree_attn_shared_merge_kernel<kManyBlocks>,
+                                            (const void*)tree_attn_shared_merge_kernel<kLongLists>}) : e;
 }
 
 }  // namespace goose
