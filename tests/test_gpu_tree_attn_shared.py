@@ -154,6 +154,19 @@ def test_long_lists_split_over_all_ctas(goose):
     Case(16, 8, 2, 64, 3000, [100 * s for s in range(16)], seed=3).spoil().check(goose)
 
 
+@pytest.mark.parametrize("S,H,Hkv,B,shared,own", [
+    (30, 16, 16, 8, 300, 140),      # a pair of M tiles over the shared rows, then single ones of a tile or two
+    (40, 16, 16, 8, 130, 100),      # a pair and a single one over the shared rows, own rows of one tile
+    (40, 64, 4, 24, 100, 250),      # a pair and a single M tile of every sequence and head in turn
+    (60, 64, 4, 16, 1, 130),        # pairs of a tile or two
+    (64, 32, 8, 2, 0, 300),         # no shared rows
+])
+def test_many_items_a_cta(goose, S, H, Hkv, B, shared, own):
+    """Several changes of item a CTA, from either kind to either kind."""
+    rng = np.random.default_rng(S)
+    Case(S, H, Hkv, B, shared, rng.integers(0, own, S).tolist(), seed=S + B).spoil().check(goose)
+
+
 def test_random_cases(goose):
     rng = np.random.default_rng(11)
     for i in range(40):
