@@ -54,16 +54,6 @@ struct SharedWork {
         total = shared_total + (long long)Hkv * own_pairs() * (sum * places(0) + (long long)change(0) * live);
         quantum = total > 0 ? divide(total + G - 1, G) : 1;
     }
-    __host__ __device__ __forceinline__ void init() {
-        long long sum = 0;
-        int live = 0;
-        for (int s = 0; s < S; ++s) {
-            const int T = tiles(s);
-            sum += T;
-            live += T > 0;
-        }
-        set(sum, live);
-    }
     static __host__ __device__ __forceinline__ long long divide(long long a, long long b) {   // 64-bit division is slow on the GPU
         return (a | b) >> 32 ? a / b : (long long)((uint32_t)a / (uint32_t)b);
     }
@@ -92,18 +82,6 @@ struct SharedCursor {         // walks the list
         t = at > 0 ? (at + u - 1) / u : 0;
         w += t * u - at;
         if (t == T) next(wk);
-    }
-    __host__ __device__ __forceinline__ void seek(const SharedWork& wk, long long w0) {
-        w = w0; s = -1; T = wk.shared_tiles;
-        if (w0 < wk.shared_total) { enter(wk, w0); return; }
-        long long rem = w0 - wk.shared_total;
-        for (s = 0; s < wk.S; ++s) {
-            T = wk.tiles(s);
-            const long long mine = (long long)wk.Hkv * wk.own_pairs() * wk.width(s, T);
-            if (rem < mine) break;
-            rem -= mine;
-        }
-        if (s < wk.S) enter(wk, rem);
     }
     // tiles from here on that are of a range which ends at w_end
     __host__ __device__ __forceinline__ int run(const SharedWork& wk, long long w_end) const {

@@ -17,13 +17,36 @@ SOURCE = r"""
 using std::max; using std::min;
 #include "shared_work.cuh"
 using namespace goose;
+// what a warp does on the GPU, a sequence after the other: the list's length, and a place in it
+static void measure(SharedWork& wk) {
+    long long sum = 0;
+    int live = 0;
+    for (int s = 0; s < wk.S; ++s) {
+        const int T = wk.tiles(s);
+        sum += T;
+        live += T > 0;
+    }
+    wk.set(sum, live);
+}
+static void seek(SharedCursor& cu, const SharedWork& wk, long long w0) {
+    cu.w = w0; cu.s = -1; cu.T = wk.shared_tiles;
+    if (w0 < wk.shared_total) { cu.enter(wk, w0); return; }
+    long long rem = w0 - wk.shared_total;
+    for (cu.s = 0; cu.s < wk.S; ++cu.s) {
+        cu.T = wk.tiles(cu.s);
+        const long long mine = (long long)wk.Hkv * wk.own_pairs() * wk.width(cu.s, cu.T);
+        if (rem < mine) break;
+        rem -= mine;
+    }
+    if (cu.s < wk.S) cu.enter(wk, rem);
+}
 // 0, or what is wrong
 extern "C" int walk(int S, int B, int Hkv, int shared_tiles, int shared_m, int own_m, int G, int kv_rows, const int32_t* ctx_len,
                     const int32_t* n_nodes, long long* longest) {
     SharedWork wk{};
     wk.ctx_len = ctx_len; wk.n_nodes = n_nodes; wk.S = S; wk.B = B; wk.Hkv = Hkv; wk.kv_rows = kv_rows;
     wk.shared_tiles = shared_tiles; wk.shared_m = shared_m; wk.own_m = own_m; wk.G = G;
-    wk.init();
+    measure(wk);
     std::map<int, std::pair<int, int>> written;             // slot -> (item, tiles of it)
     std::vector<int> dealt(wk.items(), 0);
     for (int cta = 0; cta < G; ++cta) {
@@ -31,7 +54,7 @@ extern "C" int walk(int S, int B, int Hkv, int shared_tiles, int shared_m, int o
         if (w0 > w_end) return 1;
         if (w0 == w_end) continue;
         SharedCursor cu;
-        cu.seek(wk, w0);
+        seek(cu, wk, w0);
         long long mine = 0;
         while (cu.w < w_end) {
             if (cu.s >= S || cu.s < -1 || cu.i < 0) return 2;
