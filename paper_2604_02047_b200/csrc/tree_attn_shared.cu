@@ -17,8 +17,8 @@
 // exponentials (16 a cycle and SM: 1060 cycles a tile) and a tile's products (1024 cycles) follow one another within a lane; tiles of 128 keys
 // and a row a thread, so that maximum and sum need no exchange.
 // What bounds it.  Many query rows: a pair of tiles takes 3150 to 3400 cycles, of which the exponentials are 2120, the products 2048 (16
-// sequences of 64 nodes, 32 heads over 8, under 8192 rows: 148 us, 1.07 PFLOP/s; under the power cap 175).  Few: HBM (64 sequences, a token each, 32 over 8,
-// under 16k rows: 107 us, 4.7 TB/s, 5.7 without merge).  Small calls: planner 1.8 us, first tile 1.6, epilogue 1.3, merge 3 (4 sequences, a
+// sequences of 64 nodes, 32 heads over 8, under 8192 rows: 148 us, 1.07 PFLOP/s; under the power cap 172).  Few: HBM (64 sequences, a token each, 32 over 8,
+// under 16k rows: 107 us, 4.7 TB/s, 5.7 without merge; 122 under the power cap).  Small calls: planner 1.8 us, first tile 1.6, epilogue 1.3, merge 3 (4 sequences, a
 // token each, under 512 rows: 11.7 us).  A change of item takes 3 us where the item has a tile or two (26 x 52 heads, 32 nodes, 5423 rows: 203 us).
 // Every wait is bounded: one that runs out raises the CTA's abort flag and GOOSE_ST_TIMEOUT, and every role unwinds.
 #include <cuda_fp16.h>
