@@ -610,6 +610,7 @@ tree_attn_shared_kernel(const __grid_constant__ CUtensorMap tmap_q_shared, const
                     l_run += l2.x + l2.y;
                 } else {
                     tc_fence_before();
+                    __syncwarp();                            // (all lanes' zeros are in front of the arrivals)
                     if (lane == 0) { arrive_at(at_ready); arrive_at(at_ready + 8); }
                 }
                 first = false;
