@@ -290,7 +290,10 @@ int goose_append_kv(goose_ctx* ctx, const void* q, int64_t ldq, const void* k, i
 /* Logits of a tree's nodes ahead of goose_node_topk: penalties for tokens that occurred, bias, grammar mask.  A sequence's
  * tokens are hist[s][0 .. hist_len[s]-1], of which the first n_prompt[s] are its prompt; node i's row has behind them the draft tokens on
  * the path from the root to node i, both included (the row predicts the token after node i).  For every row of a node that exists and v < V:
- *   n = occurrences of v in hist behind the prompt and on the path
+ *   n = occurrences of v in hist behind the prompt and on the path, of its nodes those that are no tokens of the prompt: the node at depth d
+ *       stands at position hist_len[s] + d, and where the prompt ends in the tree, hist_len[s] < n_prompt[s] <= hist_len[s] + B (the first
+ *       tree's root is its last token; a prompt's last chain), the positions below n_prompt[s] are prompt.  A larger n_prompt[s] ends in
+ *       no row of the tree: all of hist is prompt then, and the path is drafts
  *   x = logits[row][v];  if v occurs in hist or on the path:  x = x > 0 ? x / repetition[s] : x * repetition[s]
  *   x = x - frequency[s] * n - presence[s] * (n > 0) + bias[v];   bit v & 31 of mask[row][v >> 5] is 0:  x = -inf
  * in fp32, rounded once to bf16 (a result beyond the largest bf16 becomes an infinity).  Masked places may hold anything, NaN included; a row

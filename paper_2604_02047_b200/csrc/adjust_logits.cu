@@ -1,6 +1,6 @@
 // Logits of a tree's nodes ahead of the top-k: penalties for tokens that occurred, bias, grammar mask.
 //
-//   n  = occurrences of token v in the generated part of the sequence and on the node's path, root to node
+//   n  = occurrences of token v in the generated part of the sequence and on the node's path, root to node, where that is no longer the prompt
 //   x' = x, or, where v occurs anywhere in the sequence or on the path, x / rep for x > 0 and x * rep otherwise
 //   x' = x' - freq * n - pres * (n > 0) + bias[v];   tokens whose mask bit is 0: -inf
 //
@@ -31,18 +31,19 @@ constexpr uint32_t kInPrompt = 0x80000000u;          // of a token's word: it oc
 struct AdjustTree {
     uint4 path[kMaxB];                               // a node's path, as a set of nodes
     uint4 same[kMaxB];                               // the nodes that have its token
+    uint32_t made[kMaxB / 32];                       // the nodes that are no tokens of the prompt
     int bad;                                         // parent[] is no tree
     int pad[3];
 };
 
-// Of a path's nodes that have the token of node j (same): is j the first?  n: how many there are.
-__device__ __forceinline__ bool first_of_path(const uint4& path, const uint4& same, int j, uint32_t& n) {
-    const uint32_t both[4] = {path.x & same.x, path.y & same.y, path.z & same.z, path.w & same.w};
+// Of a path's nodes that have the token of node j (same): is j the first?  n: how many of them are generated (made).
+__device__ __forceinline__ bool first_of_path(const uint4& path, const uint4& same, const uint4& made, int j, uint32_t& n) {
+    const uint32_t both[4] = {path.x & same.x, path.y & same.y, path.z & same.z, path.w & same.w}, generated[4] = {made.x, made.y, made.z, made.w};
     int first = kMaxB;
     n = 0;
 #pragma unroll
     for (int w = 3; w >= 0; --w) {
-        n += __popc(both[w]);
+        n += __popc(both[w] & generated[w]);
         if (both[w]) first = 32 * w + __ffs(both[w]) - 1;
     }
     return first == j;
@@ -89,8 +90,13 @@ adjust_tables_kernel(const AdjustLogits a, int pieces, int64_t ldw, uint32_t* __
             }
             __syncthreads();
         }
-        if (!node) return;
         path.x |= 1u;                                          // (the root is on every path)
+        // The node at depth d stands at position hist_len + d: a token of the prompt where that is in front of n_prompt.
+        const long long left = a.hist && a.n_prompt && nn > 0 && !bad_len ? (long long)a.n_prompt[s] - a.hist_len[s] : 0;
+        const int in_prompt = left > 0 && left <= a.B ? (int)left : 0;   // (a prompt that no node is the end of: goose.h)
+        const uint32_t made = __ballot_sync(0xFFFFFFFFu, __popc(path.x) + __popc(path.y) + __popc(path.z) + __popc(path.w) > in_prompt);
+        if (tid < kMaxB && (tid & 31) == 0) trees[s].made[tid >> 5] = made;
+        if (!node) return;
         for (int j = 0; j < nn; ++j) {
             const uint32_t bit = s_tok[j] == tok ? 1u << (j & 31) : 0;
             (j < 32 ? same.x : j < 64 ? same.y : j < 96 ? same.z : same.w) |= bit;
@@ -256,15 +262,16 @@ adjust_logits_kernel(const AdjustLogits a, int rows_per_block, int64_t ldw, cons
     }
     __syncthreads();                                           // the list is complete, the stream's stores are in front of these
     const int listed = bad ? 0 : s_listed, pairs = rows * listed;
+    const uint4 made = *reinterpret_cast<const uint4*>(tree.made);
     for (int k = tid; k < pairs; k += kAdjustThreads) {
         const int of_row = k / listed, l = k - of_row * listed, j = s_list[l], t = s_tok[l], v = base + t;
         const size_t r = row0 + of_row;
         uint32_t n;
-        if (v >= a.V || !first_of_path(tree.path[i0 + of_row], tree.same[j], j, n)) continue;
+        if (v >= a.V || !first_of_path(tree.path[i0 + of_row], tree.same[j], made, j, n)) continue;
         if (kMask && !((a.mask[r * a.ldm + (v >> 5)] >> (v & 31)) & 1u)) continue;
         if (w) n += w[t] & ~kInPrompt;
         const float x1 = __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(s_row[of_row])[t]);
-        a.out[r * a.ldo + v] = __float2bfloat16_rn((x1 > 0.f ? x1 * inv_rep : x1 * rep) + ((bias ? bias[t] : 0.f) + (-freq * (float)n - pres)));
+        a.out[r * a.ldo + v] = __float2bfloat16_rn((x1 > 0.f ? x1 * inv_rep : x1 * rep) + ((bias ? bias[t] : 0.f) + (n ? -freq * (float)n - pres : 0.f)));
     }
 }
 
