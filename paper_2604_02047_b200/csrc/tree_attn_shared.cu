@@ -19,9 +19,8 @@
 // What bounds it.  Many query rows: a pair of tiles takes 3150 to 3400 cycles, of which the exponentials are 2120, the products 2048 (16
 // sequences of 64 nodes, 32 heads over 8, under 8192 rows: 148 us, 1.07 PFLOP/s; under the power cap 172).  Few: HBM (64 sequences, a token each, 32 over 8,
 // under 16k rows: 107 us, 4.7 TB/s, 5.7 without merge; 122 under the power cap).  Small calls: planner 1.8 us, first tile 1.6, epilogue 1.3, merge 3 (4 sequences, a
-// token each, under 512 rows: 11.7 us).  A change of item takes 3 us where the item has a tile or two (26 x 52 heads, 32 nodes, 5423 rows: 203 us).
+// token each, under 512 rows: 11.8 us).  A change of item takes 3 us where the item has a tile or two (26 x 52 heads, 32 nodes, 5423 rows: 203 us).
 // Every wait is bounded: one that runs out raises the CTA's abort flag and GOOSE_ST_TIMEOUT, and every role unwinds.
-#include <cuda_fp16.h>
 #include <stddef.h>
 
 #include "goose_internal.cuh"
@@ -48,12 +47,26 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kRescaleThreshold = 8.0f;                    // rescale O only when the running max grew by > 2^8
 constexpr long long kWaitCycles = 2000000000ll;              // bound of every wait: about one second of SM clock
 
-// Partial result of an M tile: O / scale as fp16, uint4 [16 groups of 8 columns][128 rows];  m fp32 [128], the maximum that the
-// exponentials are relative to (base 2);  (l, scale) fp32 [128], the exponentials' sum and the power of two of the row's largest element, so
-// that a row of any size has 11 bits of its largest elements (the output has 8).  l < 0: a sequence that cannot be computed (no
-// tree, rows outside the cache).
-constexpr int kPartWords = 16 * 128 * 4;
-constexpr int kPartFloats = kPartWords + 3 * 128;
+// Partial result of an M tile: O in three bytes an element, fp32 without its last byte: sign, exponent and 16 bits of significand (the output has 8)
+// of every element by itself, whatever its row's or its column's others are, infinities and NaN among them.  The two upper bytes lie as
+// uint4 [16 groups of 8 columns][128 rows], the third ones as uint4 [8 groups of 16 columns][128 rows];  (m, l) fp32 [128], the maximum that the
+// exponentials are relative to (base 2) and their sum.  l < 0: a sequence that cannot be computed (no tree, rows outside the cache).
+// (Half precision times a power of two of the row's largest element, two bytes, lost the elements below 2^-25 of it.  What the third byte
+// costs: 16 x 64 nodes, 32 heads over 8, under 8192 rows 148.6 -> 151.3 us, 64 sequences of a token 107.6 -> 108.2, one sequence of 4 nodes, 16 heads over 2,
+// under 30k rows 33 -> 37; 26 x 52 heads, 32 nodes, 128 rows 56.9 -> 53.4, 42 x 52 heads, a token each, 174 -> 168.)
+constexpr int kPartThird = 16 * 128 * 4;                     // in words: where the third bytes begin
+constexpr int kPartWords = kPartThird + 8 * 128 * 4;
+constexpr int kPartFloats = kPartWords + 2 * 128;
+// four elements' words: the upper halves of two, the third bytes of four, and back (the last byte comes back as a copy of the third: within 2^-15)
+__device__ __forceinline__ uint32_t upper_halves(uint32_t x0, uint32_t x1) { return __byte_perm(x0, x1, 0x7632); }
+__device__ __forceinline__ uint32_t third_bytes(uint32_t x0, uint32_t x1, uint32_t x2, uint32_t x3) {
+    return __byte_perm(__byte_perm(x0, x1, 0x0051), __byte_perm(x2, x3, 0x0051), 0x5410);
+}
+template <int kAt>                                           // element 0..3 of the four
+__device__ __forceinline__ float part_element(uint32_t halves, uint32_t thirds) {
+    constexpr uint32_t third = 4 + kAt, upper = kAt & 1 ? 0x3200 : 0x1000;
+    return __uint_as_float(__byte_perm(halves, thirds, upper | third << 4 | third));
+}
 
 // a segment, as the planner describes it
 struct Segment {
@@ -634,25 +647,17 @@ tree_attn_shared_kernel(const __grid_constant__ CUtensorMap tmap_q_shared, const
                 if (lane == 0) arrive_at(my_bars + kAtFree);
                 if (row_valid) {
                     float* part = a.parts + (size_t)(sg.slot + turn) * kPartFloats;
-                    float top4[4] = {0.f, 0.f, 0.f, 0.f};
+                    uint4* upper = reinterpret_cast<uint4*>(part) + row;
+                    uint4* third = reinterpret_cast<uint4*>(part + kPartThird) + row;
 #pragma unroll
-                    for (int c = 0; c < 128; ++c) top4[c & 3] = fmaxf(top4[c & 3], fabsf(__uint_as_float(v[c])));
-                    // power of two of the largest element; 1 where there is none (zeros, infinities)
-                    const uint32_t ex = __float_as_uint(fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3]))) & 0x7F800000u;
-                    const float scale = ex == 0 || ex >= 0x7F000000u ? 1.f : __uint_as_float(ex), inv = 1.f / scale;
-                    uint4* dst = reinterpret_cast<uint4*>(part) + row;
-#pragma unroll
-                    for (int c = 0; c < 16; ++c) {
-                        uint32_t hw[4];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const __half2 h2 = __floats2half2_rn(__uint_as_float(v[8 * c + 2 * e]) * inv, __uint_as_float(v[8 * c + 2 * e + 1]) * inv);
-                            hw[e] = *reinterpret_cast<const uint32_t*>(&h2);
-                        }
-                        dst[c * 128] = make_uint4(hw[0], hw[1], hw[2], hw[3]);
+                    for (int c = 0; c < 8; ++c) {
+                        const uint32_t* x = v + 16 * c;
+                        upper[2 * c * 128] = make_uint4(upper_halves(x[0], x[1]), upper_halves(x[2], x[3]), upper_halves(x[4], x[5]), upper_halves(x[6], x[7]));
+                        upper[(2 * c + 1) * 128] = make_uint4(upper_halves(x[8], x[9]), upper_halves(x[10], x[11]), upper_halves(x[12], x[13]), upper_halves(x[14], x[15]));
+                        third[c * 128] = make_uint4(third_bytes(x[0], x[1], x[2], x[3]), third_bytes(x[4], x[5], x[6], x[7]),
+                                                    third_bytes(x[8], x[9], x[10], x[11]), third_bytes(x[12], x[13], x[14], x[15]));
                     }
-                    part[kPartWords + row] = m_run;
-                    reinterpret_cast<float2*>(part + kPartWords + 128)[row] = make_float2(sg.bad ? -1.f : l_run, scale);
+                    reinterpret_cast<float2*>(part + kPartWords)[row] = make_float2(m_run, sg.bad ? -1.f : l_run);
                 }
             }
             tile0 += sg.n;
@@ -677,9 +682,10 @@ tree_attn_shared_kernel(const __grid_constant__ CUtensorMap tmap_q_shared, const
 //   few blocks     four parts a round in flight
 //   many           (more than two an SM) two parts a round in 64 registers, four blocks an SM.  16 x 64 nodes, 32 heads over 8: 151.4 -> 147.8 us
 //                  with the main kernel; 42 sequences, 52 heads, a token each, under 203 rows 180 -> 170; 256 blocks 46.1 -> 46.5, 32 blocks 11.9 -> 12.8
-//   long lists     (blocks fewer than the SMs, parts may be many) three times eight warps, which share the parts too: with few heads a row
-//                  has a hundred and more.  16 heads over 2: two sequences, a token each, under 21k rows 44 -> 23 us; one sequence, 4 nodes, under
-//                  30k 51 -> 33; joined without need, 4 sequences of 32 heads over 8, a token each, under 512 rows 11.4 -> 12.2
+//   long lists     (blocks fewer than the SMs, parts may be many) three times eight warps, which share the parts too, three parts a round (with
+//                  four they spill: 22 -> 24.5, 37 -> 46): with few heads a row has a hundred and more.  16 heads over 2: two sequences, a
+//                  token each, under 21k rows 44 -> 22 us; one sequence, 4 nodes, under 30k 51 -> 37; joined without need, 4 sequences of 32
+//                  heads over 8, a token each, under 512 rows 11.4 -> 12.2
 enum MergeForm { kFewBlocks, kManyBlocks, kLongLists };
 constexpr int kMaxParts = 2 * 256;                           // lanes x CTAs that an item may lie in
 
@@ -689,7 +695,7 @@ template <MergeForm kForm>
 __global__ void __launch_bounds__(kForm == kLongLists ? kJoiners * kCombineThreads : kCombineThreads, kForm == kManyBlocks ? 4 : 1)
 tree_attn_shared_merge_kernel(const __grid_constant__ SharedArgs a, int H, __nv_bfloat16* __restrict__ out, float* __restrict__ lse) {
     constexpr bool kJoin = kForm == kLongLists;
-    constexpr int kRound = kForm == kManyBlocks ? 2 : 4;     // parts whose loads are in flight together
+    constexpr int kRound = kForm == kManyBlocks ? 2 : kForm == kLongLists ? 3 : 4;   // parts whose loads are in flight together
     __shared__ int s_slot[4][kMaxParts];
     __shared__ int s_parts[4];
     __shared__ float s_join[kJoin ? 18 : 1][8][32];
@@ -746,45 +752,42 @@ tree_attn_shared_merge_kernel(const __grid_constant__ SharedArgs a, int H, __nv_
 #pragma unroll
     for (int c = 0; c < 16; ++c) acc[c] = 0.f;
     for (int k0 = sharer; k0 < n; k0 += sharers * kRound) {
-        float m[kRound];
-        float2 ls[kRound];
-        uint4 x[kRound][2];
+        float2 ml[kRound];
+        uint4 x[kRound][3];
 #pragma unroll
         for (int q = 0; q < kRound; ++q) {
             const int k = k0 + q * sharers;
-            m[q] = -INFINITY;
-            ls[q] = make_float2(0.f, 1.f);
-            x[q][0] = x[q][1] = make_uint4(0, 0, 0, 0);
+            ml[q] = make_float2(-INFINITY, 0.f);
+            x[q][0] = x[q][1] = x[q][2] = make_uint4(0, 0, 0, 0);
             if (k < n) {
                 const float* part = a.parts + (size_t)(k < n0 ? s_slot[list0][k] : s_slot[list1][k - n0]) * kPartFloats;
                 const int rr = k < n0 ? row0 : row1;
-                m[q] = __ldcg(part + kPartWords + rr);
-                ls[q] = __ldcg(reinterpret_cast<const float2*>(part + kPartWords + 128) + rr);
+                ml[q] = __ldcg(reinterpret_cast<const float2*>(part + kPartWords) + rr);
                 x[q][0] = __ldcg(reinterpret_cast<const uint4*>(part) + (2 * columns) * 128 + rr);
                 x[q][1] = __ldcg(reinterpret_cast<const uint4*>(part) + (2 * columns + 1) * 128 + rr);
+                x[q][2] = __ldcg(reinterpret_cast<const uint4*>(part + kPartThird) + columns * 128 + rr);
             }
         }
         float M_new = M;
 #pragma unroll
-        for (int q = 0; q < kRound; ++q) { M_new = fmaxf(M_new, m[q]); bad |= ls[q].x < 0.f; }
+        for (int q = 0; q < kRound; ++q) { M_new = fmaxf(M_new, ml[q].x); bad |= ml[q].y < 0.f; }
         const float old = M == -INFINITY ? 0.f : ex2(M - M_new);
         L *= old;
 #pragma unroll
         for (int c = 0; c < 16; ++c) acc[c] *= old;
 #pragma unroll
         for (int q = 0; q < kRound; ++q) {
-            if (m[q] == -INFINITY && ls[q].x == 0.f) continue; // no key of the part is visible to the row
-            const float w = ex2(m[q] - M_new), wx = w * ls[q].y;
-            L += w * ls[q].x;
+            if (ml[q].x == -INFINITY && ml[q].y == 0.f) continue;   // no key of the part is visible to the row
+            const float w = ex2(ml[q].x - M_new);
+            L += w * ml[q].y;
+            const uint32_t thirds[4] = {x[q][2].x, x[q][2].y, x[q][2].z, x[q][2].w};
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const uint32_t hw[4] = {x[q][u].x, x[q][u].y, x[q][u].z, x[q][u].w};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&hw[e]));
-                    acc[8 * u + 2 * e] += wx * f.x;
-                    acc[8 * u + 2 * e + 1] += wx * f.y;
-                }
+            for (int u = 0; u < 4; ++u) {
+                const uint32_t h0 = u & 1 ? x[q][u >> 1].z : x[q][u >> 1].x, h1 = u & 1 ? x[q][u >> 1].w : x[q][u >> 1].y;
+                acc[4 * u] += w * part_element<0>(h0, thirds[u]);
+                acc[4 * u + 1] += w * part_element<1>(h0, thirds[u]);
+                acc[4 * u + 2] += w * part_element<2>(h1, thirds[u]);
+                acc[4 * u + 3] += w * part_element<3>(h1, thirds[u]);
             }
         }
         M = M_new;

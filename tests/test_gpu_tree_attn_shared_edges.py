@@ -27,3 +27,35 @@ def test_rows_behind_the_last_key_in_tiles_of_one_warp(goose):
     for _ in range(200):
         out, lse = c.run(goose)
         assert torch.equal(out, first[0]) and torch.equal(lse, first[1])
+
+
+def _columns(c, powers):
+    """The values' column d times 2^powers[d]."""
+    c.v = (c.v.float() * torch.exp2(torch.tensor(powers, dtype=torch.float32, device="cuda"))).bfloat16()
+    return c
+
+
+# one column above all others, columns beside one another that differ, every column of a size of its own
+COLUMNS = {"one, 2^16": [16.0 * (d == 37) for d in range(128)], "one, 2^24": [24.0 * (d == 64) for d in range(128)],
+           "every other, 2^20": [20.0 * (d % 2) for d in range(128)], "2^-80 to 2^80": [float((53 * d) % 161 - 80) for d in range(128)]}
+
+
+@pytest.mark.parametrize("powers", COLUMNS.values(), ids=COLUMNS.keys())
+@pytest.mark.parametrize("S,H,Hkv,B,shared,ctxs", [(2, 4, 2, 16, 900, [300, 200]), (5, 8, 2, 1, 700, [30, 0, 500, 64, 129]), (1, 2, 1, 128, 20000, [7])])
+def test_values_whose_columns_differ_in_size(goose, S, H, Hkv, B, shared, ctxs, powers):
+    """Every column has its own bits in a partial result: the tolerance is element by element, A of an element being a sum over its column."""
+    _columns(Case(S, H, Hkv, B, shared, ctxs, seed=B), powers).check(goose)
+
+
+def test_an_infinite_value_stays_in_its_column(goose):
+    """(The sizes of the other columns include some that half precision has no numbers for.)"""
+    for size in (1.0, 1e6, 1e-10):
+        c = Case(3, 8, 2, 9, 500, [100, 0, 300], seed=4)
+        c.v = (c.v.float() * size).bfloat16()
+        clean, lse = c.run(goose)
+        c.check(goose, clean, lse)
+        clean = clean.clone()
+        c.v[c.shared_row + 7, :, 50] = float("inf")
+        out, _ = c.run(goose)
+        assert not torch.isfinite(out[..., 50]).any()
+        assert torch.equal(out[..., :50], clean[..., :50]) and torch.equal(out[..., 51:], clean[..., 51:])
