@@ -136,10 +136,14 @@ int goose_tree_attn_gqa(goose_ctx* ctx, const void* q, const void* k_cache, cons
  *   shared_row, shared_len  host numbers: rows inside the cache; shared_len 0: no shared rows.  A different prefix per part of a batch is a
  *            call per part.  The positions of a sequence's own rows start at shared_len (pos_off of goose_append_kv).
  *   out bf16 [S][B][H][D], may be q itself; lse as in goose_tree_attn, of all keys
- * What a sequence's own rows hold never reaches another sequence's output.  The call's workspace (33 KB for 128 query rows of a
- * head, about three times) is allocated by the context's first call, and again by one that needs more: such a call cannot be
- * captured into a graph (make one of that size before); graphs captured before it stay valid, and the memory of both is the context's
- * until it is destroyed.  Other arguments, limits and errors as goose_tree_attn_gqa; the kernel needs tensor maps (GOOSE_ECUDA where the
+ * What a sequence's own rows hold never reaches another sequence's output.  The call's workspace is allocated by the context's first call, and again
+ * by one that needs more: such a call cannot be captured into a graph (make one of that size before); graphs captured before it stay valid, and
+ * the memory of both is the context's until it is destroyed.  Its size: 51200 bytes for each of
+ *   2 Hkv pairs(S B) / k(S B) [where there are shared rows] + 2 S Hkv pairs(B) / k(B) + 4 SMs / the smaller k, every term rounded up, with
+ *   t = floor(128 / (H / Hkv)) tokens of a 128-row tile, pairs(n) = ceil(ceil(n / t) / 2), and k(n) the largest power of two, at most 32, for
+ *   which k(n) min(n, t) H / Hkv <= 128
+ * (148 SMs, 64 sequences of a token: 32 heads over 8 32 MB, 40 over 40 25 MB; 16 x 64 nodes, 32 over 8 57 MB; one token 1 MB), and at least twice
+ * what an earlier call had if the device has that much.  Other arguments, limits and errors as goose_tree_attn_gqa; the kernel needs tensor maps (GOOSE_ECUDA where the
  * driver cannot make them).                                                                                     */
 int goose_tree_attn_shared(goose_ctx* ctx, const void* q, const void* k_cache, const void* v_cache, int64_t kv_rows,
                            int64_t shared_row, int32_t shared_len, const int64_t* row_off, const int32_t* ctx_len,

@@ -19,6 +19,9 @@ constexpr int kSharedTile = 128;                 // keys of a tile, rows of an M
 // 8 x 52 heads, 128 nodes, 5423 shared rows 183 -> 185, 192, 189.)
 constexpr int kPairPlaces = 5, kSinglePlaces = 4, kPairChange = 16, kSingleChange = 4;
 
+constexpr int kPartWords = 25;                   // words of 16 bytes a row of a partial result
+constexpr uint32_t kPartBlock = kPartWords * kSharedTile;
+
 struct SharedWork {
     const int32_t* ctx_len;
     const int32_t* n_nodes;   // or NULL
@@ -26,6 +29,9 @@ struct SharedWork {
     int shared_tiles;         // tiles of the shared rows
     int shared_m, own_m;      // M tiles a key/value head: of the whole batch; of one sequence
     int G;                    // CTAs
+    // places of the partial results, see lay()
+    int shared_log2, own_log2, cta_log2, own_slot, cta_slot;
+    uint32_t own_place, cta_place;
     // worked out
     bool changes;             // do changes count?  (not in lists of a tile or two a CTA)
     long long shared_total, total, quantum;
@@ -59,9 +65,10 @@ struct SharedWork {
     }
     __host__ __device__ __forceinline__ long long start(int c) const { return min(c * quantum, total); }
     __host__ __device__ __forceinline__ int cta_of(long long w) const { return (int)divide(w, quantum); }
-    __host__ __device__ __forceinline__ int items() const { return Hkv * (shared_tiles > 0 ? shared_pairs() : 0) + S * Hkv * own_pairs(); }
+    __host__ __device__ __forceinline__ int shared_items() const { return shared_tiles > 0 ? Hkv * shared_pairs() : 0; }
+    __host__ __device__ __forceinline__ int items() const { return shared_items() + S * Hkv * own_pairs(); }
     __host__ __device__ __forceinline__ int item(int s, int i) const {    // s < 0: the shared rows;  i = head * pairs + pair
-        return s < 0 ? i : Hkv * (shared_tiles > 0 ? shared_pairs() : 0) + s * Hkv * own_pairs() + i;
+        return s < 0 ? i : shared_items() + s * Hkv * own_pairs() + i;
     }
     // Where the partial result of a lane lies.  A segment that is a whole item has the item's place; of any other a CTA has at most one
     // that does not start its item (its first) and one that does (its last).
@@ -69,6 +76,30 @@ struct SharedWork {
         return from_start && to_end ? 2 * item + lane : 2 * items() + 4 * cta + (from_start ? 2 : 0) + lane;
     }
     __host__ __device__ __forceinline__ int slots() const { return 2 * items() + 4 * G; }
+    // Where a slot's row 0 lies in the workspace, in words of 16 bytes.  The workspace is made of blocks of 128 rows, kPartWords words a row that lie
+    // 128 words apart; slots of M tiles that never have that many rows share a block.
+    __host__ __device__ __forceinline__ uint32_t place(int slot) const {
+        if (slot < own_slot) return shared_at(slot, shared_log2);
+        return slot < cta_slot ? own_place + shared_at(slot - own_slot, own_log2) : cta_place + shared_at(slot - cta_slot, cta_log2);
+    }
+    static __host__ __device__ __forceinline__ uint32_t shared_at(uint32_t i, int log2) {   // the i-th slot where 2^log2 share a block
+        return (i >> log2) * kPartBlock + ((i & ((1u << log2) - 1)) << (7 - log2));
+    }
+    // lays the slots out for M tiles of at most so many rows (of the batch, of one sequence); returns all blocks
+    __host__ long long lay(int of_batch, int of_sequence) {
+        auto share = [](int rows) {                          // at least 4 rows: whole sectors
+            int l = 0;
+            while (l < 5 && 2 * rows << l <= kSharedTile) ++l;
+            return l;
+        };
+        auto blocks = [](long long slots, int l) { return (slots + (1 << l) - 1) >> l; };
+        shared_log2 = share(of_batch); own_log2 = share(of_sequence);
+        cta_log2 = shared_tiles > 0 ? min(shared_log2, own_log2) : own_log2;   // (a CTA's segment may be of either kind)
+        own_slot = 2 * shared_items(); cta_slot = 2 * items();
+        const long long own = blocks(own_slot, shared_log2), cta = own + blocks(cta_slot - own_slot, own_log2);
+        own_place = (uint32_t)own * kPartBlock; cta_place = (uint32_t)cta * kPartBlock;
+        return cta + blocks(4ll * G, cta_log2);
+    }
 };
 
 struct SharedCursor {         // walks the list

@@ -48,15 +48,16 @@ constexpr float kRescaleThreshold = 8.0f;                    // rescale O only w
 constexpr long long kWaitCycles = 2000000000ll;              // bound of every wait: about one second of SM clock
 
 // Partial result of an M tile: O in three bytes an element, fp32 without its last byte: sign, exponent and 16 bits of significand (the output has 8)
-// of every element by itself, whatever its row's or its column's others are, infinities and NaN among them.  The two upper bytes lie as
-// uint4 [16 groups of 8 columns][128 rows], the third ones as uint4 [8 groups of 16 columns][128 rows];  (m, l) fp32 [128], the maximum that the
+// of every element by itself, whatever its row's or its column's others are, infinities and NaN among them.  A row is 25 words of 16 bytes: the
+// two upper bytes of 8 columns in each of 16, the third ones of 16 columns in each of 8, and (m, l) in fp32, the maximum that the
 // exponentials are relative to (base 2) and their sum.  l < 0: a sequence that cannot be computed (no tree, rows outside the cache).
 // (Half precision times a power of two of the row's largest element, two bytes, lost the elements below 2^-25 of it.  What the third byte
 // costs: 16 x 64 nodes, 32 heads over 8, under 8192 rows 148.6 -> 151.3 us, 64 sequences of a token 107.6 -> 108.2, one sequence of 4 nodes, 16 heads over 2,
 // under 30k rows 33 -> 37; 26 x 52 heads, 32 nodes, 128 rows 56.9 -> 53.4, 42 x 52 heads, a token each, 174 -> 168.)
-constexpr int kPartThird = 16 * 128 * 4;                     // in words: where the third bytes begin
-constexpr int kPartWords = kPartThird + 8 * 128 * 4;
-constexpr int kPartFloats = kPartWords + 2 * 128;
+// Words of neighbouring rows lie next to one another, a row's words 128 apart (see SharedWork::place(): with 128 rows for every M tile, however few
+// it can have, 64 sequences of a token, 40 heads, had 300 MB instead of 25; a distance of the rows that there can be instead of 128 made the
+// addresses arithmetic: 15 x 52 heads, 80 nodes 103.3 -> 106.8 us).
+constexpr int kPartThird = 16, kPartSums = 24;               // words of a row in front of the third bytes, of (m, l)
 // four elements' words: the upper halves of two, the third bytes of four, and back (the last byte comes back as a copy of the third: within 2^-15)
 __device__ __forceinline__ uint32_t upper_halves(uint32_t x0, uint32_t x1) { return __byte_perm(x0, x1, 0x7632); }
 __device__ __forceinline__ uint32_t third_bytes(uint32_t x0, uint32_t x1, uint32_t x2, uint32_t x3) {
@@ -76,11 +77,11 @@ struct Segment {
     int single, own;                                         // one M tile; a sequence's own rows
     int hk, token;                                           // key/value head, first token of the first M tile
     int row;                                                 // cache row of the first key tile
-    int slot;                                                // of the pair's first M tile; of a single one's first key tile
+    uint32_t part[2];                                        // places in the workspace: of the pair's M tiles; of a single one's even and odd key tiles
     int rows[2];                                             // query rows of the M tiles
     int node;                                                // tree node of the first M tile's first row
     int bad;
-    int pad[2];
+    int pad;
 };
 constexpr int kSegments = 6;
 
@@ -111,7 +112,7 @@ struct SharedArgs {
     int shared_nb, own_nb;                                   // tokens of an M tile: of the batch, of one sequence
     int shared_row, shared_len;
     float scale_log2;
-    float* parts;
+    uint4* parts;
     int32_t* status;
 };
 
@@ -290,12 +291,12 @@ tree_attn_shared_kernel(const __grid_constant__ CUtensorMap tmap_q_shared, const
                         for (int j = 0; j < kMaxB / 32; ++j)
                             if (lane + 32 * j < nn) hd->par[ring.at][lane + 32 * j] = (signed char)par[j];
                     }
+                    if (lane < 2) sg->part[lane] = wk.place(wk.slot(wk.item(s, cu.i), blockIdx.x, cu.t == 0, cu.t + n == cu.T, lane));
                     if (lane == 0) {
                         sg->n = n; sg->t_first = cu.t; sg->ctx = ctx; sg->n_keys = ctx + nn;
                         sg->single = m + 1 >= n_m; sg->own = !shared; sg->hk = hk;
                         sg->token = (shared ? 0 : s * wk.B) + m * nb;
                         sg->row = (int)((uint64_t)row0 + (uint64_t)cu.t * kSharedTile);
-                        sg->slot = wk.slot(wk.item(s, cu.i), blockIdx.x, cu.t == 0, cu.t + n == cu.T, 0);
                         const int left = shared ? wk.S * wk.B : nn;
                         sg->rows[0] = max(min(nb, left - m * nb), 0) * a.g;
                         sg->rows[1] = max(min(nb, left - (m + 1) * nb), 0) * a.g;
@@ -646,18 +647,16 @@ tree_attn_shared_kernel(const __grid_constant__ CUtensorMap tmap_q_shared, const
                 __syncwarp();
                 if (lane == 0) arrive_at(my_bars + kAtFree);
                 if (row_valid) {
-                    float* part = a.parts + (size_t)(sg.slot + turn) * kPartFloats;
-                    uint4* upper = reinterpret_cast<uint4*>(part) + row;
-                    uint4* third = reinterpret_cast<uint4*>(part + kPartThird) + row;
+                    uint4* part = a.parts + sg.part[turn] + row;
 #pragma unroll
                     for (int c = 0; c < 8; ++c) {
                         const uint32_t* x = v + 16 * c;
-                        upper[2 * c * 128] = make_uint4(upper_halves(x[0], x[1]), upper_halves(x[2], x[3]), upper_halves(x[4], x[5]), upper_halves(x[6], x[7]));
-                        upper[(2 * c + 1) * 128] = make_uint4(upper_halves(x[8], x[9]), upper_halves(x[10], x[11]), upper_halves(x[12], x[13]), upper_halves(x[14], x[15]));
-                        third[c * 128] = make_uint4(third_bytes(x[0], x[1], x[2], x[3]), third_bytes(x[4], x[5], x[6], x[7]),
-                                                    third_bytes(x[8], x[9], x[10], x[11]), third_bytes(x[12], x[13], x[14], x[15]));
+                        part[2 * c * 128] = make_uint4(upper_halves(x[0], x[1]), upper_halves(x[2], x[3]), upper_halves(x[4], x[5]), upper_halves(x[6], x[7]));
+                        part[(2 * c + 1) * 128] = make_uint4(upper_halves(x[8], x[9]), upper_halves(x[10], x[11]), upper_halves(x[12], x[13]), upper_halves(x[14], x[15]));
+                        part[(kPartThird + c) * 128] = make_uint4(third_bytes(x[0], x[1], x[2], x[3]), third_bytes(x[4], x[5], x[6], x[7]),
+                                                                  third_bytes(x[8], x[9], x[10], x[11]), third_bytes(x[12], x[13], x[14], x[15]));
                     }
-                    reinterpret_cast<float2*>(part + kPartWords)[row] = make_float2(m_run, sg.bad ? -1.f : l_run);
+                    *reinterpret_cast<float2*>(part + kPartSums * 128) = make_float2(m_run, sg.bad ? -1.f : l_run);
                 }
             }
             tile0 += sg.n;
@@ -696,7 +695,7 @@ __global__ void __launch_bounds__(kForm == kLongLists ? kJoiners * kCombineThrea
 tree_attn_shared_merge_kernel(const __grid_constant__ SharedArgs a, int H, __nv_bfloat16* __restrict__ out, float* __restrict__ lse) {
     constexpr bool kJoin = kForm == kLongLists;
     constexpr int kRound = kForm == kManyBlocks ? 2 : kForm == kLongLists ? 3 : 4;   // parts whose loads are in flight together
-    __shared__ int s_slot[4][kMaxParts];
+    __shared__ uint32_t s_part[4][kMaxParts];                // places in the workspace
     __shared__ int s_parts[4];
     __shared__ float s_join[kJoin ? 18 : 1][8][32];
     const int s = blockIdx.z, hk = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, columns = kJoin ? warp & 7 : warp;
@@ -732,7 +731,7 @@ tree_attn_shared_merge_kernel(const __grid_constant__ SharedArgs a, int H, __nv_
             for (int k0 = 0; k0 < ps.n; k0 += 32) {
                 const int slot = k0 + lane < ps.n ? ps.slot(wk, k0 + lane) : -1;
                 const uint32_t there = __ballot_sync(0xFFFFFFFFu, slot >= 0);
-                if (slot >= 0) s_slot[warp][n + __popc(there & ((1u << lane) - 1))] = slot;
+                if (slot >= 0) s_part[warp][n + __popc(there & ((1u << lane) - 1))] = wk.place(slot);
                 n += __popc(there);
             }
         }
@@ -760,12 +759,11 @@ tree_attn_shared_merge_kernel(const __grid_constant__ SharedArgs a, int H, __nv_
             ml[q] = make_float2(-INFINITY, 0.f);
             x[q][0] = x[q][1] = x[q][2] = make_uint4(0, 0, 0, 0);
             if (k < n) {
-                const float* part = a.parts + (size_t)(k < n0 ? s_slot[list0][k] : s_slot[list1][k - n0]) * kPartFloats;
-                const int rr = k < n0 ? row0 : row1;
-                ml[q] = __ldcg(reinterpret_cast<const float2*>(part + kPartWords) + rr);
-                x[q][0] = __ldcg(reinterpret_cast<const uint4*>(part) + (2 * columns) * 128 + rr);
-                x[q][1] = __ldcg(reinterpret_cast<const uint4*>(part) + (2 * columns + 1) * 128 + rr);
-                x[q][2] = __ldcg(reinterpret_cast<const uint4*>(part + kPartThird) + columns * 128 + rr);
+                const uint4* part = a.parts + (k < n0 ? s_part[list0][k] + row0 : s_part[list1][k - n0] + row1);
+                ml[q] = __ldcg(reinterpret_cast<const float2*>(part + kPartSums * 128));
+                x[q][0] = __ldcg(part + (2 * columns) * 128);
+                x[q][1] = __ldcg(part + (2 * columns + 1) * 128);
+                x[q][2] = __ldcg(part + (kPartThird + columns) * 128);
             }
         }
         float M_new = M;
@@ -859,9 +857,10 @@ cudaError_t launch_tree_attn_shared(goose_ctx* c, const __nv_bfloat16* q, const 
     if (!c->encode_tiled) return cudaErrorNotSupported;
     if (S == 0) return cudaSuccess;
     SharedArgs a = shared_args(c, kv_rows, shared_row, shared_len, row_off, ctx_len, parent, n_nodes, S, B, H, Hkv, scale);
-    const size_t need = sizeof(float) * (size_t)a.wk.slots() * kPartFloats;
-    if (cudaError_t e = grow(c, &c->shared_parts, &c->shared_bytes, need)) return e;
-    a.parts = static_cast<float*>(c->shared_parts);
+    const size_t words = (size_t)a.wk.lay(a.shared_nb * a.g, a.own_nb * a.g) * kPartBlock;
+    if (words > 0xFFFFFFFFull) return cudaErrorMemoryAllocation;   // (64 GB)
+    if (cudaError_t e = grow(c, &c->shared_parts, &c->shared_bytes, sizeof(uint4) * words)) return e;
+    a.parts = static_cast<uint4*>(c->shared_parts);
     CUtensorMap mqs, mqo, mk, mv;
     if (!make_q_map(c->encode_tiled, &mqs, q, (int64_t)S * B, Hkv, a.g, a.shared_nb) ||
         !make_q_map(c->encode_tiled, &mqo, q, (int64_t)S * B, Hkv, a.g, a.own_nb) ||

@@ -59,3 +59,35 @@ def test_an_infinite_value_stays_in_its_column(goose):
         out, _ = c.run(goose)
         assert not torch.isfinite(out[..., 50]).any()
         assert torch.equal(out[..., :50], clean[..., :50]) and torch.equal(out[..., 51:], clean[..., 51:])
+
+
+@pytest.mark.parametrize("S,H,Hkv,B,shared", [(64, 40, 40, 1, 1000), (64, 32, 8, 1, 1000), (1, 32, 8, 1, 500), (4, 16, 2, 128, 300), (16, 6, 2, 50, 0)])
+def test_the_workspace_is_the_headers(S, H, Hkv, B, shared):
+    """Device memory that a context's first call takes: goose.h's formula, and no more than a page or two."""
+    from paper_2604_02047_b200 import binding
+    sms, t = torch.cuda.get_device_properties(0).multi_processor_count, 128 // (H // Hkv)
+    pairs, k = (lambda n: -(-(-(-n // t)) // 2)), (lambda n: max(2 ** e for e in range(6) if 2 ** e * min(n, t) * (H // Hkv) <= 128))
+    up = lambda n, d: -(-n // d)  # noqa: E731
+    formula = 51200 * ((up(2 * Hkv * pairs(S * B), k(S * B)) if shared else 0) + up(2 * S * Hkv * pairs(B), k(B)) + up(4 * sms, k(S * B) if shared else k(B)))
+    goose = binding.Goose(max_S=S, max_B=128, max_H=64)
+    c = Case(S, H, Hkv, B, shared, [20] * S)
+    c.run(_another_context())                                      # (whatever a first call loads is there: another context's)
+    torch.cuda.synchronize()
+    before = torch.cuda.mem_get_info()[0]
+    reserved = torch.cuda.memory_reserved()
+    out, lse = c.run(goose)
+    torch.cuda.synchronize()
+    taken = before - torch.cuda.mem_get_info()[0] - (torch.cuda.memory_reserved() - reserved)
+    assert 0 < taken <= formula + (4 << 20), (taken, formula)
+    c.check(goose, out, lse)
+    goose.close()
+
+
+_warm = []
+
+
+def _another_context():
+    from paper_2604_02047_b200 import binding
+    if not _warm:
+        _warm.append(binding.Goose(max_S=64, max_B=128, max_H=64))
+    return _warm[0]
