@@ -269,13 +269,19 @@ cudaError_t launch_bounded_wait_selftest(goose_ctx* c, long long limit_cycles, i
 int mma_splits(const goose_ctx* c, int S, int H);
 
 // A workspace that a call needs `need` bytes of.  A new one has at least twice the old one's size, so that all of them together have less than
-// twice the last one's; the old one is kept, since a graph that was captured with it may be replayed as long as the context lives.
+// twice the last one's (where the device has no more than `need`, that); the old one is kept, since a graph that was captured with it may be
+// replayed as long as the context lives.
 inline cudaError_t grow(goose_ctx* c, void** p, size_t* bytes, size_t need) {
     if (need <= *bytes) return cudaSuccess;
     if (*p && c->n_outgrown == (int)(sizeof c->outgrown / sizeof c->outgrown[0])) return cudaErrorMemoryAllocation;
-    const size_t size = need > 2 * *bytes ? need : 2 * *bytes;
+    size_t size = need > 2 * *bytes ? need : 2 * *bytes;
     void* fresh = nullptr;
     cudaError_t e = cudaMalloc(&fresh, size);
+    if (e == cudaErrorMemoryAllocation && size > need) {
+        cudaGetLastError();
+        size = need;
+        e = cudaMalloc(&fresh, size);
+    }
     if (e != cudaSuccess) { cudaGetLastError(); return e; }
     if (*p) c->outgrown[c->n_outgrown++] = *p;
     *p = fresh; *bytes = size;
