@@ -35,7 +35,9 @@ bool convert(PyObject* o, T& v) {
     } else if constexpr (std::is_floating_point_v<T>) {
         v = static_cast<T>(PyFloat_AsDouble(o));
     } else {
-        v = static_cast<T>(PyLong_AsLongLong(o));
+        const long long n = PyLong_AsLongLong(o);
+        v = static_cast<T>(n);
+        if (v != n && !PyErr_Occurred()) PyErr_Format(PyExc_OverflowError, "%lld does not fit the argument's %d bits", n, (int)(8 * sizeof(T)));
     }
     return !PyErr_Occurred();
 }
