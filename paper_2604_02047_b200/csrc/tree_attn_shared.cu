@@ -385,6 +385,11 @@ tree_attn_shared_kernel(const __grid_constant__ CUtensorMap tmap_q_shared, const
                     }
                     tile0 += sg.n;
                 }
+                // The products' arrivals have landed, too, before the CTA ends: those that free stages and queries' places are behind the one
+                // that the epilogue waits for.
+                for (int i = 0; i < kStages && ok; ++i, st.next(kStages)) ok = wait_for(hd, &hd->kv_empty[st.at], st.phase ^ 1, a.status);
+                for (int b = 0; b < 2 && ok; ++b)
+                    ok = wait_for(hd, &hd->pair_empty[b], pair_parity(), a.status) && wait_for(hd, &hd->single_empty[b], single_parity(b), a.status);
                 if (!ok) {                                   // copies still in flight land before the CTA ends
                     for (int i = 0; i < kStages; ++i) {
                         const uint32_t user = users >> 2 * i & 3;
