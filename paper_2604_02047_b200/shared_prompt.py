@@ -59,10 +59,13 @@ class Model:
 
 
 class Batch:
-    """The caches of all layers (the shared rows first, then every sequence's own), the sequences' lengths and tokens."""
+    """The caches of all layers (the shared rows first, then every sequence's own), the sequences' lengths and tokens.  ``sequences``: each one's own
+    prompt, a token at least (its last is the first tree's anchor); ``room``: tokens of its own that a sequence may have."""
 
     def __init__(self, goose: binding.Goose, model: Model, prompt, sequences, room: int, nodes: int, reserved: int = 16):
-        self.g, self.m, self.S, self.B = goose, model, len(sequences), nodes
+        if not sequences or not all(len(own) for own in sequences):
+            raise ValueError("a batch has sequences, and each of them a token of its own")
+        self.g, self.m, self.S, self.B, self.room = goose, model, len(sequences), nodes, room
         self.shared = len(prompt)
         rows = self.shared + self.S * (room + CHUNK)
         shape = (rows, model.kv_heads, D)
@@ -136,10 +139,14 @@ class Batch:
 
 
 def decode(batch: Batch, tokens: int, k: int = 8):
-    """``tokens`` more tokens a sequence.  Returns (the sequences' tokens behind the shared prompt, steps)."""
+    """``tokens`` more tokens a sequence (ValueError where they do not fit).  Returns (the sequences' tokens behind the shared prompt, steps)."""
     S, B, V = batch.S, batch.B, batch.m.vocab
     table = np.full((V, k), -1, np.int32)                    # successors seen in earlier steps
     start = batch.hist_len.cpu().numpy()
+    # in front of the last step a sequence has tokens - 1 new ones, and a tree of B nodes behind them
+    most = int(start.max()) + tokens - 1
+    if most - batch.shared > batch.room or most + B > len(batch.m.rope):
+        raise ValueError("%d more tokens: room for %d of a sequence's own, positions up to %d" % (tokens, batch.room, len(batch.m.rope)))
     anchor = batch.hist[torch.arange(S), batch.hist_len.long()].cpu().numpy()
     steps = 0
     while True:
