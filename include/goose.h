@@ -143,7 +143,7 @@ int goose_tree_attn_gqa(goose_ctx* ctx, const void* q, const void* k_cache, cons
  *   t = floor(128 / (H / Hkv)) tokens of a 128-row tile, pairs(n) = ceil(ceil(n / t) / 2), and k(n) the largest power of two, at most 32, for
  *   which k(n) min(n, t) H / Hkv <= 128
  * (148 SMs, 64 sequences of a token: 32 heads over 8 32 MB, 40 over 40 25 MB; 16 x 64 nodes, 32 over 8 57 MB; one token 1 MB), and at least twice
- * what an earlier call had if the device has that much.  Other arguments, limits and errors as goose_tree_attn_gqa; the kernel needs tensor maps (GOOSE_ECUDA where the
+ * what an earlier call had if the device has that much.  S <= 65535; other arguments, limits and errors as goose_tree_attn_gqa; the kernel needs tensor maps (GOOSE_ECUDA where the
  * driver cannot make them).                                                                                     */
 int goose_tree_attn_shared(goose_ctx* ctx, const void* q, const void* k_cache, const void* v_cache, int64_t kv_rows,
                            int64_t shared_row, int32_t shared_len, const int64_t* row_off, const int32_t* ctx_len,
@@ -283,7 +283,7 @@ int goose_verify_step_harvest(goose_ctx* ctx, const void* q, void* k_cache, void
  *   row_off int64 [S], ctx_len int32 [S], pos_off int32 [S] or NULL (0), parent int32 [S][B] or NULL, n_nodes int32 [S] or NULL
  *   q_out bf16 [S][B][H][D], may be q itself (ldq == H * D); k_cache, v_cache bf16 [kv_rows][Hkv][D]; none of them may overlap an
  *            input otherwise
- * H and Hkv <= max_H, S <= max_S; B <= max_B with parent, S * B < 2^31 without.  A sequence whose parent[] is no tree or whose rows leave the
+ * H and Hkv <= max_H, S <= max_S and 65535; B <= max_B with parent, S * B < 2^31 without.  A sequence whose parent[] is no tree or whose rows leave the
  * cache, and a token whose position is outside the table (GOOSE_ST_BAD_POS): zeros in q_out, no cache row written.             */
 int goose_append_kv(goose_ctx* ctx, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv,
                     const void* q_weight, const void* k_weight, float eps, const float* rope, int rope_rows, int rope_dim,
@@ -308,7 +308,7 @@ int goose_append_kv(goose_ctx* ctx, const void* q, int64_t ldq, const void* k, i
  *   draft_tok int32 [S][B] or NULL (no token on any path), parent int32 [S][B], n_nodes int32 [S] or NULL
  *   repetition, frequency, presence  fp32 [S] or NULL (1, 0, 0)
  *   bias  fp32, row s at s * bias_stride (0: one row for all), or NULL;   mask uint32 [S*B][ldm], ldm * 32 >= V, or NULL
- * The call's workspace (4 bytes for every token of every sequence's vocabulary, where there is a history) is allocated as in
+ * S <= max_S and 65535.  The call's workspace (4 bytes for every token of every sequence's vocabulary, where there is a history) is allocated as in
  * goose_tree_attn_shared.  hist_len[s] outside [0, ldh]: GOOSE_ST_BAD_ROWS, the sequence counts as one without history; parent[] no tree: zeros.       */
 int goose_adjust_logits(goose_ctx* ctx, const void* logits, int64_t ldl, int S, int B, int V, const int32_t* hist, int64_t ldh,
                         const int32_t* hist_len, const int32_t* n_prompt, const int32_t* draft_tok, const int32_t* parent,

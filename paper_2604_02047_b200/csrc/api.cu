@@ -48,6 +48,8 @@ int check_shape(const goose_ctx* c, int S, int B, int H, int D) {
     return GOOSE_OK;
 }
 
+constexpr int kMaxGridRows = 65535;      // of the grids that have a row (or layer) a sequence
+
 }  // namespace
 
 // The step's split of the SMs: how many CTAs a head the attention gets (1: its persistent form) and, beside clusters, how many the top-k.
@@ -262,7 +264,7 @@ int goose_tree_attn_shared(goose_ctx* c, const void* q, const void* k_cache, con
                            void* out, float* lse, void* stream) {
     int rc = check_shape(c, S, B, H, D);
     if (rc) return rc;
-    if (Hkv < 1 || H % Hkv != 0 || H / Hkv > GOOSE_MAX_GROUP) return GOOSE_EINVAL;
+    if (Hkv < 1 || H % Hkv != 0 || H / Hkv > GOOSE_MAX_GROUP || S > kMaxGridRows) return GOOSE_EINVAL;
     if (!q || !k_cache || !v_cache || !row_off || !ctx_len || !parent || !out) return GOOSE_EINVAL;
     if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(out)) return GOOSE_EINVAL;
     if (kv_rows < 1 || kv_rows > 0x7FFFFFFFLL) return GOOSE_EINVAL;
@@ -342,7 +344,7 @@ int goose_append_kv(goose_ctx* c, const void* q, int64_t ldq, const void* k, int
     // (a run of tokens has no tree: its length is not that of one)
     int rc = check_shape(c, S, parent ? B : 1, H, D);
     if (rc) return rc;
-    if (B < 1 || (int64_t)S * B > 0x7FFFFFFFLL || Hkv < 1 || Hkv > c->max_H) return GOOSE_EINVAL;
+    if (B < 1 || S > kMaxGridRows || (int64_t)S * B > 0x7FFFFFFFLL || Hkv < 1 || Hkv > c->max_H) return GOOSE_EINVAL;
     if (!q || !k || !v || !row_off || !ctx_len || !q_out || !k_cache || !v_cache) return GOOSE_EINVAL;
     for (const void* p : {q, k, v, q_weight, k_weight, (const void*)rope, (const void*)q_out, (const void*)k_cache, (const void*)v_cache})
         if (!aligned16(p)) return GOOSE_EINVAL;
@@ -369,7 +371,7 @@ int goose_adjust_logits(goose_ctx* c, const void* logits, int64_t ldl, int S, in
                         const float* bias, int64_t bias_stride, const uint32_t* mask, int64_t ldm, void* out, int64_t ldo,
                         void* stream) {
     if (!c || !on_ctx_device(c) || !logits || !parent || !out) return GOOSE_EINVAL;
-    if (S < 0 || S > c->max_S || B < 1 || B > c->max_B) return GOOSE_EINVAL;
+    if (S < 0 || S > c->max_S || S > kMaxGridRows || B < 1 || B > c->max_B) return GOOSE_EINVAL;
     if (V < 1 || V > GOOSE_MAX_V || ldl < V || ldo < V || ((ldl | ldo) & 7) || !aligned16(logits) || !aligned16(out)) return GOOSE_EINVAL;
     if (hist && (!hist_len || ldh < 0 || ldh > 0x7FFFFFFFLL)) return GOOSE_EINVAL;
     if (bias && bias_stride != 0 && bias_stride < V) return GOOSE_EINVAL;
