@@ -8,8 +8,10 @@
 // prompt tokens (parent == NULL).
 //
 // What bounds it: a row of 256 bytes in, one out, and some 60 instructions for 16 bytes: HBM in long calls (two prompts of 6001 tokens, 40
-// heads: 127 us, 5.83 TB/s), the instructions with norm and half-split pairs (8192 tokens, 32 heads over 8: 59 us, 3.4 TB/s), the chain
-// ctx_len -> table row -> store in short ones (a token: 3.9 us; 16 trees of 64 nodes: 8.0).  16 lanes have a row (8 elements, one 16-byte load a lane), so that the norm is four
+// heads: 128 us, 5.78 TB/s), the instructions with norm and half-split pairs (8192 tokens, 32 heads over 8: 59 us, 3.5 TB/s; without norm 47; eight shuffles
+// a lane and row, the weights unpacked for every row, 12 to 24 bytes of spill in the streaming forms), the chain
+// ctx_len -> table row -> store in short ones (a token: 3.9 us), with node counts n_nodes in front of it, and parent -> depths beside it (16 trees
+// of 64 nodes: 8.0).  16 lanes have a row (8 elements, one 16-byte load a lane), so that the norm is four
 // shuffles and the partner of a half-split pair another lane's element of the same place; a group of 16 lanes takes
 // kRows rows of one token at a time, whose loads are all in flight together, and keeps the token's cosines and sines in registers.
 #include "goose_internal.cuh"

@@ -17,9 +17,9 @@
 // exponentials (16 a cycle and SM: 1060 cycles a tile) and a tile's products (1024 cycles) follow one another within a lane; tiles of 128 keys
 // and a row a thread, so that maximum and sum need no exchange.
 // What bounds it.  Many query rows: a pair of tiles takes 3150 to 3400 cycles, of which the exponentials are 2120, the products 2048 (16
-// sequences of 64 nodes, 32 heads over 8, under 8192 rows: 148 us, 1.07 PFLOP/s; under the power cap 172).  Few: HBM (64 sequences, a token each, 32 over 8,
-// under 16k rows: 107 us, 4.7 TB/s, 5.7 without merge; 122 under the power cap).  Small calls: planner 1.8 us, first tile 1.6, epilogue 1.3, merge 3 (4 sequences, a
-// token each, under 512 rows: 11.8 us).  A change of item takes 3 us where the item has a tile or two (26 x 52 heads, 32 nodes, 5423 rows: 203 us).
+// sequences of 64 nodes, 32 heads over 8, under 8192 rows: 151 us, 1.05 PFLOP/s; under the power cap 175).  Few: HBM (64 sequences, a token each, 32 over 8,
+// under 16k rows: 106 us, 4.7 TB/s, 5.7 without merge; 121 under the power cap).  Small calls: planner 1.8 us, first tile 1.6, epilogue 1.3, merge 3 (4 sequences, a
+// token each, under 512 rows: 11.8 to 12.2 us).  A change of item takes 3 us where the item has a tile or two (26 x 52 heads, 32 nodes, 5423 rows: 207 us).
 // Every wait is bounded: one that runs out raises the CTA's abort flag and GOOSE_ST_TIMEOUT, and every role unwinds.
 #include <stddef.h>
 
@@ -617,7 +617,7 @@ tree_attn_shared_kernel(const __grid_constant__ CUtensorMap tmap_q_shared, const
                             const float2 x2 = unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1])), scale2, neg2));
                             const float p0 = ex2(x2.x), p1 = ex2(x2.y);
                             ls2[e & 1] = add_f32x2(ls2[e & 1], pack_f32x2(p0, p1));
-                            v[e] = pack_bf16x2(p0, p1);
+                            v[e] = pack_bf16x2(p0, p1);   // P as V's type, as the product takes it: 2^-9 of a term, either way; the sum above is of p itself
                         }
                         TMEM_ST32(s_addr + 32 * h, v, 32 * h);
                         tmem_wait_st();
@@ -684,8 +684,9 @@ tree_attn_shared_kernel(const __grid_constant__ CUtensorMap tmap_q_shared, const
 // rows' work, and in two of the sequence's own; a warp makes the list of each tile's parts.  Where a sequence has no more than 16 rows, several
 // lanes share a row's parts and join what they have.  What bounds it is latency: lists, a barrier, a round of loads or two.  Three forms:
 //   few blocks     four parts a round in flight
-//   many           (more than two an SM) two parts a round in 64 registers, four blocks an SM.  16 x 64 nodes, 32 heads over 8: 151.4 -> 147.8 us
-//                  with the main kernel; 42 sequences, 52 heads, a token each, under 203 rows 180 -> 170; 256 blocks 46.1 -> 46.5, 32 blocks 11.9 -> 12.8
+//   many           (more than two an SM) two parts a round in 64 registers, four blocks an SM.  16 x 64 nodes, 32 heads over 8: 156.0 -> 151.1 us
+//                  with the main kernel; 42 sequences, 52 heads, a token each, under 203 rows 178 -> 168; 15 x 52 heads, 80 nodes 115.6 -> 105.2; with parts of
+//                  two bytes an element 256 blocks 46.1 -> 46.5, 32 blocks 11.9 -> 12.8
 //   long lists     (blocks fewer than the SMs, parts may be many) three times eight warps, which share the parts too, three parts a round (with
 //                  four they spill: 22 -> 24.5, 37 -> 46): with few heads a row has a hundred and more.  16 heads over 2: two sequences, a
 //                  token each, under 21k rows 44 -> 22 us; one sequence, 4 nodes, under 30k 51 -> 37; joined without need, 4 sequences of 32
