@@ -229,9 +229,10 @@ adjust_logits_kernel(const AdjustLogits a, int rows_per_block, int64_t ldw, cons
             if (n) add[e + f] += -freq * (float)n - pres;
         }
     }
-    const int arrived = mbar_wait_bounded(&s_full, 0, 2000000000ll, &s_abort);
-    if (arrived == 2) {                                        // (nothing raises the flag: every thread finds out for itself)
+    constexpr long long kWaitCycles = 2000000000ll;            // about one second of SM clock
+    if (mbar_wait_bounded(&s_full, 0, kWaitCycles, &s_abort) == 2) {   // (nothing raises the flag: every thread finds out for itself)
         atomicOr(&a.status[s], GOOSE_ST_TIMEOUT);
+        mbar_wait_bounded(&s_full, 0, kWaitCycles, &s_abort);  // copies still in flight land before the block ends
         return;
     }
     if (n_v > 0) {
