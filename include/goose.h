@@ -68,6 +68,8 @@ extern "C" {
 #define GOOSE_HEAD_DIM  128   /* the only supported head dimension                                 */
 #define GOOSE_MAX_V  262144   /* vocabulary size limit of goose_node_topk                          */
 #define GOOSE_STATIC_TOPK_MAX_ROWS 2048   /* row limit of goose_node_topk_static                    */
+#define GOOSE_MIN_PAGE      16   /* rows of a page of a paged cache: a power of two from here on      */
+#define GOOSE_MAX_PAGED_ROWS 1048576      /* rows that a sequence's part of a page table may name      */
 
 /* per-sequence status bits (goose_last_status) */
 #define GOOSE_ST_BAD_PARENT   1   /* parent[] is not a rooted tree in topological order */
@@ -324,6 +326,58 @@ int goose_adjust_logits(goose_ctx* ctx, const void* logits, int64_t ldl, int S, 
 int goose_append_tokens(goose_ctx* ctx, const int32_t* draft_tok, const int32_t* path, const int32_t* accept_len,
                         const int32_t* n_nodes, int S, int B, int32_t* hist, int64_t ldh, const int32_t* hist_len,
                         int32_t* new_len, void* stream);
+
+/* ---- a cache in pages ----
+ * Sessions that grow and end at different times take their rows from a pool of pages: caches bf16 [n_pages][page_size][Hkv][D], page_table
+ * int32 [S][ldt]; row j of sequence s is row j % page_size of page page_table[s][j / page_size].  page_size is a power of two, at least
+ * GOOSE_MIN_PAGE; n_pages * page_size < 2^31; ldt * page_size <= GOOSE_MAX_PAGED_ROWS.  Entries behind a sequence's last row are not read.
+ * A chunk is a run of new tokens (a prompt or a part of it, one token, the chain of a draft) of any length: token i of sequence s has row ctx_len[s] + i.
+ * n_new int32 [S] or NULL (every sequence has B tokens): the tokens 0 .. n_new[s]-1 exist, as with n_nodes above; 0: the sequence is
+ * skipped; outside [0, B]: GOOSE_ST_BAD_NODES, as 0.  S * B < 2^31, H and Hkv <= max_H, S <= max_S and 65535, B is not bounded by max_B.
+ * A sequence whose rows do not fit its part of the table (or the arrays beside it): GOOSE_ST_BAD_ROWS, zeros, nothing else written.  The same for a
+ * token whose row, or one that it sees, is in a page outside the cache (page_table is device data); tokens in front of that one may be zeros too.  */
+
+/* goose_append_kv of a run of tokens (parent = NULL there) into pages: the same norm, rotation, layouts and limits.  Besides, where the arrays are
+ * given, the new rows' entries of row_weight fp32 and row_pos int32 [S][Hkv][ldw] for every key/value head: row_weight = 0, row_pos = the token's position,
+ * pos_off[s] + ctx_len[s] + i (GOOSE_ST_BAD_POS where that is no int32).  ctx_len[s] + n_new[s] <= ldw then.                                  */
+int goose_append_kv_paged(goose_ctx* ctx, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv,
+                          const void* q_weight, const void* k_weight, float eps, const float* rope, int rope_rows, int rope_dim,
+                          int interleaved, const int32_t* page_table, int64_t ldt, const int32_t* ctx_len, const int32_t* pos_off,
+                          const int32_t* n_new, int S, int B, int H, int Hkv, int D, void* q_out, void* k_cache, void* v_cache,
+                          int n_pages, int page_size, float* row_weight, int32_t* row_pos, int64_t ldw, void* stream);
+
+/* Attention of a chunk over the pages: out[s][i][h] = softmax_j(scale q[s][i][h] . K[j][h / (H / Hkv)]) V[j][h / (H / Hkv)] over the rows
+ * j <= ctx_len[s] + i.  bf16, fp32 accumulation, one rounding to bf16; lse fp32 [S][B][H] = log-sum-exp of the scaled scores, or NULL.
+ *   q, out  bf16 [S][B][H][D], 16-byte aligned; out may be q itself.   0 < scale < 1e30
+ * What other sequences' rows and a page's rows behind the last one hold reaches no output; the chunk's own V rows must be finite (a
+ * token's weight for the tokens behind it is 0, and 0 x NaN is NaN).                                                                */
+int goose_chunk_attn(goose_ctx* ctx, const void* q, const void* k_cache, const void* v_cache, int n_pages, int page_size,
+                     const int32_t* page_table, int64_t ldt, const int32_t* ctx_len, const int32_t* n_new, int S, int B, int H,
+                     int Hkv, int D, float scale, void* out, float* lse, void* stream);
+
+/* The attention that every row got from a chunk, added up: for every key/value head hk and row j < ctx_len[s] + n_new[s]
+ *   row_weight[s][hk][j] += sum over the tokens i >= j - ctx_len[s] and the heads h of group hk of exp(scale q[s][i][h] . K[j][hk] - lse[s][i][h])
+ * in fp32, in an order that depends on the sizes alone.  lse fp32 [S][B][H] is goose_chunk_attn's; a head of a token whose lse is -infinity adds nothing.
+ * n_new may be smaller than the chunk's (the tokens of a draft that were accepted).  ctx_len[s] + n_new[s] <= ldw.  row_weight fp32 [S][Hkv][ldw].      */
+int goose_kv_weights(goose_ctx* ctx, const void* q, const float* lse, const void* k_cache, int n_pages, int page_size,
+                     const int32_t* page_table, int64_t ldt, const int32_t* ctx_len, const int32_t* n_new, int S, int B, int H,
+                     int Hkv, int D, float scale, float* row_weight, int64_t ldw, void* stream);
+
+/* Eviction: every key/value head of a sequence with more than `budget` rows keeps that many, each head its own choice:
+ *   the rows of positions below `sink` and of the last `recent` ones (row_pos >= pos_off[s] + ctx_len[s] - recent), and of the others those
+ *   of the largest row_weight; of equal ones the lower row; NaN counts as less than everything.
+ * The kept rows from `budget` on, in their order, take the places of the dropped ones in front of it, in theirs: K, V, weight and position.
+ *   new_weight, new_pos [S][Hkv][ldw_new]: entries 0 .. new_ctx_len[s]-1; others keep their contents
+ *   new_ctx_len[s] = min(ctx_len[s], budget); new_pos_off[s] = pos_off[s] + ctx_len[s] - new_ctx_len[s]  (pos_off NULL: 0), so that the next
+ *   token's position, pos_off + ctx_len, stays what it was.  None of the new arrays may overlap another array of the call.
+ *   budget >= 1, sink, recent >= 0, sink + recent <= budget.  The table's pages from ceil(new_ctx_len / page_size) on are free.
+ * The pages of a sequence that loses rows are written: no other sequence of the call may have them.  A sequence with ctx_len[s] outside [0, room], more
+ * rows left than ldw_new, or a page outside the cache: GOOSE_ST_BAD_ROWS, nothing moves, new_ctx_len = ctx_len, new_pos_off = pos_off, no new weights.
+ * The call's workspace, S Hkv (8 min(budget, ldt page_size - budget) + 16) bytes, is allocated as in goose_tree_attn_shared.                  */
+int goose_evict_kv(goose_ctx* ctx, void* k_cache, void* v_cache, int n_pages, int page_size, const int32_t* page_table, int64_t ldt,
+                   const int32_t* ctx_len, const int32_t* pos_off, const float* row_weight, const int32_t* row_pos, int64_t ldw,
+                   int budget, int sink, int recent, int S, int Hkv, int D, float* new_weight, int32_t* new_pos, int64_t ldw_new,
+                   int32_t* new_ctx_len, int32_t* new_pos_off, void* stream);
 
 /* Host-buffer variant of the whole step (the end-to-end call).  The prefix KV cache stays on the
  * device (k_cache / v_cache are device pointers, state carried from step to step); everything a

@@ -23,6 +23,7 @@ EXPORTS = [
     "goose_build_spine_tree", "goose_pad_tree", "goose_context_match", "goose_spine_ratio_tier", "goose_spine_ema",
     "goose_selftest_bounded_wait", "goose_tree_attn_gqa", "goose_verify_step_gqa", "goose_verify_step_host_gqa",
     "goose_verify_step_harvest", "goose_tree_attn_shared", "goose_append_kv", "goose_adjust_logits", "goose_append_tokens",
+    "goose_append_kv_paged", "goose_chunk_attn", "goose_kv_weights", "goose_evict_kv",
 ]
 
 ATTN_AUTO, ATTN_MMA, ATTN_UMMA = 0, 1, 2
@@ -136,6 +137,11 @@ def _token_stride(t: torch.Tensor, S: int, B: int, heads: int, D: int, name: str
         raise GooseError("%s must be a bf16 CUDA tensor [S][B][heads][D] = %s with a token's heads next to one another and all "
                          "tokens at one distance" % (name, [S, B, heads, D]))
     return ld
+
+
+def _room(*arrays: Optional[torch.Tensor]) -> int:
+    """Rows that the arrays beside a paged cache have for a head of a sequence; 0 where there are none."""
+    return next((a.shape[-1] for a in arrays if a is not None), 0)
 
 
 def _host_nn(h_n_nodes: Optional[torch.Tensor], S: int) -> Optional[torch.Tensor]:
@@ -371,6 +377,84 @@ class Goose:
         _check(self.call.append_tokens(self._h, draft_tok, path, accept_len, n_nodes, S, B, hist, room, hist_len, new_len),
                "goose_append_tokens")
         return new_len
+
+    # ------------------------------------------------------------------ a cache in pages
+    def append_kv_paged(self, q, k, v, k_cache, v_cache, page_table, ctx_len, rope: Optional[torch.Tensor] = None,
+                        n_new: Optional[torch.Tensor] = None, pos_off: Optional[torch.Tensor] = None,
+                        q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                        interleaved: bool = False, row_weight: Optional[torch.Tensor] = None, row_pos: Optional[torch.Tensor] = None,
+                        out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """``append_kv`` of a run of tokens into caches [pages][page size][Hkv][D], page_table int32 [S][entries].  ``row_weight`` fp32 and
+        ``row_pos`` int32 [S][Hkv][room] get the new rows' weights (0) and positions.  Returns the queries (``out``; q itself is allowed)."""
+        S, B, H, D = q.shape
+        pages, size, Hkv = k_cache.shape[:3]
+        width, room = page_table.shape[-1], _room(row_weight, row_pos)
+        positions, rope_dim = (0, 0) if rope is None else rope.shape
+        ldq = _token_stride(q, S, B, H, D, "q")
+        ldk = _token_stride(k, S, B, Hkv, D, "k")
+        ldv = _token_stride(v, S, B, Hkv, D, "v")
+        if out is None:
+            out = torch.empty((S, B, H, D), dtype=torch.bfloat16, device=q.device)
+        _shapes("k_cache v_cache page_table ctx_len out rope n_new pos_off q_weight k_weight row_weight row_pos",
+                "bNZKD bNZKD iSw iS bSBHD fPr? iS? iS? bD? bD? fSKl? iSKl?", "SBHDNZKwPrl", S, B, H, D, pages, size, Hkv, width, positions,
+                rope_dim, room, k_cache, v_cache, page_table, ctx_len, out, rope, n_new, pos_off, q_weight, k_weight, row_weight, row_pos)
+        _check(self.call.append_kv_paged(self._h, q, ldq, k, ldk, v, ldv, q_weight, k_weight, eps, rope, positions, rope_dim, interleaved,
+                                         page_table, width, ctx_len, pos_off, n_new, S, B, H, Hkv, D, out, k_cache, v_cache, pages, size,
+                                         row_weight, row_pos, room), "goose_append_kv_paged")
+        return out
+
+    def chunk_attn(self, q, k_cache, v_cache, page_table, ctx_len, scale: float, out: Optional[torch.Tensor] = None, want_lse: bool = False,
+                   lse: Optional[torch.Tensor] = None, n_new: Optional[torch.Tensor] = None):
+        """Attention of a chunk of new tokens q [S][B][H][D], one or thousands a sequence, over the ctx_len rows in front of them and causally
+        over their own, which append_kv_paged has put behind those.  Returns out, or (out, lse) with ``want_lse`` or ``lse``."""
+        S, B, H, D = q.shape
+        pages, size, Hkv = k_cache.shape[:3]
+        width = page_table.shape[-1]
+        if out is None:
+            out = torch.empty_like(q)
+        if want_lse and lse is None:
+            lse = torch.empty((S, B, H), dtype=torch.float32, device=q.device)
+        _shapes("q k_cache v_cache page_table ctx_len out lse n_new", "bSBHD bNZKD bNZKD iSw iS bSBHD fSBH? iS?", "SBHDNZKw",
+                S, B, H, D, pages, size, Hkv, width, q, k_cache, v_cache, page_table, ctx_len, out, lse, n_new)
+        _check(self.call.chunk_attn(self._h, q, k_cache, v_cache, pages, size, page_table, width, ctx_len, n_new, S, B, H, Hkv, D, scale,
+                                    out, lse), "goose_chunk_attn")
+        return out if lse is None else (out, lse)
+
+    def kv_weights(self, q, lse, k_cache, page_table, ctx_len, scale: float, row_weight, n_new: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Adds to ``row_weight`` fp32 [S][Hkv][room] the attention that every row gets from the chunk's tokens (all heads of its group);
+        ``lse`` is chunk_attn's.  Returns row_weight."""
+        S, B, H, D = q.shape
+        pages, size, Hkv = k_cache.shape[:3]
+        width, room = page_table.shape[-1], row_weight.shape[-1]
+        _shapes("q lse k_cache page_table ctx_len row_weight n_new", "bSBHD fSBH bNZKD iSw iS fSKl iS?", "SBHDNZKwl", S, B, H, D, pages, size,
+                Hkv, width, room, q, lse, k_cache, page_table, ctx_len, row_weight, n_new)
+        _check(self.call.kv_weights(self._h, q, lse, k_cache, pages, size, page_table, width, ctx_len, n_new, S, B, H, Hkv, D, scale,
+                                    row_weight, room), "goose_kv_weights")
+        return row_weight
+
+    def evict_kv(self, k_cache, v_cache, page_table, ctx_len, row_weight, row_pos, budget: int, sink: int, recent: int,
+                 pos_off: Optional[torch.Tensor] = None, new_weight: Optional[torch.Tensor] = None, new_pos: Optional[torch.Tensor] = None,
+                 new_ctx_len: Optional[torch.Tensor] = None, new_pos_off: Optional[torch.Tensor] = None):
+        """Every key/value head of every sequence back to ``budget`` rows: the first ``sink`` positions, the last ``recent`` ones and the
+        heaviest others stay.  Returns (new_ctx_len, new_pos_off, new_weight, new_pos); none of them may be the array that it replaces."""
+        S = page_table.shape[0]
+        pages, size, Hkv, D = k_cache.shape
+        width, room = page_table.shape[-1], row_weight.shape[-1]
+        if new_weight is None:
+            new_weight = torch.empty_like(row_weight)
+        if new_pos is None:
+            new_pos = torch.empty((S, Hkv, new_weight.shape[-1]), dtype=torch.int32, device=row_pos.device)
+        if new_ctx_len is None:
+            new_ctx_len = torch.empty_like(ctx_len)
+        if new_pos_off is None:
+            new_pos_off = torch.empty_like(ctx_len)
+        new_room = new_weight.shape[-1]
+        _shapes("k_cache v_cache page_table ctx_len row_weight row_pos pos_off new_weight new_pos new_ctx_len new_pos_off",
+                "bNZKD bNZKD iSw iS fSKl iSKl iS? fSKm iSKm iS iS", "SNZKDwlm", S, pages, size, Hkv, D, width, room, new_room, k_cache, v_cache,
+                page_table, ctx_len, row_weight, row_pos, pos_off, new_weight, new_pos, new_ctx_len, new_pos_off)
+        _check(self.call.evict_kv(self._h, k_cache, v_cache, pages, size, page_table, width, ctx_len, pos_off, row_weight, row_pos, room,
+                                  budget, sink, recent, S, Hkv, D, new_weight, new_pos, new_room, new_ctx_len, new_pos_off), "goose_evict_kv")
+        return new_ctx_len, new_pos_off, new_weight, new_pos
 
     # ------------------------------------------------------------------ whole step
     def alloc_step_outputs(self, S: int, B: int, H: int, D: int, k: int, device=None) -> dict:

@@ -16,7 +16,8 @@ LIB = os.path.join(HERE, "libgoose.so")
 MARSHAL = os.path.join(HERE, "_marshal" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 MARSHAL_SOURCE = "marshal.cpp"
 SOURCES = ["api.cu", "node_topk.cu", "harvest.cu", "accept.cu", "kv_compact.cu", "tree_attn_mma.cu",
-           "tree_attn_umma.cu", "append_kv.cu", "adjust_logits.cu", "tree_attn_shared.cu", "spine_tree.cpp"]
+           "tree_attn_umma.cu", "append_kv.cu", "adjust_logits.cu", "tree_attn_shared.cu", "chunk_attn.cu",
+           "kv_weights.cu", "evict_kv.cu", "spine_tree.cpp"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++17", "-lineinfo",
               "-Xcompiler", "-fPIC", "-I", INCLUDE, "-I", CSRC]
 

@@ -50,6 +50,24 @@ int check_shape(const goose_ctx* c, int S, int B, int H, int D) {
 
 constexpr int kMaxGridRows = 65535;      // of the grids that have a row (or layer) a sequence
 
+bool ranges_overlap(const void* p, size_t n, const void* q, size_t m) {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+    return a < b + m && b < a + n;
+}
+
+// what the calls on a paged cache have in common (chunks may be longer than a tree)
+int check_pages(const goose_ctx* c, int S, int B, int H, int Hkv, int D, const int32_t* table, int64_t ldt, int n_pages, int page_size,
+                goose::Pages* pages) {
+    if (!c || !on_ctx_device(c) || (!table && S != 0)) return GOOSE_EINVAL;
+    if (S < 0 || S > c->max_S || S > kMaxGridRows || B < 1 || (int64_t)S * B > INT32_MAX || D != GOOSE_HEAD_DIM) return GOOSE_EINVAL;
+    if (H < 1 || H > c->max_H || Hkv < 1 || H % Hkv != 0 || H / Hkv > GOOSE_MAX_GROUP) return GOOSE_EINVAL;
+    if (page_size < GOOSE_MIN_PAGE || page_size > GOOSE_MAX_PAGED_ROWS || (page_size & (page_size - 1)) != 0 || n_pages < 1) return GOOSE_EINVAL;
+    if ((int64_t)n_pages * page_size > INT32_MAX || ldt < 1 || ldt > GOOSE_MAX_PAGED_ROWS / page_size) return GOOSE_EINVAL;
+    pages->table = table; pages->ldt = ldt; pages->n = n_pages;
+    pages->size_log2 = 31 - __builtin_clz((unsigned)page_size);
+    return GOOSE_OK;
+}
+
 }  // namespace
 
 // The step's split of the SMs: how many CTAs a head the attention gets (1: its persistent form) and, beside clusters, how many the top-k.
@@ -203,7 +221,7 @@ int goose_destroy(goose_ctx* c) {
     cudaSetDevice(c->device);
     cudaFree(c->partials); cudaFree(c->head_counters); cudaFree(c->topk_cand);
     cudaFree(c->row_counters); cudaFree(c->topk_lse_ws); cudaFree(c->status); cudaFree(c->selftest_word); cudaFree(c->stage);
-    cudaFree(c->shared_parts); cudaFree(c->adjust_tables);
+    cudaFree(c->shared_parts); cudaFree(c->adjust_tables); cudaFree(c->evict_moves);
     for (int i = 0; i < c->n_outgrown; ++i) cudaFree(c->outgrown[i]);
     if (c->pin) cudaFreeHost(c->pin);
     if (c->side) cudaStreamDestroy(c->side);
@@ -398,6 +416,100 @@ int goose_append_tokens(goose_ctx* c, const int32_t* draft_tok, const int32_t* p
                                                 static_cast<cudaStream_t>(stream));
     if (e != cudaSuccess) return cuda_fail(e);
     return GOOSE_OK;
+}
+
+int goose_append_kv_paged(goose_ctx* c, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv,
+                          const void* q_weight, const void* k_weight, float eps, const float* rope, int rope_rows, int rope_dim,
+                          int interleaved, const int32_t* page_table, int64_t ldt, const int32_t* ctx_len, const int32_t* pos_off,
+                          const int32_t* n_new, int S, int B, int H, int Hkv, int D, void* q_out, void* k_cache, void* v_cache,
+                          int n_pages, int page_size, float* row_weight, int32_t* row_pos, int64_t ldw, void* stream) {
+    goose::Pages pages;
+    int rc = check_pages(c, S, B, H, Hkv, D, page_table, ldt, n_pages, page_size, &pages);
+    if (rc || S == 0) return rc;
+    if (!q || !k || !v || !ctx_len || !q_out || !k_cache || !v_cache) return GOOSE_EINVAL;
+    for (const void* p : {q, k, v, (const void*)q_out, (const void*)k_cache, (const void*)v_cache, q_weight, k_weight, (const void*)rope})
+        if (!aligned16(p)) return GOOSE_EINVAL;
+    for (int64_t ld : {ldq - (int64_t)H * D, ldk - (int64_t)Hkv * D, ldv - (int64_t)Hkv * D})
+        if (ld < 0 || (ld & 7) != 0) return GOOSE_EINVAL;
+    if (q_out == q && ldq != (int64_t)H * D) return GOOSE_EINVAL;
+    if (rope_dim < 0 || rope_dim > D || rope_dim % 16 != 0 || (rope_dim > 0 && (!rope || rope_rows < 1)) || !(eps >= 0.f)) return GOOSE_EINVAL;
+    if ((row_weight || row_pos) ? ldw < 1 : false) return GOOSE_EINVAL;
+    goose::AppendKv a{};
+    a.q = (const __nv_bfloat16*)q; a.k = (const __nv_bfloat16*)k; a.v = (const __nv_bfloat16*)v;
+    a.ldq = ldq; a.ldk = ldk; a.ldv = ldv;
+    a.q_weight = (const __nv_bfloat16*)q_weight; a.k_weight = (const __nv_bfloat16*)k_weight; a.eps = eps;
+    a.rope = rope; a.rope_rows = rope_rows; a.rope_dim = rope_dim; a.interleaved = interleaved != 0;
+    a.ctx_len = ctx_len; a.pos_off = pos_off; a.n_nodes = n_new;
+    a.B = B; a.H = H; a.Hkv = Hkv;
+    a.q_out = (__nv_bfloat16*)q_out; a.k_cache = (__nv_bfloat16*)k_cache; a.v_cache = (__nv_bfloat16*)v_cache;
+    a.pages = pages; a.row_weight = row_weight; a.row_pos = row_pos; a.ldw = row_weight || row_pos ? ldw : 0;
+    cudaError_t e = goose::launch_append_kv(c, a, S, static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? GOOSE_OK : cuda_fail(e);
+}
+
+int goose_chunk_attn(goose_ctx* c, const void* q, const void* k_cache, const void* v_cache, int n_pages, int page_size,
+                     const int32_t* page_table, int64_t ldt, const int32_t* ctx_len, const int32_t* n_new, int S, int B, int H,
+                     int Hkv, int D, float scale, void* out, float* lse, void* stream) {
+    goose::ChunkAttn a{};
+    int rc = check_pages(c, S, B, H, Hkv, D, page_table, ldt, n_pages, page_size, &a.pages);
+    if (rc || S == 0) return rc;
+    if (!q || !k_cache || !v_cache || !ctx_len || !out) return GOOSE_EINVAL;
+    if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(out)) return GOOSE_EINVAL;
+    if (!(scale > 0.f) || !(scale < 1e30f)) return GOOSE_EINVAL;
+    a.q = (const __nv_bfloat16*)q; a.k_cache = (const __nv_bfloat16*)k_cache; a.v_cache = (const __nv_bfloat16*)v_cache;
+    a.ctx_len = ctx_len; a.n_new = n_new; a.S = S; a.B = B; a.H = H; a.Hkv = Hkv; a.scale = scale;
+    a.out = (__nv_bfloat16*)out; a.lse = lse;
+    cudaError_t e = goose::launch_chunk_attn(c, a, static_cast<cudaStream_t>(stream));
+    if (e == cudaErrorMemoryAllocation) return GOOSE_ENOMEM;
+    return e == cudaSuccess ? GOOSE_OK : cuda_fail(e);
+}
+
+int goose_kv_weights(goose_ctx* c, const void* q, const float* lse, const void* k_cache, int n_pages, int page_size,
+                     const int32_t* page_table, int64_t ldt, const int32_t* ctx_len, const int32_t* n_new, int S, int B, int H,
+                     int Hkv, int D, float scale, float* row_weight, int64_t ldw, void* stream) {
+    goose::KvWeights a{};
+    int rc = check_pages(c, S, B, H, Hkv, D, page_table, ldt, n_pages, page_size, &a.pages);
+    if (rc || S == 0) return rc;
+    if (!q || !lse || !k_cache || !ctx_len || !row_weight || ldw < 1) return GOOSE_EINVAL;
+    if (!aligned16(q) || !aligned16(k_cache)) return GOOSE_EINVAL;
+    if (!(scale > 0.f) || !(scale < 1e30f)) return GOOSE_EINVAL;
+    a.q = (const __nv_bfloat16*)q; a.lse = lse; a.k_cache = (const __nv_bfloat16*)k_cache;
+    a.ctx_len = ctx_len; a.n_new = n_new; a.S = S; a.B = B; a.H = H; a.Hkv = Hkv; a.scale = scale;
+    a.row_weight = row_weight; a.ldw = ldw;
+    cudaError_t e = goose::launch_kv_weights(c, a, static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? GOOSE_OK : cuda_fail(e);
+}
+
+int goose_evict_kv(goose_ctx* c, void* k_cache, void* v_cache, int n_pages, int page_size, const int32_t* page_table, int64_t ldt,
+                   const int32_t* ctx_len, const int32_t* pos_off, const float* row_weight, const int32_t* row_pos, int64_t ldw,
+                   int budget, int sink, int recent, int S, int Hkv, int D, float* new_weight, int32_t* new_pos, int64_t ldw_new,
+                   int32_t* new_ctx_len, int32_t* new_pos_off, void* stream) {
+    goose::EvictKv a{};
+    int rc = check_pages(c, S, 1, Hkv, Hkv, D, page_table, ldt, n_pages, page_size, &a.pages);
+    if (rc || S == 0) return rc;
+    if (!k_cache || !v_cache || !ctx_len || !row_weight || !row_pos || !new_weight || !new_pos || !new_ctx_len || !new_pos_off) return GOOSE_EINVAL;
+    if (!aligned16(k_cache) || !aligned16(v_cache)) return GOOSE_EINVAL;
+    if (budget < 1 || sink < 0 || recent < 0 || (int64_t)sink + recent > budget) return GOOSE_EINVAL;
+    if (ldw < 1 || ldw_new < 1) return GOOSE_EINVAL;
+    // the new arrays are written by blocks that others' reads of the old ones run beside
+    const size_t rows = (size_t)S * Hkv * 4, n_old = rows * ldw, n_new = rows * ldw_new, words = 4 * (size_t)S;
+    const void* fresh[4] = {new_weight, new_pos, new_ctx_len, new_pos_off};
+    const size_t fresh_bytes[4] = {n_new, n_new, words, words};
+    const void* old[4] = {row_weight, row_pos, ctx_len, pos_off};
+    const size_t old_bytes[4] = {n_old, n_old, words, words};
+    for (int i = 0; i < 4; ++i) {
+        for (int j = 0; j < 4; ++j)
+            if (old[j] && ranges_overlap(fresh[i], fresh_bytes[i], old[j], old_bytes[j])) return GOOSE_EINVAL;
+        for (int j = 0; j < i; ++j)
+            if (ranges_overlap(fresh[i], fresh_bytes[i], fresh[j], fresh_bytes[j])) return GOOSE_EINVAL;
+    }
+    a.k_cache = (__nv_bfloat16*)k_cache; a.v_cache = (__nv_bfloat16*)v_cache;
+    a.ctx_len = ctx_len; a.pos_off = pos_off; a.row_weight = row_weight; a.row_pos = row_pos; a.ldw = ldw;
+    a.budget = budget; a.sink = sink; a.recent = recent; a.S = S; a.Hkv = Hkv;
+    a.new_weight = new_weight; a.new_pos = new_pos; a.ldw_new = ldw_new; a.new_ctx_len = new_ctx_len; a.new_pos_off = new_pos_off;
+    cudaError_t e = goose::launch_evict_kv(c, a, static_cast<cudaStream_t>(stream));
+    if (e == cudaErrorMemoryAllocation) return GOOSE_ENOMEM;
+    return e == cudaSuccess ? GOOSE_OK : cuda_fail(e);
 }
 
 int goose_verify_step(goose_ctx* c, const void* q, void* k_cache, void* v_cache, int64_t kv_rows,

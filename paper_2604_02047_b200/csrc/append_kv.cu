@@ -60,9 +60,10 @@ __device__ __forceinline__ bool tree_depths(const int32_t* __restrict__ parent, 
     return true;
 }
 
-// kTree: positions by the depth in a tree, else by the place in a run of tokens.  kStream: the next rows are on their way while a group's
+// kTree: positions by the depth in a tree, else by the place in a run of tokens.  kPaged: the rows lie in pages (a run of tokens), and every
+// new row gets its position and a weight of zero.  kStream: the next rows are on their way while a group's
 // rows are worked on (two prompts of 6001 tokens, 40 heads, in blocks of 16 tokens: 137 -> 132 us; 16 trees of 64 nodes, two rounds a group: 8.0 -> 8.8)
-template <bool kTree, bool kStream>
+template <bool kTree, bool kStream, bool kPaged>
 __global__ void __launch_bounds__(kAppendThreads, 3)
 append_kv_kernel(const AppendKv a, int groups_log2 /* groups of 16 lanes a token */) {
     __shared__ int s_up[kMaxB], s_depth[kMaxB];
@@ -94,9 +95,9 @@ append_kv_kernel(const AppendKv a, int groups_log2 /* groups of 16 lanes a token
     if (blockIdx.x == 0 && threadIdx.x == 0 && nodes_bad(a.n_nodes, s, a.B)) atomicOr(&a.status[s], GOOSE_ST_BAD_NODES);
     if (first >= nn) return;
     const int ctx = a.ctx_len[s];
-    const int64_t row0 = a.row_off[s];
+    const int64_t row0 = kPaged ? 0 : a.row_off[s];
     const int64_t pos0 = (int64_t)(a.pos_off ? a.pos_off[s] : 0) + ctx;
-    int flaw = rows_outside(row0, ctx, nn, a.kv_rows) ? GOOSE_ST_BAD_ROWS : 0;
+    int flaw = rows_outside(row0, ctx, nn, kPaged ? a.pages.room(a.ldw) : a.kv_rows) ? GOOSE_ST_BAD_ROWS : 0;
     int depth = i;
     if (kTree) {
         if (!tree_depths(a.parent + (size_t)s * a.B, nn, s_up, s_depth)) flaw |= GOOSE_ST_BAD_PARENT;
@@ -105,6 +106,12 @@ append_kv_kernel(const AppendKv a, int groups_log2 /* groups of 16 lanes a token
     if (i >= nn) return;                                       // (whole groups: the shuffles below name their 16 lanes)
     const int64_t pos = pos0 + depth;
     if (a.rope_dim && (pos < 0 || pos >= a.rope_rows)) flaw |= GOOSE_ST_BAD_POS;
+    int64_t place = row0 + ctx + i;                            // row of the caches
+    if (kPaged && !flaw) {
+        place = a.pages.row(s, ctx + i);
+        if (place < 0) flaw |= GOOSE_ST_BAD_ROWS;
+        if (a.row_pos && (pos < 0 || pos > INT32_MAX)) flaw |= GOOSE_ST_BAD_POS;
+    }
     if (flaw && lane == 0 && r_first == 0) atomicOr(&a.status[s], flaw);
 
     const int half = a.rope_dim >> 1;
@@ -132,7 +139,7 @@ append_kv_kernel(const AppendKv a, int groups_log2 /* groups of 16 lanes a token
         }
     }
     const uint32_t mask = 0xFFFFu << (threadIdx.x & 16);
-    const size_t cache_row = ((size_t)row0 + ctx + i) * Hkv;
+    const size_t cache_row = (size_t)place * Hkv;
     for (int r0 = r_first; r0 < rows; r0 += kRows * per_token) {
         uint4 next[kRows];
         if (kStream) load(r0 + kRows * per_token, next);
@@ -148,6 +155,11 @@ append_kv_kernel(const AppendKv a, int groups_log2 /* groups of 16 lanes a token
             if (flaw) {                                        // queries of zeros, no row of the cache touched
                 if (is_q) to[lane] = make_uint4(0, 0, 0, 0);
                 continue;
+            }
+            if (kPaged && lane == 0 && !is_q && r < H + Hkv) {
+                const size_t at = ((size_t)s * Hkv + r - H) * a.ldw + ctx + i;
+                if (a.row_weight) a.row_weight[at] = 0.f;
+                if (a.row_pos) a.row_pos[at] = (int)pos;
             }
             if (r < H + Hkv) {
                 float y[8];
@@ -201,8 +213,9 @@ cudaError_t launch_append_kv(goose_ctx* c, AppendKv a, int S, cudaStream_t st) {
     const int per_block = kAppendGroups >> lg;
     const dim3 grid((a.B + per_block - 1) / per_block, S);
     const bool stream = rows >= (4 * kRows << lg);            // four rounds a group and more
-    auto kernel = a.parent ? (stream ? append_kv_kernel<true, true> : append_kv_kernel<true, false>)
-                           : (stream ? append_kv_kernel<false, true> : append_kv_kernel<false, false>);
+    auto kernel = a.pages.table ? (stream ? append_kv_kernel<false, true, true> : append_kv_kernel<false, false, true>)
+                : a.parent ? (stream ? append_kv_kernel<true, true, false> : append_kv_kernel<true, false, false>)
+                           : (stream ? append_kv_kernel<false, true, false> : append_kv_kernel<false, false, false>);
     cudaError_t e = launch_pdl(kernel, grid, dim3(kAppendThreads), 0, st, a, lg);
     c->launches++;
     return e;
@@ -246,8 +259,10 @@ cudaError_t launch_append_tokens(goose_ctx* c, const int32_t* draft_tok, const i
 }
 
 cudaError_t init_append_kernels() {
-    return load_kernels({(const void*)append_kv_kernel<true, false>, (const void*)append_kv_kernel<true, true>, (const void*)append_kv_kernel<false, false>,
-                         (const void*)append_kv_kernel<false, true>, (const void*)append_tokens_kernel});
+    return load_kernels({(const void*)append_kv_kernel<true, false, false>, (const void*)append_kv_kernel<true, true, false>,
+                         (const void*)append_kv_kernel<false, false, false>, (const void*)append_kv_kernel<false, true, false>,
+                         (const void*)append_tokens_kernel, (const void*)append_kv_kernel<false, false, true>,
+                         (const void*)append_kv_kernel<false, true, true>});
 }
 
 }  // namespace goose

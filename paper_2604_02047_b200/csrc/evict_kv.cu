@@ -1,0 +1,197 @@
+// Eviction: the rows of a key/value head that stay, and the rows behind the budget among them to the places of those in front of it that do not.
+//
+// A row's key is an unsigned number in the order of what stays: the first and the latest positions above everything, then the weights, NaN below all.
+// The budget-th largest key is found digit by digit (eight bits a pass, a histogram a pass); of the rows that have that very key the lowest stay.
+// The first kernel, a block a (sequence, head), leaves a list of (place, row) pairs; the second copies the rows.  Places lie in front of the
+// budget, rows behind it, so that no copy reads what another one writes.
+#include "goose_internal.cuh"
+
+namespace goose {
+
+constexpr int kEvictThreads = 1024;
+constexpr int kEvictWarps = kEvictThreads / 32;
+constexpr int kMoveThreads = 256;
+constexpr int kMovesAhead = 4;                        // words that stand in front of a head's list (its length)
+
+// of the row's position and weight
+__device__ __forceinline__ uint32_t evict_key(float w, int pos, int sink, int64_t recent_from) {
+    if (pos < sink || pos >= recent_from) return 0xFFFFFFFFu;
+    if (!(w == w)) return 0;
+    const uint32_t b = __float_as_uint(w + 0.f);      // (-0 + 0 = +0)
+    return b >> 31 ? ~b : b | 0x80000000u;
+}
+
+// exclusive prefix sum over the block's threads; total in every thread.  s_warp: kEvictWarps words of its own
+__device__ __forceinline__ int block_prefix(int v, int* s_warp, int& total) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int upto = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int u = __shfl_up_sync(0xFFFFFFFFu, upto, o);
+        if (lane >= o) upto += u;
+    }
+    __syncthreads();
+    if (lane == 31) s_warp[warp] = upto;
+    __syncthreads();
+    int w = lane < kEvictWarps ? s_warp[lane] : 0;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int u = __shfl_up_sync(0xFFFFFFFFu, w, o);
+        if (lane >= o) w += u;
+    }
+    total = __shfl_sync(0xFFFFFFFFu, w, 31);
+    const int before = __shfl_sync(0xFFFFFFFFu, w, warp == 0 ? 0 : warp - 1);
+    return upto - v + (warp == 0 ? 0 : before);
+}
+
+__global__ void __launch_bounds__(kEvictThreads)
+evict_select_kernel(const EvictKv a, int32_t* __restrict__ moves, int64_t moves_ld, int32_t* __restrict__ status) {
+    extern __shared__ uint32_t s_keep[];              // a bit a row: it stays
+    __shared__ int s_hist[256], s_warp[kEvictWarps], s_digit, s_above;
+    const int s = blockIdx.y, hk = blockIdx.x, tid = threadIdx.x, lane = tid & 31;
+    const size_t head = (size_t)s * a.Hkv + hk;
+    pdl_wait();
+    pdl_trigger();
+    const int ctx = a.ctx_len[s], off = a.pos_off ? a.pos_off[s] : 0, left = min(ctx, a.budget);
+    int32_t* list = moves + head * moves_ld;
+    const int64_t room = a.pages.room(a.ldw);
+    bool bad = ctx < 0 || ctx > room || left > a.ldw_new;
+    const int pages = bad ? 0 : (ctx + (1 << a.pages.size_log2) - 1) >> a.pages.size_log2;
+    for (int p = tid; p < pages; p += kEvictThreads) {
+        const int page = a.pages.table[s * a.pages.ldt + p];
+        bad |= page < 0 || page >= a.pages.n;
+    }
+    bad = __syncthreads_or(bad);
+    if (tid == 0) {
+        list[0] = 0;
+        if (hk == 0) {
+            a.new_ctx_len[s] = bad ? ctx : left;
+            a.new_pos_off[s] = bad ? off : off + (ctx - left);
+            if (bad) atomicOr(&status[s], GOOSE_ST_BAD_ROWS);
+        }
+    }
+    if (bad) return;
+    const float* weight = a.row_weight + head * a.ldw;
+    const int32_t* pos = a.row_pos + head * a.ldw;
+    float* new_weight = a.new_weight + head * a.ldw_new;
+    int32_t* new_pos = a.new_pos + head * a.ldw_new;
+    if (ctx <= a.budget) {
+        for (int j = tid; j < ctx; j += kEvictThreads) { new_weight[j] = weight[j]; new_pos[j] = pos[j]; }
+        return;
+    }
+    const int64_t recent_from = (int64_t)off + ctx - a.recent;
+    auto key = [&](int j) { return evict_key(weight[j], pos[j], a.sink, recent_from); };
+    // the budget-th largest key: its upper digits so far, and how many of the rows that have them are still to be taken
+    uint32_t prefix = 0;
+    int need = a.budget;
+    for (int shift = 24; shift >= 0; shift -= 8) {
+        if (tid < 256) s_hist[tid] = 0;
+        __syncthreads();
+        for (int j = tid; j < ctx; j += kEvictThreads) {
+            const uint32_t k = key(j);
+            if (shift == 24 || k >> (shift + 8) == prefix) atomicAdd(&s_hist[k >> shift & 255], 1);
+        }
+        __syncthreads();
+        // thread t has digit 255 - t: how many rows have a larger one
+        const int mine = tid < 256 ? s_hist[255 - tid] : 0;
+        int total;
+        const int above = block_prefix(mine, s_warp, total);
+        if (tid < 256 && above < need && above + mine >= need) { s_digit = 255 - tid; s_above = above; }
+        __syncthreads();
+        prefix = prefix << 8 | (uint32_t)s_digit;
+        need -= s_above;
+        __syncthreads();
+    }
+    // what stays, in words of 32 rows; a warp's rows are consecutive
+    const int words = (ctx + 31) >> 5, per = (words + kEvictWarps - 1) / kEvictWarps;
+    const int w0 = min((tid >> 5) * per, words), w1 = min(w0 + per, words);
+    int equal = 0;
+    for (int w = w0; w < w1; ++w) {
+        const int j = 32 * w + lane;
+        const uint32_t k = j < ctx ? key(j) : 0u;
+        equal += __popc(__ballot_sync(0xFFFFFFFFu, j < ctx && k == prefix));
+    }
+    int total;
+    int before = block_prefix(lane == 0 ? equal : 0, s_warp, total);
+    before = __shfl_sync(0xFFFFFFFFu, before, 0);     // rows of that very key in front of the warp's
+    for (int w = w0; w < w1; ++w) {
+        const int j = 32 * w + lane;
+        const uint32_t k = j < ctx ? key(j) : 0u;
+        const uint32_t same = __ballot_sync(0xFFFFFFFFu, j < ctx && k == prefix);
+        const bool stays = j < ctx && (k > prefix || (k == prefix && before + __popc(same & ((1u << lane) - 1)) < need));
+        const uint32_t word = __ballot_sync(0xFFFFFFFFu, stays);
+        if (lane == 0) s_keep[w] = word;
+        before += __popc(same);
+    }
+    __syncthreads();
+    // pairs: dropped rows in front of the budget, kept rows from it on, each by words of 32 that a thread has in a row
+    const int bw = (a.budget + 31) >> 5, b0 = a.budget >> 5;
+    auto holes = [&](int w) {                         // of word w
+        const uint32_t inside = w < b0 ? 0xFFFFFFFFu : (1u << (a.budget & 31)) - 1;
+        return ~s_keep[w] & inside;
+    };
+    auto movers = [&](int w) { return s_keep[w] & (w > b0 ? 0xFFFFFFFFu : ~((1u << (a.budget & 31)) - 1)); };
+    int32_t* to = list + kMovesAhead;
+    int32_t* of = to + (moves_ld - kMovesAhead) / 2;
+    for (int side = 0; side < 2; ++side) {
+        const int first = side ? b0 : 0, n = side ? words - b0 : bw, each = (n + kEvictThreads - 1) / kEvictThreads;
+        const int u0 = first + min(tid * each, n), u1 = first + min((tid + 1) * each, n);
+        int count = 0;
+        for (int w = u0; w < u1; ++w) count += __popc(side ? movers(w) : holes(w));
+        int at = block_prefix(count, s_warp, total);
+        for (int w = u0; w < u1; ++w)
+            for (uint32_t bits = side ? movers(w) : holes(w); bits; bits &= bits - 1) (side ? of : to)[at++] = 32 * w + __ffs(bits) - 1;
+    }
+    if (tid == 0) list[0] = total;
+    __syncthreads();
+    // weights and positions: what stays where it is, then what changes its place (written by this block: visible behind the barrier)
+    for (int j = tid; j < a.budget; j += kEvictThreads)
+        if (s_keep[j >> 5] >> (j & 31) & 1) { new_weight[j] = weight[j]; new_pos[j] = pos[j]; }
+    for (int m = tid; m < total; m += kEvictThreads) { new_weight[to[m]] = weight[of[m]]; new_pos[to[m]] = pos[of[m]]; }
+}
+
+// 16 lanes have a row (16 bytes a lane)
+__global__ void __launch_bounds__(kMoveThreads)
+evict_move_kernel(const EvictKv a, const int32_t* __restrict__ moves, int64_t moves_ld) {
+    const int s = blockIdx.z, hk = blockIdx.y, lane = threadIdx.x & 15;
+    pdl_wait();
+    pdl_trigger();
+    const int32_t* list = moves + ((size_t)s * a.Hkv + hk) * moves_ld;
+    const int n = list[0];
+    const int32_t* to = list + kMovesAhead;
+    const int32_t* of = to + (moves_ld - kMovesAhead) / 2;
+    for (int m = blockIdx.x * (kMoveThreads / 16) + (threadIdx.x >> 4); m < n; m += gridDim.x * (kMoveThreads / 16)) {
+        const size_t from = ((size_t)a.pages.row(s, of[m]) * a.Hkv + hk) * (kHeadDim / 8) + lane;
+        const size_t at = ((size_t)a.pages.row(s, to[m]) * a.Hkv + hk) * (kHeadDim / 8) + lane;
+        uint4* k = reinterpret_cast<uint4*>(a.k_cache);
+        uint4* v = reinterpret_cast<uint4*>(a.v_cache);
+        const uint4 kx = k[from], vx = v[from];
+        k[at] = kx;
+        v[at] = vx;
+    }
+}
+
+cudaError_t launch_evict_kv(goose_ctx* c, const EvictKv& a, cudaStream_t st) {
+    if (a.S == 0) return cudaSuccess;
+    const int64_t room = a.pages.room(a.ldw);
+    int64_t most = room - a.budget < a.budget ? room - a.budget : a.budget;   // rows of a head that can change places
+    if (most < 0) most = 0;
+    const int64_t ld = kMovesAhead + 2 * most;
+    if (cudaError_t e = grow(c, &c->evict_moves, &c->evict_bytes, sizeof(int32_t) * (size_t)ld * a.S * a.Hkv)) return e;
+    int32_t* moves = static_cast<int32_t*>(c->evict_moves);
+    const size_t smem = sizeof(uint32_t) * (size_t)((room + 31) / 32);
+    cudaError_t e = launch_pdl(evict_select_kernel, dim3(a.Hkv, a.S), dim3(kEvictThreads), smem, st, a, moves, ld, c->status);
+    c->launches++;
+    if (e != cudaSuccess || most == 0) return e;
+    const int64_t blocks = (most + kMoveThreads / 16 - 1) / (kMoveThreads / 16);
+    e = launch_pdl(evict_move_kernel, dim3((unsigned)(blocks < 64 ? blocks : 64), a.Hkv, a.S), dim3(kMoveThreads), 0, st, a, moves, ld);
+    c->launches++;
+    return e;
+}
+
+cudaError_t init_evict_kernels() {
+    cudaError_t e = cudaFuncSetAttribute(evict_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, GOOSE_MAX_PAGED_ROWS / 8);
+    return e == cudaSuccess ? load_kernels({(const void*)evict_move_kernel}) : e;
+}
+
+}  // namespace goose

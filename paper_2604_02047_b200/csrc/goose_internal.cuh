@@ -41,6 +41,8 @@ struct goose_ctx {
     size_t shared_bytes;
     void* adjust_tables;
     size_t adjust_bytes;
+    void* evict_moves;        // goose_evict_kv: rows that change places
+    size_t evict_bytes;
     void* outgrown[128];      // they live as long as the context: a captured graph may still name them
     int n_outgrown;
     // per-sequence status words
@@ -222,6 +224,23 @@ int attn_cluster(const goose_ctx* c, int S, int B, int H, int Hkv, int64_t kv_ro
 struct StepSplit { int cluster, topk_ctas; };
 StepSplit step_split(const goose_ctx* c, int S, int B, int H, int Hkv, int64_t kv_rows, int V, int k, bool harvest, bool counts);
 
+// The pages of the sequences: row j of sequence s is row j % 2^size_log2 of page table[s][j >> size_log2].  The table is device data: an
+// entry outside [0, n) names no row.
+struct Pages {
+    const int32_t* table;
+    int64_t ldt;
+    int n, size_log2;
+    // rows that a sequence may have: of its part of the table, and of an array that goes with them (ldw, where there is one)
+    __host__ __device__ __forceinline__ int64_t room(int64_t ldw) const { const int64_t r = ldt << size_log2; return ldw > 0 && ldw < r ? ldw : r; }
+#ifdef __CUDACC__
+    // row of the caches, or -1
+    __device__ __forceinline__ int64_t row(int s, int j) const {
+        const int page = table[s * ldt + (j >> size_log2)];
+        return page < 0 || page >= n ? -1 : ((int64_t)page << size_log2) + (j & ((1 << size_log2) - 1));
+    }
+#endif
+};
+
 // arguments of goose_append_kv and goose_adjust_logits as the kernels take them (status: the launcher's)
 struct AppendKv {
     const __nv_bfloat16 *q, *k, *v;
@@ -236,6 +255,10 @@ struct AppendKv {
     __nv_bfloat16 *q_out, *k_cache, *v_cache;
     int64_t kv_rows;
     int32_t* status;
+    Pages pages;                                           // table == NULL: sequences of consecutive rows (row_off)
+    float* row_weight;                                     // paged: [S][Hkv][ldw] each, or NULL
+    int32_t* row_pos;
+    int64_t ldw;
 };
 cudaError_t launch_append_kv(goose_ctx* c, AppendKv a, int S, cudaStream_t st);
 cudaError_t launch_append_tokens(goose_ctx* c, const int32_t* draft_tok, const int32_t* path, const int32_t* accept_len,
@@ -262,6 +285,43 @@ cudaError_t launch_tree_attn_shared(goose_ctx* c, const __nv_bfloat16* q, const 
                                     int64_t kv_rows, int64_t shared_row, int shared_len, const int64_t* row_off,
                                     const int32_t* ctx_len, const int32_t* parent, const int32_t* n_nodes, int S, int B, int H,
                                     int Hkv, float scale, __nv_bfloat16* out, float* lse, cudaStream_t st);
+
+// the paged cache: arguments of goose_chunk_attn, goose_kv_weights and goose_evict_kv
+struct ChunkAttn {
+    const __nv_bfloat16 *q, *k_cache, *v_cache;
+    Pages pages;
+    const int32_t *ctx_len, *n_new;
+    int S, B, H, Hkv;
+    float scale;
+    __nv_bfloat16* out;
+    float* lse;
+};
+cudaError_t launch_chunk_attn(goose_ctx* c, const ChunkAttn& a, cudaStream_t st);
+struct KvWeights {
+    const __nv_bfloat16 *q, *k_cache;
+    const float* lse;
+    Pages pages;
+    const int32_t *ctx_len, *n_new;
+    int S, B, H, Hkv;
+    float scale;
+    float* row_weight;
+    int64_t ldw;
+};
+cudaError_t launch_kv_weights(goose_ctx* c, const KvWeights& a, cudaStream_t st);
+struct EvictKv {
+    __nv_bfloat16 *k_cache, *v_cache;
+    Pages pages;
+    const int32_t *ctx_len, *pos_off;
+    const float* row_weight;
+    const int32_t* row_pos;
+    int64_t ldw;
+    int budget, sink, recent, S, Hkv;
+    float* new_weight;
+    int32_t* new_pos;
+    int64_t ldw_new;
+    int32_t *new_ctx_len, *new_pos_off;
+};
+cudaError_t launch_evict_kv(goose_ctx* c, const EvictKv& a, cudaStream_t st);
 
 cudaError_t launch_bounded_wait_selftest(goose_ctx* c, long long limit_cycles, int32_t* result, cudaStream_t st);
 
@@ -308,10 +368,13 @@ cudaError_t init_accept_kernel();
 cudaError_t init_append_kernels();
 cudaError_t init_adjust_kernel();
 cudaError_t init_shared_kernel();
+cudaError_t init_chunk_kernels();
+cudaError_t init_weights_kernels();
+cudaError_t init_evict_kernels();
 inline cudaError_t init_kernels(goose_ctx* c) {
     cudaError_t e = init_umma_kernel(c);
     for (cudaError_t (*init)() : {init_topk_kernel, init_compact_kernel, init_merge_kernel, init_accept_kernel, init_table_kernel, init_mma_kernel,
-                                  init_append_kernels, init_adjust_kernel, init_shared_kernel})
+                                  init_append_kernels, init_adjust_kernel, init_shared_kernel, init_chunk_kernels, init_weights_kernels, init_evict_kernels})
         if (e == cudaSuccess) e = init();
     return e;
 }

@@ -180,6 +180,10 @@ PyMethodDef methods[] = {
     entry<&goose_append_kv>("append_kv"),
     entry<&goose_adjust_logits>("adjust_logits"),
     entry<&goose_append_tokens>("append_tokens"),
+    entry<&goose_append_kv_paged>("append_kv_paged"),
+    entry<&goose_chunk_attn>("chunk_attn"),
+    entry<&goose_kv_weights>("kv_weights"),
+    entry<&goose_evict_kv>("evict_kv"),
     {"check", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&check)), METH_FASTCALL, nullptr},
     {"shapes", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&shapes)), METH_FASTCALL, nullptr},
     {"token_stride", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&token_stride)), METH_FASTCALL, nullptr},
