@@ -41,6 +41,9 @@ struct goose_ctx {
     size_t shared_bytes;
     void* adjust_tables;
     size_t adjust_bytes;
+    void* chunk_parts;        // partial results of goose_chunk_attn
+    size_t chunk_bytes;
+    int32_t* chunk_counters;  // [num_sms][2][4], zero between launches
     void* evict_moves;        // goose_evict_kv: rows that change places
     size_t evict_bytes;
     void* outgrown[128];      // they live as long as the context: a captured graph may still name them

@@ -40,6 +40,14 @@ __device__ __forceinline__ void tma_load_3d_hint(void* dst, const CUtensorMap* m
                  "[%0], [%1, {%3, %4, %5}], [%2], %6;"
                  ::"r"(smem_u32(dst)), "l"(map), "r"(smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2), "l"(policy) : "memory");
 }
+// the same by one lane of a warp that runs converged (see umma_f16_by)
+__device__ __forceinline__ void tma_load_3d_hint_by(bool leader, uint32_t dst, const CUtensorMap* map, unsigned long long* bar,
+                                                    int c0, int c1, int c2, unsigned long long policy) {
+    asm volatile("{\n\t.reg .pred e;\n\tsetp.ne.b32 e, %7, 0;\n\t"
+                 "@e cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint "
+                 "[%0], [%1, {%3, %4, %5}], [%2], %6;\n\t}"
+                 ::"r"(dst), "l"(map), "r"(smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2), "l"(policy), "r"((uint32_t)leader) : "memory");
+}
 // brings a box of a tensor map into L2: a hint; nothing reaches the SM, and a box outside the tensor touches nothing
 __device__ __forceinline__ void tma_prefetch_3d(const CUtensorMap* map, int c0, int c1, int c2) {
     asm volatile("cp.async.bulk.prefetch.tensor.3d.L2.global [%0, {%1, %2, %3}];" ::"l"(map), "r"(c0), "r"(c1), "r"(c2) : "memory");
