@@ -194,11 +194,14 @@ int goose_create(goose_ctx** out, int device, int max_S, int max_B, int max_H, i
     ok = ok && cudaMalloc(&c->status, sizeof(int32_t) * (size_t)max_S) == cudaSuccess;
     ok = ok && cudaMalloc(&c->selftest_word, sizeof(int32_t)) == cudaSuccess;
     ok = ok && cudaMalloc(&c->chunk_counters, sizeof(int32_t) * 8 * (size_t)c->num_sms) == cudaSuccess;
+    ok = ok && cudaMalloc(&c->weight_sums, sizeof(float) * 2 * 4 * 128 * (size_t)c->num_sms) == cudaSuccess;
+    ok = ok && cudaMalloc(&c->weight_counters, sizeof(int32_t) * 16 * (size_t)c->num_sms) == cudaSuccess;
     if (ok) {
         ok = ok && cudaMemset(c->head_counters, 0, sizeof(int32_t) * (size_t)heads) == cudaSuccess;
         ok = ok && cudaMemset(c->row_counters, 0, sizeof(int32_t) * (size_t)c->topk_rows_cap) == cudaSuccess;
         ok = ok && cudaMemset(c->status, 0, sizeof(int32_t) * (size_t)max_S) == cudaSuccess;
         ok = ok && cudaMemset(c->chunk_counters, 0, sizeof(int32_t) * 8 * (size_t)c->num_sms) == cudaSuccess;
+        ok = ok && cudaMemset(c->weight_counters, 0, sizeof(int32_t) * 16 * (size_t)c->num_sms) == cudaSuccess;
     }
     if (ok) {
         cudaDriverEntryPointQueryResult qres;
@@ -224,6 +227,7 @@ int goose_destroy(goose_ctx* c) {
     cudaFree(c->partials); cudaFree(c->head_counters); cudaFree(c->topk_cand);
     cudaFree(c->row_counters); cudaFree(c->topk_lse_ws); cudaFree(c->status); cudaFree(c->selftest_word); cudaFree(c->stage);
     cudaFree(c->shared_parts); cudaFree(c->adjust_tables); cudaFree(c->evict_moves); cudaFree(c->chunk_parts); cudaFree(c->chunk_counters);
+    cudaFree(c->weight_sums); cudaFree(c->weight_counters);
     for (int i = 0; i < c->n_outgrown; ++i) cudaFree(c->outgrown[i]);
     if (c->pin) cudaFreeHost(c->pin);
     if (c->side) cudaStreamDestroy(c->side);
@@ -814,6 +818,7 @@ int goose_last_status(goose_ctx* c, int32_t* host_status, int S) {
         GOOSE_CUDA(cudaMemset(c->head_counters, 0, sizeof(int32_t) * (size_t)c->max_S * (size_t)c->max_H));
         GOOSE_CUDA(cudaMemset(c->row_counters, 0, sizeof(int32_t) * (size_t)c->topk_rows_cap));
         GOOSE_CUDA(cudaMemset(c->chunk_counters, 0, sizeof(int32_t) * 8 * (size_t)c->num_sms));
+        GOOSE_CUDA(cudaMemset(c->weight_counters, 0, sizeof(int32_t) * 16 * (size_t)c->num_sms));
     }
     return rc;
 }

@@ -44,6 +44,8 @@ struct goose_ctx {
     void* chunk_parts;        // partial results of goose_chunk_attn
     size_t chunk_bytes;
     int32_t* chunk_counters;  // [num_sms][2][4], zero between launches
+    float* weight_sums;       // goose_kv_weights: sums of items that several CTAs have, [num_sms][2][4][128]
+    int32_t* weight_counters; // [num_sms][4][4], zero between launches
     void* evict_moves;        // goose_evict_kv: rows that change places
     size_t evict_bytes;
     void* outgrown[128];      // they live as long as the context: a captured graph may still name them

@@ -1,61 +1,517 @@
 // The attention that every cached row got from a chunk's tokens: W[s][hk][j] += sum_{i, h in group hk} exp(x_ihj - lse_ih), x_ihj = scale q_ih . k_j,
 // over the tokens i >= j - ctx.
 //
-// A warp a row of a head, four of the head's elements a lane.
+// Persistent, one CTA an SM, tcgen05: S^T = K Q^T with the keys as rows, so that a thread has a key, and its sum needs no exchange; up to
+// four key tiles of a run stay in shared memory while the Q tiles pass by.  Work list: weights_work.cuh.  Roles (384 threads):
+//   warp 0            TMA producer: Q tiles into a ring of two, K tiles, a box a page, into a ring of five; its lanes look the pages up
+//   warp 1            MMA issuer: the scores of key tile u of the run into columns 128 u of tensor memory
+//   warp 2            planner: walks the work list and puts the segments' descriptions into a ring
+//   warp 3            log-sum-exps of a Q tile's rows, negated and in units of log 2, and which of the rows count
+//   warps 4..7, 8..11 exponentials of key tiles 0 and 2, of 1 and 3: a key a thread, two sums.  At the segment's end the sums are added to the
+//                     rows' weights, or, where several CTAs have Q tiles of the item, left in the workspace; the warp that completes a count adds up what
+//                     all have left, in the order of the tokens.
+// Every wait is bounded: one that runs out raises the CTA's abort flag and GOOSE_ST_TIMEOUT, and every role unwinds.
+#include <stddef.h>
+
 #include "goose_internal.cuh"
+#include "tcgen05.cuh"
+#include "tree_attn_combine.cuh"
+#include "weights_work.cuh"
 
 namespace goose {
 
-constexpr int kWeightThreads = 256;
+namespace {
 
-__global__ void __launch_bounds__(kWeightThreads)
-kv_weights_kernel(const KvWeights a, int32_t* __restrict__ status) {
-    const int s = blockIdx.z, hk = blockIdx.y, lane = threadIdx.x & 31, g = a.H / a.Hkv;
+constexpr int kStages = 5, kQStages = 2;
+constexpr int kTileBytes = kWeightTile * kHeadDim * 2;       // 32 KB: one K or one Q tile
+constexpr int kHalfBytes = kWeightTile * 128;                // 16 KB: 128 rows x 64 bf16 (one swizzle-atom column)
+constexpr int kHeaderBytes = 2048;
+constexpr int kWeightSmem = 1008 /*alignment slack*/ + (kStages + kQStages) * kTileBytes + kHeaderBytes;
+constexpr int kWeightThreads = 384;
+constexpr uint32_t kTmemCols = 512;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr long long kWaitCycles = 2000000000ll;              // bound of every wait: about one second of SM clock
+constexpr int kSegments = 6;
+
+// a segment, as the planner describes it
+struct Segment {
+    int n, q_first;                                          // Q tiles; 0: the end.  The first of them
+    int s, hk, ctx, nn;
+    int key0, run;                                           // first key, key tiles
+    int whole, slot, c0, parts;                              // the CTA has all of the item; else the place of its sums, and who has the others
+};
+
+struct Header {
+    Segment seg[kSegments];
+    alignas(16) float lse[kQStages][kWeightTile];            // -lse / log 2 of the Q tile's rows
+    alignas(16) uint32_t counts[kQStages][4];                // which rows of the Q tile count
+    unsigned long long k_full[kStages], k_empty[kStages], q_full[kQStages], q_empty[kQStages], lse_full[kQStages], lse_empty[kQStages];
+    unsigned long long seg_full[kSegments], seg_empty[kSegments];
+    unsigned long long s_full[kRun], s_free[kRun];
+    uint32_t tmem_base;
+    volatile int abort_flag;
+};
+static_assert(sizeof(Header) <= kHeaderBytes, "header");
+static_assert(kWeightSmem <= 232448, "shared memory of a block");
+
+struct WeightArgs {
+    WeightWork wk;
+    Pages pages;
+    int g, H, nb, box_log2;                                  // heads of a group, heads, tokens of a box of queries, rows of a box of keys
+    float scale_log2;
+    const float* lse;
+    float* row_weight;
+    int64_t ldw;
+    float* sums;                                             // [CTA][2][kRun][128]
+    int32_t* counters;                                       // [CTA][kRun][4], zero between launches
+    int32_t* status;
+};
+
+__device__ __forceinline__ bool wait_for(Header* hd, unsigned long long* bar, uint32_t parity, int32_t* status) {
+    const int r = mbar_wait_bounded(bar, parity, kWaitCycles, &hd->abort_flag);
+    if (r == 2) {
+        hd->abort_flag = 1;
+        atomicOr(status, GOOSE_ST_TIMEOUT);
+    }
+    return r == 0;
+}
+__device__ __forceinline__ void drain(unsigned long long* bar, uint32_t parity) {   // after an abort
+    const long long t0 = clock64();
+    while (!mbar_try_wait(bar, parity) && clock64() - t0 < kWaitCycles) {}
+}
+
+// a place in a ring of n and its phase
+struct Ring {
+    uint32_t at, phase;
+    __device__ __forceinline__ void next(uint32_t n) {
+        if (++at == n) { at = 0; phase ^= 1; }
+    }
+};
+
+__device__ __forceinline__ long long warp_sum(long long v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+    return v;
+}
+
+// the list's length and a place in it, by a whole warp (lane = sequence); false: the CTA has no range
+__device__ __forceinline__ bool locate(WeightWork& wk, WeightCursor& cu, WeightSeq& q, long long& from, long long& to, int cta, int lane) {
+    wk.short_run = 1;
+    long long tiles = 0, sum = 0;
+    bool several = false;
+    for (int s0 = 0; s0 < wk.S; s0 += 32)
+        if (s0 + lane < wk.S) {
+            const WeightSeq x = wk.seq(s0 + lane);
+            if (x.n > wk.t) several = true; else tiles += x.items;
+        }
+    wk.set_run(warp_sum(tiles));
+    for (int s0 = 0; s0 < wk.S; s0 += 32)
+        if (s0 + lane < wk.S) {
+            const WeightSeq x = wk.seq(s0 + lane);
+            sum += x.before(x.items);
+        }
+    wk.set(warp_sum(sum), __any_sync(0xFFFFFFFFu, several));
+    from = wk.start(cta);
+    to = wk.start(cta + 1);
+    if (from >= to) return false;
+    long long begin = 0;
+    for (int s0 = 0; s0 < wk.S; s0 += 32) {
+        long long own = 0;
+        if (s0 + lane < wk.S) {
+            const WeightSeq x = wk.seq(s0 + lane);
+            own = wk.Hkv * x.before(x.items);
+        }
+        long long upto = own;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long u = __shfl_up_sync(0xFFFFFFFFu, upto, o);
+            if (lane >= o) upto += u;
+        }
+        const uint32_t here = __ballot_sync(0xFFFFFFFFu, begin + upto > from);
+        if (here) {
+            const int l = __ffs(here) - 1;
+            cu.s = s0 + l;
+            q = wk.seq(cu.s);
+            cu.enter(q, begin + __shfl_sync(0xFFFFFFFFu, upto - own, l), from);
+            return true;
+        }
+        begin += __shfl_sync(0xFFFFFFFFu, upto, 31);
+    }
+    return false;
+}
+
+// M = 128 keys, N = n query rows (a multiple of 16), both K-major
+__device__ __forceinline__ uint32_t scores_desc(int n) { return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((128u >> 4) << 24); }
+
+__global__ void __launch_bounds__(kWeightThreads, 1)
+kv_weights_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ WeightArgs a) {
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char* k_smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    unsigned char* q_smem = k_smem + kStages * kTileBytes;
+    Header* hd = reinterpret_cast<Header*>(q_smem + kQStages * kTileBytes);
+    const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kStages; ++i) { mbar_init(&hd->k_full[i], 1); mbar_init(&hd->k_empty[i], 1); }
+        for (int i = 0; i < kQStages; ++i) { mbar_init(&hd->q_full[i], 1); mbar_init(&hd->q_empty[i], 1); mbar_init(&hd->lse_full[i], 1); mbar_init(&hd->lse_empty[i], 8); }
+        for (int i = 0; i < kSegments; ++i) { mbar_init(&hd->seg_full[i], 1); mbar_init(&hd->seg_empty[i], 3 + 8); }
+        for (int u = 0; u < kRun; ++u) { mbar_init(&hd->s_full[u], 1); mbar_init(&hd->s_free[u], 4); }
+        hd->abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        prefetch_tmap(&tmap_q); prefetch_tmap(&tmap_k);
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&hd->tmem_base)), "r"(kTmemCols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, hd->tmem_base, 0);
     pdl_wait();
     pdl_trigger();
-    const int nn = nodes_of(a.n_new, s, a.B), ctx = a.ctx_len[s];
-    if (blockIdx.x == 0 && hk == 0 && threadIdx.x == 0 && nodes_bad(a.n_new, s, a.B)) atomicOr(&status[s], GOOSE_ST_BAD_NODES);
-    if (nn == 0) return;
-    if (rows_outside(0, ctx, nn, a.pages.room(a.ldw))) {
-        if (blockIdx.x == 0 && threadIdx.x == 0) atomicOr(&status[s], GOOSE_ST_BAD_ROWS);
-        return;
-    }
-    const int warps = gridDim.x * (kWeightThreads / 32);
-    auto unpack = [](uint2 v, float (&x)[4]) {
-        x[0] = __uint_as_float(v.x << 16); x[1] = __uint_as_float(v.x & 0xFFFF0000u);
-        x[2] = __uint_as_float(v.y << 16); x[3] = __uint_as_float(v.y & 0xFFFF0000u);
-    };
-    for (int j = blockIdx.x * (kWeightThreads / 32) + (threadIdx.x >> 5); j < ctx + nn; j += warps) {
-        const int64_t row = a.pages.row(s, j);
-        if (row < 0) {
-            if (lane == 0) atomicOr(&status[s], GOOSE_ST_BAD_ROWS);
-            continue;
-        }
-        float k[4], q[4], sum = 0.f;
-        unpack(*reinterpret_cast<const uint2*>(a.k_cache + ((size_t)row * a.Hkv + hk) * kHeadDim + 4 * lane), k);
-        for (int i = max(j - ctx, 0); i < nn; ++i)
-            for (int u = 0; u < g; ++u) {
-                const size_t at = ((size_t)s * a.B + i) * a.H + hk * g + u;
-                unpack(*reinterpret_cast<const uint2*>(a.q + at * kHeadDim + 4 * lane), q);
-                float x = q[0] * k[0] + q[1] * k[1] + q[2] * k[2] + q[3] * k[3];
-#pragma unroll
-                for (int w = 16; w > 0; w >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, w);
-                const float lse = a.lse[at];
-                if (lse != -INFINITY) sum += __expf(x * a.scale - lse);
+    auto all = [](bool x) { return __all_sync(0xFFFFFFFFu, x) != 0; };
+
+    if (warp == 2) {
+        // =============================================================== planner
+        WeightWork wk = a.wk;
+        if (blockIdx.x == 0)
+            for (int s = lane; s < wk.S; s += 32) {
+                const int flaw = (nodes_bad(wk.n_new, s, wk.B) ? GOOSE_ST_BAD_NODES : 0) | (wk.seq(s).bad ? GOOSE_ST_BAD_ROWS : 0);
+                if (flaw) atomicOr(&a.status[s], flaw);
             }
-        if (lane == 0) a.row_weight[((size_t)s * a.Hkv + hk) * a.ldw + j] += sum;
+        WeightCursor cu{};
+        WeightSeq q{};
+        long long from, to;
+        bool live = locate(wk, cu, q, from, to, blockIdx.x, lane);
+        auto advance = [&]() {
+            if (cu.next(wk, q)) return;
+            do {
+                if (++cu.s < wk.S) q = wk.seq(cu.s);
+            } while (cu.s < wk.S && q.items == 0);
+            cu.hk = cu.k = 0;
+            live = cu.s < wk.S;
+        };
+        Ring ring{0, 0};
+        for (;;) {
+            bool any = false;
+            while (live && cu.w0 < to) {
+                cu.look(wk, q, from, to);
+                any = cu.t1 > cu.t0;
+                if (any) break;
+                advance();
+            }
+            if (!wait_for(hd, &hd->seg_empty[ring.at], ring.phase ^ 1, a.status)) break;
+            Segment* sg = &hd->seg[ring.at];
+            if (lane == 0) {
+                sg->n = any ? cu.t1 - cu.t0 : 0;
+                if (any) {
+                    sg->q_first = q.first(cu.k) + cu.t0;
+                    sg->s = cu.s; sg->hk = cu.hk; sg->ctx = q.ctx; sg->nn = q.n;
+                    sg->key0 = cu.k * q.span();
+                    sg->run = min(q.run, (q.ctx + q.n - sg->key0 + kWeightTile - 1) / kWeightTile);
+                    sg->whole = cu.c0 == cu.c1; sg->slot = 2 * blockIdx.x + (cu.t0 == 0); sg->c0 = cu.c0; sg->parts = cu.c1 - cu.c0 + 1;
+                }
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&hd->seg_full[ring.at]);
+            if (!any) break;
+            ring.next(kSegments);
+            advance();
+        }
+    } else if (warp == 0) {
+        // =============================================================== TMA producer (the warp runs converged)
+        const bool leader = elect_leader();
+        const unsigned long long pol_once = l2_policy_evict_first(), pol_again = l2_policy_evict_last();
+        const uint32_t k_addr = smem_u32(k_smem);
+        const int boxes = kWeightTile >> a.box_log2, outside = a.pages.n << a.pages.size_log2;
+        uint32_t k_loads = 0, q_loads = 0;
+        Ring ks{0, 0}, qs{0, 0}, ring{0, 0};
+        bool ok = true;
+        while (ok) {
+            ok = all(wait_for(hd, &hd->seg_full[ring.at], ring.phase, a.status));
+            if (!ok) break;
+            const Segment sg = hd->seg[ring.at];
+            __syncwarp();
+            if (leader) mbar_arrive(&hd->seg_empty[ring.at]);
+            ring.next(kSegments);
+            if (sg.n == 0) break;
+            // the cache row of this lane's box of a key tile: no page behind the sequence's last row is looked up
+            auto box_row = [&](int u) {
+                const int j = sg.key0 + u * kWeightTile + (lane << a.box_log2);
+                if (lane >= boxes || u >= sg.run || j >= sg.ctx + sg.nn) return outside;
+                const int at = a.pages.table[sg.s * a.pages.ldt + (j >> a.pages.size_log2)];
+                return at < 0 || at >= a.pages.n ? outside : (at << a.pages.size_log2) + (j & ((1 << a.pages.size_log2) - 1));
+            };
+            int rows[kRun];
+#pragma unroll
+            for (int u = 0; u < kRun; ++u) rows[u] = box_row(u);
+            const unsigned long long pol = sg.nn > a.wk.t ? pol_again : pol_once;
+            for (int i = 0; i < sg.n && ok; ++i) {
+                ok = all(wait_for(hd, &hd->q_empty[qs.at], qs.phase ^ 1, a.status));
+                if (!ok) break;
+                if (leader) {
+                    const int token = sg.s * a.wk.B + (sg.q_first + i) * a.wk.t;
+                    mbar_expect_tx(&hd->q_full[qs.at], (uint32_t)(a.nb * a.g) * 256u);
+                    tma_load_4d(q_smem + qs.at * kTileBytes, &tmap_q, &hd->q_full[qs.at], 0, 0, sg.hk, token);
+                    tma_load_4d(q_smem + qs.at * kTileBytes + kHalfBytes, &tmap_q, &hd->q_full[qs.at], 64, 0, sg.hk, token);
+                }
+                __syncwarp();
+                ++q_loads;
+                qs.next(kQStages);
+                if (i > 0) continue;
+#pragma unroll
+                for (int u = 0; u < kRun; ++u) {
+                    if (u >= sg.run || !ok) break;
+                    ok = all(wait_for(hd, &hd->k_empty[ks.at], ks.phase ^ 1, a.status));
+                    if (!ok) break;
+                    if (leader) mbar_expect_tx(&hd->k_full[ks.at], kTileBytes);
+                    __syncwarp();
+                    const uint32_t dst = k_addr + ks.at * kTileBytes;
+                    for (int b = 0; b < boxes; ++b) {
+                        const int row = __shfl_sync(0xFFFFFFFFu, rows[u], b);
+                        const uint32_t to = dst + ((uint32_t)b << (a.box_log2 + 7));
+                        tma_load_3d_hint_by(leader, to, &tmap_k, &hd->k_full[ks.at], 0, sg.hk, row, pol);
+                        tma_load_3d_hint_by(leader, to + kHalfBytes, &tmap_k, &hd->k_full[ks.at], 64, sg.hk, row, pol);
+                    }
+                    ++k_loads;
+                    ks.next(kStages);
+                }
+            }
+        }
+        // the products' arrivals have landed, too, before the CTA ends
+        for (int i = 0; i < kStages && ok; ++i, ks.next(kStages)) ok = all(wait_for(hd, &hd->k_empty[ks.at], ks.phase ^ 1, a.status));
+        for (int i = 0; i < kQStages && ok; ++i, qs.next(kQStages)) ok = all(wait_for(hd, &hd->q_empty[qs.at], qs.phase ^ 1, a.status));
+        if (!ok) {                                           // copies still in flight land before the CTA ends
+            for (uint32_t i = 0; i < kStages; ++i)
+                if (k_loads > i) drain(&hd->k_full[i], ((k_loads - 1 - i) / kStages) & 1);
+            for (uint32_t i = 0; i < kQStages; ++i)
+                if (q_loads > i) drain(&hd->q_full[i], ((q_loads - 1 - i) / kQStages) & 1);
+        }
+    } else if (warp == 1) {
+        // =============================================================== MMA issuer
+        const bool leader = elect_leader();                  // the warp runs converged, this lane acts
+        const uint32_t q_addr = smem_u32(q_smem), k_addr = smem_u32(k_smem);
+        uint32_t k_tile = 0, used = 0;                       // K tiles in front of this segment; a bit a score buffer: its parity
+        Ring qs{0, 0}, ring{0, 0};
+        bool ok = true;
+        while (ok) {
+            ok = wait_for(hd, &hd->seg_full[ring.at], ring.phase, a.status);
+            if (!ok) break;
+            const Segment* sg = &hd->seg[ring.at];
+            const int n = __shfl_sync(0xFFFFFFFFu, sg->n, 0), run = __shfl_sync(0xFFFFFFFFu, sg->run, 0);
+            const int q_first = __shfl_sync(0xFFFFFFFFu, sg->q_first, 0), nn = __shfl_sync(0xFFFFFFFFu, sg->nn, 0);
+            __syncwarp();
+            if (leader) mbar_arrive(&hd->seg_empty[ring.at]);
+            ring.next(kSegments);
+            if (n == 0) break;
+            for (int i = 0; i < n && ok; ++i) {
+                ok = wait_for(hd, &hd->q_full[qs.at], qs.phase, a.status);
+                if (!ok) break;
+                const int rows = min(nn - (q_first + i) * a.wk.t, a.wk.t) * a.g;
+                const uint32_t idesc = scores_desc((rows + 15) & ~15);
+                const uint32_t q_lo = smem_desc_lo(q_addr + qs.at * kTileBytes, 16);
+                for (int u = 0; u < run; ++u) {
+                    const uint32_t load = k_tile + u, at = load % kStages;
+                    if (i == 0 && !(ok = wait_for(hd, &hd->k_full[at], load / kStages & 1, a.status))) break;
+                    if (!(ok = wait_for(hd, &hd->s_free[u], (used >> u & 1) ^ 1, a.status))) break;
+                    used ^= 1u << u;
+                    tc_fence_after();
+                    const uint32_t k_lo = smem_desc_lo(k_addr + at * kTileBytes, 16);
+#pragma unroll
+                    for (int kk = 0; kk < 8; ++kk) {         // 16 of the 128 head dims per instruction
+                        const uint32_t off = ((kk >> 2) * kHalfBytes + (kk & 3) * 32) >> 4;
+                        umma_f16_by(leader, tmem + u * 128, smem_desc(k_lo + off), smem_desc(q_lo + off), idesc, kk > 0 ? 1u : 0u);
+                    }
+                    umma_commit_by(leader, &hd->s_full[u]);
+                    if (i == n - 1) umma_commit_by(leader, &hd->k_empty[at]);
+                }
+                if (!ok) break;
+                umma_commit_by(leader, &hd->q_empty[qs.at]);
+                qs.next(kQStages);
+            }
+            k_tile += run;
+        }
+    } else if (warp == 3) {
+        // =============================================================== log-sum-exps
+        Ring qs{0, 0}, ring{0, 0};
+        bool ok = true;
+        while (ok) {
+            ok = all(wait_for(hd, &hd->seg_full[ring.at], ring.phase, a.status));
+            if (!ok) break;
+            const Segment sg = hd->seg[ring.at];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&hd->seg_empty[ring.at]);
+            ring.next(kSegments);
+            if (sg.n == 0) break;
+            for (int i = 0; i < sg.n; ++i) {
+                const int t0 = (sg.q_first + i) * a.wk.t, rows = min(sg.nn - t0, a.wk.t) * a.g;
+                const float* lse = a.lse + ((size_t)sg.s * a.wk.B + t0) * a.H + sg.hk * a.g;
+                float x[4];
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const int r = 32 * w + lane, token = r / a.g;
+                    x[w] = r < rows ? lse[(size_t)token * a.H + (r - token * a.g)] : -INFINITY;
+                }
+                ok = all(wait_for(hd, &hd->lse_empty[qs.at], qs.phase ^ 1, a.status));
+                if (!ok) break;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const uint32_t word = __ballot_sync(0xFFFFFFFFu, x[w] != -INFINITY);   // (NaN counts)
+                    hd->lse[qs.at][32 * w + lane] = -kLog2e * x[w];
+                    if (lane == 0) hd->counts[qs.at][w] = word;
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&hd->lse_full[qs.at]);
+                qs.next(kQStages);
+            }
+        }
+    } else {
+        // =============================================================== exponentials and sums
+        const int l = (warp - 4) >> 2, wq = warp & 3;        // key tiles l and l + 2 of a run
+        const int row = 32 * wq + lane;                      // TMEM lane == key of a tile
+        const uint32_t s_addr = tmem + ((uint32_t)(32 * wq) << 16);
+        uint32_t used = 0;                                   // a bit a score buffer: its parity
+        Ring qs{0, 0}, ring{0, 0};
+        bool ok = true;
+        while (ok) {
+            ok = all(wait_for(hd, &hd->seg_full[ring.at], ring.phase, a.status));
+            if (!ok) break;
+            const Segment& sg = hd->seg[ring.at];
+            if (sg.n == 0) break;
+            // what the rows have, and whether they can be read at all
+            float sum[2] = {0.f, 0.f}, old[2] = {0.f, 0.f};
+            bool there[2] = {false, false};
+            float* weight = a.row_weight + ((size_t)sg.s * a.wk.Hkv + sg.hk) * a.ldw + sg.key0 + row;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int u = l + 2 * e, j = sg.key0 + u * kWeightTile + row;
+                if (u < sg.run && j < sg.ctx + sg.nn) {
+                    const int page = a.pages.table[sg.s * a.pages.ldt + (j >> a.pages.size_log2)];
+                    there[e] = page >= 0 && page < a.pages.n;
+                    if (!there[e]) atomicOr(&a.status[sg.s], GOOSE_ST_BAD_ROWS);
+                    if (sg.whole) old[e] = weight[u * kWeightTile];
+                }
+            }
+            for (int i = 0; i < sg.n; ++i) {
+                ok = all(wait_for(hd, &hd->lse_full[qs.at], qs.phase, a.status));
+                if (!ok) break;
+                const int t0 = (sg.q_first + i) * a.wk.t, rows = min(sg.nn - t0, a.wk.t) * a.g;
+                const uint4 counts = *reinterpret_cast<const uint4*>(hd->counts[qs.at]);
+                const bool every = (counts.x & counts.y & counts.z & counts.w) == 0xFFFFFFFFu;
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int u = l + 2 * e;
+                    if (u >= sg.run) break;
+                    ok = all(wait_for(hd, &hd->s_full[u], used >> u & 1, a.status));
+                    if (!ok) break;
+                    used ^= 1u << u;
+                    tc_fence_after();
+                    const int tile0 = sg.key0 + u * kWeightTile;
+                    const int behind = tile0 + row - sg.ctx - t0;    // tokens of the Q tile in front of the first that sees the key
+                    const bool masked = !every || tile0 + kWeightTile - 1 - sg.ctx > t0;
+                    uint32_t cw[4] = {counts.x, counts.y, counts.z, counts.w};
+                    if (masked) {
+                        const int from = max(behind, 0) * a.g;       // columns in front of it do not count
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) cw[w] &= from <= 32 * w ? 0xFFFFFFFFu : from >= 32 * w + 32 ? 0u : 0xFFFFFFFFu << (from - 32 * w);
+                    }
+                    const unsigned long long scale2 = pack_f32x2(a.scale_log2, a.scale_log2);
+                    unsigned long long part[2] = {0, 0};
+                    uint32_t v[32];
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        if (32 * w >= rows) break;
+                        TMEM_LD32(s_addr + u * 128 + 32 * w, v, 0);
+                        tmem_wait_ld();
+                        const ulonglong2* nl = reinterpret_cast<const ulonglong2*>(&hd->lse[qs.at][32 * w]);
+#pragma unroll
+                        for (int c = 0; c < 32; c += 4) {
+                            const ulonglong2 n4 = nl[c / 4];
+                            const float2 x = unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(v[c]), __uint_as_float(v[c + 1])), scale2, n4.x));
+                            const float2 y = unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(v[c + 2]), __uint_as_float(v[c + 3])), scale2, n4.y));
+                            float p0 = ex2(x.x), p1 = ex2(x.y), p2 = ex2(y.x), p3 = ex2(y.y);
+                            if (masked) {
+                                p0 = cw[w] >> c & 1 ? p0 : 0.f; p1 = cw[w] >> (c + 1) & 1 ? p1 : 0.f;
+                                p2 = cw[w] >> (c + 2) & 1 ? p2 : 0.f; p3 = cw[w] >> (c + 3) & 1 ? p3 : 0.f;
+                            }
+                            part[0] = add_f32x2(part[0], pack_f32x2(p0, p1));
+                            part[1] = add_f32x2(part[1], pack_f32x2(p2, p3));
+                        }
+                    }
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&hd->s_free[u]);
+                    const float2 s2 = unpack_f32x2(add_f32x2(part[0], part[1]));
+                    sum[e] += s2.x + s2.y;
+                }
+                if (!ok) break;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&hd->lse_empty[qs.at]);
+                qs.next(kQStages);
+            }
+            if (!ok) break;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int u = l + 2 * e;
+                if (u >= sg.run) break;
+                if (sg.whole) {
+                    if (there[e]) weight[u * kWeightTile] = old[e] + sum[e];
+                    continue;
+                }
+                a.sums[((size_t)sg.slot * kRun + u) * kWeightTile + row] = sum[e];
+                __threadfence();
+                __syncwarp();
+                int32_t* counter = a.counters + (sg.c0 * kRun + u) * 4 + wq;
+                int last = 0;
+                if (lane == 0) last = atomicAdd(counter, 1) == sg.parts - 1;
+                if (!__shfl_sync(0xFFFFFFFFu, last, 0)) continue;
+                __threadfence();
+                if (lane == 0) *counter = 0;
+                float total = 0.f;
+                for (int k = 0; k < sg.parts; ++k)
+                    total += __ldcg(&a.sums[((size_t)(2 * (sg.c0 + k) + (k == 0)) * kRun + u) * kWeightTile + row]);
+                if (there[e]) weight[u * kWeightTile] += total;
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&hd->seg_empty[ring.at]);
+            ring.next(kSegments);
+        }
+    }
+
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
     }
 }
 
-cudaError_t launch_kv_weights(goose_ctx* c, const KvWeights& a, cudaStream_t st) {
-    if (a.S == 0) return cudaSuccess;
-    const int64_t room = a.pages.room(a.ldw), per = kWeightThreads / 32;
-    const dim3 grid((unsigned)((room + per - 1) / per < 1024 ? (room + per - 1) / per : 1024), a.Hkv, a.S);
-    cudaError_t e = launch_pdl(kv_weights_kernel, grid, dim3(kWeightThreads), 0, st, a, c->status);
+}  // namespace
+
+cudaError_t launch_kv_weights(goose_ctx* c, const KvWeights& x, cudaStream_t st) {
+    if (!c->encode_tiled) return cudaErrorNotSupported;
+    if (x.S == 0) return cudaSuccess;
+    WeightArgs a{};
+    a.g = x.H / x.Hkv; a.H = x.H;
+    a.wk.ctx_len = x.ctx_len; a.wk.n_new = x.n_new; a.wk.S = x.S; a.wk.B = x.B; a.wk.Hkv = x.Hkv; a.wk.G = c->num_sms;
+    a.wk.t = kWeightTile / a.g; a.wk.room = (int)x.pages.room(x.ldw); a.wk.short_run = 1;
+    a.pages = x.pages;
+    a.nb = a.wk.t < x.B ? a.wk.t : x.B;
+    a.box_log2 = x.pages.size_log2 < 7 ? x.pages.size_log2 : 7;
+    a.scale_log2 = x.scale * kLog2e;
+    a.lse = x.lse; a.row_weight = x.row_weight; a.ldw = x.ldw;
+    a.sums = c->weight_sums; a.counters = c->weight_counters; a.status = c->status;
+    CUtensorMap mq, mk;
+    if (!make_q_map(c->encode_tiled, &mq, x.q, (int64_t)x.S * x.B, x.Hkv, a.g, a.nb) ||
+        !make_map(c->encode_tiled, &mk, x.k_cache, (int64_t)x.pages.n << x.pages.size_log2, x.Hkv, 1 << a.box_log2))
+        return cudaErrorInvalidValue;
+    cudaError_t e = launch_pdl(kv_weights_kernel, dim3(c->num_sms), dim3(kWeightThreads), kWeightSmem, st, mq, mk, a);
     c->launches++;
     return e;
 }
 
-cudaError_t init_weights_kernels() { return load_kernels({(const void*)kv_weights_kernel}); }
+cudaError_t init_weights_kernels() { return cudaFuncSetAttribute(kv_weights_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kWeightSmem); }
 
 }  // namespace goose

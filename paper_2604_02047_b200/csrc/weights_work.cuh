@@ -1,0 +1,120 @@
+// Work partition of goose_kv_weights.  It compiles for the host too, where a test walks it.
+//
+// The work list is a row of items, sequence by sequence, key/value head by head: each a run of up to four 128-key tiles with all Q tiles (t tokens with
+// the heads of a group, 128 query rows) that see any of its keys.  The list is laid out in places, as many as an item costs, and dealt to the CTAs in
+// ranges of equal length: a Q tile is of the range that its first place is in.  What a CTA does of an item is a segment.
+#pragma once
+
+#include "goose_internal.cuh"
+
+namespace goose {
+
+constexpr int kWeightTile = 128;                 // keys of a tile, rows of a Q tile
+constexpr int kRun = 4;                          // key tiles of an item, at most
+
+struct WeightSeq {            // a sequence's part of the list
+    int n, ctx, t, run;       // new tokens, rows in front of them, tokens of a Q tile, key tiles of an item
+    int items;                // of a key/value head
+    int change;               // places of the change to an item
+    bool bad;                 // its rows do not fit: nothing of it is done
+    __host__ __device__ __forceinline__ int span() const { return run * kWeightTile; }
+    // first token that sees item k
+    __host__ __device__ __forceinline__ int token(int k) const { const int i = k * span() - ctx; return i > 0 ? i : 0; }
+    __host__ __device__ __forceinline__ int first(int k) const { return token(k) / t; }               // Q tile of it
+    __host__ __device__ __forceinline__ int tiles(int k) const { return (n + t - 1) / t - first(k); }   // Q tiles of the item
+    __host__ __device__ __forceinline__ long long width(int k) const { return change + (long long)run * ((long long)n + t - token(k)); }
+    __host__ __device__ __forceinline__ long long before(int k) const {
+        long long w = k * (change + (long long)run * ((long long)n + t));
+        const int whole = (ctx + span() - 1) / span();       // items from here on begin behind the prefix
+        if (k > whole) {
+            const long long a = k, b = whole;
+            w -= run * (span() * ((a * (a - 1) - b * (b - 1)) / 2) - (long long)ctx * (a - b));
+        }
+        return w;
+    }
+    // of T Q tiles of an item that begins at place w0, those whose first place is in front of place w
+    __host__ __device__ __forceinline__ int cut(long long w0, int T, long long w) const {
+        const long long x = w - w0 - change;
+        if (x <= 0) return 0;
+        const long long pitch = (long long)run * t, all = T * pitch;
+        return x >= all ? T : (int)((x + pitch - 1) / pitch);
+    }
+};
+
+struct WeightWork {
+    const int32_t *ctx_len, *n_new;
+    int S, B, Hkv, G;         // G: CTAs
+    int t;                    // tokens of a Q tile
+    int room;                 // rows that a sequence may have
+    // worked out
+    int short_run;            // key tiles of an item of a sequence that has one Q tile
+    long long total, quantum;
+
+    __host__ __device__ __forceinline__ WeightSeq seq(int s) const {
+        WeightSeq q;
+        q.n = nodes_of(n_new, s, B);
+        q.ctx = ctx_len[s];
+        q.bad = q.n > 0 && rows_outside(0, q.ctx, q.n, room);
+        if (q.bad) q.n = 0;
+        if (q.n == 0) q.ctx = 0;
+        q.t = t;
+        q.run = q.n > t ? kRun : short_run;
+        q.items = q.n > 0 ? (q.ctx + q.n + q.span() - 1) / q.span() : 0;
+        q.change = q.n > t ? kRun * t : 0;
+        return q;
+    }
+    // key tiles of a head of the sequences that have one Q tile: with few of them an item is a tile, so that more CTAs have one
+    __host__ __device__ __forceinline__ void set_run(long long tiles) {
+        tiles *= Hkv;
+        short_run = tiles <= 2 * G ? 1 : tiles <= 8 * G ? 2 : kRun;
+    }
+    // sum: places of one key/value head of all sequences;  several: there is one of several Q tiles
+    __host__ __device__ __forceinline__ void set(long long sum, bool several) {
+        total = Hkv * sum;
+        quantum = total > 0 ? (total + G - 1) / G : 1;
+        // every CTA between an item's first and its last one has a Q tile of it
+        if (several && quantum < kRun * t) quantum = kRun * t;
+    }
+    static __host__ __device__ __forceinline__ long long divide(long long a, long long b) {   // 64-bit division is slow on the GPU
+        return (a | b) >> 32 ? a / b : (long long)((uint32_t)a / (uint32_t)b);
+    }
+    __host__ __device__ __forceinline__ long long start(int c) const { const long long w = c * quantum; return w < total ? w : total; }
+};
+
+// where a CTA is in the list: item k of head hk of sequence s, which begins at place w0
+struct WeightCursor {
+    int s, hk, k;
+    long long w0;
+    // the segment there of a CTA whose range is [from, to): Q tiles t0 .. t1 - 1 of T; c0, c1: the first and the last CTA that have Q tiles of the item
+    int t0, t1, T, c0, c1;
+    __host__ __device__ __forceinline__ void look(const WeightWork& wk, const WeightSeq& q, long long from, long long to) {
+        T = q.tiles(k);
+        t0 = q.cut(w0, T, from);
+        t1 = q.cut(w0, T, to);
+        const long long first = w0 + q.change;
+        c0 = (int)WeightWork::divide(first, wk.quantum);
+        c1 = (int)WeightWork::divide(first + (long long)(T - 1) * q.run * q.t, wk.quantum);
+    }
+    // the next item; false: the sequence has no more
+    __host__ __device__ __forceinline__ bool next(const WeightWork& wk, const WeightSeq& q) {
+        w0 += q.width(k);
+        if (++k < q.items) return true;
+        k = 0;
+        return ++hk < wk.Hkv;
+    }
+    // to the item of the sequence that begins at place `begin` which has place w
+    __host__ __device__ __forceinline__ void enter(const WeightSeq& q, long long begin, long long w) {
+        const long long of_head = q.before(q.items);
+        hk = (int)WeightWork::divide(w - begin, of_head);
+        const long long rem = w - begin - hk * of_head;
+        int lo = 0, hi = q.items;                // the last item that begins at rem or in front of it
+        while (hi - lo > 1) {
+            const int mid = lo + (hi - lo) / 2;
+            if (q.before(mid) <= rem) lo = mid; else hi = mid;
+        }
+        k = lo;
+        w0 = begin + hk * of_head + q.before(k);
+    }
+};
+
+}  // namespace goose
