@@ -373,8 +373,8 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
             // =========================================================== TMA producer (the warp runs converged)
             const bool leader = elect_leader();
             const unsigned long long pol_once = l2_policy_evict_first(), pol_again = l2_policy_evict_last();
-            const uint32_t kv_addr = smem_u32(kv_smem);
-            const int boxes = kChunkTile >> a.box_log2, outside = a.pages.n << a.pages.size_log2;
+            // a lane's box of a tile: its rows, and which half of the head's elements
+            const int boxes = kChunkTile >> a.box_log2, box = lane & (boxes - 1), half = lane >> (7 - a.box_log2), outside = a.pages.n << a.pages.size_log2;
             uint32_t pairs = 0, singles = 0, tile0 = 0;      // segments of either kind, tiles in front of this segment
             uint32_t phases = 0, users = 0;                  // a bit a kv_full barrier; two bits a stage: who has it, 3: nobody yet
             for (int i = 0; i < kStages; ++i) users |= 3u << 2 * i;
@@ -411,8 +411,8 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
             };
             // the cache row of this lane's box of tile t: no page behind the sequence's last row is looked up
             auto box_row = [&](int t) {
-                const int j = (t << 7) + (lane << a.box_log2), page = j >> a.pages.size_log2;
-                if (lane >= boxes || j >= sg.n_keys || page >= a.pages.ldt) return outside;
+                const int j = (t << 7) + (box << a.box_log2), page = j >> a.pages.size_log2;
+                if (lane >= 2 * boxes || j >= sg.n_keys || page >= a.pages.ldt) return outside;
                 const int at = a.pages.table[sg.s * a.pages.ldt + page];
                 return at < 0 || at >= a.pages.n ? outside : (at << a.pages.size_log2) + (j & ((1 << a.pages.size_log2) - 1));
             };
@@ -439,17 +439,14 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                     for (int kv = 0; kv < 2 && ok; ++kv) {
                         ok = stage_free();
                         if (!ok) break;
-                        const uint32_t dst = kv_addr + st.at * kStageBytes;
                         unsigned long long* full = &hd->kv_full[user][st.at];
                         if (leader) mbar_expect_tx(full, kStageBytes);
                         __syncwarp();
                         const CUtensorMap* mp = kv ? &tmap_v : &tmap_k;
-                        for (int b = 0; b < boxes; ++b) {
-                            const int from = __shfl_sync(0xFFFFFFFFu, row, b);
-                            const uint32_t to = dst + ((uint32_t)b << (a.box_log2 + 7));
-                            tma_load_3d_hint_by(leader, to, mp, full, 0, sg.hk, from, pol);
-                            tma_load_3d_hint_by(leader, to + kHalfBytes, mp, full, 64, sg.hk, from, pol);
-                        }
+                        // a box a lane: one instruction of the warp issues them all
+                        if (lane < 2 * boxes)
+                            tma_load_3d_hint(kv_smem + st.at * kStageBytes + half * kHalfBytes + (box << (a.box_log2 + 7)), mp, full, 64 * half, sg.hk, row, pol);
+                        __syncwarp();
                         phases ^= 1u << (user * kStages + st.at);
                         users = (users & ~(3u << 2 * st.at)) | user << 2 * st.at;
                         st.next(kStages);

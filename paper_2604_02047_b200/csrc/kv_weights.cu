@@ -27,7 +27,7 @@ constexpr int kTileBytes = kWeightTile * kHeadDim * 2;       // 32 KB: one K or 
 constexpr int kHalfBytes = kWeightTile * 128;                // 16 KB: 128 rows x 64 bf16 (one swizzle-atom column)
 constexpr int kHeaderBytes = 2048;
 constexpr int kWeightSmem = 1008 /*alignment slack*/ + (kStages + kQStages) * kTileBytes + kHeaderBytes;
-constexpr int kWeightThreads = 384;
+constexpr int kWeightThreads = 512;
 constexpr uint32_t kTmemCols = 512;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr long long kWaitCycles = 2000000000ll;              // bound of every wait: about one second of SM clock
@@ -57,7 +57,8 @@ static_assert(kWeightSmem <= 232448, "shared memory of a block");
 struct WeightArgs {
     WeightWork wk;
     Pages pages;
-    int g, H, nb, box_log2;                                  // heads of a group, heads, tokens of a box of queries, rows of a box of keys
+    const __nv_bfloat16* k_cache;
+    int g, H, nb;                                            // heads of a group, heads, tokens of a box of queries
     float scale_log2;
     const float* lse;
     float* row_weight;
@@ -144,7 +145,7 @@ __device__ __forceinline__ bool locate(WeightWork& wk, WeightCursor& cu, WeightS
 __device__ __forceinline__ uint32_t scores_desc(int n) { return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((128u >> 4) << 24); }
 
 __global__ void __launch_bounds__(kWeightThreads, 1)
-kv_weights_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ WeightArgs a) {
+kv_weights_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ WeightArgs a) {
     extern __shared__ unsigned char smem_raw[];
     unsigned char* k_smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     unsigned char* q_smem = k_smem + kStages * kTileBytes;
@@ -152,13 +153,13 @@ kv_weights_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
     const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
 
     if (threadIdx.x == 0) {
-        for (int i = 0; i < kStages; ++i) { mbar_init(&hd->k_full[i], 1); mbar_init(&hd->k_empty[i], 1); }
+        for (int i = 0; i < kStages; ++i) { mbar_init(&hd->k_full[i], 4 * 32); mbar_init(&hd->k_empty[i], 1); }
         for (int i = 0; i < kQStages; ++i) { mbar_init(&hd->q_full[i], 1); mbar_init(&hd->q_empty[i], 1); mbar_init(&hd->lse_full[i], 1); mbar_init(&hd->lse_empty[i], 8); }
-        for (int i = 0; i < kSegments; ++i) { mbar_init(&hd->seg_full[i], 1); mbar_init(&hd->seg_empty[i], 3 + 8); }
+        for (int i = 0; i < kSegments; ++i) { mbar_init(&hd->seg_full[i], 1); mbar_init(&hd->seg_empty[i], 3 + 8 + 4); }
         for (int u = 0; u < kRun; ++u) { mbar_init(&hd->s_full[u], 1); mbar_init(&hd->s_free[u], 4); }
         hd->abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        prefetch_tmap(&tmap_q); prefetch_tmap(&tmap_k);
+        prefetch_tmap(&tmap_q);
     }
     if (warp == 1) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&hd->tmem_base)), "r"(kTmemCols) : "memory");
@@ -220,13 +221,10 @@ kv_weights_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
             advance();
         }
     } else if (warp == 0) {
-        // =============================================================== TMA producer (the warp runs converged)
+        // =============================================================== Q tiles (the warp runs converged)
         const bool leader = elect_leader();
-        const unsigned long long pol_once = l2_policy_evict_first(), pol_again = l2_policy_evict_last();
-        const uint32_t k_addr = smem_u32(k_smem);
-        const int boxes = kWeightTile >> a.box_log2, outside = a.pages.n << a.pages.size_log2;
-        uint32_t k_loads = 0, q_loads = 0;
-        Ring ks{0, 0}, qs{0, 0}, ring{0, 0};
+        uint32_t loads = 0;
+        Ring qs{0, 0}, ring{0, 0};
         bool ok = true;
         while (ok) {
             ok = all(wait_for(hd, &hd->seg_full[ring.at], ring.phase, a.status));
@@ -236,18 +234,7 @@ kv_weights_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
             if (leader) mbar_arrive(&hd->seg_empty[ring.at]);
             ring.next(kSegments);
             if (sg.n == 0) break;
-            // the cache row of this lane's box of a key tile: no page behind the sequence's last row is looked up
-            auto box_row = [&](int u) {
-                const int j = sg.key0 + u * kWeightTile + (lane << a.box_log2);
-                if (lane >= boxes || u >= sg.run || j >= sg.ctx + sg.nn) return outside;
-                const int at = a.pages.table[sg.s * a.pages.ldt + (j >> a.pages.size_log2)];
-                return at < 0 || at >= a.pages.n ? outside : (at << a.pages.size_log2) + (j & ((1 << a.pages.size_log2) - 1));
-            };
-            int rows[kRun];
-#pragma unroll
-            for (int u = 0; u < kRun; ++u) rows[u] = box_row(u);
-            const unsigned long long pol = sg.nn > a.wk.t ? pol_again : pol_once;
-            for (int i = 0; i < sg.n && ok; ++i) {
+            for (int i = 0; i < sg.n; ++i) {
                 ok = all(wait_for(hd, &hd->q_empty[qs.at], qs.phase ^ 1, a.status));
                 if (!ok) break;
                 if (leader) {
@@ -257,37 +244,74 @@ kv_weights_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                     tma_load_4d(q_smem + qs.at * kTileBytes + kHalfBytes, &tmap_q, &hd->q_full[qs.at], 64, 0, sg.hk, token);
                 }
                 __syncwarp();
-                ++q_loads;
+                ++loads;
                 qs.next(kQStages);
-                if (i > 0) continue;
-#pragma unroll
-                for (int u = 0; u < kRun; ++u) {
-                    if (u >= sg.run || !ok) break;
-                    ok = all(wait_for(hd, &hd->k_empty[ks.at], ks.phase ^ 1, a.status));
-                    if (!ok) break;
-                    if (leader) mbar_expect_tx(&hd->k_full[ks.at], kTileBytes);
-                    __syncwarp();
-                    const uint32_t dst = k_addr + ks.at * kTileBytes;
-                    for (int b = 0; b < boxes; ++b) {
-                        const int row = __shfl_sync(0xFFFFFFFFu, rows[u], b);
-                        const uint32_t to = dst + ((uint32_t)b << (a.box_log2 + 7));
-                        tma_load_3d_hint_by(leader, to, &tmap_k, &hd->k_full[ks.at], 0, sg.hk, row, pol);
-                        tma_load_3d_hint_by(leader, to + kHalfBytes, &tmap_k, &hd->k_full[ks.at], 64, sg.hk, row, pol);
-                    }
-                    ++k_loads;
-                    ks.next(kStages);
-                }
             }
         }
         // the products' arrivals have landed, too, before the CTA ends
-        for (int i = 0; i < kStages && ok; ++i, ks.next(kStages)) ok = all(wait_for(hd, &hd->k_empty[ks.at], ks.phase ^ 1, a.status));
         for (int i = 0; i < kQStages && ok; ++i, qs.next(kQStages)) ok = all(wait_for(hd, &hd->q_empty[qs.at], qs.phase ^ 1, a.status));
-        if (!ok) {                                           // copies still in flight land before the CTA ends
-            for (uint32_t i = 0; i < kStages; ++i)
-                if (k_loads > i) drain(&hd->k_full[i], ((k_loads - 1 - i) / kStages) & 1);
+        if (!ok)                                             // copies still in flight land before the CTA ends
             for (uint32_t i = 0; i < kQStages; ++i)
-                if (q_loads > i) drain(&hd->q_full[i], ((q_loads - 1 - i) / kQStages) & 1);
+                if (loads > i) drain(&hd->q_full[i], ((loads - 1 - i) / kQStages) & 1);
+    } else if (warp >= 12) {
+        // =============================================================== K tiles: 32 keys of a tile a warp
+        const int part = warp - 12;
+        const uint32_t k_addr = smem_u32(k_smem) + 4096 * part;
+        const unsigned long long pol_once = l2_policy_evict_first(), pol_again = l2_policy_evict_last();
+        // 16 bytes of a row a lane, two rows at a time; where they go in a tile of swizzled rows, for each of four such pairs of rows
+        const size_t row_bytes = (size_t)a.wk.Hkv * kHeadDim * 2;
+        uint32_t place[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = 2 * i + (lane >> 4);
+            place[i] = (lane >> 3 & 1) * kHalfBytes + r * 128 + (((lane & 7) ^ r) << 4);
         }
+        Ring ks{0, 0}, ring{0, 0};
+        bool ok = true;
+        Segment next{};
+        int next_row = -1;
+        // The next segment, and the cache rows where 16 of its keys lie (a page has as many at least), lane 2 u + q: the q-th of this warp's in tile u; -1 where
+        // there are none.  No page behind the sequence's last row is looked up.
+        auto take = [&]() {
+            ok = all(wait_for(hd, &hd->seg_full[ring.at], ring.phase, a.status));
+            if (!ok) return;
+            next = hd->seg[ring.at];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&hd->seg_empty[ring.at]);
+            ring.next(kSegments);
+            const int u = lane >> 1, j = next.key0 + u * kWeightTile + 32 * part + 16 * (lane & 1);
+            next_row = -1;
+            if (next.n > 0 && u < next.run && j < next.ctx + next.nn) next_row = (int)a.pages.row(next.s, j);
+        };
+        take();
+        while (ok && next.n > 0) {
+            const Segment sg = next;
+            const int rows = next_row;
+            // the one behind it now, if the planner has it, so that its look-ups run beside these copies
+            const bool early = all(mbar_try_wait(&hd->seg_full[ring.at], ring.phase));
+            if (early) take();
+            const unsigned long long pol = sg.nn > a.wk.t ? pol_again : pol_once;
+            const char* from0 = reinterpret_cast<const char*>(a.k_cache) + (size_t)sg.hk * kHeadDim * 2 + (lane >> 4) * row_bytes + (lane & 15) * 16;
+            for (int u = 0; u < sg.run && ok; ++u) {
+                ok = all(wait_for(hd, &hd->k_empty[ks.at], ks.phase ^ 1, a.status));
+                if (!ok) break;
+                const uint32_t dst = k_addr + ks.at * kTileBytes;
+                const int keys = sg.ctx + sg.nn - sg.key0 - u * kWeightTile - 32 * part - (lane >> 4);
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    const int row = __shfl_sync(0xFFFFFFFFu, rows, 2 * u + q);
+                    const char* from = from0 + (size_t)max(row, 0) * row_bytes;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        cp_async_16(dst + 2048 * q + 1024 * (i >> 2) + place[i & 3], from + 2 * i * row_bytes, row >= 0 && 16 * q + 2 * i < keys, pol);
+                }
+                cp_async_arrive(&hd->k_full[ks.at]);
+                ks.next(kStages);
+            }
+            if (ok && !early) take();
+        }
+        for (int i = 0; i < kStages && ok; ++i, ks.next(kStages)) ok = all(wait_for(hd, &hd->k_empty[ks.at], ks.phase ^ 1, a.status));
+        if (!ok) cp_async_wait_all();
     } else if (warp == 1) {
         // =============================================================== MMA issuer
         const bool leader = elect_leader();                  // the warp runs converged, this lane acts
@@ -316,6 +340,7 @@ kv_weights_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                     if (i == 0 && !(ok = wait_for(hd, &hd->k_full[at], load / kStages & 1, a.status))) break;
                     if (!(ok = wait_for(hd, &hd->s_free[u], (used >> u & 1) ^ 1, a.status))) break;
                     used ^= 1u << u;
+                    fence_proxy_async();                     // (the copies of the keys)
                     tc_fence_after();
                     const uint32_t k_lo = smem_desc_lo(k_addr + at * kTileBytes, 16);
 #pragma unroll
@@ -379,19 +404,15 @@ kv_weights_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
             if (!ok) break;
             const Segment& sg = hd->seg[ring.at];
             if (sg.n == 0) break;
-            // what the rows have, and whether they can be read at all
-            float sum[2] = {0.f, 0.f}, old[2] = {0.f, 0.f};
-            bool there[2] = {false, false};
+            float sum[2] = {0.f, 0.f};
+            int page[2] = {-1, -1};                          // of the rows, looked at when the sums are there
+            bool mine[2] = {false, false};
             float* weight = a.row_weight + ((size_t)sg.s * a.wk.Hkv + sg.hk) * a.ldw + sg.key0 + row;
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const int u = l + 2 * e, j = sg.key0 + u * kWeightTile + row;
-                if (u < sg.run && j < sg.ctx + sg.nn) {
-                    const int page = a.pages.table[sg.s * a.pages.ldt + (j >> a.pages.size_log2)];
-                    there[e] = page >= 0 && page < a.pages.n;
-                    if (!there[e]) atomicOr(&a.status[sg.s], GOOSE_ST_BAD_ROWS);
-                    if (sg.whole) old[e] = weight[u * kWeightTile];
-                }
+                mine[e] = u < sg.run && j < sg.ctx + sg.nn;
+                if (mine[e]) page[e] = a.pages.table[sg.s * a.pages.ldt + (j >> a.pages.size_log2)];
             }
             for (int i = 0; i < sg.n; ++i) {
                 ok = all(wait_for(hd, &hd->lse_full[qs.at], qs.phase, a.status));
@@ -455,8 +476,11 @@ kv_weights_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
             for (int e = 0; e < 2; ++e) {
                 const int u = l + 2 * e;
                 if (u >= sg.run) break;
+                const bool there = page[e] >= 0 && page[e] < a.pages.n;
+                if (mine[e] && !there) atomicOr(&a.status[sg.s], GOOSE_ST_BAD_ROWS);
+                // (a reduction: nobody waits for what the row had.  One a row and call: the order of the calls is the order of the sums)
                 if (sg.whole) {
-                    if (there[e]) weight[u * kWeightTile] = old[e] + sum[e];
+                    if (there) atomicAdd(weight + u * kWeightTile, sum[e]);
                     continue;
                 }
                 a.sums[((size_t)sg.slot * kRun + u) * kWeightTile + row] = sum[e];
@@ -471,7 +495,7 @@ kv_weights_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                 float total = 0.f;
                 for (int k = 0; k < sg.parts; ++k)
                     total += __ldcg(&a.sums[((size_t)(2 * (sg.c0 + k) + (k == 0)) * kRun + u) * kWeightTile + row]);
-                if (there[e]) weight[u * kWeightTile] += total;
+                if (there) atomicAdd(weight + u * kWeightTile, total);
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(&hd->seg_empty[ring.at]);
@@ -499,15 +523,13 @@ cudaError_t launch_kv_weights(goose_ctx* c, const KvWeights& x, cudaStream_t st)
     a.wk.t = kWeightTile / a.g; a.wk.room = (int)x.pages.room(x.ldw); a.wk.short_run = 1;
     a.pages = x.pages;
     a.nb = a.wk.t < x.B ? a.wk.t : x.B;
-    a.box_log2 = x.pages.size_log2 < 7 ? x.pages.size_log2 : 7;
+    a.k_cache = x.k_cache;
     a.scale_log2 = x.scale * kLog2e;
     a.lse = x.lse; a.row_weight = x.row_weight; a.ldw = x.ldw;
     a.sums = c->weight_sums; a.counters = c->weight_counters; a.status = c->status;
-    CUtensorMap mq, mk;
-    if (!make_q_map(c->encode_tiled, &mq, x.q, (int64_t)x.S * x.B, x.Hkv, a.g, a.nb) ||
-        !make_map(c->encode_tiled, &mk, x.k_cache, (int64_t)x.pages.n << x.pages.size_log2, x.Hkv, 1 << a.box_log2))
-        return cudaErrorInvalidValue;
-    cudaError_t e = launch_pdl(kv_weights_kernel, dim3(c->num_sms), dim3(kWeightThreads), kWeightSmem, st, mq, mk, a);
+    CUtensorMap mq;
+    if (!make_q_map(c->encode_tiled, &mq, x.q, (int64_t)x.S * x.B, x.Hkv, a.g, a.nb)) return cudaErrorInvalidValue;
+    cudaError_t e = launch_pdl(kv_weights_kernel, dim3(c->num_sms), dim3(kWeightThreads), kWeightSmem, st, mq, a);
     c->launches++;
     return e;
 }

@@ -48,6 +48,17 @@ __device__ __forceinline__ void tma_load_3d_hint_by(bool leader, uint32_t dst, c
                  "[%0], [%1, {%3, %4, %5}], [%2], %6;\n\t}"
                  ::"r"(dst), "l"(map), "r"(smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2), "l"(policy), "r"((uint32_t)leader) : "memory");
 }
+// 16 bytes into shared memory by the generic proxy: what the tensor cores read of it is behind an arrival of cp_async_arrive() and a fence_proxy_async()
+// of the thread that issues the product.  there == false: zeros, and nothing is read
+__device__ __forceinline__ void cp_async_16(uint32_t dst, const void* src, bool there, unsigned long long policy) {
+    asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2, %3;"
+                 ::"r"(dst), "l"(src), "r"(there ? 16 : 0), "l"(policy) : "memory");
+}
+// an arrival when all this thread's copies have landed
+__device__ __forceinline__ void cp_async_arrive(unsigned long long* bar) {
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void cp_async_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 // brings a box of a tensor map into L2: a hint; nothing reaches the SM, and a box outside the tensor touches nothing
 __device__ __forceinline__ void tma_prefetch_3d(const CUtensorMap* map, int c0, int c1, int c2) {
     asm volatile("cp.async.bulk.prefetch.tensor.3d.L2.global [%0, {%1, %2, %3}];" ::"l"(map), "r"(c0), "r"(c1), "r"(c2) : "memory");
