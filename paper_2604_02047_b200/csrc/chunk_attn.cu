@@ -6,9 +6,9 @@
 // a softmax warpgroup and accumulators each: the two M tiles of a pair over the same key tiles, or, with a single M tile, every other key tile.
 // Roles (384 threads), barriers and waits are those of the shared-prefix attention (tree_attn_shared.cu):
 //   warp 0            TMA producer: the queries of a segment, then K and V tiles, a box a page, into a ring of 32 KB stages.  Its lanes look the
-//                     pages up, a tile ahead; rows behind the last one are a box outside the cache, which arrives as zeros
+//                     pages up, a tile ahead; rows behind the last page are a box outside the cache, which arrives as zeros
 //   warps 1, 3        MMA issuers of lane 0 and of lane 1: S = Q K^T, O += P V
-//   warp 2            planner: walks the work list and puts the segments' descriptions into a ring; the segments' pages are checked here
+//   warp 2            planner: walks the work list and puts the segments' descriptions into a ring; checks the segments' pages behind that
 //   warps 4..7, 8..11 softmax of lane 0 and of lane 1: one query row a thread; at the segment's end the results.  The lanes of a single M tile are
 //                     joined through tensor memory.  An item that is the CTA's alone is written out; of any other the CTA leaves a partial result,
 //                     and the warp that completes a count joins the 32 rows of all CTAs, in the order of the keys whoever comes last.
@@ -67,7 +67,7 @@ struct Segment {
     int rows[2];                                             // query rows of the M tiles
     int c0, parts;                                           // CTAs that have a part of the item: the first, how many
     int again;                                               // the rows are read for other items too
-    int bad;
+    int bad;                                                 // when it has been checked
     int pad;
 };
 constexpr int kSegments = 6;
@@ -79,7 +79,7 @@ struct Header {
     // for a phase of a barrier whose phases it has not all followed, and a lane does not follow the tiles of the other one.
     unsigned long long kv_full[3][kStages];
     unsigned long long kv_empty[kStages];
-    unsigned long long seg_full[kSegments], seg_empty[kSegments];
+    unsigned long long seg_full[kSegments], seg_empty[kSegments], seg_checked[kSegments];
     // The two places of query tiles.  A pair has both, each lane its own; single M tiles have them in turn.
     unsigned long long pair_full[2], pair_empty[2], single_full[2], single_empty[2];
     unsigned long long s_full[2], v_there[2], o_full[2], o_free[2];
@@ -91,12 +91,14 @@ struct Header {
 static_assert(sizeof(Header) <= kHeaderBytes, "header");
 static_assert(kChunkSmem <= 232448, "shared memory of a block");
 
+template <typename Int>
 struct ChunkArgs {
-    ChunkWork wk;
+    ChunkWork<Int> wk;
     Pages pages;
     int g, H;                                                // query heads per key/value head, query heads
     int nb;                                                  // tokens of a box of queries
     int box_log2;                                            // rows of a box of keys
+    int wide;                                                // out is aligned for 32-byte stores
     float scale_log2;
     uint4* parts;
     int32_t* counters;                                       // [CTA][M tile][warp], zero between launches
@@ -132,37 +134,39 @@ struct Ring {
     }
 };
 
-__device__ __forceinline__ long long warp_sum(long long v) {
+template <typename Int>
+__device__ __forceinline__ Int warp_sum(Int v) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
     return v;
 }
 
 // the list's length and a place in it, by a whole warp (lane = sequence); false: the CTA has no range
-__device__ __forceinline__ bool locate(ChunkWork& wk, ChunkCursor& cu, ChunkSeq& q, long long& from, long long& to, int cta, int lane) {
+template <typename Int>
+__device__ __forceinline__ bool locate(ChunkWork<Int>& wk, ChunkCursor<Int>& cu, ChunkSeq<Int>& q, Int& from, Int& to, int cta, int lane) {
     wk.changes = true;
-    long long sum = 0, of_changes = 0;
+    Int sum = 0, of_changes = 0;
     for (int s0 = 0; s0 < wk.S; s0 += 32)
         if (s0 + lane < wk.S) {
-            const ChunkSeq x = wk.seq(s0 + lane);
-            of_changes += (long long)x.pairs * x.change;
-            sum += x.before(x.pairs) - (long long)x.pairs * x.change;
+            const ChunkSeq<Int> x = wk.seq(s0 + lane);
+            of_changes += (Int)x.pairs * x.change;
+            sum += x.before(x.pairs) - (Int)x.pairs * x.change;
         }
     wk.set(warp_sum(sum), warp_sum(of_changes));
     from = wk.start(cta);
     to = wk.start(cta + 1);
     if (from >= to) return false;
-    long long begin = 0;
+    Int begin = 0;
     for (int s0 = 0; s0 < wk.S; s0 += 32) {
-        long long own = 0;
+        Int own = 0;
         if (s0 + lane < wk.S) {
-            const ChunkSeq x = wk.seq(s0 + lane);
+            const ChunkSeq<Int> x = wk.seq(s0 + lane);
             own = wk.Hkv * x.before(x.pairs);
         }
-        long long upto = own;
+        Int upto = own;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const long long u = __shfl_up_sync(0xFFFFFFFFu, upto, o);
+            const Int u = __shfl_up_sync(0xFFFFFFFFu, upto, o);
             if (lane >= o) upto += u;
         }
         const uint32_t here = __ballot_sync(0xFFFFFFFFu, begin + upto > from);
@@ -205,8 +209,8 @@ __device__ __forceinline__ void arrive_at(uint32_t bar) {
 
 // Joins the partial results of 32 rows (row0 on) of M tile l of an item that the CTAs c0 .. c0 + n - 1 have, by one warp: lanes <-> rows, and where the
 // rows are fewer, several lanes share a row's columns.  kCols columns a time, kRound parts in flight.
-template <int kCols, int kRound>
-__device__ __forceinline__ void join_parts(const ChunkArgs& a, int c0, int n, int l, int row0, int rows, int lane, size_t out_row /* of this lane's row */,
+template <int kCols, int kRound, typename Int>
+__device__ __forceinline__ void join_parts(const ChunkArgs<Int>& a, int c0, int n, int l, int row0, int rows, int lane, size_t out_row /* of this lane's row */,
                                            int width, bool write_lse) {
     const int r = lane & (width - 1);
     for (int c = lane / width * kCols; c < kHeadDim; c += 32 / width * kCols) {
@@ -235,18 +239,14 @@ __device__ __forceinline__ void join_parts(const ChunkArgs& a, int c0, int n, in
                     }
                 }
             }
-            float M_new = M;
-#pragma unroll
-            for (int u = 0; u < kRound; ++u) { M_new = fmaxf(M_new, ml[u].x); bad |= ml[u].y < 0.f; }
-            const float old = M == -INFINITY ? 0.f : ex2(M - M_new);
-            L *= old;
-#pragma unroll
-            for (int e = 0; e < kCols; ++e) acc[e] *= old;
 #pragma unroll
             for (int u = 0; u < kRound; ++u) {
+                bad |= ml[u].y < 0.f;
                 if (ml[u].x == -INFINITY && ml[u].y == 0.f) continue;   // no key of the part is visible to the row
+                const float M_new = fmaxf(M, ml[u].x), old = M == -INFINITY ? 0.f : ex2(M - M_new);
                 const float w = ml[u].x == -INFINITY ? 1.f : ex2(ml[u].x - M_new);   // (NaN alone: it stays one)
-                L += w * ml[u].y;
+                M = M_new;
+                L = __fmaf_rn(w, ml[u].y, __fmul_rn(L, old));
 #pragma unroll
                 for (int b = 0; b < kCols / 16; ++b) {
                     const uint32_t thirds[4] = {x[u][b][2].x, x[u][b][2].y, x[u][b][2].z, x[u][b][2].w};
@@ -254,14 +254,14 @@ __device__ __forceinline__ void join_parts(const ChunkArgs& a, int c0, int n, in
                     for (int v = 0; v < 4; ++v) {
                         const uint4& half = x[u][b][v >> 1];
                         const uint32_t h0 = v & 1 ? half.z : half.x, h1 = v & 1 ? half.w : half.y;
-                        acc[16 * b + 4 * v] += w * part_element<0>(h0, thirds[v]);
-                        acc[16 * b + 4 * v + 1] += w * part_element<1>(h0, thirds[v]);
-                        acc[16 * b + 4 * v + 2] += w * part_element<2>(h1, thirds[v]);
-                        acc[16 * b + 4 * v + 3] += w * part_element<3>(h1, thirds[v]);
+                        float* o = acc + 16 * b + 4 * v;
+                        o[0] = __fmaf_rn(w, part_element<0>(h0, thirds[v]), __fmul_rn(o[0], old));
+                        o[1] = __fmaf_rn(w, part_element<1>(h0, thirds[v]), __fmul_rn(o[1], old));
+                        o[2] = __fmaf_rn(w, part_element<2>(h1, thirds[v]), __fmul_rn(o[2], old));
+                        o[3] = __fmaf_rn(w, part_element<3>(h1, thirds[v]), __fmul_rn(o[3], old));
                     }
                 }
             }
-            M = M_new;
         }
         if (row0 + r < rows) {
             const float inv = bad ? 0.f : 1.f / L;
@@ -276,9 +276,10 @@ __device__ __forceinline__ void join_parts(const ChunkArgs& a, int c0, int n, in
     }
 }
 
+template <typename Int>
 __global__ void __launch_bounds__(kChunkThreads, 1)
 chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k,
-                  const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ ChunkArgs a) {
+                  const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ ChunkArgs<Int> a) {
     extern __shared__ unsigned char smem_raw[];
     unsigned char* q_smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     unsigned char* kv_smem = q_smem + 2 * kQBytes;
@@ -287,7 +288,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i) { for (int u = 0; u < 3; ++u) mbar_init(&hd->kv_full[u][i], 1); mbar_init(&hd->kv_empty[i], 2); }
-        for (int i = 0; i < kSegments; ++i) { mbar_init(&hd->seg_full[i], 1); mbar_init(&hd->seg_empty[i], 3 + 8); }
+        for (int i = 0; i < kSegments; ++i) { mbar_init(&hd->seg_full[i], 1); mbar_init(&hd->seg_empty[i], 3 + 8); mbar_init(&hd->seg_checked[i], 1); }
         for (int l = 0; l < 2; ++l) {
             mbar_init(&hd->pair_full[l], 1); mbar_init(&hd->pair_empty[l], 1); mbar_init(&hd->single_full[l], 1); mbar_init(&hd->single_empty[l], 2);
             mbar_init(&hd->s_full[l], 1); mbar_init(&hd->v_there[l], 1); mbar_init(&hd->p_ready[l][0], 4); mbar_init(&hd->p_ready[l][1], 4); mbar_init(&hd->o_full[l], 1); mbar_init(&hd->o_free[l], 4);
@@ -312,13 +313,13 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsFew));
         if (warp == 2) {
             // =========================================================== planner
-            ChunkWork wk = a.wk;
+            ChunkWork<Int> wk = a.wk;
             if (wk.n_new && blockIdx.x == 0)
                 for (int s = lane; s < wk.S; s += 32)
                     if (nodes_bad(wk.n_new, s, wk.B)) atomicOr(&a.status[s], GOOSE_ST_BAD_NODES);
-            ChunkCursor cu{};
-            ChunkSeq q{};
-            long long from, to;
+            ChunkCursor<Int> cu{};
+            ChunkSeq<Int> q{};
+            Int from, to;
             bool live = locate(wk, cu, q, from, to, blockIdx.x, lane);
             auto advance = [&]() {
                 if (cu.next(wk, q)) return;
@@ -332,22 +333,11 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
             for (;;) {
                 bool any = false;
                 while (live && cu.w0 < to) {
-                    cu.look(wk, q, from, to);
+                    cu.look(wk, q, blockIdx.x, from, to);
                     any = cu.t1 > cu.t0;
                     if (any) break;
                     advance();
                 }
-                bool bad = q.bad;
-                if (any && !bad) {                           // the segment's pages
-                    const int lg = a.pages.size_log2;
-                    const int p0 = (cu.t0 * kChunkTile) >> lg, p1 = (min(cu.t1 * kChunkTile, q.ctx + q.n) - 1) >> lg;
-                    for (int p = p0 + lane; p <= p1; p += 32) {
-                        const int page = a.pages.table[cu.s * a.pages.ldt + p];
-                        bad |= page < 0 || page >= a.pages.n;
-                    }
-                }
-                bad = __any_sync(0xFFFFFFFFu, bad);
-                if (any && bad && lane == 0) atomicOr(&a.status[cu.s], GOOSE_ST_BAD_ROWS);
                 if (!wait_for(hd, &hd->seg_empty[ring.at], ring.phase ^ 1, a.status)) break;
                 Segment* sg = &hd->seg[ring.at];
                 if (lane == 0) {
@@ -360,12 +350,29 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                         sg->rows[0] = min(here, wk.t) * a.g;
                         sg->rows[1] = max(here - wk.t, 0) * a.g;
                         sg->c0 = cu.c0; sg->parts = cu.c1 - cu.c0 + 1;
-                        sg->again = q.pairs > 1; sg->bad = bad;
+                        sg->again = q.pairs > 1;
                     }
+                    mbar_arrive(&hd->seg_full[ring.at]);
                 }
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&hd->seg_full[ring.at]);
                 if (!any) break;
+                // the segment's pages: who needs to know asks at its end
+                bool bad = q.bad;
+                if (!bad) {
+                    const int lg = a.pages.size_log2;
+                    const int p1 = (min(cu.t1 * kChunkTile, q.ctx + q.n) - 1) >> lg;
+                    for (int p = ((cu.t0 * kChunkTile) >> lg) + lane; p <= p1; p += 32) {
+                        const int page = a.pages.table[cu.s * a.pages.ldt + p];
+                        bad |= page < 0 || page >= a.pages.n;
+                    }
+                }
+                bad = __any_sync(0xFFFFFFFFu, bad);
+                if (lane == 0) {
+                    sg->bad = bad;
+                    if (bad) atomicOr(&a.status[cu.s], GOOSE_ST_BAD_ROWS);
+                    mbar_arrive(&hd->seg_checked[ring.at]);
+                }
+                __syncwarp();
                 ring.next(kSegments);
                 advance();
             }
@@ -373,8 +380,8 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
             // =========================================================== TMA producer (the warp runs converged)
             const bool leader = elect_leader();
             const unsigned long long pol_once = l2_policy_evict_first(), pol_again = l2_policy_evict_last();
-            // a lane's box of a tile: its rows, and which half of the head's elements
-            const int boxes = kChunkTile >> a.box_log2, box = lane & (boxes - 1), half = lane >> (7 - a.box_log2), outside = a.pages.n << a.pages.size_log2;
+            const uint32_t kv_addr = smem_u32(kv_smem);
+            const int boxes = kChunkTile >> a.box_log2, outside = a.pages.n << a.pages.size_log2;
             uint32_t pairs = 0, singles = 0, tile0 = 0;      // segments of either kind, tiles in front of this segment
             uint32_t phases = 0, users = 0;                  // a bit a kv_full barrier; two bits a stage: who has it, 3: nobody yet
             for (int i = 0; i < kStages; ++i) users |= 3u << 2 * i;
@@ -411,8 +418,8 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
             };
             // the cache row of this lane's box of tile t: no page behind the sequence's last row is looked up
             auto box_row = [&](int t) {
-                const int j = (t << 7) + (box << a.box_log2), page = j >> a.pages.size_log2;
-                if (lane >= 2 * boxes || j >= sg.n_keys || page >= a.pages.ldt) return outside;
+                const int j = (t << 7) + (lane << a.box_log2), page = j >> a.pages.size_log2;
+                if (lane >= boxes || j >= sg.n_keys || page >= a.pages.ldt) return outside;
                 const int at = a.pages.table[sg.s * a.pages.ldt + page];
                 return at < 0 || at >= a.pages.n ? outside : (at << a.pages.size_log2) + (j & ((1 << a.pages.size_log2) - 1));
             };
@@ -443,10 +450,17 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                         if (leader) mbar_expect_tx(full, kStageBytes);
                         __syncwarp();
                         const CUtensorMap* mp = kv ? &tmap_v : &tmap_k;
-                        // a box a lane: one instruction of the warp issues them all
-                        if (lane < 2 * boxes)
-                            tma_load_3d_hint(kv_smem + st.at * kStageBytes + half * kHalfBytes + (box << (a.box_log2 + 7)), mp, full, 64 * half, sg.hk, row, pol);
-                        __syncwarp();
+                        const uint32_t dst = kv_addr + st.at * kStageBytes;
+                        int from[8];                         // (all of them ahead of the copies: a copy behind a shuffle waits for it)
+#pragma unroll
+                        for (int b = 0; b < 8; ++b) from[b] = __shfl_sync(0xFFFFFFFFu, row, b);
+#pragma unroll
+                        for (int b = 0; b < 8; ++b) {
+                            if (b >= boxes) break;
+                            const uint32_t to = dst + ((uint32_t)b << (a.box_log2 + 7));
+                            tma_load_3d_hint_by(leader, to, mp, full, 0, sg.hk, from[b], pol);
+                            tma_load_3d_hint_by(leader, to + kHalfBytes, mp, full, 64, sg.hk, from[b], pol);
+                        }
                         phases ^= 1u << (user * kStages + st.at);
                         users = (users & ~(3u << 2 * st.at)) | user << 2 * st.at;
                         st.next(kStages);
@@ -686,6 +700,8 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                 ++ops;
             }
             if (!ok) break;
+            ok = wait_for(hd, &hd->seg_checked[ring.at], ring.phase, a.status);
+            if (!ok) break;
             const bool two = sg.single && sg.n > 1;          // both lanes have key tiles of the one M tile
             if (!first) {
                 ok = wait_at(my_bars + kAtDone, segs & 1, abort_at, a.status);
@@ -716,27 +732,27 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                     release();
                 } else {
                     const uint32_t o_addr = s_addr + (kColO - kColS);
-                    TMEM_LD32(o_addr, v, 0); TMEM_LD32(o_addr + 32, v, 32);
-                    TMEM_LD32(o_addr + 64, v, 64); TMEM_LD32(o_addr + 96, v, 96);
-                    tmem_wait_ld();
-                    if (two) {
+                    if (two) {                               // (into tensor memory again: a row and a part of another one are more than the registers hold)
                         const float2 other = hd->other[row];
                         const float m = fmaxf(m_run, other.x);
                         const float mine = m_run == -INFINITY ? 0.f : ex2(m_run - m), theirs = other.x == -INFINITY ? 0.f : ex2(other.x - m);
-                        const uint32_t other_addr = tmem + kColO + (l ^ 1) * 128 + ((uint32_t)(32 * (warp & 3)) << 16);
-                        uint32_t o[16];
-#pragma unroll
-                        for (int cc = 0; cc < 8; ++cc) {
-                            TMEM_LD16(other_addr + cc * 16, o, 0);
-                            tmem_wait_ld();
-#pragma unroll
-                            for (int c = 0; c < 16; ++c)
-                                v[16 * cc + c] = __float_as_uint(__uint_as_float(v[16 * cc + c]) * mine + __uint_as_float(o[c]) * theirs);
-                        }
                         // (a lane whose scores are all NaN has a sum of NaN and no maximum)
                         l_run = l_run * (m_run == -INFINITY ? 1.f : mine) + other.y * (other.x == -INFINITY ? 1.f : theirs);
                         m_run = m;
+                        const uint32_t other_addr = tmem + kColO + (l ^ 1) * 128 + ((uint32_t)(32 * (warp & 3)) << 16);
+#pragma unroll
+                        for (int cc = 0; cc < 4; ++cc) {
+                            TMEM_LD32(o_addr + 32 * cc, v, 0); TMEM_LD32(other_addr + 32 * cc, v, 32);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int c = 0; c < 32; ++c) v[c] = __float_as_uint(__uint_as_float(v[c]) * mine + __uint_as_float(v[32 + c]) * theirs);
+                            TMEM_ST32(o_addr + 32 * cc, v, 0);
+                        }
+                        tmem_wait_st();
                     }
+                    TMEM_LD32(o_addr, v, 0); TMEM_LD32(o_addr + 32, v, 32);
+                    TMEM_LD32(o_addr + 64, v, 64); TMEM_LD32(o_addr + 96, v, 96);
+                    tmem_wait_ld();
                     release();
                     const int first_token = sg.s * a.wk.B + sg.token + m_tile * a.wk.t;
                     if (sg.whole) {
@@ -744,14 +760,20 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                             const int node = row / a.g;
                             const size_t at = ((size_t)first_token + node) * a.H + sg.hk * a.g + (row - node * a.g);
                             const float inv = 1.f / l_run;
-                            uint4* dst = reinterpret_cast<uint4*>(a.out + at * kHeadDim);
+                            __nv_bfloat16* dst = a.out + at * kHeadDim;
 #pragma unroll
-                            for (int c = 0; c < 16; ++c) {
-                                uint32_t w[4];
+                            for (int c = 0; c < 8; ++c) {
+                                uint32_t w[8];
 #pragma unroll
-                                for (int e = 0; e < 4; ++e)
-                                    w[e] = sg.bad ? 0u : pack_bf16x2(__uint_as_float(v[8 * c + 2 * e]) * inv, __uint_as_float(v[8 * c + 2 * e + 1]) * inv);
-                                dst[c] = make_uint4(w[0], w[1], w[2], w[3]);
+                                for (int e = 0; e < 8; ++e)
+                                    w[e] = sg.bad ? 0u : pack_bf16x2(__uint_as_float(v[16 * c + 2 * e]) * inv, __uint_as_float(v[16 * c + 2 * e + 1]) * inv);
+                                if (a.wide) {                // (rows are far apart: half the requests)
+                                    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(dst + 16 * c), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
+                                                 "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+                                } else {
+                                    reinterpret_cast<uint4*>(dst)[2 * c] = make_uint4(w[0], w[1], w[2], w[3]);
+                                    reinterpret_cast<uint4*>(dst)[2 * c + 1] = make_uint4(w[4], w[5], w[6], w[7]);
+                                }
                             }
                             if (a.lse) a.lse[at] = sg.bad ? 0.f : (m_run + log2f(l_run)) * kLn2;
                         }
@@ -806,18 +828,16 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
 
 }  // namespace
 
-cudaError_t launch_chunk_attn(goose_ctx* c, const ChunkAttn& x, cudaStream_t st) {
-    if (!c->encode_tiled) return cudaErrorNotSupported;
-    if (x.S == 0) return cudaSuccess;
-    ChunkArgs a{};
+template <typename Int>
+static cudaError_t launch_as(goose_ctx* c, const ChunkAttn& x, cudaStream_t st) {
+    ChunkArgs<Int> a{};
     a.g = x.H / x.Hkv; a.H = x.H;
     a.wk.ctx_len = x.ctx_len; a.wk.n_new = x.n_new; a.wk.S = x.S; a.wk.B = x.B; a.wk.Hkv = x.Hkv; a.wk.G = c->num_sms;
     a.wk.t = kChunkTile / a.g; a.wk.room = (int)x.pages.room(0);
-    a.pages = x.pages;
+    a.pages = x.pages; a.box_log2 = x.pages.size_log2 < 7 ? x.pages.size_log2 : 7;
     a.nb = a.wk.t < x.B ? a.wk.t : x.B;
-    a.box_log2 = x.pages.size_log2 < 7 ? x.pages.size_log2 : 7;
+    a.wide = (reinterpret_cast<uintptr_t>(x.out) & 31) == 0;
     a.scale_log2 = x.scale * kLog2e;
-    if (cudaError_t e = grow(c, &c->chunk_parts, &c->chunk_bytes, sizeof(uint4) * kPartBlock * 4 * (size_t)c->num_sms)) return e;
     a.parts = static_cast<uint4*>(c->chunk_parts);
     a.counters = c->chunk_counters; a.status = c->status; a.out = x.out; a.lse = x.lse;
     CUtensorMap mq, mk, mv;
@@ -825,11 +845,22 @@ cudaError_t launch_chunk_attn(goose_ctx* c, const ChunkAttn& x, cudaStream_t st)
     if (!make_q_map(c->encode_tiled, &mq, x.q, (int64_t)x.S * x.B, x.Hkv, a.g, a.nb) || !make_map(c->encode_tiled, &mk, x.k_cache, rows, x.Hkv, 1 << a.box_log2) ||
         !make_map(c->encode_tiled, &mv, x.v_cache, rows, x.Hkv, 1 << a.box_log2))
         return cudaErrorInvalidValue;
-    cudaError_t e = launch_pdl(chunk_attn_kernel, dim3(c->num_sms), dim3(kChunkThreads), kChunkSmem, st, mq, mk, mv, a);
+    cudaError_t e = launch_pdl(chunk_attn_kernel<Int>, dim3(c->num_sms), dim3(kChunkThreads), kChunkSmem, st, mq, mk, mv, a);
     c->launches++;
     return e;
 }
 
-cudaError_t init_chunk_kernels() { return cudaFuncSetAttribute(chunk_attn_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kChunkSmem); }
+cudaError_t launch_chunk_attn(goose_ctx* c, const ChunkAttn& x, cudaStream_t st) {
+    if (!c->encode_tiled) return cudaErrorNotSupported;
+    if (x.S == 0) return cudaSuccess;
+    if (cudaError_t e = grow(c, &c->chunk_parts, &c->chunk_bytes, sizeof(uint4) * kPartBlock * 4 * (size_t)c->num_sms)) return e;
+    const bool small = ChunkWork<int>::most(x.S, x.B, x.Hkv, kChunkTile / (x.H / x.Hkv), (int)x.pages.room(0)) < kShortPlaces;
+    return small ? launch_as<int>(c, x, st) : launch_as<long long>(c, x, st);
+}
+
+cudaError_t init_chunk_kernels() {
+    cudaError_t e = cudaFuncSetAttribute(chunk_attn_kernel<int>, cudaFuncAttributeMaxDynamicSharedMemorySize, kChunkSmem);
+    return e == cudaSuccess ? cudaFuncSetAttribute(chunk_attn_kernel<long long>, cudaFuncAttributeMaxDynamicSharedMemorySize, kChunkSmem) : e;
+}
 
 }  // namespace goose

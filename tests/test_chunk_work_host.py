@@ -18,28 +18,29 @@ SOURCE = r"""
 #include "chunk_work.cuh"
 using namespace goose;
 // 0, or what is wrong
-extern "C" int walk(int S, int B, int Hkv, int t, int G, int room, const int32_t* ctx_len, const int32_t* n_new, double* worst) {
-    ChunkWork wk{};
+template <typename Int>
+static int walk_as(int S, int B, int Hkv, int t, int G, int room, const int32_t* ctx_len, const int32_t* n_new, double* worst) {
+    ChunkWork<Int> wk{};
     wk.ctx_len = ctx_len; wk.n_new = n_new; wk.S = S; wk.B = B; wk.Hkv = Hkv; wk.G = G; wk.t = t; wk.room = room;
     wk.changes = true;
-    long long sum = 0, of_changes = 0;
+    Int sum = 0, of_changes = 0;
     for (int s = 0; s < S; ++s) {
-        const ChunkSeq q = wk.seq(s);
-        sum += q.before(q.pairs) - (long long)q.pairs * q.change;
-        of_changes += (long long)q.pairs * q.change;
+        const ChunkSeq<Int> q = wk.seq(s);
+        sum += q.before(q.pairs) - (Int)q.pairs * q.change;
+        of_changes += (Int)q.pairs * q.change;
     }
     wk.set(sum, of_changes);
     std::map<std::tuple<int, int, int>, std::pair<int, int>> dealt;      // item -> (tiles so far, CTAs so far)
     long long longest = 0, all = 0;
     for (int c = 0; c < G; ++c) {
-        const long long from = wk.start(c), to = wk.start(c + 1);
+        const Int from = wk.start(c), to = wk.start(c + 1);
         if (from >= to) continue;
-        ChunkCursor cu{};
-        long long begin = 0, mine = 0;
-        ChunkSeq q{};
+        ChunkCursor<Int> cu{};
+        Int begin = 0; long long mine = 0;
+        ChunkSeq<Int> q{};
         for (cu.s = 0; cu.s < S; ++cu.s) {
             q = wk.seq(cu.s);
-            const long long all = Hkv * q.before(q.pairs);
+            const Int all = Hkv * q.before(q.pairs);
             if (from < begin + all) break;
             begin += all;
         }
@@ -48,7 +49,7 @@ extern "C" int walk(int S, int B, int Hkv, int t, int G, int room, const int32_t
         if (cu.hk < 0 || cu.hk >= Hkv || cu.p < 0 || cu.p >= q.pairs || cu.w0 > from || cu.w0 + q.width(cu.p) <= from) return 2;
         int heads = 0, tails = 0;
         while (cu.w0 < to) {
-            cu.look(wk, q, from, to);
+            cu.look(wk, q, c, from, to);
             if (cu.T < 1 || cu.T != (q.keys(cu.p) + 127) / 128) return 3;
             if (cu.t1 > cu.t0) {
                 auto& d = dealt[{cu.s, cu.hk, cu.p}];
@@ -61,7 +62,7 @@ extern "C" int walk(int S, int B, int Hkv, int t, int G, int room, const int32_t
                 heads += !starts; tails += starts && !ends;
             }
             if (!cu.next(wk, q)) {
-                do { ++cu.s; q = cu.s < S ? wk.seq(cu.s) : ChunkSeq{}; } while (cu.s < S && q.pairs == 0);
+                do { ++cu.s; q = cu.s < S ? wk.seq(cu.s) : ChunkSeq<Int>{}; } while (cu.s < S && q.pairs == 0);
                 if (cu.s == S) break;
                 cu.hk = cu.p = 0;
             }
@@ -70,7 +71,7 @@ extern "C" int walk(int S, int B, int Hkv, int t, int G, int room, const int32_t
         longest = std::max(longest, mine); all += mine;
     }
     for (int s = 0; s < S; ++s) {
-        const ChunkSeq q = wk.seq(s);
+        const ChunkSeq<Int> q = wk.seq(s);
         const int n = n_new ? (n_new[s] < 0 || n_new[s] > B ? 0 : n_new[s]) : B;
         if (q.n != n || q.pairs != (n + 2 * t - 1) / (2 * t)) return 8;
         long long rows = 0;
@@ -84,7 +85,12 @@ extern "C" int walk(int S, int B, int Hkv, int t, int G, int room, const int32_t
         if (rows != n) return 10;
     }
     *worst = all ? (double)longest * G / all : 0;
-    return 0;
+    return (double)wk.total <= ChunkWork<Int>::most(S, B, Hkv, t, room) ? 0 : 11;
+}
+extern "C" int walk(int S, int B, int Hkv, int t, int G, int room, const int32_t* ctx_len, const int32_t* n_new, double* worst) {
+    const int rc = walk_as<long long>(S, B, Hkv, t, G, room, ctx_len, n_new, worst);
+    if (rc) return rc;
+    return ChunkWork<int>::most(S, B, Hkv, t, room) < kShortPlaces ? 100 * walk_as<int>(S, B, Hkv, t, G, room, ctx_len, n_new, worst) : 0;
 }
 """
 
