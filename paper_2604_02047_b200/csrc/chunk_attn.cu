@@ -85,7 +85,6 @@ struct Header {
     unsigned long long s_full[2], v_there[2], o_full[2], o_free[2];
     unsigned long long p_ready[2][2];                        // of a lane, P of either half of a tile's keys
     unsigned long long other_full;                           // `other`, and the product behind it
-    unsigned long long turn[2];                              // the other lane's exponentials of a pair's tile are done
     uint32_t tmem_base;
     volatile int abort_flag;
 };
@@ -295,7 +294,6 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
             mbar_init(&hd->s_full[l], 1); mbar_init(&hd->v_there[l], 1); mbar_init(&hd->p_ready[l][0], 4); mbar_init(&hd->p_ready[l][1], 4); mbar_init(&hd->o_full[l], 1); mbar_init(&hd->o_free[l], 4);
         }
         mbar_init(&hd->other_full, 4);
-        for (int l = 0; l < 2; ++l) mbar_init(&hd->turn[l], 4);
         hd->abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         prefetch_tmap(&tmap_q); prefetch_tmap(&tmap_k); prefetch_tmap(&tmap_v);
@@ -601,7 +599,6 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
         const uint32_t at_ready = base + (uint32_t)offsetof(Header, p_ready) + 16 * l;
         uint32_t ops = 0, segs = 0, tile0 = 0;               // products and segments of this lane; tiles of the CTA in front of this segment
         uint32_t joins = 0;                                  // segments of the CTA whose lanes have been joined
-        uint32_t turns = 0;                                  // tiles of pairs
         Ring ring{0, 0};
         bool ok = true;
         uint32_t v[128];
@@ -619,11 +616,6 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
             // keys that the M tile's first token sees; from t_masked on a tile has keys behind a token
             auto seen = [&]() { return sg.ctx + sg.token + m_tile * a.wk.t + 1; };
             const int t_masked = seen() / kChunkTile;
-            // The exponentials of a pair's lanes take turns.  At the same time each takes twice as long, and so do the products behind them: the lanes
-            // then stay in step, exponentials beside exponentials and products beside products.
-            auto my_turn = [&]() {
-                return sg.single || wait_at(base + (uint32_t)offsetof(Header, turn) + 8 * l, (turns & 1) ^ (l ^ 1), abort_at, a.status);
-            };
             float m_run = -INFINITY, l_run = 0.f;
             bool first = true;
             for (int t = sg.t_first + (sg.single ? turn : 0); t < t_end; t += step) {
@@ -682,7 +674,6 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                     const float neg_m = (m_run == -INFINITY) ? 0.f : -m_run;
                     const unsigned long long scale2 = pack_f32x2(a.scale_log2, a.scale_log2), neg2 = pack_f32x2(neg_m, neg_m);
                     unsigned long long ls2[2] = {0, 0};
-                    if (!(ok = my_turn())) break;
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
 #pragma unroll
@@ -701,15 +692,9 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                     const float2 l2 = unpack_f32x2(add_f32x2(ls2[0], ls2[1]));
                     l_run += l2.x + l2.y;
                 } else {
-                    if (!(ok = my_turn())) break;            // (or an arrival below could be for the phase in front)
                     tc_fence_before();
                     __syncwarp();                            // (all lanes' zeros are in front of the arrivals)
                     if (lane == 0) { arrive_at(at_ready); arrive_at(at_ready + 8); }
-                }
-                if (!sg.single) {
-                    __syncwarp();
-                    if (lane == 0) arrive_at(base + (uint32_t)offsetof(Header, turn) + 8 * (l ^ 1));
-                    ++turns;
                 }
                 first = false;
                 ++ops;
