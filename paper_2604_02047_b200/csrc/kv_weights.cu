@@ -2,14 +2,16 @@
 // over the tokens i >= j - ctx.
 //
 // Persistent, one CTA an SM, tcgen05: S^T = K Q^T with the keys as rows, so that a thread has a key, and its sum needs no exchange; up to
-// four key tiles of a run stay in shared memory while the Q tiles pass by.  Work list: weights_work.cuh.  Roles (384 threads):
-//   warp 0            TMA producer: Q tiles into a ring of two, K tiles, a box a page, into a ring of five; its lanes look the pages up
+// four key tiles of a run stay in shared memory while the Q tiles pass by.  Work list: weights_work.cuh.  Roles (768 threads):
+//   warp 0            Q tiles into a ring of two, by TMA
 //   warp 1            MMA issuer: the scores of key tile u of the run into columns 128 u of tensor memory
 //   warp 2            planner: walks the work list and puts the segments' descriptions into a ring
 //   warp 3            log-sum-exps of a Q tile's rows, negated and in units of log 2, and which of the rows count
-//   warps 4..7, 8..11 exponentials of key tiles 0 and 2, of 1 and 3: a key a thread, two sums.  At the segment's end the sums are added to the
+//   warps 4..19       exponentials, four warps a key tile of the run, a key and a sum a thread.  At the segment's end the sums are added to the
 //                     rows' weights, or, where several CTAs have Q tiles of the item, left in the workspace; the warp that completes a count adds up what
 //                     all have left, in the order of the tokens.
+//   warps 20..23      K tiles into a ring of five, 32 keys of a tile a warp, by 16-byte copies: a TMA box a page took 110 to 156 cycles a box, and pages of
+//                     16 rows have sixteen a tile (64 sequences of 8192 rows, a token each: 255 us, with these 180; pages of 128 rows 218, 178)
 // Every wait is bounded: one that runs out raises the CTA's abort flag and GOOSE_ST_TIMEOUT, and every role unwinds.
 #include <stddef.h>
 
@@ -27,11 +29,17 @@ constexpr int kTileBytes = kWeightTile * kHeadDim * 2;       // 32 KB: one K or 
 constexpr int kHalfBytes = kWeightTile * 128;                // 16 KB: 128 rows x 64 bf16 (one swizzle-atom column)
 constexpr int kHeaderBytes = 2048;
 constexpr int kWeightSmem = 1008 /*alignment slack*/ + (kStages + kQStages) * kTileBytes + kHeaderBytes;
-constexpr int kWeightThreads = 512;
+// warps: four of the roles below, four a key tile of a run for the exponentials, four for the copies of the key tiles
+constexpr int kSumWarp = 4, kCopyWarp = kSumWarp + 4 * kRun, kCopyWarps = 4;
+constexpr int kWeightThreads = 32 * (kCopyWarp + kCopyWarps);
+// registers: 80 a thread at launch; the warps of the products and of the copies give 16 each to the others (64 + 64 + 4 x 88 = 6 x 80)
+constexpr int kRegsFew = 64, kRegsMany = 88;
 constexpr uint32_t kTmemCols = 512;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr long long kWaitCycles = 2000000000ll;              // bound of every wait: about one second of SM clock
 constexpr int kSegments = 6;
+// which second pairs of columns of four, of 32, get their exponentials from the FMA pipe
+constexpr uint32_t kFmaPairs = 0xEE;
 
 // a segment, as the planner describes it
 struct Segment {
@@ -54,8 +62,9 @@ struct Header {
 static_assert(sizeof(Header) <= kHeaderBytes, "header");
 static_assert(kWeightSmem <= 232448, "shared memory of a block");
 
+template <typename Int>
 struct WeightArgs {
-    WeightWork wk;
+    WeightWork<Int> wk;
     Pages pages;
     const __nv_bfloat16* k_cache;
     int g, H, nb;                                            // heads of a group, heads, tokens of a box of queries
@@ -89,43 +98,45 @@ struct Ring {
     }
 };
 
-__device__ __forceinline__ long long warp_sum(long long v) {
+template <typename Int>
+__device__ __forceinline__ Int warp_sum(Int v) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
     return v;
 }
 
 // the list's length and a place in it, by a whole warp (lane = sequence); false: the CTA has no range
-__device__ __forceinline__ bool locate(WeightWork& wk, WeightCursor& cu, WeightSeq& q, long long& from, long long& to, int cta, int lane) {
+template <typename Int>
+__device__ __forceinline__ bool locate(WeightWork<Int>& wk, WeightCursor<Int>& cu, WeightSeq<Int>& q, Int& from, Int& to, int cta, int lane) {
     wk.short_run = 1;
-    long long tiles = 0, sum = 0;
+    Int tiles = 0, sum = 0;
     bool several = false;
     for (int s0 = 0; s0 < wk.S; s0 += 32)
         if (s0 + lane < wk.S) {
-            const WeightSeq x = wk.seq(s0 + lane);
+            const WeightSeq<Int> x = wk.seq(s0 + lane);
             if (x.n > wk.t) several = true; else tiles += x.items;
         }
     wk.set_run(warp_sum(tiles));
     for (int s0 = 0; s0 < wk.S; s0 += 32)
         if (s0 + lane < wk.S) {
-            const WeightSeq x = wk.seq(s0 + lane);
+            const WeightSeq<Int> x = wk.seq(s0 + lane);
             sum += x.before(x.items);
         }
     wk.set(warp_sum(sum), __any_sync(0xFFFFFFFFu, several));
     from = wk.start(cta);
     to = wk.start(cta + 1);
     if (from >= to) return false;
-    long long begin = 0;
+    Int begin = 0;
     for (int s0 = 0; s0 < wk.S; s0 += 32) {
-        long long own = 0;
+        Int own = 0;
         if (s0 + lane < wk.S) {
-            const WeightSeq x = wk.seq(s0 + lane);
+            const WeightSeq<Int> x = wk.seq(s0 + lane);
             own = wk.Hkv * x.before(x.items);
         }
-        long long upto = own;
+        Int upto = own;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const long long u = __shfl_up_sync(0xFFFFFFFFu, upto, o);
+            const Int u = __shfl_up_sync(0xFFFFFFFFu, upto, o);
             if (lane >= o) upto += u;
         }
         const uint32_t here = __ballot_sync(0xFFFFFFFFu, begin + upto > from);
@@ -141,11 +152,54 @@ __device__ __forceinline__ bool locate(WeightWork& wk, WeightCursor& cu, WeightS
     return false;
 }
 
+// 2^x of two numbers x <= 0 on the FMA pipe: x = n + f with |f| <= 1/2 (adding 1.5 2^23 + 127 rounds x to n and leaves n + 127 in the low bits),
+// a minimax polynomial of degree 4 for 2^f (relative error 2.7e-6, of either sign), times 2^n.  NaN stays NaN; x above 0 is not met by probabilities
+// and saturates at 2^127.
+__device__ __forceinline__ unsigned long long ex2_fma(float2 x) {
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.x) : "f"(-126.f));
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.y) : "f"(-126.f));
+    asm("min.NaN.f32 %0, %0, %1;" : "+f"(x.x) : "f"(127.f));
+    asm("min.NaN.f32 %0, %0, %1;" : "+f"(x.y) : "f"(127.f));
+    auto both = [](float c) { return pack_f32x2(c, c); };
+    constexpr float kRound = 12582912.f + 127.f;
+    const unsigned long long v = pack_f32x2(x.x, x.y), r = add_f32x2(v, both(kRound)), f = fma_f32x2(add_f32x2(r, both(-kRound)), both(-1.f), v);
+    unsigned long long p = both(0.009570102f);
+    for (float c : {0.055917859f, 0.24024744f, 0.69312179f, 0.99999928f}) p = fma_f32x2(p, f, both(c));
+    const float2 n = unpack_f32x2(r);
+    return mul_f32x2(p, pack_f32x2(__uint_as_float(__float_as_uint(n.x) << 23), __uint_as_float(__float_as_uint(n.y) << 23)));
+}
+
+// sums over 32 columns of exp2(score * scale - lse): all of them, some of the exponentials by the FMA pipe; those of a mask
+__device__ __forceinline__ void add_columns(const uint32_t* v, const float* neg_lse, unsigned long long scale2, unsigned long long (&part)[2]) {
+    const ulonglong2* nl = reinterpret_cast<const ulonglong2*>(neg_lse);
+#pragma unroll
+    for (int c = 0; c < 32; c += 4) {
+        const ulonglong2 n4 = nl[c / 4];
+        const float2 x = unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(v[c]), __uint_as_float(v[c + 1])), scale2, n4.x));
+        const float2 y = unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(v[c + 2]), __uint_as_float(v[c + 3])), scale2, n4.y));
+        part[0] = add_f32x2(part[0], pack_f32x2(ex2(x.x), ex2(x.y)));
+        part[1] = add_f32x2(part[1], kFmaPairs >> (c / 4) & 1 ? ex2_fma(y) : pack_f32x2(ex2(y.x), ex2(y.y)));
+    }
+}
+__device__ __forceinline__ void add_columns(const uint32_t* v, const float* neg_lse, unsigned long long scale2, uint32_t counts, unsigned long long (&part)[2]) {
+    const ulonglong2* nl = reinterpret_cast<const ulonglong2*>(neg_lse);
+#pragma unroll
+    for (int c = 0; c < 32; c += 4) {
+        const ulonglong2 n4 = nl[c / 4];
+        const float2 x = unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(v[c]), __uint_as_float(v[c + 1])), scale2, n4.x));
+        const float2 y = unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(v[c + 2]), __uint_as_float(v[c + 3])), scale2, n4.y));
+        auto one = [&](int e, float z) { return counts >> e & 1 ? ex2(z) : 0.f; };
+        part[0] = add_f32x2(part[0], pack_f32x2(one(c, x.x), one(c + 1, x.y)));
+        part[1] = add_f32x2(part[1], pack_f32x2(one(c + 2, y.x), one(c + 3, y.y)));
+    }
+}
+
 // M = 128 keys, N = n query rows (a multiple of 16), both K-major
 __device__ __forceinline__ uint32_t scores_desc(int n) { return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((128u >> 4) << 24); }
 
+template <typename Int>
 __global__ void __launch_bounds__(kWeightThreads, 1)
-kv_weights_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ WeightArgs a) {
+kv_weights_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ WeightArgs<Int> a) {
     extern __shared__ unsigned char smem_raw[];
     unsigned char* k_smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     unsigned char* q_smem = k_smem + kStages * kTileBytes;
@@ -153,9 +207,9 @@ kv_weights_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
     const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
 
     if (threadIdx.x == 0) {
-        for (int i = 0; i < kStages; ++i) { mbar_init(&hd->k_full[i], 4 * 32); mbar_init(&hd->k_empty[i], 1); }
-        for (int i = 0; i < kQStages; ++i) { mbar_init(&hd->q_full[i], 1); mbar_init(&hd->q_empty[i], 1); mbar_init(&hd->lse_full[i], 1); mbar_init(&hd->lse_empty[i], 8); }
-        for (int i = 0; i < kSegments; ++i) { mbar_init(&hd->seg_full[i], 1); mbar_init(&hd->seg_empty[i], 3 + 8 + 4); }
+        for (int i = 0; i < kStages; ++i) { mbar_init(&hd->k_full[i], 32 * kCopyWarps); mbar_init(&hd->k_empty[i], 1); }
+        for (int i = 0; i < kQStages; ++i) { mbar_init(&hd->q_full[i], 1); mbar_init(&hd->q_empty[i], 1); mbar_init(&hd->lse_full[i], 1); mbar_init(&hd->lse_empty[i], 4 * kRun); }
+        for (int i = 0; i < kSegments; ++i) { mbar_init(&hd->seg_full[i], 1); mbar_init(&hd->seg_empty[i], 3 + 4 * kRun + kCopyWarps); }
         for (int u = 0; u < kRun; ++u) { mbar_init(&hd->s_full[u], 1); mbar_init(&hd->s_free[u], 4); }
         hd->abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -173,89 +227,172 @@ kv_weights_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
     pdl_trigger();
     auto all = [](bool x) { return __all_sync(0xFFFFFFFFu, x) != 0; };
 
-    if (warp == 2) {
-        // =============================================================== planner
-        WeightWork wk = a.wk;
-        if (blockIdx.x == 0)
-            for (int s = lane; s < wk.S; s += 32) {
-                const int flaw = (nodes_bad(wk.n_new, s, wk.B) ? GOOSE_ST_BAD_NODES : 0) | (wk.seq(s).bad ? GOOSE_ST_BAD_ROWS : 0);
-                if (flaw) atomicOr(&a.status[s], flaw);
-            }
-        WeightCursor cu{};
-        WeightSeq q{};
-        long long from, to;
-        bool live = locate(wk, cu, q, from, to, blockIdx.x, lane);
-        auto advance = [&]() {
-            if (cu.next(wk, q)) return;
-            do {
-                if (++cu.s < wk.S) q = wk.seq(cu.s);
-            } while (cu.s < wk.S && q.items == 0);
-            cu.hk = cu.k = 0;
-            live = cu.s < wk.S;
-        };
-        Ring ring{0, 0};
-        for (;;) {
-            bool any = false;
-            while (live && cu.w0 < to) {
-                cu.look(wk, q, from, to);
-                any = cu.t1 > cu.t0;
-                if (any) break;
-                advance();
-            }
-            if (!wait_for(hd, &hd->seg_empty[ring.at], ring.phase ^ 1, a.status)) break;
-            Segment* sg = &hd->seg[ring.at];
-            if (lane == 0) {
-                sg->n = any ? cu.t1 - cu.t0 : 0;
-                if (any) {
-                    sg->q_first = q.first(cu.k) + cu.t0;
-                    sg->s = cu.s; sg->hk = cu.hk; sg->ctx = q.ctx; sg->nn = q.n;
-                    sg->key0 = cu.k * q.span();
-                    sg->run = min(q.run, (q.ctx + q.n - sg->key0 + kWeightTile - 1) / kWeightTile);
-                    sg->whole = cu.c0 == cu.c1; sg->slot = 2 * blockIdx.x + (cu.t0 == 0); sg->c0 = cu.c0; sg->parts = cu.c1 - cu.c0 + 1;
+    if (warp < 4) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsFew));
+        if (warp == 2) {
+            // =============================================================== planner
+            WeightWork<Int> wk = a.wk;
+            if (blockIdx.x == 0)
+                for (int s = lane; s < wk.S; s += 32) {
+                    const int flaw = (nodes_bad(wk.n_new, s, wk.B) ? GOOSE_ST_BAD_NODES : 0) | (wk.seq(s).bad ? GOOSE_ST_BAD_ROWS : 0);
+                    if (flaw) atomicOr(&a.status[s], flaw);
                 }
-            }
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&hd->seg_full[ring.at]);
-            if (!any) break;
-            ring.next(kSegments);
-            advance();
-        }
-    } else if (warp == 0) {
-        // =============================================================== Q tiles (the warp runs converged)
-        const bool leader = elect_leader();
-        uint32_t loads = 0;
-        Ring qs{0, 0}, ring{0, 0};
-        bool ok = true;
-        while (ok) {
-            ok = all(wait_for(hd, &hd->seg_full[ring.at], ring.phase, a.status));
-            if (!ok) break;
-            const Segment sg = hd->seg[ring.at];
-            __syncwarp();
-            if (leader) mbar_arrive(&hd->seg_empty[ring.at]);
-            ring.next(kSegments);
-            if (sg.n == 0) break;
-            for (int i = 0; i < sg.n; ++i) {
-                ok = all(wait_for(hd, &hd->q_empty[qs.at], qs.phase ^ 1, a.status));
-                if (!ok) break;
-                if (leader) {
-                    const int token = sg.s * a.wk.B + (sg.q_first + i) * a.wk.t;
-                    mbar_expect_tx(&hd->q_full[qs.at], (uint32_t)(a.nb * a.g) * 256u);
-                    tma_load_4d(q_smem + qs.at * kTileBytes, &tmap_q, &hd->q_full[qs.at], 0, 0, sg.hk, token);
-                    tma_load_4d(q_smem + qs.at * kTileBytes + kHalfBytes, &tmap_q, &hd->q_full[qs.at], 64, 0, sg.hk, token);
+            WeightCursor<Int> cu{};
+            WeightSeq<Int> q{};
+            Int from, to;
+            bool live = locate(wk, cu, q, from, to, blockIdx.x, lane);
+            auto advance = [&]() {
+                if (cu.next(wk, q)) return;
+                do {
+                    if (++cu.s < wk.S) q = wk.seq(cu.s);
+                } while (cu.s < wk.S && q.items == 0);
+                cu.hk = cu.k = 0;
+                live = cu.s < wk.S;
+            };
+            Ring ring{0, 0};
+            for (;;) {
+                bool any = false;
+                while (live && cu.w0 < to) {
+                    cu.look(wk, q, blockIdx.x, from, to);
+                    any = cu.t1 > cu.t0;
+                    if (any) break;
+                    advance();
+                }
+                if (!wait_for(hd, &hd->seg_empty[ring.at], ring.phase ^ 1, a.status)) break;
+                Segment* sg = &hd->seg[ring.at];
+                if (lane == 0) {
+                    sg->n = any ? cu.t1 - cu.t0 : 0;
+                    if (any) {
+                        sg->q_first = q.first(cu.k) + cu.t0;
+                        sg->s = cu.s; sg->hk = cu.hk; sg->ctx = q.ctx; sg->nn = q.n;
+                        sg->key0 = cu.k * q.span();
+                        sg->run = min(q.run, (q.ctx + q.n - sg->key0 + kWeightTile - 1) / kWeightTile);
+                        sg->whole = cu.c0 == cu.c1; sg->slot = 2 * blockIdx.x + (cu.t0 == 0); sg->c0 = cu.c0; sg->parts = cu.c1 - cu.c0 + 1;
+                    }
                 }
                 __syncwarp();
-                ++loads;
-                qs.next(kQStages);
+                if (lane == 0) mbar_arrive(&hd->seg_full[ring.at]);
+                if (!any) break;
+                ring.next(kSegments);
+                advance();
+            }
+        } else if (warp == 0) {
+            // =============================================================== Q tiles (the warp runs converged)
+            const bool leader = elect_leader();
+            uint32_t loads = 0;
+            Ring qs{0, 0}, ring{0, 0};
+            bool ok = true;
+            while (ok) {
+                ok = all(wait_for(hd, &hd->seg_full[ring.at], ring.phase, a.status));
+                if (!ok) break;
+                const Segment sg = hd->seg[ring.at];
+                __syncwarp();
+                if (leader) mbar_arrive(&hd->seg_empty[ring.at]);
+                ring.next(kSegments);
+                if (sg.n == 0) break;
+                for (int i = 0; i < sg.n; ++i) {
+                    ok = all(wait_for(hd, &hd->q_empty[qs.at], qs.phase ^ 1, a.status));
+                    if (!ok) break;
+                    if (leader) {
+                        const int token = sg.s * a.wk.B + (sg.q_first + i) * a.wk.t;
+                        mbar_expect_tx(&hd->q_full[qs.at], (uint32_t)(a.nb * a.g) * 256u);
+                        tma_load_4d(q_smem + qs.at * kTileBytes, &tmap_q, &hd->q_full[qs.at], 0, 0, sg.hk, token);
+                        tma_load_4d(q_smem + qs.at * kTileBytes + kHalfBytes, &tmap_q, &hd->q_full[qs.at], 64, 0, sg.hk, token);
+                    }
+                    __syncwarp();
+                    ++loads;
+                    qs.next(kQStages);
+                }
+            }
+            // the products' arrivals have landed, too, before the CTA ends
+            for (int i = 0; i < kQStages && ok; ++i, qs.next(kQStages)) ok = all(wait_for(hd, &hd->q_empty[qs.at], qs.phase ^ 1, a.status));
+            if (!ok)                                             // copies still in flight land before the CTA ends
+                for (uint32_t i = 0; i < kQStages; ++i)
+                    if (loads > i) drain(&hd->q_full[i], ((loads - 1 - i) / kQStages) & 1);
+        } else if (warp == 1) {
+            // =============================================================== MMA issuer
+            const bool leader = elect_leader();                  // the warp runs converged, this lane acts
+            const uint32_t q_addr = smem_u32(q_smem), k_addr = smem_u32(k_smem);
+            uint32_t k_tile = 0, used = 0;                       // K tiles in front of this segment; a bit a score buffer: its parity
+            Ring qs{0, 0}, ring{0, 0};
+            bool ok = true;
+            while (ok) {
+                ok = wait_for(hd, &hd->seg_full[ring.at], ring.phase, a.status);
+                if (!ok) break;
+                const Segment* sg = &hd->seg[ring.at];
+                const int n = __shfl_sync(0xFFFFFFFFu, sg->n, 0), run = __shfl_sync(0xFFFFFFFFu, sg->run, 0);
+                const int q_first = __shfl_sync(0xFFFFFFFFu, sg->q_first, 0), nn = __shfl_sync(0xFFFFFFFFu, sg->nn, 0);
+                __syncwarp();
+                if (leader) mbar_arrive(&hd->seg_empty[ring.at]);
+                ring.next(kSegments);
+                if (n == 0) break;
+                for (int i = 0; i < n && ok; ++i) {
+                    ok = wait_for(hd, &hd->q_full[qs.at], qs.phase, a.status);
+                    if (!ok) break;
+                    const int rows = min(nn - (q_first + i) * a.wk.t, a.wk.t) * a.g;
+                    const uint32_t idesc = scores_desc((rows + 15) & ~15);
+                    const uint32_t q_lo = smem_desc_lo(q_addr + qs.at * kTileBytes, 16);
+                    for (int u = 0; u < run; ++u) {
+                        const uint32_t load = k_tile + u, at = load % kStages;
+                        if (i == 0 && !(ok = wait_for(hd, &hd->k_full[at], load / kStages & 1, a.status))) break;
+                        if (!(ok = wait_for(hd, &hd->s_free[u], (used >> u & 1) ^ 1, a.status))) break;
+                        used ^= 1u << u;
+                        fence_proxy_async();                     // (the copies of the keys)
+                        tc_fence_after();
+                        const uint32_t k_lo = smem_desc_lo(k_addr + at * kTileBytes, 16);
+#pragma unroll
+                        for (int kk = 0; kk < 8; ++kk) {         // 16 of the 128 head dims per instruction
+                            const uint32_t off = ((kk >> 2) * kHalfBytes + (kk & 3) * 32) >> 4;
+                            umma_f16_by(leader, tmem + u * 128, smem_desc(k_lo + off), smem_desc(q_lo + off), idesc, kk > 0 ? 1u : 0u);
+                        }
+                        umma_commit_by(leader, &hd->s_full[u]);
+                        if (i == n - 1) umma_commit_by(leader, &hd->k_empty[at]);
+                    }
+                    if (!ok) break;
+                    umma_commit_by(leader, &hd->q_empty[qs.at]);
+                    qs.next(kQStages);
+                }
+                k_tile += run;
+            }
+        } else if (warp == 3) {
+            // =============================================================== log-sum-exps
+            Ring qs{0, 0}, ring{0, 0};
+            bool ok = true;
+            while (ok) {
+                ok = all(wait_for(hd, &hd->seg_full[ring.at], ring.phase, a.status));
+                if (!ok) break;
+                const Segment sg = hd->seg[ring.at];
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&hd->seg_empty[ring.at]);
+                ring.next(kSegments);
+                if (sg.n == 0) break;
+                for (int i = 0; i < sg.n; ++i) {
+                    const int t0 = (sg.q_first + i) * a.wk.t, rows = min(sg.nn - t0, a.wk.t) * a.g;
+                    const float* lse = a.lse + ((size_t)sg.s * a.wk.B + t0) * a.H + sg.hk * a.g;
+                    float x[4];
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        const int r = 32 * w + lane, token = r / a.g;
+                        x[w] = r < rows ? lse[(size_t)token * a.H + (r - token * a.g)] : -INFINITY;
+                    }
+                    ok = all(wait_for(hd, &hd->lse_empty[qs.at], qs.phase ^ 1, a.status));
+                    if (!ok) break;
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        const uint32_t word = __ballot_sync(0xFFFFFFFFu, x[w] != -INFINITY);   // (NaN counts)
+                        hd->lse[qs.at][32 * w + lane] = -kLog2e * x[w];
+                        if (lane == 0) hd->counts[qs.at][w] = word;
+                    }
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&hd->lse_full[qs.at]);
+                    qs.next(kQStages);
+                }
             }
         }
-        // the products' arrivals have landed, too, before the CTA ends
-        for (int i = 0; i < kQStages && ok; ++i, qs.next(kQStages)) ok = all(wait_for(hd, &hd->q_empty[qs.at], qs.phase ^ 1, a.status));
-        if (!ok)                                             // copies still in flight land before the CTA ends
-            for (uint32_t i = 0; i < kQStages; ++i)
-                if (loads > i) drain(&hd->q_full[i], ((loads - 1 - i) / kQStages) & 1);
-    } else if (warp >= 12) {
+    } else if (warp >= kCopyWarp) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsFew));
         // =============================================================== K tiles: 32 keys of a tile a warp
-        const int part = warp - 12;
+        const int part = warp - kCopyWarp;
         const uint32_t k_addr = smem_u32(k_smem) + 4096 * part;
         const unsigned long long pol_once = l2_policy_evict_first(), pol_again = l2_policy_evict_last();
         // 16 bytes of a row a lane, two rows at a time; where they go in a tile of swizzled rows, for each of four such pairs of rows
@@ -312,190 +449,89 @@ kv_weights_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
         }
         for (int i = 0; i < kStages && ok; ++i, ks.next(kStages)) ok = all(wait_for(hd, &hd->k_empty[ks.at], ks.phase ^ 1, a.status));
         if (!ok) cp_async_wait_all();
-    } else if (warp == 1) {
-        // =============================================================== MMA issuer
-        const bool leader = elect_leader();                  // the warp runs converged, this lane acts
-        const uint32_t q_addr = smem_u32(q_smem), k_addr = smem_u32(k_smem);
-        uint32_t k_tile = 0, used = 0;                       // K tiles in front of this segment; a bit a score buffer: its parity
-        Ring qs{0, 0}, ring{0, 0};
-        bool ok = true;
-        while (ok) {
-            ok = wait_for(hd, &hd->seg_full[ring.at], ring.phase, a.status);
-            if (!ok) break;
-            const Segment* sg = &hd->seg[ring.at];
-            const int n = __shfl_sync(0xFFFFFFFFu, sg->n, 0), run = __shfl_sync(0xFFFFFFFFu, sg->run, 0);
-            const int q_first = __shfl_sync(0xFFFFFFFFu, sg->q_first, 0), nn = __shfl_sync(0xFFFFFFFFu, sg->nn, 0);
-            __syncwarp();
-            if (leader) mbar_arrive(&hd->seg_empty[ring.at]);
-            ring.next(kSegments);
-            if (n == 0) break;
-            for (int i = 0; i < n && ok; ++i) {
-                ok = wait_for(hd, &hd->q_full[qs.at], qs.phase, a.status);
-                if (!ok) break;
-                const int rows = min(nn - (q_first + i) * a.wk.t, a.wk.t) * a.g;
-                const uint32_t idesc = scores_desc((rows + 15) & ~15);
-                const uint32_t q_lo = smem_desc_lo(q_addr + qs.at * kTileBytes, 16);
-                for (int u = 0; u < run; ++u) {
-                    const uint32_t load = k_tile + u, at = load % kStages;
-                    if (i == 0 && !(ok = wait_for(hd, &hd->k_full[at], load / kStages & 1, a.status))) break;
-                    if (!(ok = wait_for(hd, &hd->s_free[u], (used >> u & 1) ^ 1, a.status))) break;
-                    used ^= 1u << u;
-                    fence_proxy_async();                     // (the copies of the keys)
-                    tc_fence_after();
-                    const uint32_t k_lo = smem_desc_lo(k_addr + at * kTileBytes, 16);
-#pragma unroll
-                    for (int kk = 0; kk < 8; ++kk) {         // 16 of the 128 head dims per instruction
-                        const uint32_t off = ((kk >> 2) * kHalfBytes + (kk & 3) * 32) >> 4;
-                        umma_f16_by(leader, tmem + u * 128, smem_desc(k_lo + off), smem_desc(q_lo + off), idesc, kk > 0 ? 1u : 0u);
-                    }
-                    umma_commit_by(leader, &hd->s_full[u]);
-                    if (i == n - 1) umma_commit_by(leader, &hd->k_empty[at]);
-                }
-                if (!ok) break;
-                umma_commit_by(leader, &hd->q_empty[qs.at]);
-                qs.next(kQStages);
-            }
-            k_tile += run;
-        }
-    } else if (warp == 3) {
-        // =============================================================== log-sum-exps
-        Ring qs{0, 0}, ring{0, 0};
-        bool ok = true;
-        while (ok) {
-            ok = all(wait_for(hd, &hd->seg_full[ring.at], ring.phase, a.status));
-            if (!ok) break;
-            const Segment sg = hd->seg[ring.at];
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&hd->seg_empty[ring.at]);
-            ring.next(kSegments);
-            if (sg.n == 0) break;
-            for (int i = 0; i < sg.n; ++i) {
-                const int t0 = (sg.q_first + i) * a.wk.t, rows = min(sg.nn - t0, a.wk.t) * a.g;
-                const float* lse = a.lse + ((size_t)sg.s * a.wk.B + t0) * a.H + sg.hk * a.g;
-                float x[4];
-#pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    const int r = 32 * w + lane, token = r / a.g;
-                    x[w] = r < rows ? lse[(size_t)token * a.H + (r - token * a.g)] : -INFINITY;
-                }
-                ok = all(wait_for(hd, &hd->lse_empty[qs.at], qs.phase ^ 1, a.status));
-                if (!ok) break;
-#pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    const uint32_t word = __ballot_sync(0xFFFFFFFFu, x[w] != -INFINITY);   // (NaN counts)
-                    hd->lse[qs.at][32 * w + lane] = -kLog2e * x[w];
-                    if (lane == 0) hd->counts[qs.at][w] = word;
-                }
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&hd->lse_full[qs.at]);
-                qs.next(kQStages);
-            }
-        }
     } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsMany));
         // =============================================================== exponentials and sums
-        const int l = (warp - 4) >> 2, wq = warp & 3;        // key tiles l and l + 2 of a run
-        const int row = 32 * wq + lane;                      // TMEM lane == key of a tile
-        const uint32_t s_addr = tmem + ((uint32_t)(32 * wq) << 16);
-        uint32_t used = 0;                                   // a bit a score buffer: its parity
+        const int u = (warp - kSumWarp) >> 2, wq = warp & 3; // key tile of a run
+        const int row = 32 * wq + lane;                      // TMEM lane == key of the tile
+        const uint32_t from = tmem + u * 128 + ((uint32_t)(32 * wq) << 16);
+        const unsigned long long scale2 = pack_f32x2(a.scale_log2, a.scale_log2);
+        uint32_t used = 0;                                   // the score buffer's parity
         Ring qs{0, 0}, ring{0, 0};
         bool ok = true;
         while (ok) {
             ok = all(wait_for(hd, &hd->seg_full[ring.at], ring.phase, a.status));
             if (!ok) break;
             const Segment& sg = hd->seg[ring.at];
-            if (sg.n == 0) break;
-            float sum[2] = {0.f, 0.f};
-            int page[2] = {-1, -1};                          // of the rows, looked at when the sums are there
-            bool mine[2] = {false, false};
-            float* weight = a.row_weight + ((size_t)sg.s * a.wk.Hkv + sg.hk) * a.ldw + sg.key0 + row;
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int u = l + 2 * e, j = sg.key0 + u * kWeightTile + row;
-                mine[e] = u < sg.run && j < sg.ctx + sg.nn;
-                if (mine[e]) page[e] = a.pages.table[sg.s * a.pages.ldt + (j >> a.pages.size_log2)];
-            }
-            for (int i = 0; i < sg.n; ++i) {
+            const int n = sg.n;
+            if (n == 0) break;
+            const bool live = u < sg.run;
+            const int ahead = sg.key0 + u * kWeightTile - sg.ctx, g = a.g;   // tokens of the chunk in front of the first that sees the tile's first key
+            const bool mine = live && ahead + row < sg.nn;
+            const int page = mine ? a.pages.table[sg.s * a.pages.ldt + ((ahead + sg.ctx + row) >> a.pages.size_log2)] : -1;   // (looked at when the sum is there)
+            float sum = 0.f;
+            int t0 = sg.q_first * a.wk.t, left = sg.nn - t0;
+            for (int i = 0; i < n; ++i, t0 += a.wk.t, left -= a.wk.t) {
                 ok = all(wait_for(hd, &hd->lse_full[qs.at], qs.phase, a.status));
                 if (!ok) break;
-                const int t0 = (sg.q_first + i) * a.wk.t, rows = min(sg.nn - t0, a.wk.t) * a.g;
-                const uint4 counts = *reinterpret_cast<const uint4*>(hd->counts[qs.at]);
-                const bool every = (counts.x & counts.y & counts.z & counts.w) == 0xFFFFFFFFu;
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const int u = l + 2 * e;
-                    if (u >= sg.run) break;
-                    ok = all(wait_for(hd, &hd->s_full[u], used >> u & 1, a.status));
+                if (live) {
+                    ok = all(wait_for(hd, &hd->s_full[u], used, a.status));
                     if (!ok) break;
-                    used ^= 1u << u;
+                    used ^= 1;
                     tc_fence_after();
-                    const int tile0 = sg.key0 + u * kWeightTile;
-                    const int behind = tile0 + row - sg.ctx - t0;    // tokens of the Q tile in front of the first that sees the key
-                    const bool masked = !every || tile0 + kWeightTile - 1 - sg.ctx > t0;
-                    uint32_t cw[4] = {counts.x, counts.y, counts.z, counts.w};
-                    if (masked) {
-                        const int from = max(behind, 0) * a.g;       // columns in front of it do not count
-#pragma unroll
-                        for (int w = 0; w < 4; ++w) cw[w] &= from <= 32 * w ? 0xFFFFFFFFu : from >= 32 * w + 32 ? 0u : 0xFFFFFFFFu << (from - 32 * w);
-                    }
-                    const unsigned long long scale2 = pack_f32x2(a.scale_log2, a.scale_log2);
+                    const int rows = min(left, a.wk.t) * g;
+                    const uint32_t* counts = hd->counts[qs.at];
+                    const float* neg_lse = hd->lse[qs.at];
+                    const bool masked = (counts[0] & counts[1] & counts[2] & counts[3]) != 0xFFFFFFFFu || ahead + kWeightTile - 1 > t0;
+                    const int first = max(ahead + row - t0, 0) * g;  // columns in front of it are tokens in front of the key
                     unsigned long long part[2] = {0, 0};
-                    uint32_t v[32];
-#pragma unroll
-                    for (int w = 0; w < 4; ++w) {
-                        if (32 * w >= rows) break;
-                        TMEM_LD32(s_addr + u * 128 + 32 * w, v, 0);
+#pragma unroll 1
+                    for (int w = 0; 32 * w < rows; ++w) {
+                        uint32_t v[32];
+                        TMEM_LD32(from + 32 * w, v, 0);
                         tmem_wait_ld();
-                        const ulonglong2* nl = reinterpret_cast<const ulonglong2*>(&hd->lse[qs.at][32 * w]);
-#pragma unroll
-                        for (int c = 0; c < 32; c += 4) {
-                            const ulonglong2 n4 = nl[c / 4];
-                            const float2 x = unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(v[c]), __uint_as_float(v[c + 1])), scale2, n4.x));
-                            const float2 y = unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(v[c + 2]), __uint_as_float(v[c + 3])), scale2, n4.y));
-                            float p0 = ex2(x.x), p1 = ex2(x.y), p2 = ex2(y.x), p3 = ex2(y.y);
-                            if (masked) {
-                                p0 = cw[w] >> c & 1 ? p0 : 0.f; p1 = cw[w] >> (c + 1) & 1 ? p1 : 0.f;
-                                p2 = cw[w] >> (c + 2) & 1 ? p2 : 0.f; p3 = cw[w] >> (c + 3) & 1 ? p3 : 0.f;
-                            }
-                            part[0] = add_f32x2(part[0], pack_f32x2(p0, p1));
-                            part[1] = add_f32x2(part[1], pack_f32x2(p2, p3));
+                        if (32 * w + 32 >= rows) {                   // all scores are in registers, or have been
+                            tc_fence_before();
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(&hd->s_free[u]);
+                        }
+                        if (!masked) {
+                            add_columns(v, neg_lse + 32 * w, scale2, part);
+                        } else {
+                            const int out = first - 32 * w;
+                            add_columns(v, neg_lse + 32 * w, scale2, counts[w] & (out <= 0 ? 0xFFFFFFFFu : out >= 32 ? 0u : 0xFFFFFFFFu << out), part);
                         }
                     }
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&hd->s_free[u]);
                     const float2 s2 = unpack_f32x2(add_f32x2(part[0], part[1]));
-                    sum[e] += s2.x + s2.y;
+                    sum += s2.x + s2.y;
                 }
-                if (!ok) break;
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&hd->lse_empty[qs.at]);
                 qs.next(kQStages);
             }
             if (!ok) break;
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int u = l + 2 * e;
-                if (u >= sg.run) break;
-                const bool there = page[e] >= 0 && page[e] < a.pages.n;
-                if (mine[e] && !there) atomicOr(&a.status[sg.s], GOOSE_ST_BAD_ROWS);
-                // (a reduction: nobody waits for what the row had.  One a row and call: the order of the calls is the order of the sums)
-                if (sg.whole) {
-                    if (there) atomicAdd(weight + u * kWeightTile, sum[e]);
-                    continue;
+            if (live) {
+                const bool there = page >= 0 && page < a.pages.n;
+                if (mine && !there) atomicOr(&a.status[sg.s], GOOSE_ST_BAD_ROWS);
+                float* weight = a.row_weight + ((size_t)sg.s * a.wk.Hkv + sg.hk) * a.ldw + sg.key0 + u * kWeightTile + row;
+                bool last = true;
+                if (!sg.whole) {
+                    a.sums[((size_t)sg.slot * kRun + u) * kWeightTile + row] = sum;
+                    __threadfence();
+                    __syncwarp();
+                    int32_t* counter = a.counters + (sg.c0 * kRun + u) * 4 + wq;
+                    int came = 0;
+                    if (lane == 0) came = atomicAdd(counter, 1);
+                    last = __shfl_sync(0xFFFFFFFFu, came, 0) == sg.parts - 1;
+                    if (last) {
+                        __threadfence();
+                        if (lane == 0) *counter = 0;
+                        sum = 0.f;
+                        for (int k = 0; k < sg.parts; ++k) sum += __ldcg(&a.sums[((size_t)(2 * (sg.c0 + k) + (k == 0)) * kRun + u) * kWeightTile + row]);
+                    }
                 }
-                a.sums[((size_t)sg.slot * kRun + u) * kWeightTile + row] = sum[e];
-                __threadfence();
-                __syncwarp();
-                int32_t* counter = a.counters + (sg.c0 * kRun + u) * 4 + wq;
-                int last = 0;
-                if (lane == 0) last = atomicAdd(counter, 1) == sg.parts - 1;
-                if (!__shfl_sync(0xFFFFFFFFu, last, 0)) continue;
-                __threadfence();
-                if (lane == 0) *counter = 0;
-                float total = 0.f;
-                for (int k = 0; k < sg.parts; ++k)
-                    total += __ldcg(&a.sums[((size_t)(2 * (sg.c0 + k) + (k == 0)) * kRun + u) * kWeightTile + row]);
-                if (there) atomicAdd(weight + u * kWeightTile, total);
+                // (a reduction: nobody waits for what the row had.  One a row and call: the order of the calls is the order of the sums)
+                if (last && there) atomicAdd(weight, sum);
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(&hd->seg_empty[ring.at]);
@@ -514,10 +550,9 @@ kv_weights_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
 
 }  // namespace
 
-cudaError_t launch_kv_weights(goose_ctx* c, const KvWeights& x, cudaStream_t st) {
-    if (!c->encode_tiled) return cudaErrorNotSupported;
-    if (x.S == 0) return cudaSuccess;
-    WeightArgs a{};
+template <typename Int>
+static cudaError_t launch_as(goose_ctx* c, const KvWeights& x, cudaStream_t st) {
+    WeightArgs<Int> a{};
     a.g = x.H / x.Hkv; a.H = x.H;
     a.wk.ctx_len = x.ctx_len; a.wk.n_new = x.n_new; a.wk.S = x.S; a.wk.B = x.B; a.wk.Hkv = x.Hkv; a.wk.G = c->num_sms;
     a.wk.t = kWeightTile / a.g; a.wk.room = (int)x.pages.room(x.ldw); a.wk.short_run = 1;
@@ -529,11 +564,21 @@ cudaError_t launch_kv_weights(goose_ctx* c, const KvWeights& x, cudaStream_t st)
     a.sums = c->weight_sums; a.counters = c->weight_counters; a.status = c->status;
     CUtensorMap mq;
     if (!make_q_map(c->encode_tiled, &mq, x.q, (int64_t)x.S * x.B, x.Hkv, a.g, a.nb)) return cudaErrorInvalidValue;
-    cudaError_t e = launch_pdl(kv_weights_kernel, dim3(c->num_sms), dim3(kWeightThreads), kWeightSmem, st, mq, a);
+    cudaError_t e = launch_pdl(kv_weights_kernel<Int>, dim3(c->num_sms), dim3(kWeightThreads), kWeightSmem, st, mq, a);
     c->launches++;
     return e;
 }
 
-cudaError_t init_weights_kernels() { return cudaFuncSetAttribute(kv_weights_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kWeightSmem); }
+cudaError_t launch_kv_weights(goose_ctx* c, const KvWeights& x, cudaStream_t st) {
+    if (!c->encode_tiled) return cudaErrorNotSupported;
+    if (x.S == 0) return cudaSuccess;
+    const bool small = WeightWork<int>::most(x.S, x.B, x.Hkv, kWeightTile / (x.H / x.Hkv), (int)x.pages.room(x.ldw)) < kShortWeightPlaces;
+    return small ? launch_as<int>(c, x, st) : launch_as<long long>(c, x, st);
+}
+
+cudaError_t init_weights_kernels() {
+    cudaError_t e = cudaFuncSetAttribute(kv_weights_kernel<int>, cudaFuncAttributeMaxDynamicSharedMemorySize, kWeightSmem);
+    return e == cudaSuccess ? cudaFuncSetAttribute(kv_weights_kernel<long long>, cudaFuncAttributeMaxDynamicSharedMemorySize, kWeightSmem) : e;
+}
 
 }  // namespace goose

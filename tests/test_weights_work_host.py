@@ -18,30 +18,31 @@ SOURCE = r"""
 #include "weights_work.cuh"
 using namespace goose;
 // 0, or what is wrong
-extern "C" int walk(int S, int B, int Hkv, int t, int G, int room, const int32_t* ctx_len, const int32_t* n_new, double* worst) {
-    WeightWork wk{};
+template <typename Int>
+static int walk_as(int S, int B, int Hkv, int t, int G, int room, const int32_t* ctx_len, const int32_t* n_new, double* worst) {
+    WeightWork<Int> wk{};
     wk.ctx_len = ctx_len; wk.n_new = n_new; wk.S = S; wk.B = B; wk.Hkv = Hkv; wk.G = G; wk.t = t; wk.room = room;
-    long long sum = 0, tiles = 0;
+    Int sum = 0, tiles = 0;
     bool several = false;
     wk.short_run = 1;
     for (int s = 0; s < S; ++s) {
-        const WeightSeq q = wk.seq(s);
+        const WeightSeq<Int> q = wk.seq(s);
         if (q.n > t) several = true; else tiles += q.items;
     }
     wk.set_run(tiles);
-    for (int s = 0; s < S; ++s) { const WeightSeq q = wk.seq(s); sum += q.before(q.items); }
+    for (int s = 0; s < S; ++s) { const WeightSeq<Int> q = wk.seq(s); sum += q.before(q.items); }
     wk.set(sum, several);
     std::map<std::tuple<int, int, int>, std::pair<int, int>> dealt;      // item -> (Q tiles so far, CTAs so far)
     long long longest = 0, all = 0;
     for (int c = 0; c < G; ++c) {
-        const long long from = wk.start(c), to = wk.start(c + 1);
+        const Int from = wk.start(c), to = wk.start(c + 1);
         if (from >= to) continue;
-        WeightCursor cu{};
-        long long begin = 0, mine = 0;
-        WeightSeq q{};
+        WeightCursor<Int> cu{};
+        Int begin = 0; long long mine = 0;
+        WeightSeq<Int> q{};
         for (cu.s = 0; cu.s < S; ++cu.s) {
             q = wk.seq(cu.s);
-            const long long all = Hkv * q.before(q.items);
+            const Int all = Hkv * q.before(q.items);
             if (from < begin + all) break;
             begin += all;
         }
@@ -50,7 +51,7 @@ extern "C" int walk(int S, int B, int Hkv, int t, int G, int room, const int32_t
         if (cu.hk < 0 || cu.hk >= Hkv || cu.k < 0 || cu.k >= q.items || cu.w0 > from || cu.w0 + q.width(cu.k) <= from) return 2;
         int heads = 0, tails = 0;
         while (cu.w0 < to) {
-            cu.look(wk, q, from, to);
+            cu.look(wk, q, c, from, to);
             if (cu.T < 1) return 3;
             if (cu.t1 > cu.t0) {
                 auto& d = dealt[{cu.s, cu.hk, cu.k}];
@@ -63,7 +64,7 @@ extern "C" int walk(int S, int B, int Hkv, int t, int G, int room, const int32_t
                 heads += !starts; tails += starts && !ends;
             }
             if (!cu.next(wk, q)) {
-                do { ++cu.s; q = cu.s < S ? wk.seq(cu.s) : WeightSeq{}; } while (cu.s < S && q.items == 0);
+                do { ++cu.s; q = cu.s < S ? wk.seq(cu.s) : WeightSeq<Int>{}; } while (cu.s < S && q.items == 0);
                 if (cu.s == S) break;
                 cu.hk = cu.k = 0;
             }
@@ -72,7 +73,7 @@ extern "C" int walk(int S, int B, int Hkv, int t, int G, int room, const int32_t
         longest = std::max(longest, mine); all += mine;
     }
     for (int s = 0; s < S; ++s) {
-        const WeightSeq q = wk.seq(s);
+        const WeightSeq<Int> q = wk.seq(s);
         int n = n_new ? (n_new[s] < 0 || n_new[s] > B ? 0 : n_new[s]) : B;
         if (q.bad) n = 0;
         const long long keys = n ? (long long)ctx_len[s] + n : 0;
@@ -88,7 +89,12 @@ extern "C" int walk(int S, int B, int Hkv, int t, int G, int room, const int32_t
         }
     }
     *worst = all ? (double)longest * G / all : 0;
-    return 0;
+    return (double)wk.total <= WeightWork<Int>::most(S, B, Hkv, t, room) ? 0 : 11;
+}
+extern "C" int walk(int S, int B, int Hkv, int t, int G, int room, const int32_t* ctx_len, const int32_t* n_new, double* worst) {
+    const int rc = walk_as<long long>(S, B, Hkv, t, G, room, ctx_len, n_new, worst);
+    if (rc) return rc;
+    return WeightWork<int>::most(S, B, Hkv, t, room) < kShortWeightPlaces ? 100 * walk_as<int>(S, B, Hkv, t, G, room, ctx_len, n_new, worst) : 0;
 }
 """
 
