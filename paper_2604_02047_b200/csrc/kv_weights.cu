@@ -38,8 +38,6 @@ constexpr uint32_t kTmemCols = 512;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr long long kWaitCycles = 2000000000ll;              // bound of every wait: about one second of SM clock
 constexpr int kSegments = 6;
-// which second pairs of columns of four, of 32, get their exponentials from the FMA pipe
-constexpr uint32_t kFmaPairs = 0xEE;
 
 // a segment, as the planner describes it
 struct Segment {
@@ -152,24 +150,7 @@ __device__ __forceinline__ bool locate(WeightWork<Int>& wk, WeightCursor<Int>& c
     return false;
 }
 
-// 2^x of two numbers x <= 0 on the FMA pipe: x = n + f with |f| <= 1/2 (adding 1.5 2^23 + 127 rounds x to n and leaves n + 127 in the low bits),
-// a minimax polynomial of degree 4 for 2^f (relative error 2.7e-6, of either sign), times 2^n.  NaN stays NaN; x above 0 is not met by probabilities
-// and saturates at 2^127.
-__device__ __forceinline__ unsigned long long ex2_fma(float2 x) {
-    asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.x) : "f"(-126.f));
-    asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.y) : "f"(-126.f));
-    asm("min.NaN.f32 %0, %0, %1;" : "+f"(x.x) : "f"(127.f));
-    asm("min.NaN.f32 %0, %0, %1;" : "+f"(x.y) : "f"(127.f));
-    auto both = [](float c) { return pack_f32x2(c, c); };
-    constexpr float kRound = 12582912.f + 127.f;
-    const unsigned long long v = pack_f32x2(x.x, x.y), r = add_f32x2(v, both(kRound)), f = fma_f32x2(add_f32x2(r, both(-kRound)), both(-1.f), v);
-    unsigned long long p = both(0.009570102f);
-    for (float c : {0.055917859f, 0.24024744f, 0.69312179f, 0.99999928f}) p = fma_f32x2(p, f, both(c));
-    const float2 n = unpack_f32x2(r);
-    return mul_f32x2(p, pack_f32x2(__uint_as_float(__float_as_uint(n.x) << 23), __uint_as_float(__float_as_uint(n.y) << 23)));
-}
-
-// sums over 32 columns of exp2(score * scale - lse): all of them, some of the exponentials by the FMA pipe; those of a mask
+// sums over 32 columns of exp2(score * scale - lse): all of them; those of a mask
 __device__ __forceinline__ void add_columns(const uint32_t* v, const float* neg_lse, unsigned long long scale2, unsigned long long (&part)[2]) {
     const ulonglong2* nl = reinterpret_cast<const ulonglong2*>(neg_lse);
 #pragma unroll
@@ -178,7 +159,7 @@ __device__ __forceinline__ void add_columns(const uint32_t* v, const float* neg_
         const float2 x = unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(v[c]), __uint_as_float(v[c + 1])), scale2, n4.x));
         const float2 y = unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(v[c + 2]), __uint_as_float(v[c + 3])), scale2, n4.y));
         part[0] = add_f32x2(part[0], pack_f32x2(ex2(x.x), ex2(x.y)));
-        part[1] = add_f32x2(part[1], kFmaPairs >> (c / 4) & 1 ? ex2_fma(y) : pack_f32x2(ex2(y.x), ex2(y.y)));
+        part[1] = add_f32x2(part[1], pack_f32x2(ex2(y.x), ex2(y.y)));
     }
 }
 __device__ __forceinline__ void add_columns(const uint32_t* v, const float* neg_lse, unsigned long long scale2, uint32_t counts, unsigned long long (&part)[2]) {
