@@ -1,9 +1,12 @@
 // Eviction: the rows of a key/value head that stay, and the rows behind the budget among them to the places of those in front of it that do not.
 //
 // A row's key is an unsigned number in the order of what stays: the first and the latest positions above everything, then the weights, NaN below all.
-// The budget-th largest key is found digit by digit (eight bits a pass, a histogram a pass); of the rows that have that very key the lowest stay.
-// The first kernel, a block a (sequence, head), leaves a list of (place, row) pairs; the second copies the rows.  Places lie in front of the
-// budget, rows behind it, so that no copy reads what another one writes.
+// The budget-th largest key is found digit by digit (11, 11 and 10 bits: the first has the exponent and two bits more, so that weights spread over some
+// fifty of its counters); of the rows that have that very key the lowest stay.
+// The first kernel, a block a (sequence, head), reads weights and positions once, has the keys in shared memory, and leaves a list of (place, row) pairs;
+// the second copies the rows.  Places lie in front of the budget, rows behind it, so that no copy reads what another one writes.
+#include <algorithm>
+
 #include "goose_internal.cuh"
 
 namespace goose {
@@ -11,6 +14,11 @@ namespace goose {
 constexpr int kEvictThreads = 1024;
 constexpr int kEvictWarps = kEvictThreads / 32;
 constexpr int kMoveThreads = 256;
+constexpr int kMovesOnce = 2;
+constexpr int kBins = 2 * kEvictThreads;              // counters of a digit
+constexpr int kMostKeys = 24576;                      // keys in shared memory: two blocks an SM; rows behind them are looked up again
+constexpr int kSelectSmem = 212992;                   // of a block, at most (a bit a row and the keys)
+static_assert(GOOSE_MAX_PAGED_ROWS / 8 < kSelectSmem, "a bit a row");
 constexpr int kMovesAhead = 4;                        // words that stand in front of a head's list (its length)
 
 // of the row's position and weight
@@ -45,11 +53,13 @@ __device__ __forceinline__ int block_prefix(int v, int* s_warp, int& total) {
 }
 
 __global__ void __launch_bounds__(kEvictThreads)
-evict_select_kernel(const EvictKv a, int32_t* __restrict__ moves, int64_t moves_ld, int32_t* __restrict__ status) {
+evict_select_kernel(const EvictKv a, int32_t* __restrict__ moves, int64_t moves_ld, int keep_words, int keys_there, int32_t* __restrict__ status) {
     extern __shared__ uint32_t s_keep[];              // a bit a row: it stays
-    __shared__ int s_hist[256], s_warp[kEvictWarps], s_digit, s_above;
+    uint32_t* const s_key = s_keep + keep_words;      // of the first keys_there rows
+    __shared__ int s_hist[kBins], s_warp[kEvictWarps], s_digit, s_above;
     const int s = blockIdx.y, hk = blockIdx.x, tid = threadIdx.x, lane = tid & 31;
     const size_t head = (size_t)s * a.Hkv + hk;
+    for (int b = tid; b < kBins; b += kEvictThreads) s_hist[b] = 0;
     pdl_wait();
     pdl_trigger();
     const int ctx = a.ctx_len[s], off = a.pos_off ? a.pos_off[s] : 0, left = min(ctx, a.budget);
@@ -66,41 +76,53 @@ evict_select_kernel(const EvictKv a, int32_t* __restrict__ moves, int64_t moves_
         list[0] = 0;
         if (hk == 0) {
             a.new_ctx_len[s] = bad ? ctx : left;
-            a.new_pos_off[s] = bad ? off : off + (ctx - left);
+            a.new_pos_off[s] = bad ? off : (int)((int64_t)off + (ctx - left));
             if (bad) atomicOr(&status[s], GOOSE_ST_BAD_ROWS);
         }
     }
     if (bad) return;
-    const float* weight = a.row_weight + head * a.ldw;
-    const int32_t* pos = a.row_pos + head * a.ldw;
-    float* new_weight = a.new_weight + head * a.ldw_new;
-    int32_t* new_pos = a.new_pos + head * a.ldw_new;
+    const float* __restrict__ weight = a.row_weight + head * a.ldw;
+    const int32_t* __restrict__ pos = a.row_pos + head * a.ldw;
+    float* __restrict__ new_weight = a.new_weight + head * a.ldw_new;
+    int32_t* __restrict__ new_pos = a.new_pos + head * a.ldw_new;
     if (ctx <= a.budget) {
+#pragma unroll 4
         for (int j = tid; j < ctx; j += kEvictThreads) { new_weight[j] = weight[j]; new_pos[j] = pos[j]; }
         return;
     }
     const int64_t recent_from = (int64_t)off + ctx - a.recent;
-    auto key = [&](int j) { return evict_key(weight[j], pos[j], a.sink, recent_from); };
+    auto key = [&](int j) { return j < keys_there ? s_key[j] : evict_key(weight[j], pos[j], a.sink, recent_from); };
     // the budget-th largest key: its upper digits so far, and how many of the rows that have them are still to be taken
     uint32_t prefix = 0;
-    int need = a.budget;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        if (tid < 256) s_hist[tid] = 0;
-        __syncthreads();
-        for (int j = tid; j < ctx; j += kEvictThreads) {
-            const uint32_t k = key(j);
-            if (shift == 24 || k >> (shift + 8) == prefix) atomicAdd(&s_hist[k >> shift & 255], 1);
+    int need = a.budget, total;
+    for (const int shift : {21, 10, 0}) {
+        const int digit_bits = shift == 0 ? 10 : 11;
+        if (shift == 21) {
+#pragma unroll 8
+            for (int j = tid; j < ctx; j += kEvictThreads) {
+                const uint32_t k = evict_key(weight[j], pos[j], a.sink, recent_from);
+                if (j < keys_there) s_key[j] = k;
+                atomicAdd(&s_hist[k >> 21], 1);
+            }
+        } else {
+            for (int j = tid; j < ctx; j += kEvictThreads) {
+                const uint32_t k = key(j);
+                if (k >> (shift + digit_bits) == prefix) atomicAdd(&s_hist[k >> shift & ((1 << digit_bits) - 1)], 1);
+            }
         }
         __syncthreads();
-        // thread t has digit 255 - t: how many rows have a larger one
-        const int mine = tid < 256 ? s_hist[255 - tid] : 0;
-        int total;
-        const int above = block_prefix(mine, s_warp, total);
-        if (tid < 256 && above < need && above + mine >= need) { s_digit = 255 - tid; s_above = above; }
+        // thread t has the digits kBins - 1 - 2 t and the one below: how many rows have a larger one
+        const int high = kBins - 1 - 2 * tid, mine = s_hist[high], below = s_hist[high - 1];
+        const int above = block_prefix(mine + below, s_warp, total);
+        if (above < need && above + mine + below >= need) {
+            const bool first = above + mine >= need;
+            s_digit = first ? high : high - 1;
+            s_above = first ? above : above + mine;
+        }
+        s_hist[high] = s_hist[high - 1] = 0;
         __syncthreads();
-        prefix = prefix << 8 | (uint32_t)s_digit;
+        prefix = prefix << digit_bits | (uint32_t)s_digit;
         need -= s_above;
-        __syncthreads();
     }
     // what stays, in words of 32 rows; a warp's rows are consecutive
     const int words = (ctx + 31) >> 5, per = (words + kEvictWarps - 1) / kEvictWarps;
@@ -111,7 +133,6 @@ evict_select_kernel(const EvictKv a, int32_t* __restrict__ moves, int64_t moves_
         const uint32_t k = j < ctx ? key(j) : 0u;
         equal += __popc(__ballot_sync(0xFFFFFFFFu, j < ctx && k == prefix));
     }
-    int total;
     int before = block_prefix(lane == 0 ? equal : 0, s_warp, total);
     before = __shfl_sync(0xFFFFFFFFu, before, 0);     // rows of that very key in front of the warp's
     for (int w = w0; w < w1; ++w) {
@@ -144,30 +165,50 @@ evict_select_kernel(const EvictKv a, int32_t* __restrict__ moves, int64_t moves_
     }
     if (tid == 0) list[0] = total;
     __syncthreads();
-    // weights and positions: what stays where it is, then what changes its place (written by this block: visible behind the barrier)
+    // Weights and positions: what stays where it is, then what changes its place (the lists are this block's own: visible behind the barrier).
+    // The lists go on with rows of the caches in place of the sequence's.
+#pragma unroll 4
     for (int j = tid; j < a.budget; j += kEvictThreads)
         if (s_keep[j >> 5] >> (j & 31) & 1) { new_weight[j] = weight[j]; new_pos[j] = pos[j]; }
-    for (int m = tid; m < total; m += kEvictThreads) { new_weight[to[m]] = weight[of[m]]; new_pos[to[m]] = pos[of[m]]; }
+#pragma unroll 4
+    for (int m = tid; m < total; m += kEvictThreads) {
+        const int t = to[m], f = of[m];
+        new_weight[t] = weight[f];
+        new_pos[t] = pos[f];
+        to[m] = (int32_t)a.pages.row(s, t);
+        of[m] = (int32_t)a.pages.row(s, f);
+    }
 }
 
-// 16 lanes have a row (16 bytes a lane)
+// 16 lanes have a row (16 bytes a lane), kMovesOnce rows in flight
 __global__ void __launch_bounds__(kMoveThreads)
 evict_move_kernel(const EvictKv a, const int32_t* __restrict__ moves, int64_t moves_ld) {
     const int s = blockIdx.z, hk = blockIdx.y, lane = threadIdx.x & 15;
     pdl_wait();
     pdl_trigger();
     const int32_t* list = moves + ((size_t)s * a.Hkv + hk) * moves_ld;
-    const int n = list[0];
+    const int n = list[0], step = gridDim.x * (kMoveThreads / 16);
     const int32_t* to = list + kMovesAhead;
     const int32_t* of = to + (moves_ld - kMovesAhead) / 2;
-    for (int m = blockIdx.x * (kMoveThreads / 16) + (threadIdx.x >> 4); m < n; m += gridDim.x * (kMoveThreads / 16)) {
-        const size_t from = ((size_t)a.pages.row(s, of[m]) * a.Hkv + hk) * (kHeadDim / 8) + lane;
-        const size_t at = ((size_t)a.pages.row(s, to[m]) * a.Hkv + hk) * (kHeadDim / 8) + lane;
-        uint4* k = reinterpret_cast<uint4*>(a.k_cache);
-        uint4* v = reinterpret_cast<uint4*>(a.v_cache);
-        const uint4 kx = k[from], vx = v[from];
-        k[at] = kx;
-        v[at] = vx;
+    uint4* k = reinterpret_cast<uint4*>(a.k_cache);
+    uint4* v = reinterpret_cast<uint4*>(a.v_cache);
+    for (int m = blockIdx.x * (kMoveThreads / 16) + (threadIdx.x >> 4); m < n; m += kMovesOnce * step) {
+        size_t at[kMovesOnce];
+        uint4 x[kMovesOnce], y[kMovesOnce];
+#pragma unroll
+        for (int u = 0; u < kMovesOnce; ++u)
+            if (m + u * step < n) {
+                const size_t from = ((size_t)of[m + u * step] * a.Hkv + hk) * (kHeadDim / 8) + lane;
+                at[u] = ((size_t)to[m + u * step] * a.Hkv + hk) * (kHeadDim / 8) + lane;
+                x[u] = k[from];
+                y[u] = v[from];
+            }
+#pragma unroll
+        for (int u = 0; u < kMovesOnce; ++u)
+            if (m + u * step < n) {
+                k[at[u]] = x[u];
+                v[at[u]] = y[u];
+            }
     }
 }
 
@@ -179,18 +220,19 @@ cudaError_t launch_evict_kv(goose_ctx* c, const EvictKv& a, cudaStream_t st) {
     const int64_t ld = kMovesAhead + 2 * most;
     if (cudaError_t e = grow(c, &c->evict_moves, &c->evict_bytes, sizeof(int32_t) * (size_t)ld * a.S * a.Hkv)) return e;
     int32_t* moves = static_cast<int32_t*>(c->evict_moves);
-    const size_t smem = sizeof(uint32_t) * (size_t)((room + 31) / 32);
-    cudaError_t e = launch_pdl(evict_select_kernel, dim3(a.Hkv, a.S), dim3(kEvictThreads), smem, st, a, moves, ld, c->status);
+    const int keep_words = (int)((room + 31) / 32), keys_there = std::min({(int)room, kMostKeys, kSelectSmem / 4 - keep_words});
+    const size_t smem = sizeof(uint32_t) * (size_t)(keep_words + keys_there);
+    cudaError_t e = launch_pdl(evict_select_kernel, dim3(a.Hkv, a.S), dim3(kEvictThreads), smem, st, a, moves, ld, keep_words, keys_there, c->status);
     c->launches++;
     if (e != cudaSuccess || most == 0) return e;
-    const int64_t blocks = (most + kMoveThreads / 16 - 1) / (kMoveThreads / 16);
+    const int64_t blocks = (most + kMovesOnce * kMoveThreads / 16 - 1) / (kMovesOnce * kMoveThreads / 16);
     e = launch_pdl(evict_move_kernel, dim3((unsigned)(blocks < 64 ? blocks : 64), a.Hkv, a.S), dim3(kMoveThreads), 0, st, a, moves, ld);
     c->launches++;
     return e;
 }
 
 cudaError_t init_evict_kernels() {
-    cudaError_t e = cudaFuncSetAttribute(evict_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, GOOSE_MAX_PAGED_ROWS / 8);
+    cudaError_t e = cudaFuncSetAttribute(evict_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSelectSmem);
     return e == cudaSuccess ? load_kernels({(const void*)evict_move_kernel}) : e;
 }
 
