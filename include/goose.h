@@ -69,7 +69,7 @@ extern "C" {
 #define GOOSE_MAX_V  262144   /* vocabulary size limit of goose_node_topk                          */
 #define GOOSE_STATIC_TOPK_MAX_ROWS 2048   /* row limit of goose_node_topk_static                    */
 #define GOOSE_MIN_PAGE      16   /* rows of a page of a paged cache: a power of two from here on      */
-#define GOOSE_MAX_PAGED_ROWS 1048576      /* rows that a sequence's part of a page table may name      */
+#define GOOSE_MAX_PAGED_ROWS 524288       /* rows that a sequence's part of a page table may name      */
 
 /* per-sequence status bits (goose_last_status) */
 #define GOOSE_ST_BAD_PARENT   1   /* parent[] is not a rooted tree in topological order */

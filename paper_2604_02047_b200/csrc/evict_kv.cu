@@ -15,10 +15,11 @@ constexpr int kEvictThreads = 1024;
 constexpr int kEvictWarps = kEvictThreads / 32;
 constexpr int kMoveThreads = 256;
 constexpr int kMovesOnce = 2;
+constexpr int kBatch = 4;
 constexpr int kBins = 2 * kEvictThreads;              // counters of a digit
 constexpr int kMostKeys = 24576;                      // keys in shared memory: two blocks an SM; rows behind them are looked up again
-constexpr int kSelectSmem = 212992;                   // of a block, at most (a bit a row and the keys)
-static_assert(GOOSE_MAX_PAGED_ROWS / 8 < kSelectSmem, "a bit a row");
+constexpr int kSelectSmem = 212992;                   // of a block, at most: a bit a row, a number for 32 rows, keys
+
 constexpr int kMovesAhead = 4;                        // words that stand in front of a head's list (its length)
 
 // of the row's position and weight
@@ -52,11 +53,13 @@ __device__ __forceinline__ int block_prefix(int v, int* s_warp, int& total) {
     return upto - v + (warp == 0 ? 0 : before);
 }
 
-__global__ void __launch_bounds__(kEvictThreads)
+// kBatch loads of a thread in flight: what bounds a block is the trips to L2
+__global__ void __launch_bounds__(kEvictThreads, 1)
 evict_select_kernel(const EvictKv a, int32_t* __restrict__ moves, int64_t moves_ld, int keep_words, int keys_there, int32_t* __restrict__ status) {
     extern __shared__ uint32_t s_keep[];              // a bit a row: it stays
-    uint32_t* const s_key = s_keep + keep_words;      // of the first keys_there rows
-    __shared__ int s_hist[kBins], s_warp[kEvictWarps], s_digit, s_above;
+    int* const s_rank = reinterpret_cast<int*>(s_keep + keep_words);   // of a word's first pair
+    uint32_t* const s_key = s_keep + 2 * keep_words;  // of the first keys_there rows
+    __shared__ int s_hist[kBins], s_warp[kEvictWarps], s_digit, s_above, s_equal;
     const int s = blockIdx.y, hk = blockIdx.x, tid = threadIdx.x, lane = tid & 31;
     const size_t head = (size_t)s * a.Hkv + hk;
     for (int b = tid; b < kBins; b += kEvictThreads) s_hist[b] = 0;
@@ -67,6 +70,7 @@ evict_select_kernel(const EvictKv a, int32_t* __restrict__ moves, int64_t moves_
     const int64_t room = a.pages.room(a.ldw);
     bool bad = ctx < 0 || ctx > room || left > a.ldw_new;
     const int pages = bad ? 0 : (ctx + (1 << a.pages.size_log2) - 1) >> a.pages.size_log2;
+#pragma unroll 4
     for (int p = tid; p < pages; p += kEvictThreads) {
         const int page = a.pages.table[s * a.pages.ldt + p];
         bad |= page < 0 || page >= a.pages.n;
@@ -85,9 +89,24 @@ evict_select_kernel(const EvictKv a, int32_t* __restrict__ moves, int64_t moves_
     const int32_t* __restrict__ pos = a.row_pos + head * a.ldw;
     float* __restrict__ new_weight = a.new_weight + head * a.ldw_new;
     int32_t* __restrict__ new_pos = a.new_pos + head * a.ldw_new;
+    // f(row, weight, position) for the rows first + tid, first + tid + kEvictThreads, ... in front of n
+    auto each_row = [&](int n, auto f) {
+        for (int j0 = tid; j0 < n; j0 += kBatch * kEvictThreads) {
+            float w[kBatch];
+            int p[kBatch];
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+                const int j = min(j0 + u * kEvictThreads, n - 1);
+                w[u] = weight[j];
+                p[u] = pos[j];
+            }
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u)
+                if (j0 + u * kEvictThreads < n) f(j0 + u * kEvictThreads, w[u], p[u]);
+        }
+    };
     if (ctx <= a.budget) {
-#pragma unroll 4
-        for (int j = tid; j < ctx; j += kEvictThreads) { new_weight[j] = weight[j]; new_pos[j] = pos[j]; }
+        each_row(ctx, [&](int j, float w, int p) { new_weight[j] = w; new_pos[j] = p; });
         return;
     }
     const int64_t recent_from = (int64_t)off + ctx - a.recent;
@@ -98,13 +117,13 @@ evict_select_kernel(const EvictKv a, int32_t* __restrict__ moves, int64_t moves_
     for (const int shift : {21, 10, 0}) {
         const int digit_bits = shift == 0 ? 10 : 11;
         if (shift == 21) {
-#pragma unroll 8
-            for (int j = tid; j < ctx; j += kEvictThreads) {
-                const uint32_t k = evict_key(weight[j], pos[j], a.sink, recent_from);
+            each_row(ctx, [&](int j, float w, int p) {
+                const uint32_t k = evict_key(w, p, a.sink, recent_from);
                 if (j < keys_there) s_key[j] = k;
                 atomicAdd(&s_hist[k >> 21], 1);
-            }
+            });
         } else {
+#pragma unroll 4
             for (int j = tid; j < ctx; j += kEvictThreads) {
                 const uint32_t k = key(j);
                 if (k >> (shift + digit_bits) == prefix) atomicAdd(&s_hist[k >> shift & ((1 << digit_bits) - 1)], 1);
@@ -118,6 +137,7 @@ evict_select_kernel(const EvictKv a, int32_t* __restrict__ moves, int64_t moves_
             const bool first = above + mine >= need;
             s_digit = first ? high : high - 1;
             s_above = first ? above : above + mine;
+            s_equal = first ? mine : below;
         }
         s_hist[high] = s_hist[high - 1] = 0;
         __syncthreads();
@@ -127,14 +147,17 @@ evict_select_kernel(const EvictKv a, int32_t* __restrict__ moves, int64_t moves_
     // what stays, in words of 32 rows; a warp's rows are consecutive
     const int words = (ctx + 31) >> 5, per = (words + kEvictWarps - 1) / kEvictWarps;
     const int w0 = min((tid >> 5) * per, words), w1 = min(w0 + per, words);
-    int equal = 0;
-    for (int w = w0; w < w1; ++w) {
-        const int j = 32 * w + lane;
-        const uint32_t k = j < ctx ? key(j) : 0u;
-        equal += __popc(__ballot_sync(0xFFFFFFFFu, j < ctx && k == prefix));
+    int before = 0;                                   // rows of that very key in front of the warp's
+    if (s_equal != need) {                            // (else all of them stay)
+        int equal = 0;
+        for (int w = w0; w < w1; ++w) {
+            const int j = 32 * w + lane;
+            equal += __popc(__ballot_sync(0xFFFFFFFFu, j < ctx && key(j) == prefix));
+        }
+        before = block_prefix(lane == 0 ? equal : 0, s_warp, total);
+        before = __shfl_sync(0xFFFFFFFFu, before, 0);
     }
-    int before = block_prefix(lane == 0 ? equal : 0, s_warp, total);
-    before = __shfl_sync(0xFFFFFFFFu, before, 0);     // rows of that very key in front of the warp's
+#pragma unroll 4
     for (int w = w0; w < w1; ++w) {
         const int j = 32 * w + lane;
         const uint32_t k = j < ctx ? key(j) : 0u;
@@ -142,41 +165,67 @@ evict_select_kernel(const EvictKv a, int32_t* __restrict__ moves, int64_t moves_
         const bool stays = j < ctx && (k > prefix || (k == prefix && before + __popc(same & ((1u << lane) - 1)) < need));
         const uint32_t word = __ballot_sync(0xFFFFFFFFu, stays);
         if (lane == 0) s_keep[w] = word;
-        before += __popc(same);
+        if (s_equal != need) before += __popc(same);
     }
     __syncthreads();
-    // pairs: dropped rows in front of the budget, kept rows from it on, each by words of 32 that a thread has in a row
-    const int bw = (a.budget + 31) >> 5, b0 = a.budget >> 5;
-    auto holes = [&](int w) {                         // of word w
-        const uint32_t inside = w < b0 ? 0xFFFFFFFFu : (1u << (a.budget & 31)) - 1;
-        return ~s_keep[w] & inside;
-    };
-    auto movers = [&](int w) { return s_keep[w] & (w > b0 ? 0xFFFFFFFFu : ~((1u << (a.budget & 31)) - 1)); };
-    int32_t* to = list + kMovesAhead;
-    int32_t* of = to + (moves_ld - kMovesAhead) / 2;
-    for (int side = 0; side < 2; ++side) {
-        const int first = side ? b0 : 0, n = side ? words - b0 : bw, each = (n + kEvictThreads - 1) / kEvictThreads;
-        const int u0 = first + min(tid * each, n), u1 = first + min((tid + 1) * each, n);
-        int count = 0;
-        for (int w = u0; w < u1; ++w) count += __popc(side ? movers(w) : holes(w));
-        int at = block_prefix(count, s_warp, total);
-        for (int w = u0; w < u1; ++w)
-            for (uint32_t bits = side ? movers(w) : holes(w); bits; bits &= bits - 1) (side ? of : to)[at++] = 32 * w + __ffs(bits) - 1;
+    // Pairs of a dropped row in front of the budget and a kept one from it on.  Both counted in one row of words: those of the dropped up to the word that
+    // the budget is in, then, from that word on, those of the kept.
+    const int b0 = a.budget >> 5;
+    const uint32_t inside = (1u << (a.budget & 31)) - 1;   // of word b0: rows in front of the budget
+    const int entries = words + 1, each = (entries + kEvictThreads - 1) / kEvictThreads, e0 = min(tid * each, entries), e1 = min(e0 + each, entries);
+    auto pairs = [&](int e) { return e < b0 ? ~s_keep[e] : e == b0 ? ~s_keep[e] & inside : s_keep[e - 1] & (e == b0 + 1 ? ~inside : 0xFFFFFFFFu); };
+    int count = 0;
+    for (int e = e0; e < e1; ++e) count += __popc(pairs(e));
+    int at = block_prefix(count, s_warp, total);
+    for (int e = e0; e < e1; ++e) {
+        s_rank[e] = at;
+        at += __popc(pairs(e));
     }
-    if (tid == 0) list[0] = total;
+    const int n = total / 2;                          // (as many dropped as kept)
+    int32_t* const list_to = list + kMovesAhead;
+    int32_t* const list_of = list_to + (moves_ld - kMovesAhead) / 2;
+    // (the keys are not needed any more, and the pairs are no more than half as many)
+    const bool fit = ctx <= keys_there;
+    int32_t* const to = fit ? reinterpret_cast<int32_t*>(s_key) : list_to;
+    int32_t* const of = fit ? to + ctx / 2 : list_of;
+    if (tid == 0) list[0] = n;
     __syncthreads();
-    // Weights and positions: what stays where it is, then what changes its place (the lists are this block's own: visible behind the barrier).
-    // The lists go on with rows of the caches in place of the sequence's.
-#pragma unroll 4
-    for (int j = tid; j < a.budget; j += kEvictThreads)
-        if (s_keep[j >> 5] >> (j & 31) & 1) { new_weight[j] = weight[j]; new_pos[j] = pos[j]; }
-#pragma unroll 4
-    for (int m = tid; m < total; m += kEvictThreads) {
-        const int t = to[m], f = of[m];
-        new_weight[t] = weight[f];
-        new_pos[t] = pos[f];
-        to[m] = (int32_t)a.pages.row(s, t);
-        of[m] = (int32_t)a.pages.row(s, f);
+    for (int j = a.budget + tid; j < ctx; j += kEvictThreads) {
+        const uint32_t word = s_keep[j >> 5] & (j >> 5 == b0 ? ~inside : 0xFFFFFFFFu);
+        if (word >> (j & 31) & 1) of[s_rank[(j >> 5) + 1] - n + __popc(word & ((1u << (j & 31)) - 1))] = j;
+    }
+    // weights and positions of what stays where it is, then of what changes its place; the lists go on with rows of the caches in place of the sequence's
+    each_row(a.budget, [&](int j, float w, int p) {
+        const uint32_t word = s_keep[j >> 5];
+        if (word >> (j & 31) & 1) { new_weight[j] = w; new_pos[j] = p; }
+        else to[s_rank[j >> 5] + __popc(~word & ((1u << (j & 31)) - 1))] = j;
+    });
+    __syncthreads();
+    for (int m0 = tid; m0 < n; m0 += kBatch * kEvictThreads) {
+        int t[kBatch], f[kBatch], p[kBatch], row_t[kBatch], row_f[kBatch];
+        float w[kBatch];
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            const int m = m0 + u * kEvictThreads < n ? m0 + u * kEvictThreads : m0;   // (its own: the lists may lie where the results go)
+            t[u] = to[m];
+            f[u] = of[m];
+        }
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            w[u] = weight[f[u]];
+            p[u] = pos[f[u]];
+            row_t[u] = (int32_t)a.pages.row(s, t[u]);
+            row_f[u] = (int32_t)a.pages.row(s, f[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            const int m = m0 + u * kEvictThreads;
+            if (m >= n) break;
+            new_weight[t[u]] = w[u];
+            new_pos[t[u]] = p[u];
+            list_to[m] = row_t[u];
+            list_of[m] = row_f[u];
+        }
     }
 }
 
@@ -220,8 +269,8 @@ cudaError_t launch_evict_kv(goose_ctx* c, const EvictKv& a, cudaStream_t st) {
     const int64_t ld = kMovesAhead + 2 * most;
     if (cudaError_t e = grow(c, &c->evict_moves, &c->evict_bytes, sizeof(int32_t) * (size_t)ld * a.S * a.Hkv)) return e;
     int32_t* moves = static_cast<int32_t*>(c->evict_moves);
-    const int keep_words = (int)((room + 31) / 32), keys_there = std::min({(int)room, kMostKeys, kSelectSmem / 4 - keep_words});
-    const size_t smem = sizeof(uint32_t) * (size_t)(keep_words + keys_there);
+    const int keep_words = (int)((room + 31) / 32) + 1, keys_there = std::min({(int)room, kMostKeys, kSelectSmem / 4 - 2 * keep_words});
+    const size_t smem = sizeof(uint32_t) * (size_t)(2 * keep_words + keys_there);
     cudaError_t e = launch_pdl(evict_select_kernel, dim3(a.Hkv, a.S), dim3(kEvictThreads), smem, st, a, moves, ld, keep_words, keys_there, c->status);
     c->launches++;
     if (e != cudaSuccess || most == 0) return e;
