@@ -103,16 +103,17 @@ append_kv_kernel(const AppendKv a, int groups_log2 /* groups of 16 lanes a token
         if (!tree_depths(a.parent + (size_t)s * a.B, nn, s_up, s_depth)) flaw |= GOOSE_ST_BAD_PARENT;
         else if (i < nn) depth = s_depth[i];
     }
-    if (i >= nn) return;                                       // (whole groups: the shuffles below name their 16 lanes)
+    const bool live = i < nn;
+    if (!kPaged && !live) return;                              // (whole groups: the shuffles below name their 16 lanes)
     const int64_t pos = pos0 + depth;
     if (a.rope_dim && (pos < 0 || pos >= a.rope_rows)) flaw |= GOOSE_ST_BAD_POS;
     int64_t place = row0 + ctx + i;                            // row of the caches
-    if (kPaged && !flaw) {
+    if (kPaged && live && !flaw) {
         place = a.pages.row(s, ctx + i);
         if (place < 0) flaw |= GOOSE_ST_BAD_ROWS;
         if (a.row_pos && (pos < 0 || pos > INT32_MAX)) flaw |= GOOSE_ST_BAD_POS;
     }
-    if (flaw && lane == 0 && r_first == 0) atomicOr(&a.status[s], flaw);
+    if (flaw && live && lane == 0 && r_first == 0) atomicOr(&a.status[s], flaw);
 
     const int half = a.rope_dim >> 1;
     // cosines and sines of this lane's elements, and the lane that has their partners (half-split pairs)
@@ -140,7 +141,7 @@ append_kv_kernel(const AppendKv a, int groups_log2 /* groups of 16 lanes a token
     }
     const uint32_t mask = 0xFFFFu << (threadIdx.x & 16);
     const size_t cache_row = (size_t)place * Hkv;
-    for (int r0 = r_first; r0 < rows; r0 += kRows * per_token) {
+    for (int r0 = kPaged && !live ? rows : r_first; r0 < rows; r0 += kRows * per_token) {
         uint4 next[kRows];
         if (kStream) load(r0 + kRows * per_token, next);
         else if (r0 != r_first) load(r0, x);
@@ -155,11 +156,6 @@ append_kv_kernel(const AppendKv a, int groups_log2 /* groups of 16 lanes a token
             if (flaw) {                                        // queries of zeros, no row of the cache touched
                 if (is_q) to[lane] = make_uint4(0, 0, 0, 0);
                 continue;
-            }
-            if (kPaged && lane == 0 && !is_q && r < H + Hkv) {
-                const size_t at = ((size_t)s * Hkv + r - H) * a.ldw + ctx + i;
-                if (a.row_weight) a.row_weight[at] = 0.f;
-                if (a.row_pos) a.row_pos[at] = (int)pos;
             }
             if (r < H + Hkv) {
                 float y[8];
@@ -197,6 +193,20 @@ append_kv_kernel(const AppendKv a, int groups_log2 /* groups of 16 lanes a token
         if (kStream)
 #pragma unroll
             for (int u = 0; u < kRows; ++u) x[u] = next[u];
+    }
+    if (kPaged && (a.row_weight || a.row_pos)) {
+        // the new rows' weights and positions, a head's neighbouring tokens side by side (each token's by itself, two prompts of 6001 tokens, 40 heads: 135 -> 150 us)
+        __shared__ int s_pos[kAppendGroups];
+        const int tokens_log2 = 4 - groups_log2;
+        if (lane == 0 && r_first == 0) s_pos[group >> groups_log2] = live && !flaw ? a.row_pos ? (int)pos : 0 : -1;
+        __syncthreads();
+        for (int e = threadIdx.x; e < Hkv << tokens_log2; e += kAppendThreads) {
+            const int t = e & ((1 << tokens_log2) - 1), p = s_pos[t];
+            if (p < 0) continue;
+            const size_t at = ((size_t)s * Hkv + (e >> tokens_log2)) * a.ldw + ctx + first + t;
+            if (a.row_weight) a.row_weight[at] = 0.f;
+            if (a.row_pos) a.row_pos[at] = p;
+        }
     }
 }
 
