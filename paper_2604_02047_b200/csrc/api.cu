@@ -478,7 +478,7 @@ int goose_kv_weights(goose_ctx* c, const void* q, const float* lse, const void* 
     if (rc || S == 0) return rc;
     if (!q || !lse || !k_cache || !ctx_len || !row_weight || ldw < 1) return GOOSE_EINVAL;
     if (!aligned16(q) || !aligned16(k_cache)) return GOOSE_EINVAL;
-    if (!(scale > 0.f) || !(scale < 1e30f)) return GOOSE_EINVAL;
+    if (!(scale > 1e-30f) || !(scale < 1e30f)) return GOOSE_EINVAL;
     a.q = (const __nv_bfloat16*)q; a.lse = lse; a.k_cache = (const __nv_bfloat16*)k_cache;
     a.ctx_len = ctx_len; a.n_new = n_new; a.S = S; a.B = B; a.H = H; a.Hkv = Hkv; a.scale = scale;
     a.row_weight = row_weight; a.ldw = ldw;

@@ -2,15 +2,18 @@
 // over the tokens i >= j - ctx.
 //
 // Persistent, one CTA an SM, tcgen05: S^T = K Q^T with the keys as rows, so that a thread has a key, and its sum needs no exchange; up to
-// four key tiles of a run stay in shared memory while the Q tiles pass by.  Work list: weights_work.cuh.  Roles (768 threads):
+// four key tiles of a run stay in shared memory while the Q tiles pass by.  The log-sum-exps come with the product: one more step of 16 of its inner
+// dimension adds -lse / scale to every score of a column, in three bf16 that together have its 24 bits, times ones.  It is the last step, so that the
+// steps in front of it are rounded by the size of the scores alone.  (A thread that reads every column's from shared memory instead, 16 bytes at a
+// time, takes as much of its bandwidth as the product does: 2048 tokens behind 4096, 32 heads over 8: 127 us, so 112.)  Work list: weights_work.cuh.  Roles (768 threads):
 //   warp 0            Q tiles into a ring of two, by TMA
 //   warp 1            MMA issuer: the scores of key tile u of the run into columns 128 u of tensor memory
 //   warp 2            planner: walks the work list and puts the segments' descriptions into a ring
-//   warp 3            log-sum-exps of a Q tile's rows, negated and in units of log 2, and which of the rows count
+//   warp 3            the product's last step for a Q tile's rows, and which of the rows count
 //   warps 4..19       exponentials, four warps a key tile of the run, a key and a sum a thread.  At the segment's end the sums are added to the
 //                     rows' weights, or, where several CTAs have Q tiles of the item, left in the workspace; the warp that completes a count adds up what
 //                     all have left, in the order of the tokens.
-//   warps 20..23      K tiles into a ring of five, 32 keys of a tile a warp, by 16-byte copies: a TMA box a page took 110 to 156 cycles a box, and pages of
+//   warps 20..23      K tiles into a ring of four, 32 keys of a tile a warp, by 16-byte copies: a TMA box a page took 110 to 156 cycles a box, and pages of
 //                     16 rows have sixteen a tile (64 sequences of 8192 rows, a token each: 255 us, with these 180; pages of 128 rows 218, 178)
 // Every wait is bounded: one that runs out raises the CTA's abort flag and GOOSE_ST_TIMEOUT, and every role unwinds.
 #include <stddef.h>
@@ -24,16 +27,15 @@ namespace goose {
 
 namespace {
 
-constexpr int kStages = 5, kQStages = 2;
+constexpr int kStages = 4, kQStages = 2;
 constexpr int kTileBytes = kWeightTile * kHeadDim * 2;       // 32 KB: one K or one Q tile
 constexpr int kHalfBytes = kWeightTile * 128;                // 16 KB: 128 rows x 64 bf16 (one swizzle-atom column)
-constexpr int kHeaderBytes = 2048;
-constexpr int kWeightSmem = 1008 /*alignment slack*/ + (kStages + kQStages) * kTileBytes + kHeaderBytes;
+constexpr int kStepBytes = kWeightTile * 32;                 // 4 KB: 128 rows x 16 bf16, without swizzle
+constexpr int kHeaderBytes = 1024;
+constexpr int kWeightSmem = 1008 /*alignment slack*/ + (kStages + kQStages) * kTileBytes + (1 + kQStages) * kStepBytes + kHeaderBytes;
 // warps: four of the roles below, four a key tile of a run for the exponentials, four for the copies of the key tiles
 constexpr int kSumWarp = 4, kCopyWarp = kSumWarp + 4 * kRun, kCopyWarps = 4;
 constexpr int kWeightThreads = 32 * (kCopyWarp + kCopyWarps);
-// registers: 80 a thread at launch; the warps of the products and of the copies give 16 each to the others (64 + 64 + 4 x 88 = 6 x 80)
-constexpr int kRegsFew = 64, kRegsMany = 88;
 constexpr uint32_t kTmemCols = 512;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr long long kWaitCycles = 2000000000ll;              // bound of every wait: about one second of SM clock
@@ -49,7 +51,6 @@ struct Segment {
 
 struct Header {
     Segment seg[kSegments];
-    alignas(16) float lse[kQStages][kWeightTile];            // -lse / log 2 of the Q tile's rows
     alignas(16) uint32_t counts[kQStages][4];                // which rows of the Q tile count
     unsigned long long k_full[kStages], k_empty[kStages], q_full[kQStages], q_empty[kQStages], lse_full[kQStages], lse_empty[kQStages];
     unsigned long long seg_full[kSegments], seg_empty[kSegments];
@@ -66,7 +67,7 @@ struct WeightArgs {
     Pages pages;
     const __nv_bfloat16* k_cache;
     int g, H, nb;                                            // heads of a group, heads, tokens of a box of queries
-    float scale_log2;
+    float scale_log2, inv_scale;
     const float* lse;
     float* row_weight;
     int64_t ldw;
@@ -150,31 +151,23 @@ __device__ __forceinline__ bool locate(WeightWork<Int>& wk, WeightCursor<Int>& c
     return false;
 }
 
-// sums over 32 columns of exp2(score * scale - lse): all of them; those of a mask
-__device__ __forceinline__ void add_columns(const uint32_t* v, const float* neg_lse, unsigned long long scale2, unsigned long long (&part)[2]) {
-    const ulonglong2* nl = reinterpret_cast<const ulonglong2*>(neg_lse);
+// sums over 32 columns of exp2(score * scale); kMasked: over those that count
+template <bool kMasked>
+__device__ __forceinline__ void add_columns(const uint32_t (&v)[32], unsigned long long scale2, uint32_t counts, unsigned long long (&part)[2]) {
 #pragma unroll
-    for (int c = 0; c < 32; c += 4) {
-        const ulonglong2 n4 = nl[c / 4];
-        const float2 x = unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(v[c]), __uint_as_float(v[c + 1])), scale2, n4.x));
-        const float2 y = unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(v[c + 2]), __uint_as_float(v[c + 3])), scale2, n4.y));
-        part[0] = add_f32x2(part[0], pack_f32x2(ex2(x.x), ex2(x.y)));
-        part[1] = add_f32x2(part[1], pack_f32x2(ex2(y.x), ex2(y.y)));
-    }
-}
-__device__ __forceinline__ void add_columns(const uint32_t* v, const float* neg_lse, unsigned long long scale2, uint32_t counts, unsigned long long (&part)[2]) {
-    const ulonglong2* nl = reinterpret_cast<const ulonglong2*>(neg_lse);
-#pragma unroll
-    for (int c = 0; c < 32; c += 4) {
-        const ulonglong2 n4 = nl[c / 4];
-        const float2 x = unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(v[c]), __uint_as_float(v[c + 1])), scale2, n4.x));
-        const float2 y = unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(v[c + 2]), __uint_as_float(v[c + 3])), scale2, n4.y));
-        auto one = [&](int e, float z) { return counts >> e & 1 ? ex2(z) : 0.f; };
-        part[0] = add_f32x2(part[0], pack_f32x2(one(c, x.x), one(c + 1, x.y)));
-        part[1] = add_f32x2(part[1], pack_f32x2(one(c + 2, y.x), one(c + 3, y.y)));
+    for (int c = 0; c < 32; c += 2) {
+        const float2 x = unpack_f32x2(mul_f32x2(pack_f32x2(__uint_as_float(v[c]), __uint_as_float(v[c + 1])), scale2));
+        auto one = [&](int b, float z) { return !kMasked || (counts >> b & 1) ? ex2(z) : 0.f; };
+        part[c >> 1 & 1] = add_f32x2(part[c >> 1 & 1], pack_f32x2(one(c, x.x), one(c + 1, x.y)));
     }
 }
 
+// matrix descriptor of 16 K-major columns without swizzle: 8 rows x 16 bytes together, the other 16 bytes of the rows 128 further, the next 8 rows 256
+__device__ __forceinline__ uint64_t step_desc(uint32_t addr) {
+    uint64_t d;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "r"(((addr >> 4) & 0x3FFF) | ((128u >> 4) << 16)), "r"((256u >> 4) | (1u << 14)));
+    return d;
+}
 // M = 128 keys, N = n query rows (a multiple of 16), both K-major
 __device__ __forceinline__ uint32_t scores_desc(int n) { return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((128u >> 4) << 24); }
 
@@ -184,7 +177,8 @@ kv_weights_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
     extern __shared__ unsigned char smem_raw[];
     unsigned char* k_smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     unsigned char* q_smem = k_smem + kStages * kTileBytes;
-    Header* hd = reinterpret_cast<Header*>(q_smem + kQStages * kTileBytes);
+    unsigned char* step_smem = q_smem + kQStages * kTileBytes;   // ones, then a Q tile's log-sum-exps each
+    Header* hd = reinterpret_cast<Header*>(step_smem + (1 + kQStages) * kStepBytes);
     const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
 
     if (threadIdx.x == 0) {
@@ -196,6 +190,11 @@ kv_weights_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         prefetch_tmap(&tmap_q);
     }
+    for (int i = threadIdx.x; i < (1 + kQStages) * kStepBytes / 16; i += kWeightThreads) {   // of 16 bytes: 8 rows' first halves, their second ones, ...
+        const bool one = i < kStepBytes / 16 && !(i >> 3 & 1);
+        reinterpret_cast<uint4*>(step_smem)[i] = one ? make_uint4(0x3F803F80u, 0x00003F80u, 0u, 0u) : make_uint4(0, 0, 0, 0);
+    }
+    fence_proxy_async();
     if (warp == 1) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&hd->tmem_base)), "r"(kTmemCols) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -209,7 +208,6 @@ kv_weights_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
     auto all = [](bool x) { return __all_sync(0xFFFFFFFFu, x) != 0; };
 
     if (warp < 4) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsFew));
         if (warp == 2) {
             // =============================================================== planner
             WeightWork<Int> wk = a.wk;
@@ -293,7 +291,7 @@ kv_weights_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
         } else if (warp == 1) {
             // =============================================================== MMA issuer
             const bool leader = elect_leader();                  // the warp runs converged, this lane acts
-            const uint32_t q_addr = smem_u32(q_smem), k_addr = smem_u32(k_smem);
+            const uint32_t q_addr = smem_u32(q_smem), k_addr = smem_u32(k_smem), step_addr = smem_u32(step_smem);
             uint32_t k_tile = 0, used = 0;                       // K tiles in front of this segment; a bit a score buffer: its parity
             Ring qs{0, 0}, ring{0, 0};
             bool ok = true;
@@ -308,7 +306,7 @@ kv_weights_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                 ring.next(kSegments);
                 if (n == 0) break;
                 for (int i = 0; i < n && ok; ++i) {
-                    ok = wait_for(hd, &hd->q_full[qs.at], qs.phase, a.status);
+                    ok = wait_for(hd, &hd->q_full[qs.at], qs.phase, a.status) && wait_for(hd, &hd->lse_full[qs.at], qs.phase, a.status);
                     if (!ok) break;
                     const int rows = min(nn - (q_first + i) * a.wk.t, a.wk.t) * a.g;
                     const uint32_t idesc = scores_desc((rows + 15) & ~15);
@@ -326,6 +324,7 @@ kv_weights_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                             const uint32_t off = ((kk >> 2) * kHalfBytes + (kk & 3) * 32) >> 4;
                             umma_f16_by(leader, tmem + u * 128, smem_desc(k_lo + off), smem_desc(q_lo + off), idesc, kk > 0 ? 1u : 0u);
                         }
+                        umma_f16_by(leader, tmem + u * 128, step_desc(step_addr), step_desc(step_addr + (1 + qs.at) * kStepBytes), idesc, 1u);
                         umma_commit_by(leader, &hd->s_full[u]);
                         if (i == n - 1) umma_commit_by(leader, &hd->k_empty[at]);
                     }
@@ -361,9 +360,16 @@ kv_weights_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
 #pragma unroll
                     for (int w = 0; w < 4; ++w) {
                         const uint32_t word = __ballot_sync(0xFFFFFFFFu, x[w] != -INFINITY);   // (NaN counts)
-                        hd->lse[qs.at][32 * w + lane] = -kLog2e * x[w];
+                        const float v = x[w] == -INFINITY ? 0.f : -a.inv_scale * x[w];
+                        const __nv_bfloat16 high = __float2bfloat16_rn(v);
+                        const float left = isinf(v) ? 0.f : v - __bfloat162float(high);
+                        const __nv_bfloat16 mid = __float2bfloat16_rn(left), low = __float2bfloat16_rn(left - __bfloat162float(mid));
+                        const int r = 32 * w + lane;
+                        *reinterpret_cast<uint4*>(step_smem + (1 + qs.at) * kStepBytes + (r >> 3) * 256 + (r & 7) * 16) =
+                            make_uint4((uint32_t)__bfloat16_as_ushort(high) | (uint32_t)__bfloat16_as_ushort(mid) << 16, __bfloat16_as_ushort(low), 0u, 0u);
                         if (lane == 0) hd->counts[qs.at][w] = word;
                     }
+                    fence_proxy_async();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&hd->lse_full[qs.at]);
                     qs.next(kQStages);
@@ -371,7 +377,6 @@ kv_weights_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
             }
         }
     } else if (warp >= kCopyWarp) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsFew));
         // =============================================================== K tiles: 32 keys of a tile a warp
         const int part = warp - kCopyWarp;
         const uint32_t k_addr = smem_u32(k_smem) + 4096 * part;
@@ -431,7 +436,6 @@ kv_weights_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
         for (int i = 0; i < kStages && ok; ++i, ks.next(kStages)) ok = all(wait_for(hd, &hd->k_empty[ks.at], ks.phase ^ 1, a.status));
         if (!ok) cp_async_wait_all();
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsMany));
         // =============================================================== exponentials and sums
         const int u = (warp - kSumWarp) >> 2, wq = warp & 3; // key tile of a run
         const int row = 32 * wq + lane;                      // TMEM lane == key of the tile
@@ -462,7 +466,6 @@ kv_weights_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                     tc_fence_after();
                     const int rows = min(left, a.wk.t) * g;
                     const uint32_t* counts = hd->counts[qs.at];
-                    const float* neg_lse = hd->lse[qs.at];
                     const bool masked = (counts[0] & counts[1] & counts[2] & counts[3]) != 0xFFFFFFFFu || ahead + kWeightTile - 1 > t0;
                     const int first = max(ahead + row - t0, 0) * g;  // columns in front of it are tokens in front of the key
                     unsigned long long part[2] = {0, 0};
@@ -477,10 +480,10 @@ kv_weights_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                             if (lane == 0) mbar_arrive(&hd->s_free[u]);
                         }
                         if (!masked) {
-                            add_columns(v, neg_lse + 32 * w, scale2, part);
+                            add_columns<false>(v, scale2, 0, part);
                         } else {
                             const int out = first - 32 * w;
-                            add_columns(v, neg_lse + 32 * w, scale2, counts[w] & (out <= 0 ? 0xFFFFFFFFu : out >= 32 ? 0u : 0xFFFFFFFFu << out), part);
+                            add_columns<true>(v, scale2, counts[w] & (out <= 0 ? 0xFFFFFFFFu : out >= 32 ? 0u : 0xFFFFFFFFu << out), part);
                         }
                     }
                     const float2 s2 = unpack_f32x2(add_f32x2(part[0], part[1]));
@@ -540,7 +543,7 @@ static cudaError_t launch_as(goose_ctx* c, const KvWeights& x, cudaStream_t st) 
     a.pages = x.pages;
     a.nb = a.wk.t < x.B ? a.wk.t : x.B;
     a.k_cache = x.k_cache;
-    a.scale_log2 = x.scale * kLog2e;
+    a.scale_log2 = x.scale * kLog2e; a.inv_scale = 1.f / x.scale;
     a.lse = x.lse; a.row_weight = x.row_weight; a.ldw = x.ldw;
     a.sums = c->weight_sums; a.counters = c->weight_counters; a.status = c->status;
     CUtensorMap mq;
