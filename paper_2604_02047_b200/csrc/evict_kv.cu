@@ -1,7 +1,7 @@
 // Eviction: the rows of a key/value head that stay, and the rows behind the budget among them to the places of those in front of it that do not.
 //
 // A row's key is an unsigned number in the order of what stays: the first and the latest positions above everything, then the weights, NaN below all.
-// The budget-th largest key is found digit by digit (11, 11 and 10 bits: the first has the exponent and two bits more, so that weights spread over some
+// The budget-th largest key is found digit by digit (11, 11 and 10 bits, as far as it takes: the first has the exponent and two bits more, so that weights spread over some
 // fifty of its counters); of the rows that have that very key the lowest stay.
 // The first kernel, a block a (sequence, head), reads weights and positions once, has the keys in shared memory, and leaves a list of (place, row) pairs;
 // the second copies the rows.  Places lie in front of the budget, rows behind it, so that no copy reads what another one writes.
@@ -113,7 +113,7 @@ evict_select_kernel(const EvictKv a, int32_t* __restrict__ moves, int64_t moves_
     auto key = [&](int j) { return j < keys_there ? s_key[j] : evict_key(weight[j], pos[j], a.sink, recent_from); };
     // the budget-th largest key: its upper digits so far, and how many of the rows that have them are still to be taken
     uint32_t prefix = 0;
-    int need = a.budget, total;
+    int need = a.budget, total, low = 0;
     for (const int shift : {21, 10, 0}) {
         const int digit_bits = shift == 0 ? 10 : 11;
         if (shift == 21) {
@@ -143,12 +143,15 @@ evict_select_kernel(const EvictKv a, int32_t* __restrict__ moves, int64_t moves_
         __syncthreads();
         prefix = prefix << digit_bits | (uint32_t)s_digit;
         need -= s_above;
+        low = shift;
+        if (s_equal == need) break;                   // all that have these digits stay: the others do not matter
     }
     // what stays, in words of 32 rows; a warp's rows are consecutive
     const int words = (ctx + 31) >> 5, per = (words + kEvictWarps - 1) / kEvictWarps;
     const int w0 = min((tid >> 5) * per, words), w1 = min(w0 + per, words);
     int before = 0;                                   // rows of that very key in front of the warp's
-    if (s_equal != need) {                            // (else all of them stay)
+    const bool ties = s_equal != need;                // (else all of them stay)
+    if (ties) {
         int equal = 0;
         for (int w = w0; w < w1; ++w) {
             const int j = 32 * w + lane;
@@ -160,12 +163,15 @@ evict_select_kernel(const EvictKv a, int32_t* __restrict__ moves, int64_t moves_
 #pragma unroll 4
     for (int w = w0; w < w1; ++w) {
         const int j = 32 * w + lane;
-        const uint32_t k = j < ctx ? key(j) : 0u;
-        const uint32_t same = __ballot_sync(0xFFFFFFFFu, j < ctx && k == prefix);
-        const bool stays = j < ctx && (k > prefix || (k == prefix && before + __popc(same & ((1u << lane) - 1)) < need));
+        const uint32_t k = j < ctx ? key(j) >> low : 0u;
+        bool stays = j < ctx && k >= prefix;
+        if (ties) {
+            const uint32_t same = __ballot_sync(0xFFFFFFFFu, j < ctx && k == prefix);
+            stays = stays && (k > prefix || before + __popc(same & ((1u << lane) - 1)) < need);
+            before += __popc(same);
+        }
         const uint32_t word = __ballot_sync(0xFFFFFFFFu, stays);
         if (lane == 0) s_keep[w] = word;
-        if (s_equal != need) before += __popc(same);
     }
     __syncthreads();
     // Pairs of a dropped row in front of the budget and a kept one from it on.  Both counted in one row of words: those of the dropped up to the word that
