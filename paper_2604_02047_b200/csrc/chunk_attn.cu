@@ -10,7 +10,7 @@
 //   warps 1, 3        MMA issuers of lane 0 and of lane 1: S = Q K^T, O += P V
 //   warp 2            planner: walks the work list and puts the segments' descriptions into a ring; checks the segments' pages behind that
 //   warps 4..7, 8..11 softmax of lane 0 and of lane 1: one query row a thread; at the segment's end the results.  The lanes of a single M tile are
-//                     joined through tensor memory.  An item that is the CTA's alone is written out; of any other the CTA leaves a partial result,
+//                     joined through tensor memory, by the one that has the last tile.  An item that is the CTA's alone is written out; of any other the CTA leaves a partial result,
 //                     and the warp that completes a count joins the 32 rows of all CTAs, in the order of the keys whoever comes last.
 // Every wait is bounded: one that runs out raises the CTA's abort flag and GOOSE_ST_TIMEOUT, and every role unwinds.
 #include <stddef.h>
@@ -74,7 +74,7 @@ constexpr int kSegments = 6;
 
 struct Header {
     Segment seg[kSegments];
-    float2 other[kChunkTile];                                // (m, l) of the lane that has a single M tile's odd key tiles
+    float2 other[kChunkTile];                                // (m, l) of the lane that does not have a single M tile's last key tile
     // Full: of the key tiles of single M tiles lane by lane (0, 1), of pairs (2).  A parity tells two phases apart, not three: nobody may wait
     // for a phase of a barrier whose phases it has not all followed, and a lane does not follow the tiles of the other one.
     unsigned long long kv_full[3][kStages];
@@ -709,7 +709,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                 ++segs;
                 tc_fence_after();
             }
-            if (!first && two && turn == 1) {                // the other lane takes what this one has
+            if (!first && two && turn != ((sg.n - 1) & 1)) { // the lane that has the last tile takes what this one has
                 hd->other[row] = make_float2(m_run, l_run);
                 tc_fence_before();
                 __syncwarp();

@@ -68,7 +68,7 @@ class Chunk(Kernel):
                     yield
                 segs += 1
                 assert self.O[l][0] == k
-            if not first and two and turn == 1:
+            if not first and two and turn != (n - 1) % 2:
                 assert self.other[warp] is None, "still to be read"
                 self.other[warp] = k
                 yield
@@ -84,7 +84,7 @@ class Chunk(Kernel):
                     for _ in range(self.r.randrange(20)):
                         yield
                     assert self.O[l ^ 1][0] == k, "the other lane's accumulators are another segment's"
-                    self.results[k, 1, warp] = list(self.O[l ^ 1][1])
+                    self.results[k, 1 - turn, warp] = list(self.O[l ^ 1][1])
                 self.results[k, turn, warp] = list(self.O[l][1])
                 yield
                 self.o_free[l].arrive()
