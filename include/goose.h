@@ -334,8 +334,9 @@ int goose_append_tokens(goose_ctx* ctx, const int32_t* draft_tok, const int32_t*
  * A chunk is a run of new tokens (a prompt or a part of it, one token, the chain of a draft) of any length: token i of sequence s has row ctx_len[s] + i.
  * n_new int32 [S] or NULL (every sequence has B tokens): the tokens 0 .. n_new[s]-1 exist, as with n_nodes above; 0: the sequence is
  * skipped; outside [0, B]: GOOSE_ST_BAD_NODES, as 0.  S * B < 2^31, H and Hkv <= max_H, S <= max_S and 65535, B is not bounded by max_B.
- * A sequence whose rows do not fit its part of the table (or the arrays beside it): GOOSE_ST_BAD_ROWS, zeros, nothing else written.  The same for a
- * token whose row, or one that it sees, is in a page outside the cache (page_table is device data); tokens in front of that one may be zeros too.  */
+ * A sequence whose rows do not fit its part of the table (or the arrays beside it): GOOSE_ST_BAD_ROWS, zeros in q_out, out and lse, nothing else written.  A page outside
+ * the cache (page_table is device data): GOOSE_ST_BAD_ROWS, and zeros for the tokens whose row is in it or that see it (tokens in front of those may be zeros too); its
+ * rows get no weights.                                                                                                              */
 
 /* goose_append_kv of a run of tokens (parent = NULL there) into pages: the same norm, rotation, layouts and limits.  Besides, where the arrays are
  * given, the new rows' entries of row_weight fp32 and row_pos int32 [S][Hkv][ldw] for every key/value head: row_weight = 0, row_pos = the token's position,
@@ -350,7 +351,8 @@ int goose_append_kv_paged(goose_ctx* ctx, const void* q, int64_t ldq, const void
  * j <= ctx_len[s] + i.  bf16, fp32 accumulation, one rounding to bf16; lse fp32 [S][B][H] = log-sum-exp of the scaled scores, or NULL.
  *   q, out  bf16 [S][B][H][D], 16-byte aligned; out may be q itself.   0 < scale < 1e30
  * What other sequences' rows and a page's rows behind the last one hold reaches no output; the chunk's own V rows must be finite (a
- * token's weight for the tokens behind it is 0, and 0 x NaN is NaN).                                                                */
+ * token's weight for the tokens behind it is 0, and 0 x NaN is NaN).  The call's workspace, 204800 bytes for every SM (30 MB), is allocated by the context's
+ * first call, which cannot be captured into a graph.  The kernel needs tensor maps, as goose_tree_attn_shared.                       */
 int goose_chunk_attn(goose_ctx* ctx, const void* q, const void* k_cache, const void* v_cache, int n_pages, int page_size,
                      const int32_t* page_table, int64_t ldt, const int32_t* ctx_len, const int32_t* n_new, int S, int B, int H,
                      int Hkv, int D, float scale, void* out, float* lse, void* stream);
@@ -358,7 +360,9 @@ int goose_chunk_attn(goose_ctx* ctx, const void* q, const void* k_cache, const v
 /* The attention that every row got from a chunk, added up: for every key/value head hk and row j < ctx_len[s] + n_new[s]
  *   row_weight[s][hk][j] += sum over the tokens i >= j - ctx_len[s] and the heads h of group hk of exp(scale q[s][i][h] . K[j][hk] - lse[s][i][h])
  * in fp32, in an order that depends on the sizes alone.  lse fp32 [S][B][H] is goose_chunk_attn's; a head of a token whose lse is -infinity adds nothing.
- * n_new may be smaller than the chunk's (the tokens of a draft that were accepted).  ctx_len[s] + n_new[s] <= ldw.  row_weight fp32 [S][Hkv][ldw].      */
+ * n_new may be smaller than the chunk's (the tokens of a draft that were accepted).  ctx_len[s] + n_new[s] <= ldw.  row_weight fp32 [S][Hkv][ldw].
+ * q 16-byte aligned; 1e-30 < scale < 1e30.  The probabilities of tokens and rows that belong together are at most 1: what an lse that is none gives is
+ * of that size times exp of what it lacks.                                                                                            */
 int goose_kv_weights(goose_ctx* ctx, const void* q, const float* lse, const void* k_cache, int n_pages, int page_size,
                      const int32_t* page_table, int64_t ldt, const int32_t* ctx_len, const int32_t* n_new, int S, int B, int H,
                      int Hkv, int D, float scale, float* row_weight, int64_t ldw, void* stream);
