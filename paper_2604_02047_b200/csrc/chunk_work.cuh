@@ -12,8 +12,10 @@
 namespace goose {
 
 constexpr int kChunkTile = 128;                  // keys of a tile, rows of an M tile
-// places of a key, and of the change to another item, for items of which some are pairs and for single M tiles
-constexpr double kShortPlaces = 1 << 30;         // so many fit 32 bits, sums of a few included
+// so many places fit 32 bits, sums of a few included (64 bits wherever that is so too: one token behind 511 rows 13.2 us instead of 12.5, drafts of 8 tokens, 40 heads, 145 instead of 143)
+constexpr double kShortPlaces = 1 << 30;
+// places of a key, and of the change to another item, for items of which some are pairs and for single M tiles.  Short lists have the changes too, although they leave
+// CTAs idle: fewer parts of an item to join (60 tokens behind 500, 32 heads over 8: 24 us, without them 41; one token behind 511 rows 10.8 and 12.5).
 constexpr int kPairKey = 5, kSingleKey = 4, kPairChange = 16 * kChunkTile, kSingleChange = 4 * kChunkTile;
 
 template <typename Int>
@@ -45,7 +47,6 @@ struct ChunkWork {
     int t;                    // tokens of an M tile
     int room;                 // rows that a sequence may have
     // worked out
-    bool changes;             // do changes count?  (not in lists of a tile or two a CTA)
     Int total, quantum;
 
     __host__ __device__ __forceinline__ ChunkSeq<Int> seq(int s) const {
@@ -57,7 +58,7 @@ struct ChunkWork {
         q.step = q.n > 2 * t ? 2 * t : q.n;
         q.pairs = q.n > q.step ? (q.n + q.step - 1) / q.step : q.n > 0;
         q.key = q.n > t ? kPairKey : kSingleKey;
-        q.change = !changes ? 0 : q.n > t ? kPairChange : kSingleChange;
+        q.change = q.n > t ? kPairChange : kSingleChange;
         return q;
     }
     // a bound of all places, whatever the lengths are
@@ -65,11 +66,10 @@ struct ChunkWork {
         const double pairs = B > t ? (B + 2.0 * t - 1) / (2.0 * t) + 1 : 1;
         return (double)S * Hkv * pairs * (kPairKey * (room + t * pairs + 2.0 * t) + kPairChange);
     }
-    // sum: places of one key/value head of all sequences, changes aside;  of_changes: those of its changes
-    __host__ __device__ __forceinline__ void set(Int sum, Int of_changes) {
+    // sum: places of one key/value head of all sequences
+    __host__ __device__ __forceinline__ void set(Int sum) {
         const Int tile = kPairKey * kChunkTile;
-        changes = sum * Hkv >= 2 * tile * G;
-        total = Hkv * (sum + (changes ? of_changes : 0));
+        total = Hkv * sum;
         quantum = total > 0 ? (total + G - 1) / G : 1;
         if (quantum < tile) quantum = tile;      // every CTA between an item's first and its last one then has a tile of it
     }

@@ -14,7 +14,7 @@
 //                     rows' weights, or, where several CTAs have Q tiles of the item, left in the workspace; the warp that completes a count adds up what
 //                     all have left, in the order of the tokens.
 //   warps 20..23      K tiles into a ring of four, 32 keys of a tile a warp, by 16-byte copies: a TMA box a page took 110 to 156 cycles a box, and pages of
-//                     16 rows have sixteen a tile (64 sequences of 8192 rows, a token each: 255 us then, 173 now, 6.4 TB/s; pages of 128 rows 218)
+//                     16 rows have sixteen a tile (64 sequences of 8192 rows, a token each: 255 us then, 177 now, 6.25 TB/s; pages of 128 rows 218, 173)
 // What bounds it.  Many tokens: the exponentials, 770 cycles a tile of 128 x 128 of the special function units', and scores that wait for their buffers, of which
 // tensor memory has no more (4096 tokens behind 8192, 32 heads over 8: 365 us, 1210 cycles a tile; 2048 behind 4096: 109).  A token a sequence: HBM (16 sequences of 1000 to
 // 8192 rows, 32 over 8: 37.7 us).
@@ -110,18 +110,12 @@ __device__ __forceinline__ Int warp_sum(Int v) {
 // the list's length and a place in it, by a whole warp (lane = sequence); false: the CTA has no range
 template <typename Int>
 __device__ __forceinline__ bool locate(WeightWork<Int>& wk, WeightCursor<Int>& cu, WeightSeq<Int>& q, Int& from, Int& to, int cta, int lane) {
-    wk.short_run = 1;
-    Int tiles = 0, sum = 0;
+    Int sum = 0;
     bool several = false;
     for (int s0 = 0; s0 < wk.S; s0 += 32)
         if (s0 + lane < wk.S) {
             const WeightSeq<Int> x = wk.seq(s0 + lane);
-            if (x.n > wk.t) several = true; else tiles += x.items;
-        }
-    wk.set_run(warp_sum(tiles));
-    for (int s0 = 0; s0 < wk.S; s0 += 32)
-        if (s0 + lane < wk.S) {
-            const WeightSeq<Int> x = wk.seq(s0 + lane);
+            several |= x.n > wk.t;
             sum += x.before(x.items);
         }
     wk.set(warp_sum(sum), __any_sync(0xFFFFFFFFu, several));
@@ -266,7 +260,7 @@ kv_weights_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                         sg->q_first = q.first(cu.k) + cu.t0;
                         sg->s = cu.s; sg->hk = cu.hk; sg->ctx = q.ctx; sg->nn = q.n;
                         sg->key0 = cu.k * q.span();
-                        sg->run = min(q.run, (q.ctx + q.n - sg->key0 + kWeightTile - 1) / kWeightTile);
+                        sg->run = min(kRun, (q.ctx + q.n - sg->key0 + kWeightTile - 1) / kWeightTile);
                         sg->whole = cu.c0 == cu.c1; sg->slot = 2 * blockIdx.x + (cu.t0 == 0); sg->c0 = cu.c0; sg->parts = cu.c1 - cu.c0 + 1;
                     }
                 }
@@ -560,7 +554,7 @@ static cudaError_t launch_as(goose_ctx* c, const KvWeights& x, cudaStream_t st) 
     WeightArgs<Int> a{};
     a.g = x.H / x.Hkv; a.H = x.H;
     a.wk.ctx_len = x.ctx_len; a.wk.n_new = x.n_new; a.wk.S = x.S; a.wk.B = x.B; a.wk.Hkv = x.Hkv; a.wk.G = c->num_sms;
-    a.wk.t = kWeightTile / a.g; a.wk.room = (int)x.pages.room(x.ldw); a.wk.short_run = 1;
+    a.wk.t = kWeightTile / a.g; a.wk.room = (int)x.pages.room(x.ldw);
     a.pages = x.pages;
     a.nb = a.wk.t < x.B ? a.wk.t : x.B;
     a.k_cache = x.k_cache;

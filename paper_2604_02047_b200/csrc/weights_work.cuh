@@ -11,30 +11,32 @@
 namespace goose {
 
 constexpr int kWeightTile = 128;                 // keys of a tile, rows of a Q tile
-constexpr double kShortWeightPlaces = 1 << 30;   // so many fit 32 bits, sums of a few included
-constexpr int kRun = 4;                          // key tiles of an item, at most
+// so many places fit 32 bits, sums of a few included (64 bits wherever that is so too: one token behind 511 rows 8.7 us instead of 8.1, 17 tokens behind 3000 10.7 instead of 10.0)
+constexpr double kShortWeightPlaces = 1 << 30;
+// key tiles of an item, at most; short lists have runs too (16 sequences of a token: 37.8 us, runs of two 42.6, none 65; a token behind 6000 rows 10, 11, 11.5)
+constexpr int kRun = 4;
 
 template <typename Int>
 struct WeightWork;
 
 template <typename Int>
 struct WeightSeq {            // a sequence's part of the list
-    int n, ctx, t, run;       // new tokens, rows in front of them, tokens of a Q tile, key tiles of an item
+    int n, ctx, t;            // new tokens, rows in front of them, tokens of a Q tile
     int items;                // of a key/value head
     int change;               // places of the change to an item
     bool bad;                 // its rows do not fit: nothing of it is done
-    __host__ __device__ __forceinline__ int span() const { return run * kWeightTile; }
+    static __host__ __device__ __forceinline__ int span() { return kRun * kWeightTile; }
     // first token that sees item k
     __host__ __device__ __forceinline__ int token(int k) const { const int i = k * span() - ctx; return i > 0 ? i : 0; }
     __host__ __device__ __forceinline__ int first(int k) const { return token(k) / t; }               // Q tile of it
     __host__ __device__ __forceinline__ int tiles(int k) const { return (n + t - 1) / t - first(k); }   // Q tiles of the item
-    __host__ __device__ __forceinline__ Int width(int k) const { return change + (Int)run * ((Int)n + t - token(k)); }
+    __host__ __device__ __forceinline__ Int width(int k) const { return change + (Int)kRun * ((Int)n + t - token(k)); }
     __host__ __device__ __forceinline__ Int before(int k) const {
-        Int w = (Int)k * (change + (Int)run * ((Int)n + t));
+        Int w = (Int)k * (change + (Int)kRun * ((Int)n + t));
         const int whole = (ctx + span() - 1) / span();       // items from here on begin behind the prefix
         if (k > whole) {
             const Int a = k, b = whole;
-            w -= run * (span() * ((a * (a - 1) - b * (b - 1)) / 2) - (Int)ctx * (a - b));
+            w -= kRun * (span() * ((a * (a - 1) - b * (b - 1)) / 2) - (Int)ctx * (a - b));
         }
         return w;
     }
@@ -42,7 +44,7 @@ struct WeightSeq {            // a sequence's part of the list
     __host__ __device__ __forceinline__ int cut(Int w0, int T, Int w) const {
         const Int x = w - w0 - change;
         if (x <= 0) return 0;
-        const Int pitch = run * t;
+        const Int pitch = kRun * t;
         return x >= T * pitch ? T : (int)WeightWork<Int>::divide(x + pitch - 1, pitch);
     }
 };
@@ -54,7 +56,6 @@ struct WeightWork {
     int t;                    // tokens of a Q tile
     int room;                 // rows that a sequence may have
     // worked out
-    int short_run;            // key tiles of an item of a sequence that has one Q tile
     Int total, quantum;
 
     __host__ __device__ __forceinline__ WeightSeq<Int> seq(int s) const {
@@ -65,15 +66,9 @@ struct WeightWork {
         if (q.bad) q.n = 0;
         if (q.n == 0) q.ctx = 0;
         q.t = t;
-        q.run = q.n > t ? kRun : short_run;
         q.items = q.n > 0 ? (q.ctx + q.n + q.span() - 1) / q.span() : 0;
         q.change = q.n > t ? kRun * t : 0;
         return q;
-    }
-    // key tiles of a head of the sequences that have one Q tile: with few of them an item is a tile, so that more CTAs have one
-    __host__ __device__ __forceinline__ void set_run(Int tiles) {
-        tiles *= Hkv;
-        short_run = tiles <= 2 * G ? 1 : tiles <= 8 * G ? 2 : kRun;
     }
     // sum: places of one key/value head of all sequences;  several: there is one of several Q tiles
     __host__ __device__ __forceinline__ void set(Int sum, bool several) {
@@ -107,7 +102,7 @@ struct WeightCursor {
         c0 = c1 = cta;                           // (what begins or ends here needs no division)
         const Int first = w0 + q.change;
         if (t0 > 0) c0 = (int)WeightWork<Int>::divide(first, wk.quantum);
-        if (t1 < T) c1 = (int)WeightWork<Int>::divide(first + (Int)(T - 1) * q.run * q.t, wk.quantum);
+        if (t1 < T) c1 = (int)WeightWork<Int>::divide(first + (Int)(T - 1) * kRun * q.t, wk.quantum);
     }
     // the next item; false: the sequence has no more
     __host__ __device__ __forceinline__ bool next(const WeightWork<Int>& wk, const WeightSeq<Int>& q) {

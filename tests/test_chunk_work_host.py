@@ -22,14 +22,12 @@ template <typename Int>
 static int walk_as(int S, int B, int Hkv, int t, int G, int room, const int32_t* ctx_len, const int32_t* n_new, double* worst) {
     ChunkWork<Int> wk{};
     wk.ctx_len = ctx_len; wk.n_new = n_new; wk.S = S; wk.B = B; wk.Hkv = Hkv; wk.G = G; wk.t = t; wk.room = room;
-    wk.changes = true;
-    Int sum = 0, of_changes = 0;
+    Int sum = 0;
     for (int s = 0; s < S; ++s) {
         const ChunkSeq<Int> q = wk.seq(s);
-        sum += q.before(q.pairs) - (Int)q.pairs * q.change;
-        of_changes += (Int)q.pairs * q.change;
+        sum += q.before(q.pairs);
     }
-    wk.set(sum, of_changes);
+    wk.set(sum);
     std::map<std::tuple<int, int, int>, std::pair<int, int>> dealt;      // item -> (tiles so far, CTAs so far)
     long long longest = 0, all = 0;
     for (int c = 0; c < G; ++c) {

@@ -22,15 +22,13 @@ template <typename Int>
 static int walk_as(int S, int B, int Hkv, int t, int G, int room, const int32_t* ctx_len, const int32_t* n_new, double* worst) {
     WeightWork<Int> wk{};
     wk.ctx_len = ctx_len; wk.n_new = n_new; wk.S = S; wk.B = B; wk.Hkv = Hkv; wk.G = G; wk.t = t; wk.room = room;
-    Int sum = 0, tiles = 0;
+    Int sum = 0;
     bool several = false;
-    wk.short_run = 1;
     for (int s = 0; s < S; ++s) {
         const WeightSeq<Int> q = wk.seq(s);
-        if (q.n > t) several = true; else tiles += q.items;
+        several |= q.n > t;
+        sum += q.before(q.items);
     }
-    wk.set_run(tiles);
-    for (int s = 0; s < S; ++s) { const WeightSeq<Int> q = wk.seq(s); sum += q.before(q.items); }
     wk.set(sum, several);
     std::map<std::tuple<int, int, int>, std::pair<int, int>> dealt;      // item -> (Q tiles so far, CTAs so far)
     long long longest = 0, all = 0;
@@ -58,7 +56,7 @@ static int walk_as(int S, int B, int Hkv, int t, int G, int room, const int32_t*
                 if (d.first != cu.t0) return 4;
                 if (c != cu.c0 + d.second || c > cu.c1) return 5;
                 d.first = cu.t1; d.second++;
-                mine += (long long)(cu.t1 - cu.t0) * q.run;
+                mine += (long long)(cu.t1 - cu.t0) * kRun;
                 const bool starts = cu.t0 == 0, ends = cu.t1 == cu.T;
                 if (starts != (c == cu.c0) || ends != (c == cu.c1)) return 6;
                 heads += !starts; tails += starts && !ends;
