@@ -3,7 +3,7 @@
 // A row's key is an unsigned number in the order of what stays: the first and the latest positions above everything, then the weights, NaN below all.
 // The budget-th largest key is found digit by digit (11, 11 and 10 bits, as far as it takes: the first has the exponent and two bits more, so that weights spread over some
 // fifty of its counters); of the rows that have that very key the lowest stay.
-// The first kernel, a block a (sequence, head), reads weights and positions once, has the keys in shared memory, and leaves a list of (place, row) pairs;
+// The first kernel, a block of 256 to 1024 threads a (sequence, head), reads weights and positions once, has the keys in shared memory, and leaves a list of (place, row) pairs;
 // the second copies the rows.  Places lie in front of the budget, rows behind it, so that no copy reads what another one writes.
 // (Closing the rows up instead would move nearly every row that stays.)  What bounds it: trips to L2 and barriers of the first kernel, 8 us for 4096 rows, 13 for 9000,
 // then HBM (16 sequences of 9000 rows, 8 heads, to 4096: 72 us, of which the copies of 308 MB are 55).
@@ -13,14 +13,14 @@
 
 namespace goose {
 
-constexpr int kEvictThreads = 1024;
-constexpr int kEvictWarps = kEvictThreads / 32;
 constexpr int kMoveThreads = 256;
 constexpr int kMovesOnce = 2;
 constexpr int kBatch = 4;
-constexpr int kBins = 2 * kEvictThreads;              // counters of a digit
+constexpr int kBins = 2048;                           // counters of a digit
 constexpr int kMostKeys = 24576;                      // keys in shared memory: two blocks an SM; rows behind them are looked up again
 constexpr int kSelectSmem = 212992;                   // of a block, at most: a bit a row, a number for 32 rows, keys
+constexpr int kSelectStatic = 4 * kBins + 1536;       // and what it has besides (the system's 1024 bytes included)
+constexpr int kSmemOfAnSm = 233472;
 
 constexpr int kMovesAhead = 4;                        // words that stand in front of a head's list (its length)
 
@@ -32,7 +32,8 @@ __device__ __forceinline__ uint32_t evict_key(float w, int pos, int sink, int64_
     return b >> 31 ? ~b : b | 0x80000000u;
 }
 
-// exclusive prefix sum over the block's threads; total in every thread.  s_warp: kEvictWarps words of its own
+// exclusive prefix sum over the block's threads; total in every thread.  s_warp: kThreads / 32 words of its own
+template <int kThreads>
 __device__ __forceinline__ int block_prefix(int v, int* s_warp, int& total) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int upto = v;
@@ -44,7 +45,7 @@ __device__ __forceinline__ int block_prefix(int v, int* s_warp, int& total) {
     __syncthreads();
     if (lane == 31) s_warp[warp] = upto;
     __syncthreads();
-    int w = lane < kEvictWarps ? s_warp[lane] : 0;
+    int w = lane < kThreads / 32 ? s_warp[lane] : 0;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
         const int u = __shfl_up_sync(0xFFFFFFFFu, w, o);
@@ -57,15 +58,17 @@ __device__ __forceinline__ int block_prefix(int v, int* s_warp, int& total) {
 
 // kBatch loads of a thread in flight: what bounds a block is the trips to L2 (one at a time, and one row a lane group in the copies: 4096 rows to 2048 12.7 us, 16 sequences
 // 45.9; these 12.4, 45.2; 8 and 4 of them 16.8, 53: registers)
-__global__ void __launch_bounds__(kEvictThreads, 1)
+template <int kThreads>
+__global__ void __launch_bounds__(kThreads, 1024 / kThreads)
 evict_select_kernel(const EvictKv a, int32_t* __restrict__ moves, int64_t moves_ld, int keep_words, int keys_there, int32_t* __restrict__ status) {
     extern __shared__ uint32_t s_keep[];              // a bit a row: it stays
     int* const s_rank = reinterpret_cast<int*>(s_keep + keep_words);   // of a word's first pair
     uint32_t* const s_key = s_keep + 2 * keep_words;  // of the first keys_there rows
-    __shared__ int s_hist[kBins], s_warp[kEvictWarps], s_digit, s_above, s_equal;
+    __shared__ int s_hist[kBins], s_warp[kThreads / 32], s_digit, s_above, s_equal;
+    constexpr int kDigits = kBins / kThreads;
     const int s = blockIdx.y, hk = blockIdx.x, tid = threadIdx.x, lane = tid & 31;
     const size_t head = (size_t)s * a.Hkv + hk;
-    for (int b = tid; b < kBins; b += kEvictThreads) s_hist[b] = 0;
+    for (int b = tid; b < kBins; b += kThreads) s_hist[b] = 0;
     pdl_wait();
     pdl_trigger();
     const int ctx = a.ctx_len[s], off = a.pos_off ? a.pos_off[s] : 0, left = min(ctx, a.budget);
@@ -74,7 +77,7 @@ evict_select_kernel(const EvictKv a, int32_t* __restrict__ moves, int64_t moves_
     bool bad = ctx < 0 || ctx > room || left > a.ldw_new;
     const int pages = bad ? 0 : (ctx + (1 << a.pages.size_log2) - 1) >> a.pages.size_log2;
 #pragma unroll 4
-    for (int p = tid; p < pages; p += kEvictThreads) {
+    for (int p = tid; p < pages; p += kThreads) {
         const int page = a.pages.table[s * a.pages.ldt + p];
         bad |= page < 0 || page >= a.pages.n;
     }
@@ -92,20 +95,20 @@ evict_select_kernel(const EvictKv a, int32_t* __restrict__ moves, int64_t moves_
     const int32_t* __restrict__ pos = a.row_pos + head * a.ldw;
     float* __restrict__ new_weight = a.new_weight + head * a.ldw_new;
     int32_t* __restrict__ new_pos = a.new_pos + head * a.ldw_new;
-    // f(row, weight, position) for the rows first + tid, first + tid + kEvictThreads, ... in front of n
+    // f(row, weight, position) for the rows first + tid, first + tid + kThreads, ... in front of n
     auto each_row = [&](int n, auto f) {
-        for (int j0 = tid; j0 < n; j0 += kBatch * kEvictThreads) {
+        for (int j0 = tid; j0 < n; j0 += kBatch * kThreads) {
             float w[kBatch];
             int p[kBatch];
 #pragma unroll
             for (int u = 0; u < kBatch; ++u) {
-                const int j = min(j0 + u * kEvictThreads, n - 1);
+                const int j = min(j0 + u * kThreads, n - 1);
                 w[u] = weight[j];
                 p[u] = pos[j];
             }
 #pragma unroll
             for (int u = 0; u < kBatch; ++u)
-                if (j0 + u * kEvictThreads < n) f(j0 + u * kEvictThreads, w[u], p[u]);
+                if (j0 + u * kThreads < n) f(j0 + u * kThreads, w[u], p[u]);
         }
     };
     if (ctx <= a.budget) {
@@ -127,22 +130,31 @@ evict_select_kernel(const EvictKv a, int32_t* __restrict__ moves, int64_t moves_
             });
         } else {
 #pragma unroll 4
-            for (int j = tid; j < ctx; j += kEvictThreads) {
+            for (int j = tid; j < ctx; j += kThreads) {
                 const uint32_t k = key(j);
                 if (k >> (shift + digit_bits) == prefix) atomicAdd(&s_hist[k >> shift & ((1 << digit_bits) - 1)], 1);
             }
         }
         __syncthreads();
-        // thread t has the digits kBins - 1 - 2 t and the one below: how many rows have a larger one
-        const int high = kBins - 1 - 2 * tid, mine = s_hist[high], below = s_hist[high - 1];
-        const int above = block_prefix(mine + below, s_warp, total);
-        if (above < need && above + mine + below >= need) {
-            const bool first = above + mine >= need;
-            s_digit = first ? high : high - 1;
-            s_above = first ? above : above + mine;
-            s_equal = first ? mine : below;
+        // thread t has the digits from kBins - 1 - kDigits t down: how many rows have a larger one
+        const int high = kBins - 1 - kDigits * tid;
+        int mine[kDigits], sum = 0;
+#pragma unroll
+        for (int u = 0; u < kDigits; ++u) {
+            mine[u] = s_hist[high - u];
+            s_hist[high - u] = 0;
+            sum += mine[u];
         }
-        s_hist[high] = s_hist[high - 1] = 0;
+        int above = block_prefix<kThreads>(sum, s_warp, total);
+#pragma unroll
+        for (int u = 0; u < kDigits; ++u) {
+            if (above < need && above + mine[u] >= need) {
+                s_digit = high - u;
+                s_above = above;
+                s_equal = mine[u];
+            }
+            above += mine[u];
+        }
         __syncthreads();
         prefix = prefix << digit_bits | (uint32_t)s_digit;
         need -= s_above;
@@ -150,7 +162,7 @@ evict_select_kernel(const EvictKv a, int32_t* __restrict__ moves, int64_t moves_
         if (s_equal == need) break;                   // all that have these digits stay: the others do not matter
     }
     // what stays, in words of 32 rows; a warp's rows are consecutive
-    const int words = (ctx + 31) >> 5, per = (words + kEvictWarps - 1) / kEvictWarps;
+    const int words = (ctx + 31) >> 5, per = (words + kThreads / 32 - 1) / (kThreads / 32);
     const int w0 = min((tid >> 5) * per, words), w1 = min(w0 + per, words);
     int before = 0;                                   // rows of that very key in front of the warp's
     const bool ties = s_equal != need;                // (else all of them stay)
@@ -160,7 +172,7 @@ evict_select_kernel(const EvictKv a, int32_t* __restrict__ moves, int64_t moves_
             const int j = 32 * w + lane;
             equal += __popc(__ballot_sync(0xFFFFFFFFu, j < ctx && key(j) == prefix));
         }
-        before = block_prefix(lane == 0 ? equal : 0, s_warp, total);
+        before = block_prefix<kThreads>(lane == 0 ? equal : 0, s_warp, total);
         before = __shfl_sync(0xFFFFFFFFu, before, 0);
     }
 #pragma unroll 4
@@ -181,11 +193,11 @@ evict_select_kernel(const EvictKv a, int32_t* __restrict__ moves, int64_t moves_
     // the budget is in, then, from that word on, those of the kept.
     const int b0 = a.budget >> 5;
     const uint32_t inside = (1u << (a.budget & 31)) - 1;   // of word b0: rows in front of the budget
-    const int entries = words + 1, each = (entries + kEvictThreads - 1) / kEvictThreads, e0 = min(tid * each, entries), e1 = min(e0 + each, entries);
+    const int entries = words + 1, each = (entries + kThreads - 1) / kThreads, e0 = min(tid * each, entries), e1 = min(e0 + each, entries);
     auto pairs = [&](int e) { return e < b0 ? ~s_keep[e] : e == b0 ? ~s_keep[e] & inside : s_keep[e - 1] & (e == b0 + 1 ? ~inside : 0xFFFFFFFFu); };
     int count = 0;
     for (int e = e0; e < e1; ++e) count += __popc(pairs(e));
-    int at = block_prefix(count, s_warp, total);
+    int at = block_prefix<kThreads>(count, s_warp, total);
     for (int e = e0; e < e1; ++e) {
         s_rank[e] = at;
         at += __popc(pairs(e));
@@ -199,7 +211,7 @@ evict_select_kernel(const EvictKv a, int32_t* __restrict__ moves, int64_t moves_
     int32_t* const of = fit ? to + ctx / 2 : list_of;
     if (tid == 0) list[0] = n;
     __syncthreads();
-    for (int j = a.budget + tid; j < ctx; j += kEvictThreads) {
+    for (int j = a.budget + tid; j < ctx; j += kThreads) {
         const uint32_t word = s_keep[j >> 5] & (j >> 5 == b0 ? ~inside : 0xFFFFFFFFu);
         if (word >> (j & 31) & 1) of[s_rank[(j >> 5) + 1] - n + __popc(word & ((1u << (j & 31)) - 1))] = j;
     }
@@ -210,12 +222,12 @@ evict_select_kernel(const EvictKv a, int32_t* __restrict__ moves, int64_t moves_
         else to[s_rank[j >> 5] + __popc(~word & ((1u << (j & 31)) - 1))] = j;
     });
     __syncthreads();
-    for (int m0 = tid; m0 < n; m0 += kBatch * kEvictThreads) {
+    for (int m0 = tid; m0 < n; m0 += kBatch * kThreads) {
         int t[kBatch], f[kBatch], p[kBatch], row_t[kBatch], row_f[kBatch];
         float w[kBatch];
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
-            const int m = m0 + u * kEvictThreads < n ? m0 + u * kEvictThreads : m0;   // (its own: the lists may lie where the results go)
+            const int m = m0 + u * kThreads < n ? m0 + u * kThreads : m0;   // (its own: the lists may lie where the results go)
             t[u] = to[m];
             f[u] = of[m];
         }
@@ -228,7 +240,7 @@ evict_select_kernel(const EvictKv a, int32_t* __restrict__ moves, int64_t moves_
         }
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
-            const int m = m0 + u * kEvictThreads;
+            const int m = m0 + u * kThreads;
             if (m >= n) break;
             new_weight[t[u]] = w[u];
             new_pos[t[u]] = p[u];
@@ -280,7 +292,13 @@ cudaError_t launch_evict_kv(goose_ctx* c, const EvictKv& a, cudaStream_t st) {
     int32_t* moves = static_cast<int32_t*>(c->evict_moves);
     const int keep_words = (int)((room + 31) / 32) + 1, keys_there = std::min({(int)room, kMostKeys, kSelectSmem / 4 - 2 * keep_words});
     const size_t smem = sizeof(uint32_t) * (size_t)(2 * keep_words + keys_there);
-    cudaError_t e = launch_pdl(evict_select_kernel, dim3(a.Hkv, a.S), dim3(kEvictThreads), smem, st, a, moves, ld, keep_words, keys_there, c->status);
+    // Of more heads than SMs smaller blocks, two or four an SM where their shared memory allows it, so that one's trips to L2 go beside another's work (512 heads of 2500
+    // rows to 2048: 72 us, two 63, four 59; of 517 to 500 33, 22, 19; 320 of 4200 to 4096 46, 40, 40).  Fewer heads want all threads (128 heads of 3500 to 9000 rows 45, 51, 65).
+    auto fits = [&](int blocks) { return (size_t)blocks * (smem + kSelectStatic) <= (size_t)kSmemOfAnSm; };
+    const int64_t heads = (int64_t)a.S * a.Hkv;
+    auto select = heads > 2 * c->num_sms && fits(4) ? evict_select_kernel<256> : heads > c->num_sms && fits(2) ? evict_select_kernel<512> : evict_select_kernel<1024>;
+    const int threads = select == evict_select_kernel<256> ? 256 : select == evict_select_kernel<512> ? 512 : 1024;
+    cudaError_t e = launch_pdl(select, dim3(a.Hkv, a.S), dim3(threads), smem, st, a, moves, ld, keep_words, keys_there, c->status);
     c->launches++;
     if (e != cudaSuccess || most == 0) return e;
     const int64_t blocks = (most + kMovesOnce * kMoveThreads / 16 - 1) / (kMovesOnce * kMoveThreads / 16);
@@ -290,7 +308,9 @@ cudaError_t launch_evict_kv(goose_ctx* c, const EvictKv& a, cudaStream_t st) {
 }
 
 cudaError_t init_evict_kernels() {
-    cudaError_t e = cudaFuncSetAttribute(evict_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSelectSmem);
+    cudaError_t e = cudaSuccess;
+    for (auto select : {evict_select_kernel<1024>, evict_select_kernel<512>, evict_select_kernel<256>})
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(select, cudaFuncAttributeMaxDynamicSharedMemorySize, kSelectSmem);
     return e == cudaSuccess ? load_kernels({(const void*)evict_move_kernel}) : e;
 }
 

@@ -201,3 +201,21 @@ def test_refusals(goose):
         goose.evict_kv(**{**base, "budget": 2 ** 31})
     torch.cuda.synchronize()
     assert not goose.last_status(2).any()
+
+
+@pytest.mark.parametrize("Hkv,S,page", [(8, 20, 16), (5, 64, 32), (64, 3, 16), (64, 6, 64), (20, 15, 16)])
+def test_more_heads_than_the_device_has_sms(goose, Hkv, S, page):
+    """All sizes of blocks, ragged sequences, some that lose nothing; ties."""
+    rng = np.random.default_rng([Hkv, S])
+    ctxs = rng.integers(0, 700, S).tolist()
+    ctxs[0], ctxs[-1] = 300, 301
+    Case(Hkv, ctxs, page, 300, 3, 20, off=rng.integers(0, 50, S).tolist(), seed=S).check(goose)
+    Case(Hkv, ctxs, page, 129, 0, 0, seed=S + 1, weights=lambda r, shape: r.integers(0, 3, shape)).check(goose)
+
+
+def test_more_heads_with_long_tables(goose):
+    """Room for more keys than two or four blocks an SM have, sequences short and long."""
+    Case(64, [500, 30, 700, 129, 128, 0], 16, 128, 4, 10, seed=20, width=900).check(goose)
+    Case(40, [500, 30, 700, 129, 128, 0], 16, 128, 4, 10, seed=21, width=32768, room=40000).check(goose)
+    Case(2, [17000] + [90] * 69, 16, 100, 4, 10, seed=22, room=25000, width=1700).check(goose)
+    Case(2, [26000] + [90] * 69, 16, 25000, 4, 10, seed=23, room=26100, width=1700).check(goose)
