@@ -6,7 +6,7 @@
 // The first kernel, a block of 256 to 1024 threads a (sequence, head), reads weights and positions once, has the keys in shared memory, and leaves a list of (place, row) pairs;
 // the second copies the rows.  Places lie in front of the budget, rows behind it, so that no copy reads what another one writes.
 // (Closing the rows up instead would move nearly every row that stays.)  What bounds it: trips to L2 and barriers of the first kernel, 8 us for 4096 rows, 13 for 9000,
-// then HBM (16 sequences of 9000 rows, 8 heads, to 4096: 72 us, of which the copies of 308 MB are 55).
+// then HBM (16 sequences of 9000 rows, 8 heads, to 4096: 71 us, of which the copies of 308 MB are 55).
 #include <algorithm>
 
 #include "goose_internal.cuh"
@@ -301,8 +301,11 @@ cudaError_t launch_evict_kv(goose_ctx* c, const EvictKv& a, cudaStream_t st) {
     cudaError_t e = launch_pdl(select, dim3(a.Hkv, a.S), dim3(threads), smem, st, a, moves, ld, keep_words, keys_there, c->status);
     c->launches++;
     if (e != cudaSuccess || most == 0) return e;
-    const int64_t blocks = (most + kMovesOnce * kMoveThreads / 16 - 1) / (kMovesOnce * kMoveThreads / 16);
-    e = launch_pdl(evict_move_kernel, dim3((unsigned)(blocks < 64 ? blocks : 64), a.Hkv, a.S), dim3(kMoveThreads), 0, st, a, moves, ld);
+    // blocks of a head: one for every batch of rows that can move, but few of them beyond two rounds of what the SMs hold, since most heads move fewer (always 64: 512 heads of
+    // 2500 rows to 2048 60 us, these 57; 128 heads 45 and 43; one round 58, 46)
+    const int64_t rows = kMovesOnce * kMoveThreads / 16;
+    const int64_t blocks = std::min({(most + rows - 1) / rows, (int64_t)64, (2 * 8 * c->num_sms + heads - 1) / heads});
+    e = launch_pdl(evict_move_kernel, dim3((unsigned)blocks, a.Hkv, a.S), dim3(kMoveThreads), 0, st, a, moves, ld);
     c->launches++;
     return e;
 }
