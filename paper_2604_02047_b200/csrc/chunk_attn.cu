@@ -151,12 +151,14 @@ __device__ __forceinline__ Int warp_sum(Int v) {
 template <typename Int>
 __device__ __forceinline__ bool locate(ChunkWork<Int>& wk, ChunkCursor<Int>& cu, ChunkSeq<Int>& q, Int& from, Int& to, int cta, int lane) {
     Int sum = 0;
+    bool several = false;
     for (int s0 = 0; s0 < wk.S; s0 += 32)
         if (s0 + lane < wk.S) {
             const ChunkSeq<Int> x = wk.seq(s0 + lane);
             sum += x.before(x.pairs);
+            several |= x.n > wk.t;
         }
-    wk.set(warp_sum(sum));
+    wk.set(warp_sum(sum), __any_sync(0xFFFFFFFFu, several));
     from = wk.start(cta);
     to = wk.start(cta + 1);
     if (from >= to) return false;

@@ -15,8 +15,9 @@ constexpr int kChunkTile = 128;                  // keys of a tile, rows of an M
 // so many places fit 32 bits, sums of a few included (64 bits wherever that is so too: one token behind 511 rows 13.2 us instead of 12.5, drafts of 8 tokens, 40 heads, 145 instead of 143)
 constexpr double kShortPlaces = 1 << 30;
 // places of a key, and of the change to another item, for items of which some are pairs and for single M tiles.  Short lists have the changes too, although they leave
-// CTAs idle: fewer parts of an item to join (60 tokens behind 500, 32 heads over 8: 24 us, without them 41; one token behind 511 rows 10.8 and 12.5).
-constexpr int kPairKey = 5, kSingleKey = 4, kPairChange = 16 * kChunkTile, kSingleChange = 4 * kChunkTile;
+// CTAs idle: fewer parts of an item to join (60 tokens behind 500, 32 heads over 8: 24 us, without them 41; one token behind 511 rows 10.8 and 12.5).  A change of single tiles as 4, 6
+// and 8 x 128 places: 16 drafts of up to 17 tokens, 40 heads 144, 140, 140 us; 32 sequences of a token, 40 heads 155, 151, 148; 64, 32 over 8 235, 235.5, 237.
+constexpr int kPairKey = 5, kSingleKey = 4, kPairChange = 16 * kChunkTile, kSingleChange = 6 * kChunkTile;
 
 template <typename Int>
 struct ChunkSeq {             // a sequence's part of the list
@@ -66,9 +67,9 @@ struct ChunkWork {
         const double pairs = B > t ? (B + 2.0 * t - 1) / (2.0 * t) + 1 : 1;
         return (double)S * Hkv * pairs * (kPairKey * (room + t * pairs + 2.0 * t) + kPairChange);
     }
-    // sum: places of one key/value head of all sequences
-    __host__ __device__ __forceinline__ void set(Int sum) {
-        const Int tile = kPairKey * kChunkTile;
+    // sum: places of one key/value head of all sequences;  several: there are pairs
+    __host__ __device__ __forceinline__ void set(Int sum, bool several) {
+        const Int tile = (several ? kPairKey : kSingleKey) * kChunkTile;
         total = Hkv * sum;
         quantum = total > 0 ? (total + G - 1) / G : 1;
         if (quantum < tile) quantum = tile;      // every CTA between an item's first and its last one then has a tile of it

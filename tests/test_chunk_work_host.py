@@ -23,11 +23,13 @@ static int walk_as(int S, int B, int Hkv, int t, int G, int room, const int32_t*
     ChunkWork<Int> wk{};
     wk.ctx_len = ctx_len; wk.n_new = n_new; wk.S = S; wk.B = B; wk.Hkv = Hkv; wk.G = G; wk.t = t; wk.room = room;
     Int sum = 0;
+    bool several = false;
     for (int s = 0; s < S; ++s) {
         const ChunkSeq<Int> q = wk.seq(s);
         sum += q.before(q.pairs);
+        several |= q.n > t;
     }
-    wk.set(sum);
+    wk.set(sum, several);
     std::map<std::tuple<int, int, int>, std::pair<int, int>> dealt;      // item -> (tiles so far, CTAs so far)
     long long longest = 0, all = 0;
     for (int c = 0; c < G; ++c) {
