@@ -14,10 +14,10 @@
 //                     the CTA leaves a partial result, and the warp that completes a count joins the 32 rows of all CTAs, in the order of the keys
 //                     whoever comes last.
 // What bounds it.  Long chunks: a lane's chain (scores, exponentials, product), 3080 cycles a pair of tiles of which the exponentials are 2048 and the
-// products 2048 (4096 tokens behind 8192, 32 heads over 8: 538 to 551 us, 1.25 to 1.28 PFLOP/s in bursts; under the power cap 627).  Short ones: changes of item, some
-// 10000 cycles with the first tile behind them (5 prompts of 500 to 1500 tokens, 52 heads: 138 to 145 us), and the causal edge.  A token a sequence: HBM, and the TMA boxes of
-// pages of 16 rows, some 100 cycles each (64 sequences of 500 to 8192 rows, 32 over 8: 232 us, 5.1 TB/s; pages of 128 rows and equal lengths 5.8).  One token: serial latency
-// (511 rows: 12.2 us).
+// products 2048 (4096 tokens behind 8192, 32 heads over 8: 544 us, 1.26 PFLOP/s in bursts; under the power cap 623).  Short ones: changes of item, some
+// 10000 cycles with the first tile behind them (5 prompts of 500 to 1500 tokens, 52 heads: 144 us), and the causal edge.  A token a sequence: HBM, and the TMA boxes of
+// pages of 16 rows, some 100 cycles each (64 sequences of 500 to 8192 rows, 32 over 8: 235 us, 5.1 TB/s; pages of 128 rows and equal lengths 5.8).  One token: serial latency
+// (511 rows: 10.6 to 11.4 us).
 // Every wait is bounded: one that runs out raises the CTA's abort flag and GOOSE_ST_TIMEOUT, and every role unwinds.
 #include <stddef.h>
 

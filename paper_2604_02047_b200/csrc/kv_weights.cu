@@ -16,8 +16,8 @@
 //   warps 20..23      K tiles into a ring of four, 32 keys of a tile a warp, by 16-byte copies: a TMA box a page took 110 to 156 cycles a box, and pages of
 //                     16 rows have sixteen a tile (64 sequences of 8192 rows, a token each: 255 us then, 177 now, 6.25 TB/s; pages of 128 rows 218, 173)
 // What bounds it.  Many tokens: the exponentials, 770 cycles a tile of 128 x 128 of the special function units', and scores that wait for their buffers, of which
-// tensor memory has no more (4096 tokens behind 8192, 32 heads over 8: 365 us, 1210 cycles a tile; 2048 behind 4096: 109).  A token a sequence: HBM (16 sequences of 1000 to
-// 8192 rows, 32 over 8: 37.7 us).
+// tensor memory has no more (4096 tokens behind 8192, 32 heads over 8: 365 us, 1210 cycles a tile; 2048 behind 4096: 107).  A token a sequence: HBM (16 sequences of 1000 to
+// 8192 rows, 32 over 8: 36 us).
 // Every wait is bounded: one that runs out raises the CTA's abort flag and GOOSE_ST_TIMEOUT, and every role unwinds.
 #include <stddef.h>
 
