@@ -351,7 +351,7 @@ int goose_append_kv_paged(goose_ctx* ctx, const void* q, int64_t ldq, const void
  * j <= ctx_len[s] + i.  bf16, fp32 accumulation, one rounding to bf16; lse fp32 [S][B][H] = log-sum-exp of the scaled scores, or NULL.
  *   q, out  bf16 [S][B][H][D], 16-byte aligned; out may be q itself.   0 < scale < 1e30
  * What other sequences' rows and a page's rows behind the last one hold reaches no output; the chunk's own V rows must be finite (a
- * token's weight for the tokens behind it is 0, and 0 x NaN is NaN).  The call's workspace, 204800 bytes for every SM (30 MB), is allocated by the context's
+ * token's weight for the tokens behind it is 0, and 0 x NaN is NaN).  The call's workspace, 270336 bytes for every SM (40 MB), is allocated by the context's
  * first call, which cannot be captured into a graph.  The kernel needs tensor maps, as goose_tree_attn_shared.                       */
 int goose_chunk_attn(goose_ctx* ctx, const void* q, const void* k_cache, const void* v_cache, int n_pages, int page_size,
                      const int32_t* page_table, int64_t ldt, const int32_t* ctx_len, const int32_t* n_new, int S, int B, int H,

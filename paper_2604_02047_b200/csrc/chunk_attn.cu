@@ -45,22 +45,12 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kRescaleThreshold = 8.0f;                    // rescale O only when the running max grew by > 2^8
 constexpr long long kWaitCycles = 2000000000ll;              // bound of every wait: about one second of SM clock
 
-// Partial result of an M tile: 25 words of 16 bytes a row, words of neighbouring rows next to one another.  O in three bytes an element, fp32
-// without its last byte (16 bits of significand of every element by itself; the output has 8): the two upper bytes of 8 columns in each of 16
-// words, the third ones of 16 columns in each of 8, then (m, l) in fp32.  l < 0: rows that cannot be computed.
+// Partial result of an M tile: 33 words of 16 bytes a row, words of neighbouring rows next to one another: O in fp32, 4 columns a word, as it was summed (rounded
+// to fewer bits, parts that nearly cancel would leave the error of the larger ones), then (m, l).  l < 0: rows that cannot be computed.
 // A CTA has four places: of its segment that does not begin an item (at most one, its first) and of the one that begins an item and does not end it
 // (its last), two M tiles each.
-constexpr int kPartThird = 16, kPartSums = 24, kPartWords = 25;
+constexpr int kPartSums = kHeadDim / 4, kPartWords = kPartSums + 1;
 constexpr uint32_t kPartBlock = kPartWords * kChunkTile;
-__device__ __forceinline__ uint32_t upper_halves(uint32_t x0, uint32_t x1) { return __byte_perm(x0, x1, 0x7632); }
-__device__ __forceinline__ uint32_t third_bytes(uint32_t x0, uint32_t x1, uint32_t x2, uint32_t x3) {
-    return __byte_perm(__byte_perm(x0, x1, 0x0051), __byte_perm(x2, x3, 0x0051), 0x5410);
-}
-template <int kAt>                                           // element 0..3 of the four
-__device__ __forceinline__ float part_element(uint32_t halves, uint32_t thirds) {
-    constexpr uint32_t third = 4 + kAt, upper = kAt & 1 ? 0x3200 : 0x1000;
-    return __uint_as_float(__byte_perm(halves, thirds, upper | third << 4 | third));
-}
 
 // a segment, as the planner describes it
 struct Segment {
@@ -226,23 +216,18 @@ __device__ __forceinline__ void join_parts(const ChunkArgs<Int>& a, int c0, int 
         for (int e = 0; e < kCols; ++e) acc[e] = 0.f;
         for (int k0 = 0; k0 < n; k0 += kRound) {
             float2 ml[kRound];
-            uint4 x[kRound][kCols / 16][3];
+            float4 x[kRound][kCols / 4];
 #pragma unroll
             for (int u = 0; u < kRound; ++u) {
                 const int k = k0 + u;
                 ml[u] = make_float2(-INFINITY, 0.f);
 #pragma unroll
-                for (int b = 0; b < kCols / 16; ++b) x[u][b][0] = x[u][b][1] = x[u][b][2] = make_uint4(0, 0, 0, 0);
+                for (int w = 0; w < kCols / 4; ++w) x[u][w] = make_float4(0.f, 0.f, 0.f, 0.f);
                 if (k < n && row0 + r < rows) {
                     const uint4* part = a.parts + (size_t)(4 * (c0 + k) + (k == 0 ? 2 : 0) + l) * kPartBlock + row0 + r;
                     ml[u] = __ldcg(reinterpret_cast<const float2*>(part + kPartSums * kChunkTile));
 #pragma unroll
-                    for (int b = 0; b < kCols / 16; ++b) {
-                        const int w = c / 16 + b;
-                        x[u][b][0] = __ldcg(part + (2 * w) * kChunkTile);
-                        x[u][b][1] = __ldcg(part + (2 * w + 1) * kChunkTile);
-                        x[u][b][2] = __ldcg(part + (kPartThird + w) * kChunkTile);
-                    }
+                    for (int w = 0; w < kCols / 4; ++w) x[u][w] = __ldcg(reinterpret_cast<const float4*>(part + (c / 4 + w) * kChunkTile));
                 }
             }
 #pragma unroll
@@ -254,18 +239,12 @@ __device__ __forceinline__ void join_parts(const ChunkArgs<Int>& a, int c0, int 
                 M = M_new;
                 L = __fmaf_rn(w, ml[u].y, __fmul_rn(L, old));
 #pragma unroll
-                for (int b = 0; b < kCols / 16; ++b) {
-                    const uint32_t thirds[4] = {x[u][b][2].x, x[u][b][2].y, x[u][b][2].z, x[u][b][2].w};
-#pragma unroll
-                    for (int v = 0; v < 4; ++v) {
-                        const uint4& half = x[u][b][v >> 1];
-                        const uint32_t h0 = v & 1 ? half.z : half.x, h1 = v & 1 ? half.w : half.y;
-                        float* o = acc + 16 * b + 4 * v;
-                        o[0] = __fmaf_rn(w, part_element<0>(h0, thirds[v]), __fmul_rn(o[0], old));
-                        o[1] = __fmaf_rn(w, part_element<1>(h0, thirds[v]), __fmul_rn(o[1], old));
-                        o[2] = __fmaf_rn(w, part_element<2>(h1, thirds[v]), __fmul_rn(o[2], old));
-                        o[3] = __fmaf_rn(w, part_element<3>(h1, thirds[v]), __fmul_rn(o[3], old));
-                    }
+                for (int v = 0; v < kCols / 4; ++v) {
+                    float* o = acc + 4 * v;
+                    o[0] = __fmaf_rn(w, x[u][v].x, __fmul_rn(o[0], old));
+                    o[1] = __fmaf_rn(w, x[u][v].y, __fmul_rn(o[1], old));
+                    o[2] = __fmaf_rn(w, x[u][v].z, __fmul_rn(o[2], old));
+                    o[3] = __fmaf_rn(w, x[u][v].w, __fmul_rn(o[3], old));
                 }
             }
         }
@@ -787,13 +766,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                         if (row_valid) {
                             uint4* part = a.parts + (size_t)(4 * blockIdx.x + (sg.t_first == 0 ? 2 : 0) + m_tile) * kPartBlock + row;
 #pragma unroll
-                            for (int c = 0; c < 8; ++c) {
-                                const uint32_t* x = v + 16 * c;
-                                part[2 * c * kChunkTile] = make_uint4(upper_halves(x[0], x[1]), upper_halves(x[2], x[3]), upper_halves(x[4], x[5]), upper_halves(x[6], x[7]));
-                                part[(2 * c + 1) * kChunkTile] = make_uint4(upper_halves(x[8], x[9]), upper_halves(x[10], x[11]), upper_halves(x[12], x[13]), upper_halves(x[14], x[15]));
-                                part[(kPartThird + c) * kChunkTile] = make_uint4(third_bytes(x[0], x[1], x[2], x[3]), third_bytes(x[4], x[5], x[6], x[7]),
-                                                                                 third_bytes(x[8], x[9], x[10], x[11]), third_bytes(x[12], x[13], x[14], x[15]));
-                            }
+                            for (int c = 0; c < kPartSums; ++c) part[c * kChunkTile] = make_uint4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
                             *reinterpret_cast<float2*>(part + kPartSums * kChunkTile) = make_float2(m_run, sg.bad ? -1.f : l_run);
                         }
                         __threadfence();
