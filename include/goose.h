@@ -336,7 +336,7 @@ int goose_append_tokens(goose_ctx* ctx, const int32_t* draft_tok, const int32_t*
  * skipped; outside [0, B]: GOOSE_ST_BAD_NODES, as 0.  S * B < 2^31, H and Hkv <= max_H, S <= max_S and 65535, B is not bounded by max_B.
  * A sequence whose rows do not fit its part of the table (or the arrays beside it): GOOSE_ST_BAD_ROWS, zeros in q_out, out and lse, nothing else written.  A page outside
  * the cache (page_table is device data): GOOSE_ST_BAD_ROWS, and zeros for the tokens whose row is in it or that see it (tokens in front of those may be zeros too); its
- * rows get no weights.                                                                                                              */
+ * rows get no weights.  The zero of such an lse is -0.0f, which no log-sum-exp of goose_chunk_attn's is: goose_kv_weights adds nothing for it.     */
 
 /* goose_append_kv of a run of tokens (parent = NULL there) into pages: the same norm, rotation, layouts and limits.  Besides, where the arrays are
  * given, the new rows' entries of row_weight fp32 and row_pos int32 [S][Hkv][ldw] for every key/value head: row_weight = 0, row_pos = the token's position,
@@ -359,7 +359,8 @@ int goose_chunk_attn(goose_ctx* ctx, const void* q, const void* k_cache, const v
 
 /* The attention that every row got from a chunk, added up: for every key/value head hk and row j < ctx_len[s] + n_new[s]
  *   row_weight[s][hk][j] += sum over the tokens i >= j - ctx_len[s] and the heads h of group hk of exp(scale q[s][i][h] . K[j][hk] - lse[s][i][h])
- * in fp32, in an order that depends on the sizes alone.  lse fp32 [S][B][H] is goose_chunk_attn's; a head of a token whose lse is -infinity adds nothing.
+ * in fp32, in an order that depends on the sizes alone.  lse fp32 [S][B][H] is goose_chunk_attn's; a head of a token whose lse is
+ * -infinity or -0.0f adds nothing.
  * n_new may be smaller than the chunk's (the tokens of a draft that were accepted).  ctx_len[s] + n_new[s] <= ldw.  row_weight fp32 [S][Hkv][ldw].
  * q 16-byte aligned; 1e-30 < scale < 1e30.  The probabilities of tokens and rows that belong together are at most 1: what an lse that is none gives is
  * of that size times exp of what it lacks.                                                                                            */

@@ -256,7 +256,7 @@ __device__ __forceinline__ void join_parts(const ChunkArgs<Int>& a, int c0, int 
                 dst[e / 8] = bad ? make_uint4(0, 0, 0, 0)
                                  : make_uint4(pack_bf16x2(acc[e] * inv, acc[e + 1] * inv), pack_bf16x2(acc[e + 2] * inv, acc[e + 3] * inv),
                                               pack_bf16x2(acc[e + 4] * inv, acc[e + 5] * inv), pack_bf16x2(acc[e + 6] * inv, acc[e + 7] * inv));
-            if (write_lse && c == 0) a.lse[out_row] = bad ? 0.f : (M + log2f(L)) * kLn2;
+            if (write_lse && c == 0) a.lse[out_row] = bad ? kNoLse : (M + log2f(L)) * kLn2;
         }
     }
 }
@@ -760,7 +760,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                                     reinterpret_cast<uint4*>(dst)[2 * c + 1] = make_uint4(w[4], w[5], w[6], w[7]);
                                 }
                             }
-                            if (a.lse) a.lse[at] = sg.bad ? 0.f : (m_run + log2f(l_run)) * kLn2;
+                            if (a.lse) a.lse[at] = sg.bad ? kNoLse : (m_run + log2f(l_run)) * kLn2;
                         }
                     } else {
                         if (row_valid) {

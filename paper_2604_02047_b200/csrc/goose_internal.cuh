@@ -291,6 +291,9 @@ cudaError_t launch_tree_attn_shared(goose_ctx* c, const __nv_bfloat16* q, const 
                                     const int32_t* ctx_len, const int32_t* parent, const int32_t* n_nodes, int S, int B, int H,
                                     int Hkv, float scale, __nv_bfloat16* out, float* lse, cudaStream_t st);
 
+// What goose_chunk_attn leaves as the log-sum-exp of a token that cannot be computed: a zero that no sum is (a maximum and a logarithm whose sum is zero give +0), so that
+// goose_kv_weights can tell it from scores that do add up to one.
+constexpr float kNoLse = -0.f;
 // the paged cache: arguments of goose_chunk_attn, goose_kv_weights and goose_evict_kv
 struct ChunkAttn {
     const __nv_bfloat16 *q, *k_cache, *v_cache;

@@ -369,6 +369,7 @@ kv_weights_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                     for (int w = 0; w < 4; ++w) {
                         const int r = 32 * w + lane, token = r / a.g;
                         x[w] = r < rows ? lse[(size_t)token * a.H + (r - token * a.g)] : -INFINITY;
+                        if (__float_as_uint(x[w]) == __float_as_uint(kNoLse)) x[w] = -INFINITY;
                     }
                     ok = all(wait_for(hd, &hd->lse_empty[qs.at], qs.phase ^ 1, a.status));
                     if (!ok) break;

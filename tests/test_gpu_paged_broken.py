@@ -1,0 +1,78 @@
+"""Tables with a page outside the pool and sequences that do not fit: what the calls that belong together make of one another's results.  Tolerances are those
+of each call's own tests."""
+import pytest
+import torch
+
+from _pages import D, attention, i32
+from test_gpu_chunk_attn import Case as Chunk
+
+pytestmark = pytest.mark.gpu
+SCALE = D ** -0.5
+
+
+@pytest.fixture(scope="module")
+def goose():
+    from paper_2604_02047_b200 import binding, build
+    build.build()
+    g = binding.Goose(max_S=70, max_B=16, max_H=64)
+    yield g
+    g.close()
+
+
+def _added(c, s, lse):
+    """What the tokens of sequence s that have been computed add to its rows, in 64 bits, [Hkv][rows]."""
+    n, ctx = c.n[s], c.ctxs[s]
+    K = c.c.keys(s, ctx + n)
+    _, _, l, p = attention(c.q[s, :n], K, K, ctx, SCALE)
+    Hkv = K.shape[1]
+    off = (l - lse[s, :n].double()).view(n, Hkv, -1).permute(1, 2, 0)
+    there = (lse[s, :n] != 0).view(n, Hkv, -1).permute(1, 2, 0)
+    return (p * torch.where(there, torch.exp(off), 0.0)[..., None]).sum((1, 2))
+
+
+@pytest.mark.parametrize("repaired", [False, True])
+@pytest.mark.parametrize("B,ctx,broken", [(1, 9000, 500), (300, 200, 30), (300, 4000, 100), (17, 500, 31)])
+def test_tokens_that_could_not_be_computed_add_nothing(goose, B, ctx, broken, repaired):
+    """chunk_attn over a page outside the pool, kv_weights with its lse, before and after the table has been put right."""
+    from paper_2604_02047_b200 import binding
+    c = Chunk(8, 2, B, [ctx, 100], 16, seed=17)
+    right = c.c.table
+    wrong = right.clone()
+    wrong[0, broken] = c.c.n_pages
+    c.c.table = wrong
+    out, lse = c.run(goose)
+    assert goose.last_status(2).tolist() == [binding.ST_BAD_ROWS, 0]
+    first = max(0, broken * 16 - ctx)
+    assert not lse[0, first:].any()
+    before = torch.rand(2, 2, ctx + B, device="cuda")
+    weight = before.clone()
+    goose.kv_weights(c.q, lse, c.c.k, right if repaired else wrong, c.ctx, SCALE, weight)
+    assert goose.last_status(2).tolist() == [0 if repaired else binding.ST_BAD_ROWS, 0]
+    for s in range(2):
+        rows = c.ctxs[s] + B
+        ref = _added(c, s, lse)
+        if s == 0:
+            page = slice(broken * 16, broken * 16 + 16)
+            if not repaired:
+                assert torch.equal(weight[0, :, page], before[0, :, page])
+                ref[:, page] = 0
+            if first == 0:
+                assert torch.equal(weight[0], before[0])
+        total = ref + before[s, :, :rows].double()
+        over = (weight[s, :, :rows].double() - total).abs() - (1e-4 + B * 4 * 2.0 ** -24) * ref - 2.0 ** -23 * total
+        assert over.max().item() <= 0, (s, over.max().item())
+        assert torch.equal(weight[s, :, rows:], before[s, :, rows:])
+
+
+def test_a_chunk_that_did_not_fit_and_a_part_of_it_that_does(goose):
+    """The draft runs over the sequence's room, its first token alone would not: what the attention could not compute adds nothing."""
+    from paper_2604_02047_b200 import binding
+    c = Chunk(8, 2, 5, [59, 40], 16, seed=3, width=4)
+    c.ctxs[0], c.ctx = 62, i32([62, 40])
+    out, lse = c.run(goose)
+    assert goose.last_status(2).tolist() == [binding.ST_BAD_ROWS, 0] and not out[0].any() and not lse[0].any()
+    before = torch.rand(2, 2, 64, device="cuda")
+    weight = before.clone()
+    goose.kv_weights(c.q, lse, c.c.k, c.c.table, c.ctx, SCALE, weight, n_new=i32([1, 5]))
+    assert not goose.last_status(2).any()
+    assert torch.equal(weight[0], before[0]) and not torch.equal(weight[1], before[1])
