@@ -76,3 +76,26 @@ def test_a_chunk_that_did_not_fit_and_a_part_of_it_that_does(goose):
     goose.kv_weights(c.q, lse, c.c.k, c.c.table, c.ctx, SCALE, weight, n_new=i32([1, 5]))
     assert not goose.last_status(2).any()
     assert torch.equal(weight[0], before[0]) and not torch.equal(weight[1], before[1])
+
+
+@pytest.mark.parametrize("B,ctx,broken", [(300, 200, 30), (300, 4000, 260), (1000, 3000, 230), (60, 5000, 314)])
+def test_tokens_in_front_of_a_broken_page(goose, B, ctx, broken):
+    """Right or zeros, every token and head for itself, wherever the work on their rows was split; zeros from the first that sees the page on."""
+    from paper_2604_02047_b200 import binding
+    c = Chunk(8, 2, B, [ctx, 100], 16, seed=B)
+    c.c.table_host[0, broken] = -1
+    K, V = c.c.keys(0, ctx + B), c.c.values(0, ctx + B)        # (the page's rows are of some other one here, which no token in front of it sees)
+    c.c.table = i32(c.c.table_host)
+    out, lse = c.run(goose)
+    assert goose.last_status(2).tolist() == [binding.ST_BAD_ROWS, 0]
+    first = broken * 16 - ctx
+    assert 0 < first < B and not out[0, first:].any() and not lse[0, first:].any()
+    K[broken * 16:], V[broken * 16:] = 0, 0
+    ref, A, l, _ = attention(c.q[0], K, V, ctx, SCALE)
+    zero = (out[0, :first] == 0).all(-1)
+    assert torch.equal(zero, lse[0, :first] == 0)
+    near = ((out[0, :first].double() - ref[:first]).abs() <= 2.0 ** -8 * (1.2 * A + ref.abs())[:first]).all(-1)
+    assert (zero | near).all()
+    near = (lse[0, :first].double() - l[:first]).abs() <= 2e-4 + 2.0 ** -20 * l[:first].abs()
+    assert (zero | near).all()
+    c.check(goose, out, lse, skip=[0])
