@@ -41,16 +41,18 @@ class Batch:
         self.budget, self.sink, self.recent, self.slack = budget, sink, recent, slack
         self.free = list(range(-(-rows // page)))[::-1]
         pages = len(self.free)
-        most = max(len(p) for p in prompts) + chunk if budget is None else budget + slack + max(chunk, self.B)
-        self.width = min(pages, -(-max(most, len(max(prompts, key=len)) if budget is None else 0) // page) + 64)
+        # entries of a sequence's part of the table: the whole pool, or what a budget, what it may be beyond that and a chunk need
+        most = pages if budget is None else -(-(budget + slack + max(chunk, self.B)) // page)
+        self.width = min(pages, most, binding.MAX_PAGED_ROWS // page)
         self.table = np.full((self.S, self.width), -1, np.int32)
         self.owned = [0] * self.S                              # pages of a sequence
         shape = (pages, page, model.kv_heads, D)
         self.caches = [(torch.zeros(shape, dtype=torch.bfloat16, device="cuda"), torch.zeros(shape, dtype=torch.bfloat16, device="cuda"))
                        for _ in range(model.layers)]
-        room = (self.S, model.kv_heads, self.width * page)
-        self.weight = [torch.zeros(room, device="cuda") for _ in range(model.layers)]
-        self.pos = [torch.zeros(room, dtype=torch.int32, device="cuda") for _ in range(model.layers)]
+        # weights and positions of the rows, which eviction goes by
+        room, layers = (self.S, model.kv_heads, self.width * page), range(model.layers)
+        self.weight = [None if budget is None else torch.zeros(room, device="cuda") for _ in layers]
+        self.pos = [None if budget is None else torch.zeros(room, dtype=torch.int32, device="cuda") for _ in layers]
         self.ctx = np.zeros(self.S, np.int32)                  # rows of a sequence, and what has left it
         self.off = np.zeros(self.S, np.int32)
         self.tokens = [list(p) for p in prompts]               # the last one of each has no row yet
