@@ -26,13 +26,15 @@ from .shared_prompt import D, Model
 
 
 class Batch:
-    """``prompts``: a token at least each, the last one is the first chunk's anchor.  ``rows``: rows of the pool, of all sequences together.
+    """``prompts``: a token at least each, as many as the model has positions for, the last one is the first chunk's anchor.  ``rows``: rows of the pool, of all sequences together.
     ``budget``: rows that a sequence keeps when it has ``slack`` more than that (None: no eviction)."""
 
     def __init__(self, goose: binding.Goose, model: Model, prompts, rows: int, page: int = 16, chunk: int = 512, draft: int = 8,
                  budget=None, sink: int = 4, recent: int = 64, slack: int = 64):
         if not prompts or not all(len(p) for p in prompts):
             raise ValueError("a batch has sequences, and each of them a token")
+        if max(len(p) for p in prompts) - 1 > len(model.rope):
+            raise ValueError("a prompt of %d tokens: positions up to %d" % (max(len(p) for p in prompts), len(model.rope)))
         if draft + 1 > goose.max_B:
             raise ValueError("a draft of %d tokens and its anchor: a context of %d nodes" % (draft, goose.max_B))
         if budget is not None and sink + recent > budget:
@@ -82,6 +84,9 @@ class Batch:
 
     def _forward(self, tokens, n_new):
         """Logits of a chunk, and what kv_weights needs of its layers."""
+        most = int((np.where(n_new > 0, self.off + self.ctx, 0) + n_new).max())
+        if most > len(self.m.rope):
+            raise ValueError("%d tokens of a sequence: positions up to %d" % (most, len(self.m.rope)))
         table, ctx, off, n = self._pages(n_new), self._dev(self.ctx), self._dev(self.off), self._dev(n_new)
         seen = []
 
@@ -122,7 +127,8 @@ class Batch:
         draft, n = np.full((self.S, self.B), -1, np.int32), np.zeros(self.S, np.int32)
         for s in range(self.S):
             if live[s]:
-                chain, _ = binding.context_match(self.tokens[s], self.B - 1)
+                left = len(self.m.rope) - int(self.off[s] + self.ctx[s]) - 1   # positions behind the last token's
+                chain, _ = binding.context_match(self.tokens[s], max(min(self.B - 1, left), 0))
                 n[s] = 1 + len(chain)
                 draft[s, :n[s]] = [self.tokens[s][-1]] + list(chain)
         logits, state = self._forward(draft, n)
@@ -138,7 +144,10 @@ class Batch:
 
 
 def decode(batch: Batch, tokens: int):
-    """``tokens`` more tokens a sequence.  Returns (the sequences, steps)."""
+    """``tokens`` more tokens a sequence (ValueError where there are no positions for them).  Returns (the sequences, steps)."""
+    most = max(len(t) for t in batch.tokens) + tokens - 1      # rows of the longest, when its last token is chosen
+    if most > len(batch.m.rope):
+        raise ValueError("%d more tokens: positions up to %d" % (tokens, len(batch.m.rope)))
     want, steps = [len(t) + tokens for t in batch.tokens], 0
     while True:
         live = [len(t) < w for t, w in zip(batch.tokens, want)]

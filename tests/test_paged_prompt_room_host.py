@@ -84,3 +84,23 @@ def test_with_a_budget_a_table_has_room_for_the_budget_and_a_chunk():
     out, _ = paged_prompt.decode(batch, 1500)
     assert [len(t) for t in out] == [4500, 1510] and goose.furthest >= 4499
     assert int(batch.ctx.max()) <= 530
+
+
+@pytest.mark.parametrize("budget", [None, 60])
+def test_positions_end_with_the_rotation_table(budget):
+    """As many tokens as it has positions for, drafts cut where it ends; one more is an error, ahead of the first step."""
+    kw = dict(rows=1000, budget=budget, slack=16, recent=20, chunk=32)
+    goose, batch = _batch([100, 7], positions=300, **kw)
+    out, _ = paged_prompt.decode(batch, 201)
+    assert [len(t) for t in out] == [301, 208] and goose.furthest == 300
+    goose, batch = _batch([100, 7], positions=300, **kw)
+    at = goose.furthest
+    with pytest.raises(ValueError):
+        paged_prompt.decode(batch, 202)
+    assert goose.furthest == at
+    with pytest.raises(ValueError):
+        _batch([302], positions=300, **kw)
+    goose, batch = _batch([301], positions=300, **kw)
+    with pytest.raises(ValueError):
+        batch.step([True])
+    assert goose.furthest == 300
