@@ -437,14 +437,19 @@ class Goose:
                  pos_off: Optional[torch.Tensor] = None, new_weight: Optional[torch.Tensor] = None, new_pos: Optional[torch.Tensor] = None,
                  new_ctx_len: Optional[torch.Tensor] = None, new_pos_off: Optional[torch.Tensor] = None):
         """Every key/value head of every sequence back to ``budget`` rows: the first ``sink`` positions, the last ``recent`` ones and the
-        heaviest others stay.  Returns (new_ctx_len, new_pos_off, new_weight, new_pos); none of them may be the array that it replaces."""
+        heaviest others stay.  Returns (new_ctx_len, new_pos_off, new_weight, new_pos); none of them may be the array that it replaces.  Of a sequence
+        that cannot be cut (last_status says so) the call writes no weights and positions: arrays that are made here begin as copies of the
+        old ones, and it goes on with those; arrays that are given, which saves the copies, keep what they hold."""
         S = page_table.shape[0]
         pages, size, Hkv, D = k_cache.shape
         width, room = page_table.shape[-1], row_weight.shape[-1]
         if new_weight is None:
-            new_weight = torch.empty_like(row_weight)
+            new_weight = row_weight.clone()
         if new_pos is None:
-            new_pos = torch.empty((S, Hkv, new_weight.shape[-1]), dtype=torch.int32, device=row_pos.device)
+            new_pos = torch.zeros((S, Hkv, new_weight.shape[-1]), dtype=torch.int32, device=row_pos.device)
+            kept = min(new_pos.shape[-1], row_pos.shape[-1])
+            if row_pos.shape[:-1] == new_pos.shape[:-1] and row_pos.dtype == new_pos.dtype:
+                new_pos[..., :kept] = row_pos[..., :kept]
         if new_ctx_len is None:
             new_ctx_len = torch.empty_like(ctx_len)
         if new_pos_off is None:

@@ -5,6 +5,7 @@ import torch
 
 from _pages import D, attention, i32
 from test_gpu_chunk_attn import Case as Chunk
+from test_gpu_evict_kv import Case as Evict
 
 pytestmark = pytest.mark.gpu
 SCALE = D ** -0.5
@@ -99,3 +100,24 @@ def test_tokens_in_front_of_a_broken_page(goose, B, ctx, broken):
     near = (lse[0, :first].double() - l[:first]).abs() <= 2e-4 + 2.0 ** -20 * l[:first].abs()
     assert (zero | near).all()
     c.check(goose, out, lse, skip=[0])
+
+
+@pytest.mark.parametrize("given", [(), ("new_weight",), ("new_pos",)])
+def test_a_sequence_that_cannot_be_cut_keeps_weights_and_positions(goose, given):
+    """In arrays that the call makes; the next call ranks its rows by them."""
+    from paper_2604_02047_b200 import binding
+    c = Evict(2, [400, 300, 90], 16, 120, 4, 40, seed=10)
+    c.c.table_host[1, 18] = c.c.n_pages
+    c.c.table = i32(c.c.table_host)
+    w, p = torch.tensor(c.weight, device="cuda"), i32(c.pos)
+    spoilt = [torch.full_like(t, 7) for t in (w, p)]           # (what the allocator hands out next)
+    del spoilt
+    new = {n: {"new_weight": torch.full((2 * 3 * 310,), 9.0, device="cuda").view(3, 2, 310), "new_pos": torch.full_like(p, 9)}[n] for n in given}
+    r = goose.evict_kv(c.c.k, c.c.v, c.c.table, c.ctx, w, p, 120, 4, 40, **new)
+    assert goose.last_status(3).tolist() == [0, binding.ST_BAD_ROWS, 0] and r[0].tolist() == [120, 300, 90] and r[1].tolist() == [280, 0, 0]
+    for got, old, name in ((r[2], w, "new_weight"), (r[3], p, "new_pos")):
+        if name in given:
+            assert (got[1] == 9).all()
+        else:
+            assert torch.equal(got[1, :, :300], old[1, :, :300])
+        assert torch.equal(got[2, :, :90], old[2, :, :90])
