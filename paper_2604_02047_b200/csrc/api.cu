@@ -501,10 +501,12 @@ int goose_evict_kv(goose_ctx* c, void* k_cache, void* v_cache, int n_pages, int 
     const size_t rows = (size_t)S * Hkv * 4, n_old = rows * ldw, n_new = rows * ldw_new, words = 4 * (size_t)S;
     const void* fresh[4] = {new_weight, new_pos, new_ctx_len, new_pos_off};
     const size_t fresh_bytes[4] = {n_new, n_new, words, words};
-    const void* old[4] = {row_weight, row_pos, ctx_len, pos_off};
-    const size_t old_bytes[4] = {n_old, n_old, words, words};
+    // (a page table that changes under the call would name rows that nobody has checked)
+    const size_t n_cache = (size_t)n_pages * page_size * Hkv * D * 2;
+    const void* old[7] = {row_weight, row_pos, ctx_len, pos_off, page_table, k_cache, v_cache};
+    const size_t old_bytes[7] = {n_old, n_old, words, words, words * ldt, n_cache, n_cache};
     for (int i = 0; i < 4; ++i) {
-        for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < 7; ++j)
             if (old[j] && ranges_overlap(fresh[i], fresh_bytes[i], old[j], old_bytes[j])) return GOOSE_EINVAL;
         for (int j = 0; j < i; ++j)
             if (ranges_overlap(fresh[i], fresh_bytes[i], fresh[j], fresh_bytes[j])) return GOOSE_EINVAL;

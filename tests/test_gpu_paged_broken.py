@@ -121,3 +121,29 @@ def test_a_sequence_that_cannot_be_cut_keeps_weights_and_positions(goose, given)
         else:
             assert torch.equal(got[1, :, :300], old[1, :, :300])
         assert torch.equal(got[2, :, :90], old[2, :, :90])
+
+
+def test_new_arrays_of_an_eviction_lie_in_nothing_that_it_reads(goose):
+    """Refused ahead of any launch: the table and the caches too."""
+    from paper_2604_02047_b200.binding import GooseError
+    c = Evict(1, [300, 90], 16, 120, 4, 40, seed=11)
+    w, p, k, v = torch.tensor(c.weight, device="cuda"), i32(c.pos), c.c.k, c.c.v
+    ld = c.c.table.shape[1]
+    inside = [dict(new_pos=c.c.table.view(2, 1, ld), new_weight=torch.zeros(2, 1, ld, device="cuda")),
+              dict(new_weight=c.c.table.view(torch.float32).view(2, 1, ld), new_pos=torch.zeros(2, 1, ld, dtype=torch.int32, device="cuda")),
+              dict(new_ctx_len=c.c.table.flatten()[3:5]), dict(new_pos_off=c.c.table.flatten()[-2:])]
+    for cache in (k, v):
+        words = cache.flatten().view(torch.int32)
+        inside += [dict(new_ctx_len=words[:2]), dict(new_pos_off=words[-2:]), dict(new_pos=words[100:100 + p.numel()].view(p.shape)),
+                   dict(new_weight=words[100:100 + p.numel()].view(torch.float32).view(p.shape))]
+    before = [t.clone() for t in (c.c.table, k, v)]
+    for new in inside:
+        with pytest.raises(GooseError):
+            goose.evict_kv(k, v, c.c.table, c.ctx, w, p, 120, 4, 40, **new)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a.view(torch.int16), b.view(torch.int16)) for a, b in zip((c.c.table, k, v), before)) and not goose.last_status(2).any()
+    # arrays next to one another are allowed
+    both = torch.zeros(2, *p.shape, dtype=torch.int32, device="cuda")
+    lens = torch.zeros(4, dtype=torch.int32, device="cuda")
+    r = goose.evict_kv(k, v, c.c.table, c.ctx, w, p, 120, 4, 40, new_weight=both[0].view(torch.float32), new_pos=both[1], new_ctx_len=lens[:2], new_pos_off=lens[2:])
+    assert r[0].tolist() == [120, 90] and lens.tolist() == [120, 90, 180, 0] and not goose.last_status(2).any()
