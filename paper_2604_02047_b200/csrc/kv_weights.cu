@@ -380,7 +380,7 @@ kv_weights_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                         const uint32_t word = __ballot_sync(0xFFFFFFFFu, x[w] != -INFINITY);   // (NaN counts)
                         const float v = x[w] == -INFINITY ? 0.f : -a.inv_scale * x[w];
                         const __nv_bfloat16 high = __float2bfloat16_rn(v);
-                        const float left = isinf(v) ? 0.f : v - __bfloat162float(high);
+                        const float left = __hisinf(high) ? 0.f : v - __bfloat162float(high);   // (the largest fp32 round to infinity)
                         const __nv_bfloat16 mid = __float2bfloat16_rn(left), low = __float2bfloat16_rn(left - __bfloat162float(mid));
                         const int r = 32 * w + lane;
                         *reinterpret_cast<uint4*>(step_smem + (1 + qs.at) * kStepBytes + (r >> 3) * 256 + (r & 7) * 16) =

@@ -40,3 +40,23 @@ def test_every_exponential(goose, low, high):
         ref = torch.exp(-x.double())[..., None]
         off = (weight[..., :ctx].double() / ref - 1).abs() - 2.4e-7 - (1.5 * 2.0 ** -22 * x.double().abs())[..., None] - 2.0 ** -121 / ref
         assert off.max().item() <= 0, off.max().item()
+
+
+@pytest.mark.parametrize("size", [3.3895e38, 3.3953e38, 3.3961e38, 3.4e38, 3.4028e38, float("inf")])
+def test_the_largest_log_sum_exps(goose, size):
+    """-lse / scale of a size that bf16 has just, or rounds to infinity: nothing is added where exp(-lse) is 0, and rows that do not see the token are as they were."""
+    scale = 2.0 ** -97
+    c = Paged([300], 2, 16)
+    c.k.zero_()
+    q = torch.zeros(1, 140, 2, D, dtype=torch.bfloat16, device="cuda")
+    lse = torch.zeros(1, 140, 2, device="cuda")
+    plain = torch.zeros(1, 2, 300, device="cuda")
+    goose.kv_weights(q, lse, c.k, c.table, i32([160]), scale, plain)
+    lse[0, 6, 0] = lse[0, 135, 0] = torch.tensor(size).float() * scale
+    weight = torch.zeros(1, 2, 300, device="cuda")
+    goose.kv_weights(q, lse, c.k, c.table, i32([160]), scale, weight)
+    assert not goose.last_status(1).any()
+    sees = (torch.arange(300, device="cuda") <= 160 + 6).float() + (torch.arange(300, device="cuda") <= 160 + 135).float()
+    assert torch.equal(weight[0, 1], plain[0, 1])
+    # (140 terms of exp(0): each to 2.4e-7, sums of them to 2^-24 an addition)
+    assert (weight[0, 0] - (plain[0, 0] - sees)).abs().max() <= 140 * (2.4e-7 + 2.0 ** -24 * 140)
