@@ -14,10 +14,11 @@
 //                     the CTA leaves a partial result, and the warp that completes a count joins the 32 rows of all CTAs, in the order of the keys
 //                     whoever comes last.
 // What bounds it.  Long chunks: a lane's chain (scores, exponentials, product), 3080 cycles a pair of tiles of which the exponentials are 2048 and the
-// products 2048 (4096 tokens behind 8192, 32 heads over 8: 544 us, 1.26 PFLOP/s in bursts; under the power cap 623).  Short ones: changes of item, some
-// 10000 cycles with the first tile behind them (5 prompts of 500 to 1500 tokens, 52 heads: 144 us), and the causal edge.  A token a sequence: HBM, and the TMA boxes of
+// products 2048 (4096 tokens behind 8192, 32 heads over 8: 546 us, 1.26 PFLOP/s in bursts; under the power cap 622).  Short ones: changes of item, some
+// 10000 cycles with the first tile behind them (5 prompts of 500 to 1500 tokens, 52 heads: 145 us), and the causal edge
+// (with heads of their own lane 0 of a pair has a tile that is masked for all of its tokens).  A token a sequence: HBM, and the TMA boxes of
 // pages of 16 rows, some 100 cycles each (64 sequences of 500 to 8192 rows, 32 over 8: 235 us, 5.1 TB/s; pages of 128 rows and equal lengths 5.8).  One token: serial latency
-// (511 rows: 10.6 to 11.4 us).
+// (511 rows: 10.3 to 12 us).
 // Every wait is bounded: one that runs out raises the CTA's abort flag and GOOSE_ST_TIMEOUT, and every role unwinds.
 #include <stddef.h>
 
@@ -782,7 +783,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_const
                             const int width = here > 1 ? 1 << (32 - __clz(here - 1)) : 1;
                             const int r = row0 + (lane & (width - 1)), node = r / a.g;
                             const size_t at = ((size_t)first_token + node) * a.H + sg.hk * a.g + (r - node * a.g);
-                            // few rows are a chain of parts, many are requests (a token behind 2400 rows, groups of 4: 17 us, the other way 20; 60 tokens behind 500: 41, and 46)
+                            // few rows are a chain of parts, many are requests (a token behind 2400 rows, groups of 4: 18 us, the other way 20; 60 tokens behind 500: 25, and 29)
                             if (width <= 4) join_parts<16, 4>(a, sg.c0, sg.parts, m_tile, row0, rows, lane, at, width, a.lse != nullptr);
                             else join_parts<32, 2>(a, sg.c0, sg.parts, m_tile, row0, rows, lane, at, width, a.lse != nullptr);
                         }

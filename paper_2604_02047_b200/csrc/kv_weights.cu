@@ -16,7 +16,7 @@
 //   warps 20..23      K tiles into a ring of four, 32 keys of a tile a warp, by 16-byte copies: a TMA box a page took 110 to 156 cycles a box, and pages of
 //                     16 rows have sixteen a tile (64 sequences of 8192 rows, a token each: 255 us then, 177 now, 6.25 TB/s; pages of 128 rows 218, 173)
 // What bounds it.  Many tokens: the exponentials, 770 cycles a tile of 128 x 128 of the special function units', and scores that wait for their buffers, of which
-// tensor memory has no more (4096 tokens behind 8192, 32 heads over 8: 365 us, 1210 cycles a tile; 2048 behind 4096: 107).  A token a sequence: HBM (16 sequences of 1000 to
+// tensor memory has no more (4096 tokens behind 8192, 32 heads over 8: 371 us, 1230 cycles a tile; 2048 behind 4096: 109.5).  A token a sequence: HBM (16 sequences of 1000 to
 // 8192 rows, 32 over 8: 36 us).
 // Every wait is bounded: one that runs out raises the CTA's abort flag and GOOSE_ST_TIMEOUT, and every role unwinds.
 #include <stddef.h>
@@ -167,8 +167,8 @@ __device__ __forceinline__ unsigned long long ex2_fma(float2 x) {
 }
 
 // Sums over 32 columns of exp2(score * scale); kMasked: over those that count.  Of whole tiles every fourth pair's exponentials come from the FMA pipe: the
-// special function unit has 16 a cycle (none of them, one in eight, one in four, one in three, 4096 tokens behind 8192, 32 heads over 8: 400, 367, 362, 365 us with a
-// polynomial of degree 4, whose error was 2.6e-6; of degree 5 one in four 1 % more)
+// special function unit has 16 a cycle (none of them, one in eight, one in four, one in three, 4096 tokens behind 8192, 32 heads over 8: 412, 380, 381, 387 us on one and the same device;
+// with a polynomial of degree 4, whose error was 2.6e-6, 1 % less)
 template <bool kMasked>
 __device__ __forceinline__ void add_columns(const uint32_t (&v)[32], unsigned long long scale2, uint32_t counts, unsigned long long (&part)[2]) {
 #pragma unroll
